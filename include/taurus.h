@@ -41,6 +41,13 @@ typedef enum {
 
 typedef enum { TAURUS_F32 = 0, TAURUS_BF16 = 1, TAURUS_F16 = 2 } taurus_dtype;
 
+/* Activations of taurus_group_norm. */
+typedef enum {
+    TAURUS_ACT_NONE = 0,
+    TAURUS_ACT_RELU = 1, /* max(z, 0), as the layers' (a NaN becomes 0)                  */
+    TAURUS_ACT_SILU = 2  /* z / (1 + exp(-z))                                            */
+} taurus_activation;
+
 /* Eviction policies of a budgeted layer (desc.eviction).  The paper's
  * policy evicts the partial states with the fewest pending messages
  * (Sec. 3.5.3); random, FIFO and LRU are the policies it is compared with
@@ -386,6 +393,125 @@ int taurus_relabel_graph(const taurus_graph* g, const int32_t* new_of_old, int64
  */
 int taurus_permute_rows(const void* in, void* out, int64_t n, int64_t row_bytes, const int32_t* new_of_old,
                         int32_t inverse, void* stream);
+
+/*
+ * Operators on rows, for what comes before the first layer and between two
+ * layers.  They share these rules:
+ *   - Everything is enqueued on `stream`; nothing is copied to the host, no
+ *     call waits, allocates or keeps anything, and calls can be captured
+ *     into a HIP graph.  Calls on several streams run side by side as long
+ *     as each has a workspace of its own.
+ *   - Pointers are device memory aligned to their element type.  Row arrays
+ *     are [rows][stride] with the row's values first, stride >= the row's
+ *     length (at most 2^29); 16-byte aligned arrays whose row length and
+ *     stride are whole 16-byte pieces are the fast case, any other is
+ *     correct.  Outputs must not overlap inputs.
+ *   - Arithmetic is fp32 (fp32 matrix cores, or 16-bit ones with fp32
+ *     accumulation); stored results are rounded to nearest even once.  Sums
+ *     run in an order that the sizes, offsets and ids fix: equal calls on
+ *     equal inputs give equal bits.
+ *   - Offsets `off` (device int64[parts + 1], non-decreasing, within [0, m])
+ *     cut rows into ranges; off[0] need not be 0 nor off[parts] m, and the
+ *     output rows no range holds are left as they were.  Empty ranges are
+ *     allowed.  Offsets are clamped to [0, m], so no other memory is touched
+ *     if they break these rules; the results are then unspecified.
+ *   - work: device memory, 16-byte aligned, of at least the bytes the
+ *     call's *_bytes function names (work may be NULL where that is 0); its
+ *     contents are unspecified afterwards.  *_bytes functions return the
+ *     bytes, or a negative status.
+ *   - Counts below 2^31.  A bad argument is TAURUS_E_INVALID before anything
+ *     is enqueued.
+ */
+
+/*
+ * Rows looked up by id, scaled: out[i] = scale * table[ids[i]] for i < m
+ * (learned features of vertices that have none, or the rows of asked-for
+ * vertices out of a layer's output).  table: [n][table_stride] of
+ * table_dtype, rows of d values (1 <= d <= 2^24); ids: int32[m], in any
+ * order, repeats allowed; an id outside [0, n) names no row and its output
+ * row is zeros (-1 pads a batch).  out: [m][out_stride] of out_dtype.
+ */
+int taurus_lookup_rows(const void* table, int32_t table_dtype, int64_t n, int64_t d, int64_t table_stride,
+                       const int32_t* ids, int64_t m, float scale, void* out, int32_t out_dtype,
+                       int64_t out_stride, void* stream);
+
+/*
+ * Gradient of taurus_lookup_rows with respect to its table:
+ *     out[u] = scale * sum over i with ids[i] = u of grad[i]   (zeros if none)
+ * or, with accumulate != 0, out[u] += that for the rows some id names (other
+ * rows are then neither read nor written).  grad: [m][grad_stride] of
+ * grad_dtype; out: [n][out_stride] of out_dtype.  Ids outside [0, n) are
+ * left out.  Sums are fp32.
+ */
+int64_t taurus_lookup_rows_grad_bytes(int64_t m, int64_t d);
+int taurus_lookup_rows_grad(const void* grad, int32_t grad_dtype, int64_t grad_stride, const int32_t* ids,
+                            int64_t m, int64_t n, int64_t d, float scale, int32_t accumulate, void* out,
+                            int32_t out_dtype, int64_t out_stride, void* work, int64_t work_bytes,
+                            void* stream);
+
+/*
+ * Linear map of rows grouped by type (vertices of a graph with several
+ * vertex types, each with a weight of its own):
+ *     out[r] = x[r] weight[g] + bias[g]   for off[g] <= r < off[g + 1].
+ * x: [m][x_stride] of dtype, rows of d_in values; weight: [groups][d_in]
+ * [d_out] of dtype, contiguous; bias: float[groups][d_out] or NULL; out:
+ * [m][out_stride] of out_dtype, rows of d_out values.  1 <= d_in, d_out <=
+ * 2^16.  The sizes of the types are read on the device.
+ */
+int taurus_grouped_linear(const void* x, int32_t dtype, int64_t m, int64_t d_in, int64_t x_stride,
+                          const int64_t* off, int64_t groups, const void* weight, int64_t d_out,
+                          const float* bias, void* out, int32_t out_dtype, int64_t out_stride, void* stream);
+
+/*
+ * Gradients of taurus_grouped_linear, from grad = d(loss)/d(out), [m]
+ * [grad_stride] of dtype:
+ *     dx[r]      = grad[r] weight[g]^T            [m][dx_stride] of dtype
+ *     dweight[g] = sum over g's rows of x[r]^T grad[r]
+ *                  [groups][d_in][d_out] of dweight_dtype, contiguous
+ *     dbias[g]   = sum over g's rows of grad[r]   float[groups][d_out]
+ * Each may be NULL and is then not computed.  Every type's dweight and dbias
+ * are written (zeros for a type without rows).
+ */
+int64_t taurus_grouped_linear_grad_bytes(int64_t m, int64_t d_in, int64_t d_out);
+int taurus_grouped_linear_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride,
+                               int32_t dtype, int64_t m, int64_t d_in, int64_t d_out, const int64_t* off,
+                               int64_t groups, const void* weight, void* dx, int64_t dx_stride, void* dweight,
+                               int32_t dweight_dtype, float* dbias, void* work, int64_t work_bytes,
+                               void* stream);
+
+/*
+ * Group norm with an activation over rows of d channels (1 <= d <= 2048),
+ * channels last.  A group is d / groups consecutive channels (groups divides
+ * d) of one row (off = NULL: every vertex by itself; groups = 1 is layer
+ * norm), or of all rows of a segment off[s] <= r < off[s + 1], s < segments
+ * (the vertices of one graph of a batch).  With mean and var = mean square
+ * deviation over the group's values and rstd = (var + eps)^-1/2,
+ *     out = act((x - mean) * rstd * weight[c] + bias[c]).
+ * x: [m][x_stride] of dtype; weight, bias: float[d], or NULL for 1 and 0;
+ * act: taurus_activation; out: [m][out_stride] of out_dtype; mean, rstd:
+ * float[rows or segments][groups], written for the gradient, or both NULL
+ * (a segment without rows gets zeros).  segments is ignored when off is NULL.
+ */
+int64_t taurus_group_norm_bytes(int64_t m, int64_t d, int64_t groups, int64_t segments, int32_t by_segment,
+                                int32_t grad);
+int taurus_group_norm(const void* x, int32_t dtype, int64_t m, int64_t d, int64_t x_stride, int64_t groups,
+                      const int64_t* off, int64_t segments, const float* weight, const float* bias, float eps,
+                      int32_t act, void* out, int32_t out_dtype, int64_t out_stride, float* mean, float* rstd,
+                      void* work, int64_t work_bytes, void* stream);
+
+/*
+ * Gradients of taurus_group_norm from grad = d(loss)/d(out), [m]
+ * [grad_stride] of dtype, at the mean and rstd the forward call wrote:
+ *     dx [m][dx_stride] of dtype, dweight and dbias float[d]; each may be
+ * NULL and is then not written.  ReLU passes gradient where its argument,
+ * formed exactly from x, mean, rstd, weight and bias, is positive.  Rows
+ * outside the segments add nothing to dweight and dbias.
+ */
+int taurus_group_norm_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int32_t dtype,
+                           int64_t m, int64_t d, int64_t groups, const int64_t* off, int64_t segments,
+                           const float* weight, const float* bias, const float* mean, const float* rstd,
+                           int32_t act, void* dx, int64_t dx_stride, float* dweight, float* dbias, void* work,
+                           int64_t work_bytes, void* stream);
 
 /*
  * A plan holds the per-graph structures that layers over one graph and chunk

@@ -17,6 +17,7 @@ OK, E_INVALID, E_OOM, E_DEVICE, E_STATE, E_INCOMPLETE, E_BUDGET = 0, -1, -2, -3,
 F32, BF16, F16 = 0, 1, 2
 SAGE_MEAN, GCN_SYM, GIN_SUM, GAT_ATT, GIN_MLP = 0, 1, 2, 3, 4
 EVICT_PENDING, EVICT_RANDOM, EVICT_FIFO, EVICT_LRU = 0, 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 NOALLOC_SCRATCH_BYTES, NOALLOC_MAX_EDGES = 32 << 20, 1 << 20
 
 STATUS_NAMES = {OK: "OK", E_INVALID: "E_INVALID", E_OOM: "E_OOM", E_DEVICE: "E_DEVICE",
@@ -108,6 +109,20 @@ SIGNATURES = {
                                           ctypes.POINTER(ctypes.c_void_p)]),
     "taurus_plan_destroy": (None, [ctypes.c_void_p]),
 }
+
+# the operators on rows, one letter an argument: p pointer, i int32, l int64, f float
+_ARG = {"p": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float}
+for _name, _res, _args in (
+        ("taurus_lookup_rows", ctypes.c_int, "pilllplfpilp"),
+        ("taurus_lookup_rows_grad_bytes", ctypes.c_int64, "ll"),
+        ("taurus_lookup_rows_grad", ctypes.c_int, "pilplllfipilplp"),
+        ("taurus_grouped_linear", ctypes.c_int, "pilllplplppilp"),
+        ("taurus_grouped_linear_grad_bytes", ctypes.c_int64, "lll"),
+        ("taurus_grouped_linear_grad", ctypes.c_int, "plplilllplpplpipplp"),
+        ("taurus_group_norm_bytes", ctypes.c_int64, "llllii"),
+        ("taurus_group_norm", ctypes.c_int, "pillllplppfipilppplp"),
+        ("taurus_group_norm_grad", ctypes.c_int, "plplilllplppppiplppplp")):
+    SIGNATURES[_name] = (_res, [_ARG[_c] for _c in _args])
 
 _lib = None
 

@@ -14,6 +14,7 @@ import numpy as np
 import torch
 
 from . import _native as N
+from .rowops import group_norm, grouped_linear, lookup_rows
 
 _TORCH_DTYPE = {N.F32: torch.float32, N.BF16: torch.bfloat16, N.F16: torch.float16}
 
@@ -358,22 +359,52 @@ class Layer:
             pass
 
 
+def _encode(x: torch.Tensor, encoder: dict, stream):
+    """The first layer's input rows: vertex v's features (x[v], or scale *
+    x[ids[v]]), times its type's weight plus bias, normalised."""
+    enc = dict(encoder)
+    ids, scale, norm = enc.pop("ids", None), enc.pop("scale", 1.0), enc.pop("norm", None)
+    off, weight, bias = enc.pop("off", None), enc.pop("weight", None), enc.pop("bias", None)
+    if enc:
+        raise ValueError(f"encoder does not know {', '.join(sorted(enc))}")
+    if (off is None) != (weight is None) or (bias is not None and weight is None):
+        raise ValueError("the encoder's linear map needs off and weight together")
+    h = x if ids is None else lookup_rows(x, ids, scale, stream=stream)
+    if weight is not None:
+        h = grouped_linear(h, off, weight, bias, stream=stream)
+    return h if norm is None else group_norm(h, stream=stream, **norm)
+
+
 def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Tensor, layers: list,
-               *, chunk: int, stream=None, profile: bool = False, outs: Optional[list] = None):
+               *, chunk: int, stream=None, profile: bool = False, outs: Optional[list] = None,
+               encoder: Optional[dict] = None):
     """Layer-wise inference: layer l's output is layer l+1's input.
 
     ``layers`` holds dicts with keys agg, d_in, d_out, weight_cat, bias,
-    in_dtype, out_dtype, relu, fanout, layer, seed.  Returns (outputs, stats)."""
-    h = x
+    in_dtype, out_dtype, relu, fanout, layer, seed, and optionally norm, a
+    dict of group_norm's arguments (groups, weight, bias, off, eps, act) that
+    is applied to the layer's output rows before the next layer takes them
+    (the layer itself then usually has relu off).  encoder makes the first
+    layer's input from x: a dict with off, weight and bias (vertices grouped
+    by type, one linear map each: grouped_linear's), ids and scale (x is a
+    table, vertex v's row scale * x[ids[v]]: lookup_rows') and norm, each
+    optional; offsets must hold every vertex.  Returns (outputs, stats)."""
+    h = x if encoder is None else _encode(x, encoder, stream)
     results, stats = [], []
     plan = Plan(n, row_off, col_dst, chunk, stream=stream)
     for i, spec in enumerate(layers):
-        out = outs[i] if outs is not None else torch.empty(
-            (n, spec["d_out"]), dtype=_TORCH_DTYPE[spec.get("out_dtype", N.F32)], device=x.device)
+        spec = dict(spec)
+        norm = spec.pop("norm", None)
+        given = outs[i] if outs is not None else None
+        dtype = _TORCH_DTYPE[spec.get("out_dtype", N.F32)]
+        out = given if given is not None and norm is None else torch.empty((n, spec["d_out"]), dtype=dtype,
+                                                                           device=x.device)
         L = Layer(n, row_off, col_dst, out=out, chunk=chunk, stream=stream, profile=profile, plan=plan, **spec)
         L.push_all(h)
         stats.append(L.finalize())
         L.destroy()
+        if norm is not None:
+            out = group_norm(out, out=given, stream=stream, **norm)
         results.append(out)
         h = out
     if plan is not None:

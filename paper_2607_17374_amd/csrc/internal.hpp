@@ -177,6 +177,8 @@ void radix_sort_u64(SortBuffers& b, int64_t n, int key_bits, Arena& arena, hipSt
                     int bad_bit, uint32_t* first_hist = nullptr, int first_bit = 0);
 // The same for 32-bit keys (key_bits <= 32): half the key traffic per pass.
 void radix_sort_u32(SortBuffers32& b, int64_t n, int key_bits, Arena& arena, hipStream_t s, int* bad, int bad_bit);
+// the most a fixed-region arena needs for either sort of n items
+int64_t radix_sort_bytes(int64_t n);
 
 // In-edges grouped by destination, sources ascending (sample.hip): built once
 // per graph for the fanout sampler.  Complete when build_csc returns.

@@ -1043,6 +1043,14 @@ static void radix_sort_impl(SortBuffersT<K>& b, int64_t n, int key_bits, Arena& 
     arena.free_ptr(hist);
 }
 
+int64_t radix_sort_bytes(int64_t n) {
+    // the tiles' histograms at the widest digit, a pass's group counts and
+    // offsets and digit totals, each at a multiple of 256 bytes
+    constexpr int64_t NB = 1 << 10;
+    const int64_t nblocks = ceil_div(n, RS_TILE), ng = ceil_div(nblocks, radix_group_tiles(nblocks));
+    return NB * nblocks * 4 + 2 * ng * NB * 8 + NB * 8 + 4 * 256;
+}
+
 void radix_sort_u64(SortBuffers& b, int64_t n, int key_bits, Arena& arena, hipStream_t s, int* bad,
                     int bad_bit, uint32_t* first_hist, int first_bit) {
     radix_sort_impl<uint64_t>(b, n, key_bits, arena, s, bad, bad_bit, first_hist, first_bit);

@@ -1,0 +1,282 @@
+// What the operators on rows share (rows.hip, grouped.hip, norm.hip):
+// vectors of a storage type read and written as fp32, the units that ragged
+// row ranges are cut into, workspaces, argument checks.
+#pragma once
+
+#include <algorithm>
+#include <exception>
+
+#include "device.hpp"
+#include "internal.hpp"
+
+namespace taurus {
+
+// Runs an entry point's body: library failures become their status, any
+// other exception TAURUS_E_DEVICE; nothing crosses the C boundary.
+template <typename F>
+inline int guarded_call(F&& f) {
+    try {
+        return f();
+    } catch (const Failure& x) {
+        return x.status;
+    } catch (const std::exception& x) {
+        set_error("internal error: %s", x.what());
+        return TAURUS_E_DEVICE;
+    }
+}
+
+inline int dtype_size(int dtype) { return dtype == TAURUS_F32 ? 4 : 2; }
+
+// ------------------------------------------------------------ host checks --
+
+constexpr int64_t ROWS_MAX = ((int64_t)1 << 31) - 1;
+
+inline void check_dtype(int dtype, const char* what) {
+    if (dtype != TAURUS_F32 && dtype != TAURUS_BF16 && dtype != TAURUS_F16)
+        fail(TAURUS_E_INVALID, "%s: type %d is none of fp32, bf16, fp16", what, dtype);
+}
+inline void check_count(int64_t v, int64_t lo, int64_t hi, const char* what) {
+    if (v < lo || v > hi)
+        fail(TAURUS_E_INVALID, "%s is %lld, not in [%lld, %lld]", what, (long long)v, (long long)lo, (long long)hi);
+}
+// a row array: rows of `cols` values at least `cols` apart; the last value's
+// byte offset fits 62 bits; values lie at multiples of their size
+inline void check_rows(const void* p, int dtype, int64_t rows, int64_t cols, int64_t stride, const char* what) {
+    if (rows <= 0) return;
+    if (!p) fail(TAURUS_E_INVALID, "%s is null", what);
+    if (stride < cols || stride > ((int64_t)1 << 29))
+        fail(TAURUS_E_INVALID, "%s: rows of %lld values are %lld apart", what, (long long)cols, (long long)stride);
+    if (reinterpret_cast<uintptr_t>(p) % dtype_size(dtype))
+        fail(TAURUS_E_INVALID, "%s is not aligned to its type", what);
+}
+inline void check_ptr(const void* p, int align, const char* what) {
+    if (!p) fail(TAURUS_E_INVALID, "%s is null", what);
+    if (reinterpret_cast<uintptr_t>(p) % align) fail(TAURUS_E_INVALID, "%s is not aligned to its type", what);
+}
+
+// Consecutive pieces of a caller's workspace, each at a multiple of 256
+// bytes.  Built over a null pointer it counts the bytes only, so that the
+// size a caller asks for and the layout a call uses are one piece of code.
+class Carve {
+public:
+    explicit Carve(void* p = nullptr) : base_(static_cast<char*>(p)) {}
+    template <typename T>
+    T* take(int64_t count) {
+        const int64_t at = top_;
+        top_ += (count * (int64_t)sizeof(T) + 255) & ~(int64_t)255;
+        return base_ ? reinterpret_cast<T*>(base_ + at) : nullptr;
+    }
+    int64_t bytes() const { return top_; }
+
+private:
+    char* base_;
+    int64_t top_ = 0;
+};
+inline void check_work(const void* work, int64_t have, int64_t need, const char* call) {
+    if (need <= 0) return;
+    if (!work) fail(TAURUS_E_INVALID, "%s: the workspace is null", call);
+    if (reinterpret_cast<uintptr_t>(work) % 16) fail(TAURUS_E_INVALID, "%s: the workspace is not 16-byte aligned", call);
+    if (have < need)
+        fail(TAURUS_E_INVALID, "%s: the workspace has %lld bytes, %lld are needed", call, (long long)have,
+             (long long)need);
+}
+
+// Widest vector, of at most `most` values, in which every row of an array
+// can be taken: it divides the row's length and stride, and the address is
+// aligned to it (to 16 bytes, the widest access, for longer vectors).
+inline int vec_width(int most, int dtype, const void* p, int64_t cols, int64_t stride) {
+    int e = most;
+    while (e > 1 && (cols % e || stride % e ||
+                     reinterpret_cast<uintptr_t>(p) % (size_t)std::min(16, e * dtype_size(dtype))))
+        e >>= 1;
+    return e;
+}
+
+// A launch covers fewer than 2^32 threads: kernels whose work can be longer
+// take at most this many workgroups of 256 and walk the rest in steps.
+constexpr int64_t GRID_MAX = (int64_t)1 << 23;
+inline unsigned grid_for(int64_t blocks) { return (unsigned)std::min(blocks, GRID_MAX); }
+
+// ---------------------------------------------------------------- vectors --
+
+template <int BYTES>
+struct Raw;
+template <>
+struct Raw<2> {
+    typedef uint16_t type;
+};
+template <>
+struct Raw<4> {
+    typedef uint32_t type;
+};
+template <>
+struct Raw<8> {
+    typedef uint2 type;
+};
+template <>
+struct Raw<16> {
+    typedef uint4 type;
+};
+template <int DT>
+constexpr int type_bytes = DT == TAURUS_F32 ? 4 : 2;
+
+// E values of a row as stored
+template <int DT, int E>
+struct Stored {
+    static constexpr int BYTES = E * type_bytes<DT>;
+    static constexpr int PART = BYTES < 16 ? BYTES : 16, PARTS = BYTES / PART;
+    typedef typename Raw<PART>::type part;
+    part v[PARTS];
+};
+template <int DT, int E>
+__device__ inline Stored<DT, E> load_stored(const void* p, int64_t at) {
+    typedef Stored<DT, E> S;
+    S s;
+    const auto* q = reinterpret_cast<const typename S::part*>(static_cast<const char*>(p) + at * type_bytes<DT>);
+#pragma unroll
+    for (int i = 0; i < S::PARTS; i++) s.v[i] = q[i];
+    return s;
+}
+template <int DT, int E>
+__device__ inline Stored<DT, E> zero_stored() {
+    Stored<DT, E> s;
+    __builtin_memset(&s, 0, sizeof(s));
+    return s;
+}
+template <int DT, int E>
+__device__ inline void decode(const Stored<DT, E>& s, float (&f)[E]) {
+    if constexpr (DT == TAURUS_F32) {
+        __builtin_memcpy(f, &s, sizeof(f));
+    } else {
+        uint16_t h[E];
+        __builtin_memcpy(h, &s, sizeof(h));
+#pragma unroll
+        for (int i = 0; i < E; i++) {
+            if constexpr (DT == TAURUS_BF16) f[i] = __uint_as_float((uint32_t)h[i] << 16);
+            else f[i] = (float)__builtin_bit_cast(_Float16, h[i]);
+        }
+    }
+}
+// E fp32 values rounded to nearest even in the stored type
+template <int DT, int E>
+__device__ inline void store_vec(void* p, int64_t at, const float (&f)[E]) {
+    typedef Stored<DT, E> S;
+    S s;
+    if constexpr (DT == TAURUS_F32) {
+        __builtin_memcpy(&s, f, sizeof(s));
+    } else {
+        uint16_t h[E];
+#pragma unroll
+        for (int i = 0; i < E; i++) {
+            if constexpr (DT == TAURUS_BF16) h[i] = __builtin_bit_cast(uint16_t, (__bf16)f[i]);
+            else h[i] = __builtin_bit_cast(uint16_t, (_Float16)f[i]);
+        }
+        __builtin_memcpy(&s, h, sizeof(s));
+    }
+    auto* q = reinterpret_cast<typename S::part*>(static_cast<char*>(p) + at * type_bytes<DT>);
+#pragma unroll
+    for (int i = 0; i < S::PARTS; i++) q[i] = s.v[i];
+}
+// the same with the stored type known at run time (uniform)
+template <int E>
+__device__ inline void store_as(int dtype, void* p, int64_t at, const float (&f)[E]) {
+    if (dtype == TAURUS_F32) store_vec<TAURUS_F32, E>(p, at, f);
+    else if (dtype == TAURUS_BF16) store_vec<TAURUS_BF16, E>(p, at, f);
+    else store_vec<TAURUS_F16, E>(p, at, f);
+}
+template <int DT, int E>
+__device__ inline void load_vec(const void* p, int64_t at, float (&f)[E]) {
+    decode<DT, E>(load_stored<DT, E>(p, at), f);
+}
+
+// ------------------------------------------------------------------ units --
+// Rows [off[g], off[g + 1]) belong to range g of `parts`.  Work over them is
+// cut into units of at most R = 2^lr rows that never cross a range.  Nothing
+// on the host knows the ranges, so a launch has a slot for every unit there
+// can be: range g owns slots f(g) .. f(g + 1) - 1 with
+//     f(g) = floor(off[g] / R) + g,
+// which increases with g and leaves a range of n rows at least ceil(n / R)
+// slots: with off[g] = qR + s and off[g + 1] = pR + t (s, t < R), it has
+// p - q + 1 slots and p - q + ceil((t - s) / R) <= p - q + 1 units.  So a
+// slot finds its range by a search of off alone, without prefix sums, and
+// there are floor(m / R) + parts slots in all.  Slot i of range g takes rows
+// [off[g] + i R, off[g + 1]) up to R of them; slots past the last unit have
+// none.  An empty range keeps one slot.  Offsets are clamped to [0, m], so
+// that no row outside the array is touched whatever they hold.
+struct Unit {
+    int g;            // range; -1: none (offsets do not start at 0)
+    int slot;         // which of the range's slots
+    int64_t r0, r1;   // rows
+    int64_t begin, end;  // the whole range
+    __device__ int64_t units(int lr) const { return (end - begin + ((int64_t)1 << lr) - 1) >> lr; }
+};
+inline int64_t unit_slots(int64_t m, int64_t parts, int lr) { return (m >> lr) + parts; }
+
+__device__ inline int64_t off_at(const int64_t* __restrict__ off, int64_t i, int64_t m) {
+    return min(max(off[i], (int64_t)0), m);
+}
+// Slot k's unit, for a whole wave (every lane passes the same k and gets the
+// same unit): the largest g with f(g) <= k, 64 probes a step.
+__device__ inline Unit wave_unit(const int64_t* __restrict__ off, int64_t parts, int64_t m, int lr, int64_t k) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = parts;  // f(lo) <= k or lo = 0; the answer is below hi
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + 63) >> 6;
+        const int64_t p = lo + (int64_t)(lane + 1) * step;
+        const bool in = p < hi;
+        const bool le = in && (off_at(off, in ? p : lo, m) >> lr) + p <= k;
+        const int c = __popcll(__ballot(le));  // f increases: the first c probes
+        lo += (int64_t)c * step;
+        hi = min(lo + step, hi);
+    }
+    Unit u;
+    u.begin = off_at(off, lo, m);
+    u.end = max(off_at(off, lo + 1, m), u.begin);
+    const int64_t slot = k - ((u.begin >> lr) + lo);
+    u.g = slot < 0 ? -1 : (int)lo;
+    u.slot = (int)max(slot, (int64_t)0);
+    u.r0 = min(u.begin + ((int64_t)u.slot << lr), u.end);
+    u.r1 = slot < 0 ? u.r0 : min(u.r0 + ((int64_t)1 << lr), u.end);
+    return u;
+}
+
+// A range of more than one unit, among those a launch enumerates: by range
+// where there are few of them, else by window of R rows, in which at most
+// one such range starts (its rows reach past the window), the last to start
+// there.  The window names its place in a workspace.  For a whole wave.
+struct Long {
+    int64_t g, begin, end, window;
+    bool found;
+};
+inline int64_t long_places(int64_t m, int lr) { return (m >> lr) + 1; }
+inline int64_t long_count(int64_t m, int64_t parts, int lr) { return std::min(parts, long_places(m, lr)); }
+__device__ inline Long wave_long(const int64_t* __restrict__ off, int64_t parts, int64_t m, int lr, int64_t i) {
+    const int lane = threadIdx.x & 63;
+    const bool by_range = parts < (m >> lr) + 1;
+    Long s;
+    if (by_range) {
+        s.g = i;
+    } else {
+        const int64_t want = ((i + 1) << lr) - 1;
+        int64_t lo = 0, hi = parts;
+        while (hi - lo > 1) {
+            const int64_t step = (hi - lo + 63) >> 6, p = lo + (int64_t)(lane + 1) * step;
+            const int c = __popcll(__ballot(p < hi && off_at(off, p < hi ? p : lo, m) <= want));
+            lo += (int64_t)c * step;
+            hi = min(lo + step, hi);
+        }
+        s.g = lo;
+    }
+    s.begin = off_at(off, s.g, m);
+    s.end = off_at(off, s.g + 1, m);
+    s.window = s.begin >> lr;
+    s.found = s.end - s.begin > ((int64_t)1 << lr) && (by_range || s.window == i);
+    return s;
+}
+// Workspace place of such a range's unit `slot`, which starts at row r0: of
+// the units of longer ranges at most two start in any window, one of them
+// its range's first.
+__device__ inline int64_t unit_place(int64_t r0, int slot, int lr) { return 2 * (r0 >> lr) + (slot == 0); }
+inline int64_t unit_places(int64_t m, int lr) { return 2 * ((m >> lr) + 1); }
+
+}  // namespace taurus

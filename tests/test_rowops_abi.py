@@ -1,0 +1,159 @@
+"""The operators on rows at the C boundary, without a GPU: signatures of the
+binding against the header, refusals before any device work, workspace sizes,
+and the wrapper's own checks."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2607_17374_amd import _native as N
+import paper_2607_17374_amd as T
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CALLS = ("taurus_lookup_rows", "taurus_lookup_rows_grad_bytes", "taurus_lookup_rows_grad", "taurus_grouped_linear",
+         "taurus_grouped_linear_grad_bytes", "taurus_grouped_linear_grad", "taurus_group_norm_bytes",
+         "taurus_group_norm", "taurus_group_norm_grad")
+
+
+def test_argument_types_match_the_header():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "taurus.h")).read(), flags=re.S)
+    kinds = {"int32_t": ctypes.c_int32, "int64_t": ctypes.c_int64, "float": ctypes.c_float, "int": ctypes.c_int}
+    for name in CALLS:
+        m = re.search(r"(\w+)\s+%s\s*\(([^)]*)\)\s*;" % name, text)
+        want = [ctypes.c_void_p if "*" in p else kinds[p.split()[0]] for p in m.group(2).split(",")]
+        assert N.SIGNATURES[name][1] == want, name
+        assert N.SIGNATURES[name][0] == kinds[m.group(1)], name
+
+
+P = 1 << 20  # a pointer no refused call follows
+
+
+def _lookup(**kw):
+    a = dict(table=P, dt=N.F32, n=10, d=8, ts=8, ids=P, m=4, scale=1.0, out=P, odt=N.F32, os=8, stream=None)
+    a.update(kw)
+    return N.lib().taurus_lookup_rows(*a.values())
+
+
+def _lookup_grad(**kw):
+    a = dict(grad=P, dt=N.F32, gs=8, ids=P, m=4, n=10, d=8, scale=1.0, acc=0, out=P, odt=N.F32, os=8, work=P,
+             bytes=1 << 40, stream=None)
+    a.update(kw)
+    return N.lib().taurus_lookup_rows_grad(*a.values())
+
+
+def _linear(**kw):
+    a = dict(x=P, dt=N.BF16, m=16, k=8, xs=8, off=P, groups=2, w=P, n=8, bias=None, out=P, odt=N.F32, os=8,
+             stream=None)
+    a.update(kw)
+    return N.lib().taurus_grouped_linear(*a.values())
+
+
+def _linear_grad(**kw):
+    a = dict(grad=P, gs=8, x=P, xs=8, dt=N.BF16, m=16, k=8, n=8, off=P, groups=2, w=P, dx=P, dxs=8, dw=P, wdt=N.F32,
+             db=P, work=P, bytes=1 << 40, stream=None)
+    a.update(kw)
+    return N.lib().taurus_grouped_linear_grad(*a.values())
+
+
+def _norm(**kw):
+    a = dict(x=P, dt=N.BF16, m=16, d=8, xs=8, groups=2, off=None, segs=0, w=None, b=None, eps=1e-5, act=0, out=P,
+             odt=N.F32, os=8, mean=None, rstd=None, work=P, bytes=1 << 40, stream=None)
+    a.update(kw)
+    return N.lib().taurus_group_norm(*a.values())
+
+
+def _norm_grad(**kw):
+    a = dict(grad=P, gs=8, x=P, xs=8, dt=N.BF16, m=16, d=8, groups=2, off=None, segs=0, w=None, b=None, mean=P,
+             rstd=P, act=0, dx=P, dxs=8, dw=P, db=P, work=P, bytes=1 << 40, stream=None)
+    a.update(kw)
+    return N.lib().taurus_group_norm_grad(*a.values())
+
+
+BAD = [
+    (_lookup, dict(dt=3), "none of"), (_lookup, dict(odt=-1), "none of"), (_lookup, dict(n=-1), "table rows"),
+    (_lookup, dict(n=1 << 31), "table rows"), (_lookup, dict(m=-1), "ids"), (_lookup, dict(m=1 << 31), "ids"),
+    (_lookup, dict(d=0), "row length"), (_lookup, dict(d=(1 << 24) + 1), "row length"),
+    (_lookup, dict(ts=7), "apart"), (_lookup, dict(os=7), "apart"), (_lookup, dict(ts=1 << 30), "apart"),
+    (_lookup, dict(table=None), "table is null"), (_lookup, dict(out=None), "out is null"),
+    (_lookup, dict(ids=None), "ids is null"), (_lookup, dict(ids=P + 2), "ids is not aligned"),
+    (_lookup, dict(table=P + 2), "table is not aligned"), (_lookup, dict(odt=N.BF16, out=P + 1), "out is not aligned"),
+    (_lookup_grad, dict(dt=9), "none of"), (_lookup_grad, dict(gs=7), "apart"), (_lookup_grad, dict(os=7), "apart"),
+    (_lookup_grad, dict(m=5000, bytes=16), "workspace has 16"), (_lookup_grad, dict(m=5000, work=None), "workspace is null"),
+    (_lookup_grad, dict(m=5000, work=P + 4), "16-byte aligned"), (_lookup_grad, dict(grad=None), "grad is null"),
+    (_lookup_grad, dict(ids=None), "ids is null"), (_lookup_grad, dict(out=None), "out is null"),
+    (_linear, dict(dt=7), "none of"), (_linear, dict(odt=7), "none of"), (_linear, dict(m=-1), "rows"),
+    (_linear, dict(groups=-1), "types"), (_linear, dict(k=0), "input width"), (_linear, dict(n=0), "output width"),
+    (_linear, dict(k=65537), "input width"), (_linear, dict(off=None), "off is null"),
+    (_linear, dict(off=P + 4), "off is not aligned"), (_linear, dict(w=None), "weight is null"),
+    (_linear, dict(x=None), "x is null"), (_linear, dict(xs=7), "apart"), (_linear, dict(os=7), "apart"),
+    (_linear, dict(bias=P + 2), "bias is not aligned"), (_linear, dict(x=P + 1), "x is not aligned"),
+    (_linear_grad, dict(wdt=5), "none of"), (_linear_grad, dict(gs=7), "apart"), (_linear_grad, dict(xs=7), "apart"),
+    (_linear_grad, dict(dxs=7), "apart"), (_linear_grad, dict(w=None), "weight is null"),
+    (_linear_grad, dict(x=None), "x is null"), (_linear_grad, dict(m=5000, bytes=1), "workspace has 1"),
+    (_linear_grad, dict(m=5000, work=None), "workspace is null"), (_linear_grad, dict(dw=P + 2), "dweight is not"),
+    (_linear_grad, dict(db=P + 2), "dbias is not"),
+    (_norm, dict(d=0), "channels"), (_norm, dict(d=2049, xs=2049, os=2049), "channels"),
+    (_norm, dict(groups=3), "do not make"), (_norm, dict(groups=0), "groups"), (_norm, dict(groups=9), "groups"),
+    (_norm, dict(act=3), "activation"), (_norm, dict(eps=-1.0), "eps"), (_norm, dict(eps=float("nan")), "eps"),
+    (_norm, dict(mean=P), "together"), (_norm, dict(rstd=P), "together"), (_norm, dict(xs=7), "apart"),
+    (_norm, dict(off=P + 4, segs=2), "off is not aligned"), (_norm, dict(segs=-1), "segments"),
+    (_norm, dict(w=P + 1), "not aligned"), (_norm, dict(off=P, segs=2, m=5000, bytes=8), "workspace has 8"),
+    (_norm, dict(x=None), "x is null"), (_norm, dict(out=None), "out is null"),
+    (_norm_grad, dict(mean=None), "mean is null"), (_norm_grad, dict(rstd=None), "rstd is null"),
+    (_norm_grad, dict(bytes=8), "workspace has 8"), (_norm_grad, dict(work=None), "workspace is null"),
+    (_norm_grad, dict(dxs=7), "apart"), (_norm_grad, dict(gs=7), "apart"), (_norm_grad, dict(db=P + 2), "not aligned"),
+    (_norm_grad, dict(act=-1), "activation"), (_norm_grad, dict(grad=None), "grad is null"),
+]
+
+
+@pytest.mark.parametrize("i", range(len(BAD)))
+def test_refused_before_device_work(i):
+    call, change, text = BAD[i]
+    assert call(**change) == N.E_INVALID, change
+    assert text in N.last_error(), N.last_error()
+
+
+def test_nothing_to_do_is_ok_without_pointers():
+    assert _lookup(m=0, table=None, ids=None, out=None) == N.OK
+    assert _lookup_grad(n=0, grad=None, ids=None, out=None, work=None, bytes=0) == N.OK
+    assert _linear(m=0, x=None, out=None, w=None) == N.OK
+    assert _linear(groups=0, off=None) == N.OK
+    assert _linear_grad(groups=0, off=None) == N.OK
+    assert _norm(m=0, x=None, out=None) == N.OK
+    assert _norm(off=P, segs=0) == N.OK
+
+
+def test_workspace_sizes():
+    L = N.lib()
+    for m in (0, 1, 1024):
+        assert L.taurus_lookup_rows_grad_bytes(m, 64) == 0
+    assert L.taurus_lookup_rows_grad_bytes(1025, 64) > 16 * 1025
+    # two sums of 32 places each at the first level, then 1/16 as many a level
+    m, d = 1 << 20, 128
+    level = 2 * (m // 32) * (4 * d + 8)
+    assert 16 * m + level < L.taurus_lookup_rows_grad_bytes(m, d) < 18 * m + 1.1 * level + (1 << 20)
+    assert L.taurus_grouped_linear_grad_bytes(256, 64, 64) == 0
+    assert L.taurus_grouped_linear_grad_bytes(257, 64, 64) >= 2 * 2 * 64 * 65 * 4
+    assert L.taurus_group_norm_bytes(10**6, 128, 8, 0, 0, 0) == 0
+    assert L.taurus_group_norm_bytes(10**6, 128, 8, 100, 1, 0) > 0
+    assert L.taurus_group_norm_bytes(10**6, 128, 8, 0, 0, 1) > 0
+    for bad in (L.taurus_lookup_rows_grad_bytes(-1, 4), L.taurus_lookup_rows_grad_bytes(4, 0),
+                L.taurus_grouped_linear_grad_bytes(4, 0, 4), L.taurus_grouped_linear_grad_bytes(1 << 31, 4, 4),
+                L.taurus_group_norm_bytes(4, 6, 4, 0, 0, 0), L.taurus_group_norm_bytes(4, 4096, 4, 0, 0, 1)):
+        assert bad == N.E_INVALID
+
+
+def test_wrapper_refuses_host_tensors():
+    x, ids, off = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int32), torch.tensor([0, 4])
+    for call in (lambda: T.lookup_rows(x, ids), lambda: T.lookup_rows_grad(x, ids, 4),
+                 lambda: T.grouped_linear(x, off, torch.zeros(1, 8, 8)),
+                 lambda: T.grouped_linear_grad(x, x, off, torch.zeros(1, 8, 8)), lambda: T.group_norm(x),
+                 lambda: T.group_norm_grad(x, x, 1, None, None, x, x)):
+        with pytest.raises(ValueError, match="device tensor"):
+            call()
+    with pytest.raises(ValueError, match="out, which must be given"):
+        T.lookup_rows_grad(x, ids, 4, accumulate=True)
+    with pytest.raises(ValueError, match="need names"):
+        T.group_norm_grad(x, x, 1, None, None, x, x, need=("dx",))
