@@ -403,7 +403,7 @@ int taurus_permute_rows(const void* in, void* out, int64_t n, int64_t row_bytes,
  *     as each has a workspace of its own.
  *   - Pointers are device memory aligned to their element type.  Row arrays
  *     are [rows][stride] with the row's values first, stride >= the row's
- *     length (at most 2^29); 16-byte aligned arrays whose row length and
+ *     length (at most 2^22); 16-byte aligned arrays whose row length and
  *     stride are whole 16-byte pieces are the fast case, any other is
  *     correct.  Outputs must not overlap inputs.
  *   - Arithmetic is fp32 (fp32 matrix cores, or 16-bit ones with fp32
@@ -427,7 +427,7 @@ int taurus_permute_rows(const void* in, void* out, int64_t n, int64_t row_bytes,
  * Rows looked up by id, scaled: out[i] = scale * table[ids[i]] for i < m
  * (learned features of vertices that have none, or the rows of asked-for
  * vertices out of a layer's output).  table: [n][table_stride] of
- * table_dtype, rows of d values (1 <= d <= 2^24); ids: int32[m], in any
+ * table_dtype, rows of d values (1 <= d <= 2^22); ids: int32[m], in any
  * order, repeats allowed; an id outside [0, n) names no row and its output
  * row is zeros (-1 pads a batch).  out: [m][out_stride] of out_dtype.
  */
@@ -472,7 +472,8 @@ int taurus_grouped_linear(const void* x, int32_t dtype, int64_t m, int64_t d_in,
  * Each may be NULL and is then not computed.  Every type's dweight and dbias
  * are written (zeros for a type without rows).
  */
-int64_t taurus_grouped_linear_grad_bytes(int64_t m, int64_t d_in, int64_t d_out);
+int64_t taurus_grouped_linear_grad_bytes(int32_t dtype, int64_t m, int64_t groups, int64_t d_in,
+                                         int64_t d_out);
 int taurus_grouped_linear_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride,
                                int32_t dtype, int64_t m, int64_t d_in, int64_t d_out, const int64_t* off,
                                int64_t groups, const void* weight, void* dx, int64_t dx_stride, void* dweight,

@@ -117,7 +117,7 @@ for _name, _res, _args in (
         ("taurus_lookup_rows_grad_bytes", ctypes.c_int64, "ll"),
         ("taurus_lookup_rows_grad", ctypes.c_int, "pilplllfipilplp"),
         ("taurus_grouped_linear", ctypes.c_int, "pilllplplppilp"),
-        ("taurus_grouped_linear_grad_bytes", ctypes.c_int64, "lll"),
+        ("taurus_grouped_linear_grad_bytes", ctypes.c_int64, "illll"),
         ("taurus_grouped_linear_grad", ctypes.c_int, "plplilllplpplpipplp"),
         ("taurus_group_norm_bytes", ctypes.c_int64, "llllii"),
         ("taurus_group_norm", ctypes.c_int, "pillllplppfipilppplp"),

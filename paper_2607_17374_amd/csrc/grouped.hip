@@ -38,9 +38,19 @@ struct Tile {
     static constexpr int E = 8, STAGE = 64, KBS = 2;  // KBS: matrix steps a stage (32 deep)
     typedef uint4 frag;
     static __device__ inline floatx4 mma(frag a, frag b, floatx4 c) { return mfma16<DT>(a, b, c); }
-    static __device__ inline frag ones() {
+    template <int MI, int NI>
+    static __device__ inline void mma_all(const frag (&fn)[NI], const frag (&fm)[MI], floatx4 (&acc)[MI][NI]) {
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+#pragma unroll
+            for (int j = 0; j < NI; j++) acc[i][j] = mma(fn[j], fm[i], acc[i][j]);
+    }
+    // sums of a column over the contraction: its products with ones, which
+    // are exact; a lane of column block row 0 ends with four columns' sums
+    typedef floatx4 sums_t;
+    static __device__ inline void add_sums(frag a, sums_t& s) {
         const uint32_t one = DT == TAURUS_BF16 ? 0x3f803f80u : 0x3c003c00u;
-        return make_uint4(one, one, one, one);
+        s = mma(a, make_uint4(one, one, one, one), s);
     }
 };
 template <>
@@ -53,52 +63,89 @@ struct Tile<TAURUS_F32> {
         c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.z, b.z, c, 0, 0, 0);
         return __builtin_amdgcn_mfma_f32_16x16x4f32(a.w, b.w, c, 0, 0, 0);
     }
-    static __device__ inline frag ones() { return make_float4(1.f, 1.f, 1.f, 1.f); }
+    // one component of the contraction at a time: consecutive products go to
+    // different accumulators instead of one dependent chain
+    template <int MI, int NI>
+    static __device__ inline void mma_all(const frag (&fn)[NI], const frag (&fm)[MI], floatx4 (&acc)[MI][NI]) {
+        auto step = [&](auto get) {
+#pragma unroll
+            for (int i = 0; i < MI; i++)
+#pragma unroll
+                for (int j = 0; j < NI; j++)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(get(fn[j]), get(fm[i]), acc[i][j], 0, 0, 0);
+        };
+        step([](const frag& f) { return f.x; });
+        step([](const frag& f) { return f.y; });
+        step([](const frag& f) { return f.z; });
+        step([](const frag& f) { return f.w; });
+    }
+    // here by the vector units (products with ones would take a quarter of
+    // the matrix cores' time again): a lane's part of its column's sum
+    typedef float sums_t;
+    static __device__ inline void add_sums(frag a, sums_t& s) { s += (a.x + a.y) + (a.z + a.w); }
 };
 
-// Sixteen bytes at column c of a row of `cols` values; values past the end
-// (and everything, unless `in`) are zero.  AL: rows are whole 16-byte pieces.
-template <int DT, bool AL>
-__device__ inline uint4 load_piece(const void* __restrict__ base, int64_t row_at, int c, int cols, bool in) {
+// Sixteen bytes at column c of a row of `cols` values, value by value; values
+// past the end (and everything, unless `in`) are zero.
+template <int DT>
+__device__ inline uint4 load_values(const void* __restrict__ base, int64_t row_at, int c, int cols, bool in) {
     constexpr int E = Tile<DT>::E, SZ = type_bytes<DT>;
     const char* p = static_cast<const char*>(base) + row_at * SZ;
-    if constexpr (AL) {
-        return in && c < cols ? *reinterpret_cast<const uint4*>(p + (int64_t)c * SZ) : make_uint4(0, 0, 0, 0);
-    } else {
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (in)
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (in)
 #pragma unroll
-            for (int e = 0; e < E; e++)
-                if (c + e < cols) {
-                    if constexpr (SZ == 4) w[e] = *reinterpret_cast<const uint32_t*>(p + (int64_t)(c + e) * 4);
-                    else w[e >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + (int64_t)(c + e) * 2) << (16 * (e & 1));
-                }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
+        for (int e = 0; e < E; e++)
+            if (c + e < cols) {
+                if constexpr (SZ == 4) w[e] = *reinterpret_cast<const uint32_t*>(p + (int64_t)(c + e) * 4);
+                else w[e >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + (int64_t)(c + e) * 2) << (16 * (e & 1));
+            }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Rows of whole 16-byte pieces (AL) go through a buffer resource over the
+// rows that exist: a thread's pieces differ by a fixed number of rows, so it
+// keeps one 32-bit offset, and what lies past the resource's end reads as
+// zeros without a branch.  A piece past its row's end takes the offset
+// OUTSIDE, which stays past every end (tiles span less than 2^31 bytes, at
+// most 128 rows of the widest stride) and wraps for no row of the tile.
+constexpr uint32_t OUTSIDE = 0x80000000u;
+__device__ inline __amdgpu_buffer_rsrc_t piece_rsrc(const void* base, int64_t at, int64_t bytes) {
+    const char* p = static_cast<const char*>(base) + at;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0,
+                                             (int)(uint32_t)min(max(bytes, (int64_t)0), (int64_t)OUTSIDE), 0x00020000);
+}
+__device__ inline uint4 load_buffer(__amdgpu_buffer_rsrc_t rs, uint32_t offset) {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, offset, 0, 0));
 }
 
 // An operand along the contraction: ROWS rows of one stage.
 template <int DT, int ROWS, bool AL>
 struct Along {
-    static constexpr int BYTES = ROWS * 128, PER = ROWS * 8 / 256;
+    static constexpr int BYTES = ROWS * 128, PER = ROWS * 8 / 256, SZ = type_bytes<DT>;
     static_assert(ROWS * 8 % 256 == 0, "whole pieces per thread");
     const void* base;
     int64_t at0, stride;  // first row's offset, values between rows
     int rows, depth;      // rows that exist (others are zero), contraction length
     __device__ inline void load(int k0, uint4 (&v)[PER]) const {
+        const int r0 = threadIdx.x >> 3, p = threadIdx.x & 7, c = k0 + p * Tile<DT>::E;
+        if constexpr (AL) {
+            const auto rs = piece_rsrc(base, at0 * SZ, (int64_t)rows * stride * SZ);
+            const uint32_t row = (uint32_t)stride * SZ;
+            const uint32_t off = c < depth ? (uint32_t)r0 * row + (uint32_t)c * SZ : OUTSIDE;
 #pragma unroll
-        for (int q = 0; q < PER; q++) {
-            const int i = q * 256 + threadIdx.x, r = i >> 3, p = i & 7;
-            v[q] = load_piece<DT, AL>(base, at0 + (int64_t)min(r, rows - 1) * stride, k0 + p * Tile<DT>::E, depth,
-                                      r < rows);
+            for (int q = 0; q < PER; q++) v[q] = load_buffer(rs, off + q * 32 * row);
+        } else {
+#pragma unroll
+            for (int q = 0; q < PER; q++) {
+                const int r = q * 32 + r0;
+                v[q] = load_values<DT>(base, at0 + (int64_t)min(r, rows - 1) * stride, c, depth, r < rows);
+            }
         }
     }
     static __device__ inline void stage(char* lds, const uint4 (&v)[PER]) {
+        const int r0 = threadIdx.x >> 3, p = threadIdx.x & 7;
+        char* at = lds + r0 * 128 + ((p ^ (r0 & 7)) << 4);  // 32 rows on, the exchange is the same
 #pragma unroll
-        for (int q = 0; q < PER; q++) {
-            const int i = q * 256 + threadIdx.x, r = i >> 3, p = i & 7;
-            *reinterpret_cast<uint4*>(lds + r * 128 + ((p ^ (r & 7)) << 4)) = v[q];
-        }
+        for (int q = 0; q < PER; q++) *reinterpret_cast<uint4*>(at + q * 32 * 128) = v[q];
     }
     // rows [r0, r0 + 16), matrix step kb
     static __device__ inline typename Tile<DT>::frag read(const char* lds, int r0, int kb) {
@@ -110,10 +157,10 @@ struct Along {
 // An operand across the contraction: one stage of contraction rows, COLS wide.
 template <int DT, int COLS, bool AL>
 struct Across {
-    static constexpr int PIECES = COLS / Tile<DT>::E;  // a row
+    static constexpr int PIECES = COLS / Tile<DT>::E, STEP = 256 / PIECES, SZ = type_bytes<DT>;
     static constexpr int PITCH = DT == TAURUS_F32 ? COLS * 4 + 16 : COLS * 2;
-    static constexpr int BYTES = Tile<DT>::STAGE * PITCH, PER = Tile<DT>::STAGE * PIECES / 256;
-    static_assert(Tile<DT>::STAGE * PIECES % 256 == 0, "whole pieces per thread");
+    static constexpr int BYTES = Tile<DT>::STAGE * PITCH, PER = Tile<DT>::STAGE / STEP;
+    static_assert(256 % PIECES == 0 && Tile<DT>::STAGE % STEP == 0 && STEP % 4 == 0, "whole pieces per thread");
     const void* base;
     int64_t at0, stride;  // first contraction row's offset at the tile's first column; values between rows
     int depth, cols;      // contraction rows that exist, columns from the tile's first on
@@ -128,19 +175,26 @@ struct Across {
         else return k * PITCH + unit_of(k, p >> 1) * 32 + (p & 1) * 16;
     }
     __device__ inline void load(int k0, uint4 (&v)[PER]) const {
+        const int k = threadIdx.x / PIECES, p = threadIdx.x % PIECES, c = p * Tile<DT>::E;
+        if constexpr (AL) {
+            const auto rs = piece_rsrc(base, (at0 + (int64_t)k0 * stride) * SZ, (int64_t)(depth - k0) * stride * SZ);
+            const uint32_t row = (uint32_t)stride * SZ;
+            const uint32_t off = c < cols ? (uint32_t)k * row + (uint32_t)c * SZ : OUTSIDE;
 #pragma unroll
-        for (int q = 0; q < PER; q++) {
-            const int i = q * 256 + threadIdx.x, k = i / PIECES, p = i % PIECES;
-            const bool in = k0 + k < depth;
-            v[q] = load_piece<DT, AL>(base, at0 + (int64_t)(in ? k0 + k : 0) * stride, p * Tile<DT>::E, cols, in);
+            for (int q = 0; q < PER; q++) v[q] = load_buffer(rs, off + q * STEP * row);
+        } else {
+#pragma unroll
+            for (int q = 0; q < PER; q++) {
+                const int r = k0 + k + q * STEP;
+                const bool in = r < depth;
+                v[q] = load_values<DT>(base, at0 + (int64_t)(in ? r : 0) * stride, c, cols, in);
+            }
         }
     }
     static __device__ inline void stage(char* lds, const uint4 (&v)[PER]) {
+        const int k = threadIdx.x / PIECES, p = threadIdx.x % PIECES;
 #pragma unroll
-        for (int q = 0; q < PER; q++) {
-            const int i = q * 256 + threadIdx.x;
-            *reinterpret_cast<uint4*>(lds + piece_at(i / PIECES, i % PIECES)) = v[q];
-        }
+        for (int q = 0; q < PER; q++) *reinterpret_cast<uint4*>(lds + piece_at(k + q * STEP, p)) = v[q];
     }
     // columns [c0, c0 + 16), matrix step kb
     static __device__ inline typename Tile<DT>::frag read(const char* lds, int c0, int kb) {
@@ -164,57 +218,73 @@ struct Across {
     }
 };
 
-// One tile's products over the contraction [0, depth): the wave's rows from
-// m0 on (MI blocks of 16) and columns from n0 on (NI blocks).  SUMS: the
-// sums of the second operand over the contraction too, as its products with
-// ones (bias gradient).
+// One stage's products: the wave's rows from m0 on (MI blocks of 16) and
+// columns from n0 on (NI blocks).  SUMS: the sums of the second operand over
+// the contraction too, as its products with ones (bias gradient).
 template <int DT, class OpM, class OpN, int MI, int NI, bool SUMS>
-__device__ inline void tile_product(const OpM& om, const OpN& on, int depth, char* lds, int m0, int n0, bool sums,
-                                    floatx4 (&acc)[MI][NI], floatx4 (&nsum)[NI]) {
-    constexpr int STAGE = Tile<DT>::STAGE, BUF = OpM::BYTES + OpN::BYTES;
-    const int stages = (depth + STAGE - 1) / STAGE;
+__device__ inline void stage_product(const char* lds, int m0, int n0, bool sums, floatx4 (&acc)[MI][NI],
+                                     typename Tile<DT>::sums_t (&nsum)[SUMS ? NI : 1]) {
 #pragma unroll
-    for (int j = 0; j < NI; j++) {
-        nsum[j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int kb = 0; kb < Tile<DT>::KBS; kb++) {
+        typename Tile<DT>::frag fm[MI], fn[NI];
 #pragma unroll
-        for (int i = 0; i < MI; i++) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NI; j++) fn[j] = OpN::read(lds + OpM::BYTES, n0 + 16 * j, kb);
+#pragma unroll
+        for (int i = 0; i < MI; i++) fm[i] = OpM::read(lds, m0 + 16 * i, kb);
+        Tile<DT>::mma_all(fn, fm, acc);
+        if constexpr (SUMS)
+            if (sums)
+#pragma unroll
+                for (int j = 0; j < NI; j++) Tile<DT>::add_sums(fn[j], nsum[j]);
     }
+}
+
+// A workgroup's tiles, one after another, as one stream of stages: while a
+// stage's products run, the next one's pieces, of this tile or the next, are
+// on their way to registers, so that only the first stage waits for memory.
+// (A workgroup a tile took 353 us for 1M bf16 rows 128 -> 256, two stages a
+// tile, most of it spent starting.)  tiles.seek moves to the next tile with
+// work and says whether there is one, tiles.done ends the one before it.
+template <int DT, class OpM, class OpN, int MI, int NI, bool SUMS, class Tiles>
+__device__ inline void stream_tiles(Tiles& tiles, char* lds, int m0, int n0) {
+    constexpr int STAGE = Tile<DT>::STAGE;
+    OpM om;
+    OpN on;
+    int depth = 0;
     uint4 vm[OpM::PER], vn[OpN::PER];
-    om.load(0, vm);
-    on.load(0, vn);
-    __syncthreads();  // the buffers may still be read for an earlier tile
-    OpM::stage(lds, vm);
-    OpN::stage(lds + OpM::BYTES, vn);
-    __syncthreads();
-    for (int st = 0; st < stages; st++) {
-        const char* b = lds + (st & 1) * BUF;
-        const bool more = st + 1 < stages;
-        if (more) {
-            om.load((st + 1) * STAGE, vm);
-            on.load((st + 1) * STAGE, vn);
+    bool have = tiles.seek(om, on, depth);
+    if (have) {
+        om.load(0, vm);
+        on.load(0, vn);
+    }
+    while (have) {
+        floatx4 acc[MI][NI];
+        typename Tile<DT>::sums_t nsum[SUMS ? NI : 1] = {};
+#pragma unroll
+        for (int j = 0; j < NI; j++) {
+#pragma unroll
+            for (int i = 0; i < MI; i++) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
-#pragma unroll
-        for (int kb = 0; kb < Tile<DT>::KBS; kb++) {
-            typename Tile<DT>::frag fm[MI], fn[NI];
-#pragma unroll
-            for (int j = 0; j < NI; j++) fn[j] = OpN::read(b + OpM::BYTES, n0 + 16 * j, kb);
-#pragma unroll
-            for (int i = 0; i < MI; i++) fm[i] = OpM::read(b, m0 + 16 * i, kb);
-#pragma unroll
-            for (int i = 0; i < MI; i++)
-#pragma unroll
-                for (int j = 0; j < NI; j++) acc[i][j] = Tile<DT>::mma(fn[j], fm[i], acc[i][j]);
-            if constexpr (SUMS)
-                if (sums)
-#pragma unroll
-                    for (int j = 0; j < NI; j++) nsum[j] = Tile<DT>::mma(fn[j], Tile<DT>::ones(), nsum[j]);
+        const bool sums = SUMS && tiles.enter(m0);
+        const int stages = max((depth + STAGE - 1) / STAGE, 1);  // none: one of zeros
+        for (int st = 0; st < stages; st++) {
+            __syncthreads();  // the stage before is read
+            OpM::stage(lds, vm);
+            OpN::stage(lds + OpM::BYTES, vn);
+            __syncthreads();
+            if (st + 1 < stages) {
+                om.load((st + 1) * STAGE, vm);
+                on.load((st + 1) * STAGE, vn);
+            } else {
+                have = tiles.seek(om, on, depth);
+                if (have) {
+                    om.load(0, vm);
+                    on.load(0, vn);
+                }
+            }
+            stage_product<DT, OpM, OpN, MI, NI, SUMS>(lds, m0, n0, sums, acc, nsum);
         }
-        if (more) {  // the other buffer was last read before the previous barrier
-            char* o = lds + ((st + 1) & 1) * BUF;
-            OpM::stage(o, vm);
-            OpN::stage(o + OpM::BYTES, vn);
-        }
-        __syncthreads();
+        tiles.done(acc, nsum);
     }
 }
 
@@ -234,7 +304,8 @@ __device__ inline void place_of(int64_t b, int64_t slots, int tiles, int64_t& sl
     }
 }
 
-// Four consecutive values of an output row of n columns, at column c
+// Four consecutive values of an output row of n columns, at column c; whole:
+// rows are whole vectors of four.
 __device__ inline void put4(void* out, int dtype, int64_t row_at, int c, int n, bool whole, floatx4 v) {
     if (whole) {
         if (c < n) {
@@ -250,10 +321,32 @@ __device__ inline void put4(void* out, int dtype, int64_t row_at, int c, int n, 
             store_as<1>(dtype, out, row_at + c + e, f);
         }
 }
+// Two blocks of 16 columns of a row, columns c + 4 lk of each in v and w,
+// stored as 16-bit values.  Lanes 16 apart exchange halves, so that a lane
+// stores eight consecutive values: the first block's for even lk, the
+// second's for odd.
+template <int DT>
+__device__ inline void put_pair16(void* out, int64_t row_at, int c, int n, bool in, floatx4 v, floatx4 w) {
+    auto pack = [](float a, float b) {
+        if constexpr (DT == TAURUS_BF16)
+            return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) |
+                   (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
+        else
+            return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)a) |
+                   (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
+    };
+    const int lk = (threadIdx.x & 63) >> 4;
+    // rows 1 and 3 of the first with rows 0 and 2 of the second
+    const auto lo = __builtin_amdgcn_permlane16_swap(pack(v[0], v[1]), pack(w[0], w[1]), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(pack(v[2], v[3]), pack(w[2], w[3]), false, false);
+    const int at = c + 16 * (lk & 1) + 8 * (lk >> 1);
+    if (in && at < n)
+        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + row_at + at) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+}
 
 // ------------------------------------------------------- y = x W, dx = dy W^T
 
-constexpr int ROW_LG = 7, ROW_TILE = 1 << ROW_LG;  // rows a workgroup
+constexpr int ROW_TILE = 128;  // rows a tile
 struct RowsArgs {
     const void* x;
     int64_t m, xs;
@@ -263,53 +356,97 @@ struct RowsArgs {
     const void* w;
     const float* bias;
     void* y;
-    int y_dtype, whole;  // whole: output rows are whole vectors of four
+    int y_dtype, whole;  // whole: rows of y are whole vectors of four (1) or, 16-bit, eight (2)
     int64_t ys, slots;
     int tiles;
 };
 // WT: W_g is [cols][depth] (dx), else [depth][cols] (y)
 template <int DT, bool WT, int TN, bool AL>
-__global__ __launch_bounds__(256) void k_grouped_rows(RowsArgs a) {
+struct RowTiles {
     typedef Along<DT, ROW_TILE, AL> OpM;
     typedef std::conditional_t<WT, Along<DT, TN, AL>, Across<DT, TN, AL>> OpN;
-    constexpr int WN = TN / 64, WM = 4 / WN, MI = ROW_TILE / WM / 16, NI = 4;
-    __shared__ __align__(16) char lds[2 * (OpM::BYTES + OpN::BYTES)];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
-    const int m0 = wave / WN * MI * 16, n0 = wave % WN * 64;
-    for (int64_t b = blockIdx.x; b < a.slots * a.tiles; b += gridDim.x) {
-        int64_t slot;
-        int tile;
-        place_of(b, a.slots, a.tiles, slot, tile);
-        const Unit u = wave_unit(a.off, a.groups, a.m, ROW_LG, slot);
-        if (u.r0 >= u.r1) continue;  // the same for the whole workgroup
-        const int c0 = tile * TN;
-        const int64_t w0 = (int64_t)u.g * a.depth * a.cols;
-        const OpM om{a.x, u.r0 * a.xs, a.xs, (int)(u.r1 - u.r0), a.depth};
-        OpN on;
-        if constexpr (WT) on = OpN{a.w, w0 + (int64_t)c0 * a.depth, a.depth, min(TN, a.cols - c0), a.depth};
-        else on = OpN{a.w, w0 + c0, a.cols, a.depth, a.cols - c0};
-        floatx4 acc[MI][NI], none[NI];
-        tile_product<DT, OpM, OpN, MI, NI, false>(om, on, a.depth, lds, m0, n0, false, acc, none);
+    static constexpr int WN = TN / 64, WM = 4 / WN, MI = ROW_TILE / WM / 16, NI = 4;
+    const RowsArgs& a;
+    Units units;
+    int64_t b;
+    int m0, n0;
+    int64_t r0, r1, next_r0 = 0, next_r1 = 0;
+    int g, c0, next_g = 0, next_c0 = 0;
+    __device__ RowTiles(const RowsArgs& a_, int m0_, int n0_)
+        : a(a_), units(a_.off, a_.groups, a_.m, ROW_TILE), b(blockIdx.x), m0(m0_), n0(n0_) {}
+    __device__ bool enter(int) { return false; }
+    __device__ bool seek(OpM& om, OpN& on, int& depth) {
+        r0 = next_r0;  // the tile that is now under way
+        r1 = next_r1;
+        g = next_g;
+        c0 = next_c0;
+        for (; b < a.slots * a.tiles; b += gridDim.x) {
+            int64_t slot;
+            int tile;
+            place_of(b, a.slots, a.tiles, slot, tile);
+            const Unit u = units.at(slot);
+            if (u.r0 >= u.r1) continue;  // the same for the whole workgroup
+            next_r0 = u.r0;
+            next_r1 = u.r1;
+            next_g = u.g;
+            next_c0 = tile * TN;
+            depth = a.depth;
+            const int64_t w0 = (int64_t)u.g * a.depth * a.cols;
+            om = OpM{a.x, u.r0 * a.xs, a.xs, (int)(u.r1 - u.r0), a.depth};
+            if constexpr (WT) on = OpN{a.w, w0 + (int64_t)next_c0 * a.depth, a.depth, min(TN, a.cols - next_c0), a.depth};
+            else on = OpN{a.w, w0 + next_c0, a.cols, a.depth, a.cols - next_c0};
+            b += gridDim.x;
+            return true;
+        }
+        return false;
+    }
+    __device__ void done(floatx4 (&acc)[MI][NI], typename Tile<DT>::sums_t (&)[1]) {
+        const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
 #pragma unroll
         for (int j = 0; j < NI; j++) {
             const int c = c0 + n0 + 16 * j + 4 * lk;
-            floatx4 bias = floatx4{0.f, 0.f, 0.f, 0.f};
-            if (a.bias)
+            if (a.bias) {
+                floatx4 bias;
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (c + e < a.cols) bias[e] = a.bias[(int64_t)u.g * a.cols + c + e];
+                for (int e = 0; e < 4; e++) bias[e] = c + e < a.cols ? a.bias[(int64_t)g * a.cols + c + e] : 0.f;
 #pragma unroll
-            for (int i = 0; i < MI; i++) {
-                const int64_t r = u.r0 + m0 + 16 * i + li;
-                if (r < u.r1) put4(a.y, a.y_dtype, r * a.ys, c, a.cols, a.whole, acc[i][j] + bias);
+                for (int i = 0; i < MI; i++) acc[i][j] += bias;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const int64_t r = r0 + m0 + 16 * i + li;
+            const bool in = r < r1;
+            if (a.whole == 2) {
+#pragma unroll
+                for (int j = 0; j < NI; j += 2) {
+                    const int c = c0 + n0 + 16 * j;
+                    if (a.y_dtype == TAURUS_BF16)
+                        put_pair16<TAURUS_BF16>(a.y, r * a.ys, c, a.cols, in, acc[i][j], acc[i][j + 1]);
+                    else
+                        put_pair16<TAURUS_F16>(a.y, r * a.ys, c, a.cols, in, acc[i][j], acc[i][j + 1]);
+                }
+            } else if (in) {
+#pragma unroll
+                for (int j = 0; j < NI; j++)
+                    put4(a.y, a.y_dtype, r * a.ys, c0 + n0 + 16 * j + 4 * lk, a.cols, a.whole, acc[i][j]);
             }
         }
     }
+};
+template <int DT, bool WT, int TN, bool AL>
+__global__ __launch_bounds__(256, TN == 64 ? 4 : 3) void k_grouped_rows(RowsArgs a) {
+    typedef RowTiles<DT, WT, TN, AL> T;
+    __shared__ __align__(16) char lds[T::OpM::BYTES + T::OpN::BYTES];
+    const int wave = threadIdx.x >> 6, m0 = wave / T::WN * T::MI * 16, n0 = wave % T::WN * 64;
+    T tiles(a, m0, n0);
+    stream_tiles<DT, typename T::OpM, typename T::OpN, T::MI, T::NI, false>(tiles, lds, m0, n0);
 }
 
 template <int DT, bool WT, int TN>
 static void rows_al(bool al, const RowsArgs& a, hipStream_t s) {
-    const unsigned grid = grid_for(a.slots * a.tiles);
+    // as many workgroups as are resident at once
+    const unsigned grid = (unsigned)std::min(a.slots * a.tiles, (int64_t)(TN == 64 ? 4 : 3) * compute_units());
     if (al) k_grouped_rows<DT, WT, TN, true><<<grid, 256, 0, s>>>(a);
     else k_grouped_rows<DT, WT, TN, false><<<grid, 256, 0, s>>>(a);
     TAURUS_CHECK_LAUNCH();
@@ -317,14 +454,15 @@ static void rows_al(bool al, const RowsArgs& a, hipStream_t s) {
 template <int DT, bool WT>
 static void grouped_rows(RowsArgs a, hipStream_t s) {
     constexpr int E = Tile<DT>::E;
-    a.slots = unit_slots(a.m, a.groups, ROW_LG);
+    a.slots = unit_slots(a.m, a.groups, ROW_TILE);
     const int wrow = WT ? a.depth : a.cols;  // weights' contiguous length
     const bool al = vec_width(E, DT, a.x, a.depth, a.xs) == E && vec_width(E, DT, a.w, wrow, wrow) == E;
-    a.whole = vec_width(4, a.y_dtype, a.y, a.cols, a.ys) == 4;
-    if (a.cols <= 64) {
-        a.tiles = 1;
+    const int yv = vec_width(8, a.y_dtype, a.y, a.cols, a.ys);
+    a.whole = yv == 8 && a.y_dtype != TAURUS_F32 ? 2 : yv >= 4;
+    if (DT == TAURUS_F32 || a.cols <= 64) {
+        a.tiles = (int)ceil_div(a.cols, 64);
         rows_al<DT, WT, 64>(al, a, s);
-    } else {
+    } else if constexpr (DT != TAURUS_F32) {
         a.tiles = (int)ceil_div(a.cols, 128);
         rows_al<DT, WT, 128>(al, a, s);
     }
@@ -332,9 +470,9 @@ static void grouped_rows(RowsArgs a, hipStream_t s) {
 
 // ----------------------------------------------------------------- dW, db --
 
-// A unit of 2^lr rows and a tile of W_g a workgroup.  A type whose rows are
-// one unit is written at once; the units of longer types leave their fp32
-// sums in the workspace, and k_grouped_join adds them in row order.
+// A unit of R rows and a tile of W_g at a time.  A type whose rows are one
+// unit is written at once; the units of longer types leave their fp32 sums in
+// the workspace, and k_grouped_join adds them in row order.
 struct WeightArgs {
     const void *x, *dy;
     int64_t m, xs, ds;
@@ -346,34 +484,54 @@ struct WeightArgs {
     float* db;
     float *part, *part_b;
     int64_t slots;
-    int tiles_k, tiles_n, lr;
+    int tiles_k, tiles_n, R;
 };
 template <int DT, int TK, int TN, bool AL>
-__global__ __launch_bounds__(256) void k_grouped_weight(WeightArgs a) {
+struct WeightTiles {
     typedef Across<DT, TK, AL> OpM;
     typedef Across<DT, TN, AL> OpN;
-    constexpr int WN = TN / 64, WM = 4 / WN, MI = TK / WM / 16, NI = 4;
-    __shared__ __align__(16) char lds[2 * (OpM::BYTES + OpN::BYTES)];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
-    const int m0 = wave / WN * MI * 16, n0 = wave % WN * 64;
-    const int tiles = a.tiles_k * a.tiles_n;
-    for (int64_t b = blockIdx.x; b < a.slots * tiles; b += gridDim.x) {
-        int64_t slot;
-        int tile;
-        place_of(b, a.slots, tiles, slot, tile);
-        const Unit u = wave_unit(a.off, a.groups, a.m, a.lr, slot);
-        const int64_t units = u.units(a.lr);
-        // an empty type's first slot writes its zeros
-        if (u.g < 0 || (units > 0 ? u.slot >= units : u.slot > 0)) continue;
-        const int k0 = tile / a.tiles_n * TK, c0 = tile % a.tiles_n * TN;
-        const bool sums = a.db && k0 == 0 && m0 == 0;
-        const int depth = (int)(u.r1 - u.r0);
-        const OpM om{a.x, u.r0 * a.xs + k0, a.xs, depth, a.k - k0};
-        const OpN on{a.dy, u.r0 * a.ds + c0, a.ds, depth, a.n - c0};
-        floatx4 acc[MI][NI], nsum[NI];
-        tile_product<DT, OpM, OpN, MI, NI, true>(om, on, depth, lds, m0, n0, sums, acc, nsum);
-        const bool last = units <= 1;
-        const int64_t p = last ? u.g : unit_place(u.r0, u.slot, a.lr);
+    static constexpr int WN = TN / 64, WM = 4 / WN, MI = TK / WM / 16, NI = 4;
+    const WeightArgs& a;
+    Units units;
+    int64_t b;
+    int m0, n0;
+    int64_t place = 0, next_place = 0;
+    int k0 = 0, c0 = 0, next_k0 = 0, next_c0 = 0;
+    bool last = false, next_last = false, sums = false;
+    __device__ WeightTiles(const WeightArgs& a_, int m0_, int n0_)
+        : a(a_), units(a_.off, a_.groups, a_.m, a_.R), b(blockIdx.x), m0(m0_), n0(n0_) {}
+    // whether this wave takes the sums of dy for the tile under way
+    __device__ bool enter(int wave_m0) {
+        sums = a.db && next_k0 == 0 && wave_m0 == 0;
+        return sums;
+    }
+    __device__ bool seek(OpM& om, OpN& on, int& depth) {
+        place = next_place;
+        last = next_last;
+        k0 = next_k0;
+        c0 = next_c0;
+        const int tiles = a.tiles_k * a.tiles_n;
+        for (; b < a.slots * tiles; b += gridDim.x) {
+            int64_t slot;
+            int tile;
+            place_of(b, a.slots, tiles, slot, tile);
+            const Unit u = units.at(slot);
+            // an empty type's first slot writes its zeros
+            if (u.g < 0 || (u.units > 0 ? u.slot >= u.units : u.slot > 0)) continue;
+            next_k0 = tile / a.tiles_n * TK;
+            next_c0 = tile % a.tiles_n * TN;
+            next_last = u.units <= 1;
+            next_place = next_last ? u.g : unit_place(u.r0, u.slot, a.R);
+            depth = (int)(u.r1 - u.r0);
+            om = OpM{a.x, u.r0 * a.xs + next_k0, a.xs, depth, a.k - next_k0};
+            on = OpN{a.dy, u.r0 * a.ds + next_c0, a.ds, depth, a.n - next_c0};
+            b += gridDim.x;
+            return true;
+        }
+        return false;
+    }
+    __device__ void done(floatx4 (&acc)[MI][NI], typename Tile<DT>::sums_t (&nsum)[NI]) {
+        const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
         void* out = last ? a.dw : a.part;
         float* out_b = last ? a.db : a.part_b;
         const int dtype = last ? a.dw_dtype : (int)TAURUS_F32;
@@ -384,76 +542,117 @@ __global__ __launch_bounds__(256) void k_grouped_weight(WeightArgs a) {
 #pragma unroll
                 for (int i = 0; i < MI; i++) {
                     const int k = k0 + m0 + 16 * i + li;
-                    if (k < a.k) put4(out, dtype, (p * a.k + k) * a.n, c, a.n, a.whole, acc[i][j]);
+                    if (k < a.k) put4(out, dtype, (place * a.k + k) * a.n, c, a.n, a.whole, acc[i][j]);
                 }
-            if (sums && li == 0) put4(out_b, TAURUS_F32, p * a.n, c, a.n, false, nsum[j]);
+            if (!sums) continue;  // the same for the whole wave
+            if constexpr (DT == TAURUS_F32) {
+                float v = nsum[j];
+                v += __shfl_xor(v, 16, 64);
+                v += __shfl_xor(v, 32, 64);
+                const int cc = c0 + n0 + 16 * j + li;
+                if (lk == 0 && cc < a.n) out_b[place * a.n + cc] = v;
+            } else if (li == 0) {
+                put4(out_b, TAURUS_F32, place * a.n, c, a.n, false, nsum[j]);
+            }
         }
     }
+};
+template <int DT, int TK, int TN, bool AL>
+__global__ __launch_bounds__(256, TK * TN == 128 * 128 ? 3 : 4) void k_grouped_weight(WeightArgs a) {
+    typedef WeightTiles<DT, TK, TN, AL> T;
+    __shared__ __align__(16) char lds[T::OpM::BYTES + T::OpN::BYTES];
+    const int wave = threadIdx.x >> 6, m0 = wave / T::WN * T::MI * 16, n0 = wave % T::WN * 64;
+    T tiles(a, m0, n0);
+    stream_tiles<DT, typename T::OpM, typename T::OpN, T::MI, T::NI, true>(tiles, lds, m0, n0);
 }
 
-// Types of more than one unit; a workgroup takes 1,024 values of one.
+// Types of more than one unit: a workgroup takes 128 values of one, eight
+// units at a time, each eighth's sum in unit order and the eighths in order.
 __global__ __launch_bounds__(256) void k_grouped_join(WeightArgs a, int64_t types, int chunks_w, int chunks) {
+    __shared__ float4 sum[8][32];
+    const int v = threadIdx.x & 31, eighth = threadIdx.x >> 5;
     for (int64_t b = blockIdx.x; b < types * chunks; b += gridDim.x) {
         const int chunk = (int)(b % chunks);
-        const Long t = wave_long(a.off, a.groups, a.m, a.lr, b / chunks);
-        if (!t.found) continue;
-        const int64_t units = (t.end - t.begin + ((int64_t)1 << a.lr) - 1) >> a.lr;
+        const Long t = wave_long(a.off, a.groups, a.m, a.R, b / chunks);
+        if (!t.found) continue;  // the same for the whole workgroup
         const bool of_w = chunk < chunks_w;
         const int64_t size = of_w ? (int64_t)a.k * a.n : a.n;
         const float* part = of_w ? a.part : a.part_b;
-        void* out = of_w ? a.dw : (void*)a.db;
-        const int dtype = of_w ? a.dw_dtype : (int)TAURUS_F32;
-        const int64_t at = ((int64_t)(of_w ? chunk : chunk - chunks_w) * 256 + threadIdx.x) * 4;
-        if (at >= size) continue;
-        const bool whole = size % 4 == 0 && (of_w ? a.whole : 0);
+        const int64_t at = (int64_t)(of_w ? chunk : chunk - chunks_w) * 128 + v * 4;
+        const bool whole = size % 4 == 0;
         float f[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int64_t i = 0; i < units; i++) {
-            const float* q = part + unit_place(t.begin + (i << a.lr), (int)min(i, (int64_t)1), a.lr) * size + at;
-            if (whole) {
-                const float4 v = *reinterpret_cast<const float4*>(q);
-                f[0] += v.x;
-                f[1] += v.y;
-                f[2] += v.z;
-                f[3] += v.w;
+        // unit i starts in window t.window + i
+        auto unit = [&](int64_t i) { return part + (2 * (t.window + i) + (i == 0)) * size + at; };
+        int64_t i = eighth;
+        if (whole && at < size) {
+            constexpr int U = 4;
+            for (; i + 8 * (U - 1) < t.units; i += 8 * U) {
+                float4 x[U];
+#pragma unroll
+                for (int j = 0; j < U; j++) x[j] = *reinterpret_cast<const float4*>(unit(i + 8 * j));
+#pragma unroll
+                for (int j = 0; j < U; j++) {
+                    f[0] += x[j].x;
+                    f[1] += x[j].y;
+                    f[2] += x[j].z;
+                    f[3] += x[j].w;
+                }
+            }
+        }
+        for (; i < t.units; i += 8)
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (at + e < size) f[e] += unit(i)[e];
+        sum[eighth][v] = make_float4(f[0], f[1], f[2], f[3]);
+        __syncthreads();
+        if (eighth == 0 && at < size) {
+#pragma unroll
+            for (int j = 1; j < 8; j++) {
+                const float4 x = sum[j][v];
+                f[0] += x.x;
+                f[1] += x.y;
+                f[2] += x.z;
+                f[3] += x.w;
+            }
+            void* out = of_w ? a.dw : (void*)a.db;
+            const int dtype = of_w ? a.dw_dtype : (int)TAURUS_F32;
+            if (of_w && a.whole) {
+                store_as<4>(dtype, out, t.g * size + at, f);
             } else {
 #pragma unroll
                 for (int e = 0; e < 4; e++)
-                    if (at + e < size) f[e] += q[e];
+                    if (at + e < size) {
+                        const float one[1] = {f[e]};
+                        store_as<1>(dtype, out, t.g * size + at + e, one);
+                    }
             }
         }
-        if (whole) {
-            store_as<4>(dtype, out, t.g * size + at, f);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (at + e < size) {
-                    const float one[1] = {f[e]};
-                    store_as<1>(dtype, out, t.g * size + at + e, one);
-                }
-        }
+        __syncthreads();
     }
 }
 
-// Rows a unit of dW takes: as many as leave enough workgroups for the chip
-// (two fit a compute unit), since every unit of a long type writes and reads
-// a copy of W.
-static int weight_lr(int64_t m, int64_t k, int64_t n) {
-    const int64_t tiles = ceil_div(k, k <= 64 ? 64 : 128) * ceil_div(n, n <= 64 ? 64 : 128);
-    int lr = 13;
-    while (lr > 8 && (m >> lr) * tiles < 768) lr--;
-    return lr;
+// Rows a unit of dW takes: every unit of a long type writes and reads a copy
+// of W, so as few units as fill the chip's 256 compute units once, ranges
+// that end inside a unit counted in; at least 256 rows.
+static int weight_tile_k(int64_t k) { return k <= 64 ? 64 : 128; }
+static int weight_tile_n(int dtype, int64_t n) { return dtype == TAURUS_F32 || n <= 64 ? 64 : 128; }
+static int weight_rows(int dtype, int64_t m, int64_t groups, int64_t k, int64_t n) {
+    const int64_t tiles = ceil_div(k, weight_tile_k(k)) * ceil_div(n, weight_tile_n(dtype, n));
+    const int64_t resident = 256 * (weight_tile_k(k) * weight_tile_n(dtype, n) == 128 * 128 ? 3 : 4);
+    const int64_t units = std::max<int64_t>(resident / tiles - std::min(groups, resident), 1);
+    return (int)std::min<int64_t>(std::max<int64_t>(ceil_div(ceil_div(m, units), 64) * 64, 256), 8192);
 }
 struct WeightWork {
     float *part, *part_b;
     int64_t bytes;
 };
-static WeightWork weight_work(void* work, int64_t m, int64_t k, int64_t n) {
-    const int lr = weight_lr(m, k, n);
+static WeightWork weight_work(void* work, int dtype, int64_t m, int64_t groups, int64_t k, int64_t n) {
+    const int R = weight_rows(dtype, m, groups, k, n);
     Carve c(work);
     WeightWork w{};
-    if (m > (int64_t)1 << lr) {  // else every type is one unit
-        w.part = c.take<float>(unit_places(m, lr) * k * n);
-        w.part_b = c.take<float>(unit_places(m, lr) * n);
+    if (m > R) {  // else every type is one unit
+        w.part = c.take<float>(unit_places(m, R) * k * n);
+        w.part_b = c.take<float>(unit_places(m, R) * n);
     }
     w.bytes = c.bytes();
     return w;
@@ -461,7 +660,7 @@ static WeightWork weight_work(void* work, int64_t m, int64_t k, int64_t n) {
 
 template <int DT, int TK, int TN>
 static void weight_al(bool al, const WeightArgs& a, hipStream_t s) {
-    const unsigned grid = grid_for(a.slots * a.tiles_k * a.tiles_n);
+    const unsigned grid = (unsigned)std::min(a.slots * a.tiles_k * a.tiles_n, (int64_t)(TK * TN == 128 * 128 ? 3 : 4) * compute_units());
     if (al) k_grouped_weight<DT, TK, TN, true><<<grid, 256, 0, s>>>(a);
     else k_grouped_weight<DT, TK, TN, false><<<grid, 256, 0, s>>>(a);
     TAURUS_CHECK_LAUNCH();
@@ -469,24 +668,26 @@ static void weight_al(bool al, const WeightArgs& a, hipStream_t s) {
 template <int DT>
 static void grouped_weight(WeightArgs a, void* work, hipStream_t s) {
     constexpr int E = Tile<DT>::E;
-    a.lr = weight_lr(a.m, a.k, a.n);
-    const WeightWork w = weight_work(work, a.m, a.k, a.n);
+    a.R = weight_rows(DT, a.m, a.groups, a.k, a.n);
+    const WeightWork w = weight_work(work, DT, a.m, a.groups, a.k, a.n);
     a.part = w.part;
     a.part_b = w.part_b;
-    a.slots = unit_slots(a.m, a.groups, a.lr);
-    const int tk = a.k <= 64 ? 64 : 128, tn = a.n <= 64 ? 64 : 128;
+    a.slots = unit_slots(a.m, a.groups, a.R);
+    const int tk = weight_tile_k(a.k), tn = weight_tile_n(DT, a.n);
     a.tiles_k = a.dw ? (int)ceil_div(a.k, tk) : 1;  // the first tile holds the sums of dy
     a.tiles_n = (int)ceil_div(a.n, tn);
     a.whole = a.dw && vec_width(4, a.dw_dtype, a.dw, a.n, a.n) == 4;
     const bool al = vec_width(E, DT, a.x, a.k, a.xs) == E && vec_width(E, DT, a.dy, a.n, a.ds) == E;
     if (tk == 64 && tn == 64) weight_al<DT, 64, 64>(al, a, s);
-    else if (tk == 64) weight_al<DT, 64, 128>(al, a, s);
     else if (tn == 64) weight_al<DT, 128, 64>(al, a, s);
-    else weight_al<DT, 128, 128>(al, a, s);
+    else if constexpr (DT != TAURUS_F32) {
+        if (tk == 64) weight_al<DT, 64, 128>(al, a, s);
+        else weight_al<DT, 128, 128>(al, a, s);
+    }
     if (!a.part) return;
-    const int chunks_w = a.dw ? (int)ceil_div((int64_t)a.k * a.n, 1024) : 0;
-    const int chunks = chunks_w + (a.db ? (int)ceil_div(a.n, 1024) : 0);
-    const int64_t types = long_count(a.m, a.groups, a.lr);
+    const int chunks_w = a.dw ? (int)ceil_div((int64_t)a.k * a.n, 128) : 0;
+    const int chunks = chunks_w + (a.db ? (int)ceil_div(a.n, 128) : 0);
+    const int64_t types = long_count(a.m, a.groups, a.R);
     k_grouped_join<<<grid_for(types * chunks), 256, 0, s>>>(a, types, chunks_w, chunks);
     TAURUS_CHECK_LAUNCH();
 }
@@ -531,11 +732,11 @@ int taurus_grouped_linear(const void* x, int32_t dtype, int64_t m, int64_t d_in,
     });
 }
 
-int64_t taurus_grouped_linear_grad_bytes(int64_t m, int64_t d_in, int64_t d_out) {
+int64_t taurus_grouped_linear_grad_bytes(int32_t dtype, int64_t m, int64_t groups, int64_t d_in, int64_t d_out) {
     int64_t bytes = 0;
     const int rc = guarded_call([&] {
-        check_linear(TAURUS_F32, m, 0, d_in, d_out, nullptr);
-        bytes = weight_work(nullptr, m, d_in, d_out).bytes;
+        check_linear(dtype, m, groups, d_in, d_out, reinterpret_cast<const int64_t*>(16));
+        bytes = weight_work(nullptr, dtype, m, groups, d_in, d_out).bytes;
         return (int)TAURUS_OK;
     });
     return rc == TAURUS_OK ? bytes : rc;
@@ -559,7 +760,7 @@ int taurus_grouped_linear_grad(const void* grad, int64_t grad_stride, const void
             check_rows(x, dtype, m, d_in, x_stride, "x");
             if (dweight) check_ptr(dweight, dtype_size(dweight_dtype), "dweight");
             if (dbias) check_ptr(dbias, 4, "dbias");
-            check_work(work, work_bytes, weight_work(nullptr, m, d_in, d_out).bytes, "taurus_grouped_linear_grad");
+            check_work(work, work_bytes, weight_work(nullptr, dtype, m, groups, d_in, d_out).bytes, "taurus_grouped_linear_grad");
         }
         auto s = static_cast<hipStream_t>(stream);
         if (dx && m > 0) {

@@ -48,7 +48,7 @@ struct NormArgs {
     float* part;    // [unit_places][groups][2]
     float* stat;    // [long_places][groups][2] of the segments of several units
     int64_t slots;
-    int lr, per_block;
+    int R, per_block;
 };
 
 __device__ inline float act_of(float z, int act) {
@@ -290,9 +290,10 @@ __global__ __launch_bounds__(256) void k_norm_units(NormArgs a) {
     extern __shared__ float lds[];
     float *cm = lds, *cq = cm + a.d, *gm = cq + a.d, *gr = gm + a.groups, *scratch = gr + a.groups;
     const Spread t(a.d, E);
+    const Units find(a.off, a.segs, a.m, a.R);
     for (int64_t k = blockIdx.x; k < a.slots; k += gridDim.x) {
-        const Unit u = wave_unit(a.off, a.segs, a.m, a.lr, k);
-        const int64_t units = u.units(a.lr);
+        const Unit u = find.at(k);
+        const int64_t units = u.units;
         if (u.g < 0 || (units > 0 ? u.slot >= units : u.slot > 0)) continue;  // for the whole workgroup
         const int rows = (int)(u.r1 - u.r0);
         if (rows == 0) {
@@ -397,7 +398,7 @@ __global__ __launch_bounds__(256) void k_norm_units(NormArgs a) {
                     a.rstd[(int64_t)u.g * a.groups + g] = rstd;
                 }
             } else {
-                const int64_t p = unit_place(u.r0, u.slot, a.lr) * a.groups + g;
+                const int64_t p = unit_place(u.r0, u.slot, a.R) * a.groups + g;
                 a.part[2 * p] = mean;
                 a.part[2 * p + 1] = m2;
             }
@@ -443,12 +444,12 @@ __global__ __launch_bounds__(256) void k_norm_join(NormArgs a, int64_t longs) {
     __shared__ float red[4];
     for (int64_t b = blockIdx.x; b < longs * a.groups; b += gridDim.x) {
         const int g = (int)(b % a.groups);
-        const Long s = wave_long(a.off, a.segs, a.m, a.lr, b / a.groups);
+        const Long s = wave_long(a.off, a.segs, a.m, a.R, b / a.groups);
         if (!s.found) continue;  // for the whole workgroup
-        const int64_t R = (int64_t)1 << a.lr, units = (s.end - s.begin + R - 1) >> a.lr;
+        const int64_t R = a.R, units = s.units;
         const float size = (float)(s.end - s.begin) * (float)a.cg;
         auto part = [&](int64_t i) {
-            return a.part + 2 * (unit_place(s.begin + i * R, i == 0 ? 0 : 1, a.lr) * a.groups + g);
+            return a.part + 2 * (unit_place(s.begin + i * R, i == 0 ? 0 : 1, a.R) * a.groups + g);
         };
         auto rows = [&](int64_t i) { return (float)min(R, s.end - s.begin - i * R); };
         float p = 0.f, q = 0.f;
@@ -485,11 +486,12 @@ __global__ __launch_bounds__(256) void k_norm_join(NormArgs a, int64_t longs) {
 template <int DT, int E>
 __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
     const Spread t(a.d, E);
+    const Units find(a.off, a.segs, a.m, a.R);
     for (int64_t k = blockIdx.x; k < a.slots; k += gridDim.x) {
-        const Unit u = wave_unit(a.off, a.segs, a.m, a.lr, k);
-        if (u.g < 0 || u.units(a.lr) <= 1 || t.ry >= t.RY) continue;
+        const Unit u = find.at(k);
+        if (u.g < 0 || u.units <= 1 || t.ry >= t.RY) continue;
         const int rows = (int)(u.r1 - u.r0);
-        const float* st = a.stat + 2 * (u.begin >> a.lr) * a.groups;
+        const float* st = a.stat + 2 * (u.begin / a.R) * a.groups;
         for (int v = t.cx; v < t.nv; v += t.nvb) {
             float mu[E], rs[E], w[E], b[E];
 #pragma unroll
@@ -582,11 +584,12 @@ __global__ __launch_bounds__(256) void k_norm_units_grad(NormArgs a) {
     float *ca = lds, *cb = ca + a.d, *ga = cb + a.d, *gb = ga + a.groups;
     float *ta = gb + a.groups, *tb = ta + a.d, *scratch = tb + a.d;
     const Spread t(a.d, E);
+    const Units find(a.off, a.segs, a.m, a.R);
     for (int c = threadIdx.x; c < a.d; c += 256) ta[c] = tb[c] = 0.f;
     const int64_t k0 = (int64_t)blockIdx.x * a.per_block, k1 = min(k0 + a.per_block, a.slots);
     for (int64_t k = k0; k < k1; k++) {
-        const Unit u = wave_unit(a.off, a.segs, a.m, a.lr, k);
-        const int64_t units = u.units(a.lr);
+        const Unit u = find.at(k);
+        const int64_t units = u.units;
         if (u.g < 0 || u.slot >= units) continue;  // for the whole workgroup
         const int rows = (int)(u.r1 - u.r0);
         __syncthreads();
@@ -669,7 +672,7 @@ __global__ __launch_bounds__(256) void k_norm_units_grad(NormArgs a) {
                 ga[g] = s1 * inv;
                 gb[g] = s2 * inv;
             } else {
-                const int64_t p = unit_place(u.r0, u.slot, a.lr) * a.groups + g;
+                const int64_t p = unit_place(u.r0, u.slot, a.R) * a.groups + g;
                 a.part[2 * p] = s1;
                 a.part[2 * p + 1] = s2;
             }
@@ -701,10 +704,11 @@ __global__ __launch_bounds__(256) void k_norm_units_grad(NormArgs a) {
 template <int DT, int E>
 __global__ __launch_bounds__(256) void k_norm_apply_grad(NormArgs a) {
     const Spread t(a.d, E);
+    const Units find(a.off, a.segs, a.m, a.R);
     for (int64_t k = blockIdx.x; k < a.slots; k += gridDim.x) {
-        const Unit u = wave_unit(a.off, a.segs, a.m, a.lr, k);
-        if (u.g < 0 || u.units(a.lr) <= 1 || u.r0 >= u.r1 || t.ry >= t.RY) continue;
-        const float* st = a.stat + 2 * (u.begin >> a.lr) * a.groups;
+        const Unit u = find.at(k);
+        if (u.g < 0 || u.units <= 1 || u.r0 >= u.r1 || t.ry >= t.RY) continue;
+        const float* st = a.stat + 2 * (u.begin / a.R) * a.groups;
         for (int v = t.cx; v < t.nv; v += t.nvb) {
             GradCols<DT, E> g;
             g.set(a, u.g, v);
@@ -825,8 +829,8 @@ static void norm_rows(const NormArgs& a, const RowPlan& r, int64_t blocks, bool 
 template <int DT, int E>
 static void segs_e(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
     const size_t lds = ((size_t)(grad ? 4 : 2) * a.d + 2 * a.groups + scratch_floats(E)) * 4;
-    const int64_t longs = long_count(a.m, a.segs, a.lr);
-    const bool longer = a.m > (int64_t)1 << a.lr;  // a segment can take several units
+    const int64_t longs = long_count(a.m, a.segs, a.R);
+    const bool longer = a.m > a.R;  // a segment can take several units
     if (grad) k_norm_units_grad<DT, E><<<(unsigned)blocks, 256, lds, s>>>(a);
     else k_norm_units<DT, E><<<grid_for(a.slots), 256, lds, s>>>(a);
     TAURUS_CHECK_LAUNCH();
@@ -851,21 +855,21 @@ static void norm_segs(const NormArgs& a, int e, int64_t blocks, bool grad, hipSt
 struct NormWork {
     float *cols = nullptr, *part = nullptr, *stat = nullptr;
     int64_t col_rows = 0, slots = 0, blocks = 0, bytes = 0;
-    int lr = 0, per_block = 1;
+    int R = 1, per_block = 1;
 };
 static NormWork norm_work(void* work, int64_t m, int64_t d, int64_t groups, int64_t segs, bool by_segment, bool grad,
                           int lg) {
     NormWork w;
     Carve c(work);
     if (by_segment) {
-        w.lr = norm_lr(m, d, segs);
-        w.slots = unit_slots(m, segs, w.lr);
+        w.R = 1 << norm_lr(m, d, segs);
+        w.slots = unit_slots(m, segs, w.R);
         w.per_block = (int)std::max<int64_t>(1, w.slots / 4096);
         w.blocks = ceil_div(w.slots, w.per_block);
         w.col_rows = w.blocks;
-        if (m > (int64_t)1 << w.lr) {
-            w.part = c.take<float>(unit_places(m, w.lr) * groups * 2);
-            w.stat = c.take<float>(long_places(m, w.lr) * groups * 2);
+        if (m > w.R) {
+            w.part = c.take<float>(unit_places(m, w.R) * groups * 2);
+            w.stat = c.take<float>(long_places(m, w.R) * groups * 2);
         }
     } else {
         w.blocks = walk_blocks(m, (int)groups, lg, grad);
@@ -913,7 +917,7 @@ static void norm_run(NormArgs a, int dtype, int e, bool grad, void* work, int64_
     a.part = w.part;
     a.stat = w.stat;
     a.slots = w.slots;
-    a.lr = w.lr;
+    a.R = w.R;
     a.per_block = w.per_block;
     const bool none = a.off && a.segs == 0;  // no segment holds a row: the column sums are zeros
     if (none) {

@@ -39,12 +39,14 @@ inline void check_count(int64_t v, int64_t lo, int64_t hi, const char* what) {
     if (v < lo || v > hi)
         fail(TAURUS_E_INVALID, "%s is %lld, not in [%lld, %lld]", what, (long long)v, (long long)lo, (long long)hi);
 }
-// a row array: rows of `cols` values at least `cols` apart; the last value's
-// byte offset fits 62 bits; values lie at multiples of their size
+// a row array: rows of `cols` values, at least `cols` and at most STRIDE_MAX
+// apart (128 rows of 4-byte values then span at most 2^31 bytes); values lie
+// at multiples of their size
+constexpr int64_t STRIDE_MAX = (int64_t)1 << 22;
 inline void check_rows(const void* p, int dtype, int64_t rows, int64_t cols, int64_t stride, const char* what) {
     if (rows <= 0) return;
     if (!p) fail(TAURUS_E_INVALID, "%s is null", what);
-    if (stride < cols || stride > ((int64_t)1 << 29))
+    if (stride < cols || stride > STRIDE_MAX)
         fail(TAURUS_E_INVALID, "%s: rows of %lld values are %lld apart", what, (long long)cols, (long long)stride);
     if (reinterpret_cast<uintptr_t>(p) % dtype_size(dtype))
         fail(TAURUS_E_INVALID, "%s is not aligned to its type", what);
@@ -191,9 +193,9 @@ __device__ inline void load_vec(const void* p, int64_t at, float (&f)[E]) {
 
 // ------------------------------------------------------------------ units --
 // Rows [off[g], off[g + 1]) belong to range g of `parts`.  Work over them is
-// cut into units of at most R = 2^lr rows that never cross a range.  Nothing
-// on the host knows the ranges, so a launch has a slot for every unit there
-// can be: range g owns slots f(g) .. f(g + 1) - 1 with
+// cut into units of at most R rows that never cross a range.  Nothing on the
+// host knows the ranges, so a launch has a slot for every unit there can be:
+// range g owns slots f(g) .. f(g + 1) - 1 with
 //     f(g) = floor(off[g] / R) + g,
 // which increases with g and leaves a range of n rows at least ceil(n / R)
 // slots: with off[g] = qR + s and off[g + 1] = pR + t (s, t < R), it has
@@ -204,79 +206,109 @@ __device__ inline void load_vec(const void* p, int64_t at, float (&f)[E]) {
 // none.  An empty range keeps one slot.  Offsets are clamped to [0, m], so
 // that no row outside the array is touched whatever they hold.
 struct Unit {
-    int g;            // range; -1: none (offsets do not start at 0)
-    int slot;         // which of the range's slots
-    int64_t r0, r1;   // rows
+    int g;               // range; -1: none (offsets do not start at 0)
+    int slot;            // which of the range's slots
+    int64_t r0, r1;      // rows
     int64_t begin, end;  // the whole range
-    __device__ int64_t units(int lr) const { return (end - begin + ((int64_t)1 << lr) - 1) >> lr; }
+    int64_t units;       // units of the range
 };
-inline int64_t unit_slots(int64_t m, int64_t parts, int lr) { return (m >> lr) + parts; }
+inline int64_t unit_slots(int64_t m, int64_t parts, int R) { return m / R + parts; }
 
-__device__ inline int64_t off_at(const int64_t* __restrict__ off, int64_t i, int64_t m) {
-    return min(max(off[i], (int64_t)0), m);
+__device__ inline uint32_t off_at(const int64_t* __restrict__ off, int64_t i, int64_t m) {
+    return (uint32_t)min(max(off[i], (int64_t)0), m);  // m < 2^31
 }
-// Slot k's unit, for a whole wave (every lane passes the same k and gets the
-// same unit): the largest g with f(g) <= k, 64 probes a step.
-__device__ inline Unit wave_unit(const int64_t* __restrict__ off, int64_t parts, int64_t m, int lr, int64_t k) {
+// The largest i in [0, parts) with ok(i), ok being true up to some i, for a
+// whole wave, 64 probes a step; 0 if there is none.
+template <class Ok>
+__device__ inline int64_t wave_last(int64_t parts, Ok&& ok) {
     const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = parts;  // f(lo) <= k or lo = 0; the answer is below hi
+    int64_t lo = 0, hi = parts;
     while (hi - lo > 1) {
-        const int64_t step = (hi - lo + 63) >> 6;
-        const int64_t p = lo + (int64_t)(lane + 1) * step;
-        const bool in = p < hi;
-        const bool le = in && (off_at(off, in ? p : lo, m) >> lr) + p <= k;
-        const int c = __popcll(__ballot(le));  // f increases: the first c probes
+        const int64_t step = (hi - lo + 63) >> 6, p = lo + (int64_t)(lane + 1) * step;
+        const int c = __popcll(__ballot(p < hi && ok(p < hi ? p : lo)));
         lo += (int64_t)c * step;
         hi = min(lo + step, hi);
     }
-    Unit u;
-    u.begin = off_at(off, lo, m);
-    u.end = max(off_at(off, lo + 1, m), u.begin);
-    const int64_t slot = k - ((u.begin >> lr) + lo);
-    u.g = slot < 0 ? -1 : (int)lo;
-    u.slot = (int)max(slot, (int64_t)0);
-    u.r0 = min(u.begin + ((int64_t)u.slot << lr), u.end);
-    u.r1 = slot < 0 ? u.r0 : min(u.r0 + ((int64_t)1 << lr), u.end);
-    return u;
+    return lo;
 }
+// Finds slots' units for a whole wave (every lane passes the same slot and
+// gets the same unit).  Up to 64 ranges wait in the wave's lanes, so that a
+// search reads no memory.
+struct Units {
+    const int64_t* off;
+    int64_t parts, m;
+    uint32_t R, mine, next;
+    bool few;
+    __device__ Units(const int64_t* off_, int64_t parts_, int64_t m_, int R_)
+        : off(off_), parts(parts_), m(m_), R((uint32_t)R_), mine(0), next(0), few(parts_ <= 64) {
+        if (few) {
+            const int64_t lane = threadIdx.x & 63;
+            mine = off_at(off, min(lane, parts), m);
+            next = off_at(off, min(lane + 1, parts), m);
+        }
+    }
+    __device__ Unit at(int64_t k) const {
+        int64_t lo;
+        uint32_t b, e;
+        if (few) {
+            const int lane = threadIdx.x & 63;
+            const int c = __popcll(__ballot(lane < parts && (int64_t)(mine / R) + lane <= k));
+            const int i = max(c - 1, 0);
+            lo = i;
+            b = (uint32_t)__builtin_amdgcn_readlane((int)mine, i);
+            e = (uint32_t)__builtin_amdgcn_readlane((int)next, i);
+        } else {
+            lo = wave_last(parts, [&](int64_t p) { return (int64_t)(off_at(off, p, m) / R) + p <= k; });
+            b = off_at(off, lo, m);
+            e = off_at(off, lo + 1, m);
+        }
+        e = max(e, b);
+        Unit u;
+        u.begin = b;
+        u.end = e;
+        u.units = (e - b + R - 1) / R;
+        const int64_t slot = k - ((int64_t)(b / R) + lo);
+        u.g = slot < 0 ? -1 : (int)lo;
+        u.slot = (int)max(slot, (int64_t)0);
+        u.r0 = min(u.begin + (int64_t)u.slot * R, u.end);
+        u.r1 = slot < 0 ? u.r0 : min(u.r0 + R, u.end);
+        return u;
+    }
+};
 
 // A range of more than one unit, among those a launch enumerates: by range
 // where there are few of them, else by window of R rows, in which at most
 // one such range starts (its rows reach past the window), the last to start
 // there.  The window names its place in a workspace.  For a whole wave.
 struct Long {
-    int64_t g, begin, end, window;
+    int64_t g, begin, end, window, units;
     bool found;
 };
-inline int64_t long_places(int64_t m, int lr) { return (m >> lr) + 1; }
-inline int64_t long_count(int64_t m, int64_t parts, int lr) { return std::min(parts, long_places(m, lr)); }
-__device__ inline Long wave_long(const int64_t* __restrict__ off, int64_t parts, int64_t m, int lr, int64_t i) {
-    const int lane = threadIdx.x & 63;
-    const bool by_range = parts < (m >> lr) + 1;
+inline int64_t long_places(int64_t m, int R) { return m / R + 1; }
+inline int64_t long_count(int64_t m, int64_t parts, int R) { return std::min(parts, long_places(m, R)); }
+__device__ inline Long wave_long(const int64_t* __restrict__ off, int64_t parts, int64_t m, int R, int64_t i) {
+    const bool by_range = parts < m / R + 1;
     Long s;
-    if (by_range) {
-        s.g = i;
-    } else {
-        const int64_t want = ((i + 1) << lr) - 1;
-        int64_t lo = 0, hi = parts;
-        while (hi - lo > 1) {
-            const int64_t step = (hi - lo + 63) >> 6, p = lo + (int64_t)(lane + 1) * step;
-            const int c = __popcll(__ballot(p < hi && off_at(off, p < hi ? p : lo, m) <= want));
-            lo += (int64_t)c * step;
-            hi = min(lo + step, hi);
-        }
-        s.g = lo;
-    }
+    s.g = by_range ? i : wave_last(parts, [&](int64_t p) { return (int64_t)off_at(off, p, m) < (i + 1) * R; });
     s.begin = off_at(off, s.g, m);
     s.end = off_at(off, s.g + 1, m);
-    s.window = s.begin >> lr;
-    s.found = s.end - s.begin > ((int64_t)1 << lr) && (by_range || s.window == i);
+    s.window = s.begin / R;
+    s.units = (s.end - s.begin + R - 1) / R;
+    s.found = s.end - s.begin > R && (by_range || s.window == i);
     return s;
 }
 // Workspace place of such a range's unit `slot`, which starts at row r0: of
 // the units of longer ranges at most two start in any window, one of them
 // its range's first.
-__device__ inline int64_t unit_place(int64_t r0, int slot, int lr) { return 2 * (r0 >> lr) + (slot == 0); }
-inline int64_t unit_places(int64_t m, int lr) { return 2 * ((m >> lr) + 1); }
+__device__ inline int64_t unit_place(int64_t r0, int slot, int R) { return 2 * (r0 / R) + (slot == 0); }
+inline int64_t unit_places(int64_t m, int R) { return 2 * (m / R + 1); }
+
+// Compute units of the current device.
+inline int compute_units() {
+    int dev = 0, cus = 0;
+    TAURUS_HIP(hipGetDevice(&dev));
+    TAURUS_HIP(hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev));
+    return cus;
+}
 
 }  // namespace taurus

@@ -445,7 +445,7 @@ static void grad_t(int e, const void* grad, int64_t gs, const int32_t* ids, int6
     grad_e<TI, 1>(grad, gs, ids, m, d, o, work, s);
 }
 
-static constexpr int64_t LOOKUP_COLS = (int64_t)1 << 24;
+static constexpr int64_t LOOKUP_COLS = STRIDE_MAX;
 
 }  // namespace taurus
 

@@ -233,7 +233,7 @@ def grouped_linear_grad(grad: torch.Tensor, x: torch.Tensor, off: torch.Tensor, 
         L = N.lib()
         work, kp, nbytes = None, None, 0
         if dw is not None or db is not None:
-            nbytes = L.taurus_grouped_linear_grad_bytes(m, d_in, d_out)
+            nbytes = L.taurus_grouped_linear_grad_bytes(code, m, groups, d_in, d_out)
             work, kp = c.work(nbytes, "taurus_grouped_linear_grad_bytes")
         N.check(L.taurus_grouped_linear_grad(
             gp, gs, xp, xs, code, m, d_in, d_out, fp, groups, wp, None if dx is None else dx.data_ptr(), d_in,

@@ -74,8 +74,8 @@ def _norm_grad(**kw):
 BAD = [
     (_lookup, dict(dt=3), "none of"), (_lookup, dict(odt=-1), "none of"), (_lookup, dict(n=-1), "table rows"),
     (_lookup, dict(n=1 << 31), "table rows"), (_lookup, dict(m=-1), "ids"), (_lookup, dict(m=1 << 31), "ids"),
-    (_lookup, dict(d=0), "row length"), (_lookup, dict(d=(1 << 24) + 1), "row length"),
-    (_lookup, dict(ts=7), "apart"), (_lookup, dict(os=7), "apart"), (_lookup, dict(ts=1 << 30), "apart"),
+    (_lookup, dict(d=0), "row length"), (_lookup, dict(d=(1 << 22) + 1), "row length"),
+    (_lookup, dict(ts=7), "apart"), (_lookup, dict(os=7), "apart"), (_lookup, dict(ts=(1 << 22) + 1), "apart"),
     (_lookup, dict(table=None), "table is null"), (_lookup, dict(out=None), "out is null"),
     (_lookup, dict(ids=None), "ids is null"), (_lookup, dict(ids=P + 2), "ids is not aligned"),
     (_lookup, dict(table=P + 2), "table is not aligned"), (_lookup, dict(odt=N.BF16, out=P + 1), "out is not aligned"),
@@ -134,13 +134,13 @@ def test_workspace_sizes():
     m, d = 1 << 20, 128
     level = 2 * (m // 32) * (4 * d + 8)
     assert 16 * m + level < L.taurus_lookup_rows_grad_bytes(m, d) < 18 * m + 1.1 * level + (1 << 20)
-    assert L.taurus_grouped_linear_grad_bytes(256, 64, 64) == 0
-    assert L.taurus_grouped_linear_grad_bytes(257, 64, 64) >= 2 * 2 * 64 * 65 * 4
+    assert L.taurus_grouped_linear_grad_bytes(N.F32, 256, 2, 64, 64) == 0
+    assert L.taurus_grouped_linear_grad_bytes(N.F32, 257, 2, 64, 64) >= 2 * 2 * 64 * 65 * 4
     assert L.taurus_group_norm_bytes(10**6, 128, 8, 0, 0, 0) == 0
     assert L.taurus_group_norm_bytes(10**6, 128, 8, 100, 1, 0) > 0
     assert L.taurus_group_norm_bytes(10**6, 128, 8, 0, 0, 1) > 0
     for bad in (L.taurus_lookup_rows_grad_bytes(-1, 4), L.taurus_lookup_rows_grad_bytes(4, 0),
-                L.taurus_grouped_linear_grad_bytes(4, 0, 4), L.taurus_grouped_linear_grad_bytes(1 << 31, 4, 4),
+                L.taurus_grouped_linear_grad_bytes(N.F32, 4, 1, 0, 4), L.taurus_grouped_linear_grad_bytes(N.F32, 1 << 31, 1, 4, 4),
                 L.taurus_group_norm_bytes(4, 6, 4, 0, 0, 0), L.taurus_group_norm_bytes(4, 4096, 4, 0, 0, 1)):
         assert bad == N.E_INVALID
 
