@@ -49,12 +49,19 @@ struct NormArgs {
     float* stat;    // [long_places][groups][2] of the segments of several units
     int64_t slots;
     int R, per_block;
+    int64_t places;  // units of segments of several units, at most
 };
 
 __device__ inline float act_of(float z, int act) {
     if (act == TAURUS_ACT_RELU) return fmaxf(z, 0.f);
     if (act == TAURUS_ACT_SILU) return z / (1.f + expf(-z));
     return z;
+}
+// The sign of (x - mean) rstd w + b in 64 bits.  The conversions stay where
+// they are: taken out of a loop they hold two registers a value.
+__device__ inline bool open_exactly(float x, float mean, float rstd, float w, float b) {
+    asm volatile("" : "+v"(mean), "+v"(rstd), "+v"(w), "+v"(b));
+    return ((double)x - (double)mean) * (double)rstd * (double)w + (double)b > 0.0;
 }
 // dy act'(z).  Which side of ReLU's border z lies on is decided by the sign
 // of z's exact value: where rounding could change it (the four roundings of
@@ -65,7 +72,7 @@ __device__ inline float act_grad(float dy, float x, float mean, float rstd, floa
     if (act == TAURUS_ACT_RELU) {
         bool open = z > 0.f;
         if (fabsf(z) <= 0x1p-20f * (fabsf(t) + fabsf(b)))
-            open = ((double)x - (double)mean) * (double)rstd * (double)w + (double)b > 0.0;
+            open = open_exactly(x, mean, rstd, w, b);
         return open ? dy : 0.f;
     }
     const float q = 1.f / (1.f + expf(-z));
@@ -252,28 +259,71 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a, int lg) {
 
 // ------------------------------------------------------------- segments ----
 
-// A workgroup's threads over a unit: nvb vectors of a row side by side, ry
-// of the rows at a time (threads past the last whole row rest).  Rows of
-// more than 256 vectors are taken 256 at a time.
+// A workgroup's BT threads over a unit: nvb vectors of a row side by side,
+// RY rows at a time (threads past the last whole row rest).  Rows of more
+// than BT vectors (WIDE) are taken BT vectors at a time, one row at a time.
+// A vector lies in one group.
+template <int BT>
 struct Spread {
     int nv, nvb, RY, cx, ry;
     __device__ Spread(int d, int E) {
         nv = d / E;
-        nvb = min(nv, 256);
-        RY = 256 / nvb;
+        nvb = min(nv, BT);
+        RY = BT / nvb;
         cx = threadIdx.x % nvb;
         ry = threadIdx.x / nvb;
     }
+    // rows of a unit that row lane r takes
+    __device__ int count(int rows, int r) const { return (rows - r + RY - 1) / RY; }
 };
-static size_t scratch_floats(int E) { return (size_t)128 * 2 * E + 128; }
 
-// Sums of the channels' pairs p[c], q[c] over each group's channels, each
-// weighed: every group by 2^gl lanes of a wave, to both gp[g] and gq[g].
-template <class F>
-__device__ inline void over_groups(int groups, int cg, F&& f) {
+// A workgroup's consecutive slots: the first by search, the others by
+// stepping along the offsets, the next of which is already requested.
+struct SlotWalk {
+    const int64_t* off;
+    int64_t parts, m, g, slot, slots, k, k1;
+    uint32_t R, b, e, ahead;
+    __device__ SlotWalk(const NormArgs& a, int64_t k0, int64_t k1_)
+        : off(a.off), parts(a.segs), m(a.m), k(k0), k1(k1_), R((uint32_t)a.R) {
+        g = wave_last(parts, [&](int64_t p) { return (int64_t)(off_at(off, p, m) / R) + p <= k0; });
+        set(off_at(off, g, m), off_at(off, g + 1, m));
+        slot = k0 - ((int64_t)(b / R) + g);
+    }
+    __device__ void set(uint32_t begin, uint32_t end) {
+        b = begin;
+        e = max(end, begin);
+        slots = (int64_t)(e / R) - (int64_t)(b / R) + 1;
+        ahead = off_at(off, min(g + 2, parts), m);
+    }
+    __device__ bool more() const { return k < k1 && g < parts; }
+    __device__ void step() {
+        k++;
+        if (++slot >= slots) {
+            g++;
+            slot = 0;
+            set(e, ahead);
+        }
+    }
+    __device__ Unit unit() const {
+        Unit u;
+        u.g = slot < 0 ? -1 : (int)g;
+        u.slot = (int)max(slot, (int64_t)0);
+        u.begin = b;
+        u.end = e;
+        u.units = (e - b + R - 1) / R;
+        u.r0 = min(u.begin + (int64_t)u.slot * R, u.end);
+        u.r1 = slot < 0 ? u.r0 : min(u.r0 + R, u.end);
+        return u;
+    }
+};
+
+// Calls f(g, lane, gl) for every group, 2^gl lanes of a wave each (g = -1:
+// lanes without one, which take part in shuffles): entries = values a group.
+template <int BT, class F>
+__device__ inline void over_groups(int groups, int entries, F&& f) {
     int gl = 0;
-    while (gl < 6 && 1 << gl < cg) gl++;
-    const int per = 256 >> gl, lane = threadIdx.x & ((1 << gl) - 1);
+    while (gl < 6 && 1 << gl < entries) gl++;
+    const int per = BT >> gl, lane = threadIdx.x & ((1 << gl) - 1);
     for (int g0 = 0; g0 < groups; g0 += per) {  // the same number of turns for every thread
         const int g = g0 + (threadIdx.x >> gl);
         f(g < groups ? g : -1, lane, gl);
@@ -284,108 +334,140 @@ __device__ inline float sub_sum(float v, int gl) {
     return v;
 }
 
-// The statistics of each unit; whole segments are normalised at once.
+// The affine map of one vector's channels.
+template <int E>
+struct Affine {
+    float w[E], b[E];
+    __device__ void set(const NormArgs& a, int v, bool in) {
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+            w[e] = in && a.weight ? a.weight[v * E + e] : 1.f;
+            b[e] = in && a.bias ? a.bias[v * E + e] : 0.f;
+        }
+    }
+};
+
+constexpr int SEG_ROWS = 8;  // rows of a vector that a thread has in flight
+
+// decode, where it stands: a 16-bit value's fp32 form is cheap, so that the
+// compiler forms it as soon as the value is loaded and keeps both (240
+// registers a thread, two waves a SIMD, for eight rows of fp16).
 template <int DT, int E>
-__global__ __launch_bounds__(256) void k_norm_units(NormArgs a) {
+__device__ inline void decode_here(Stored<DT, E> s, float (&f)[E]) {
+    if constexpr (DT != TAURUS_F32 && E > 1) {
+        uint32_t w[E / 2];
+        __builtin_memcpy(w, &s, sizeof(w));
+#pragma unroll
+        for (int i = 0; i < E / 2; i++) asm volatile("" : "+v"(w[i]));
+        __builtin_memcpy(&s, w, sizeof(w));
+    }
+    decode<DT, E>(s, f);
+}
+// One vector of SEG_ROWS rows from row r on in steps of RY.
+template <int DT, int E>
+struct RowsOf {
+    Stored<DT, E> v[SEG_ROWS];
+    __device__ void load(const void* p, int64_t stride, int64_t r0, int rows, int r, int RY, int64_t c) {
+#pragma unroll
+        for (int j = 0; j < SEG_ROWS; j++) {
+            const int rr = r + j * RY;
+            v[j] = rr < rows ? load_stored<DT, E>(p, (r0 + rr) * stride + c) : zero_stored<DT, E>();
+        }
+    }
+};
+
+template <int DT, int E>
+__device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E>& x, int64_t r0, int rows, int r, int RY, int v,
+                                  float mu, float rs, const Affine<E>& f) {
+    float w[E];
+#pragma unroll
+    for (int e = 0; e < E; e++) w[e] = rs * f.w[e];
+#pragma unroll
+    for (int j = 0; j < SEG_ROWS; j++) {
+        const int rr = r + j * RY;
+        if (rr >= rows) continue;
+        float z[E];
+        decode_here<DT, E>(x.v[j], z);
+#pragma unroll
+        for (int e = 0; e < E; e++) z[e] = act_of((z[e] - mu) * w[e] + f.b[e], a.act);
+        store_as<E>(a.out_dtype, a.out, (r0 + rr) * a.os + (int64_t)v * E, z);
+    }
+}
+
+// The statistics of each unit; whole segments are normalised at once, from
+// the registers they were read into where they fit.
+template <int DT, int E, int BT>
+__global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
     extern __shared__ float lds[];
-    float *cm = lds, *cq = cm + a.d, *gm = cq + a.d, *gr = gm + a.groups, *scratch = gr + a.groups;
-    const Spread t(a.d, E);
-    const Units find(a.off, a.segs, a.m, a.R);
-    for (int64_t k = blockIdx.x; k < a.slots; k += gridDim.x) {
-        const Unit u = find.at(k);
-        const int64_t units = u.units;
-        if (u.g < 0 || (units > 0 ? u.slot >= units : u.slot > 0)) continue;  // for the whole workgroup
+    const Spread<BT> t(a.d, E);
+    const int entries = max(t.nv, BT);
+    float *sm = lds, *sq = sm + entries, *gm = sq + entries, *gr = gm + a.groups;
+    const bool wide = t.nv > BT;
+    const int cgv = a.cg / E;  // vectors a group
+    Affine<E> f;
+    if (!wide) f.set(a, t.cx, true);
+    const int64_t k0 = (int64_t)blockIdx.x * a.per_block;
+    for (SlotWalk walk(a, k0, min(k0 + a.per_block, a.slots)); walk.more(); walk.step()) {
+        const Unit u = walk.unit();
+        if (u.g < 0 || (u.units > 0 ? u.slot >= u.units : u.slot > 0)) continue;  // for the whole workgroup
         const int rows = (int)(u.r1 - u.r0);
         if (rows == 0) {
-            for (int g = threadIdx.x; g < a.groups && a.mean; g += 256) {
+            for (int g = threadIdx.x; g < a.groups && a.mean; g += BT) {
                 a.mean[(int64_t)u.g * a.groups + g] = 0.f;
                 a.rstd[(int64_t)u.g * a.groups + g] = 0.f;
             }
             continue;
         }
+        RowsOf<DT, E> x;
         __syncthreads();  // the arrays may still be read for an earlier unit
-        for (int v0 = 0; v0 < t.nv; v0 += t.nvb) {
-            const int v = v0 + t.cx;
-            const bool in = t.ry < t.RY && v < t.nv;
-            float n = 0.f, mean[E] = {}, m2[E] = {};
-            constexpr int U = 4;
-            for (int r = t.ry; in && r < rows; r += U * t.RY) {
-                float x[U][E], cnt = 0.f;
+        for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
+            float n = 0.f, mean = 0.f, m2 = 0.f;
+            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
+                float s = 0.f, cnt = 0.f;
 #pragma unroll
-                for (int j = 0; j < U; j++) {
-                    const int rr = r + j * t.RY;
-                    const auto s = rr < rows ? load_stored<DT, E>(a.x, (u.r0 + rr) * a.xs + v * E) : zero_stored<DT, E>();
-                    decode<DT, E>(s, x[j]);
-                    cnt += rr < rows ? 1.f : 0.f;
+                for (int j = 0; j < SEG_ROWS; j++) {
+                    float y[E];
+                    decode_here<DT, E>(x.v[j], y);
+                    cnt += r + j * t.RY < rows ? (float)E : 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; e++) s += y[e];
                 }
-                const float inv = 1.f / cnt, share = cnt / (n + cnt), cross = n * share;
+                const float mb = s / cnt, share = cnt / (n + cnt);
+                float q = 0.f;
 #pragma unroll
-                for (int e = 0; e < E; e++) {
-                    float s = 0.f;
+                for (int j = 0; j < SEG_ROWS; j++) {
+                    float y[E];
+                    decode_here<DT, E>(x.v[j], y);
+                    if (r + j * t.RY < rows)
 #pragma unroll
-                    for (int j = 0; j < U; j++) s += x[j][e];
-                    const float mb = s * inv;
-                    float q = 0.f;
-#pragma unroll
-                    for (int j = 0; j < U; j++) {
-                        const float dev = x[j][e] - mb;
-                        if (r + j * t.RY < rows) q += dev * dev;
-                    }
-                    const float delta = mb - mean[e];
-                    mean[e] += delta * share;
-                    m2[e] += q + delta * delta * cross;
+                        for (int e = 0; e < E; e++) q += (y[e] - mb) * (y[e] - mb);
                 }
+                const float delta = mb - mean;
+                mean += delta * share;
+                m2 += q + delta * delta * n * share;
                 n += cnt;
             }
-            // the row lanes' parts, halved until one is left
-            float* sn = scratch + 128 * 2 * E;
-            for (int cnt = t.RY; cnt > 1;) {
-                const int half = (cnt + 1) / 2;
-                if (t.ry >= half && t.ry < cnt) {
-                    const int at = (t.ry - half) * t.nvb + t.cx;
-#pragma unroll
-                    for (int e = 0; e < E; e++) {
-                        scratch[at + 128 * e] = mean[e];
-                        scratch[at + 128 * (E + e)] = m2[e];
-                    }
-                    sn[at] = n;
-                }
-                __syncthreads();
-                if (t.ry + half < cnt) {
-                    const int at = t.ry * t.nvb + t.cx;
-                    const float nb = sn[at];
-                    if (nb > 0.f) {
-                        const float share = nb / (n + nb), cross = n * share;
-#pragma unroll
-                        for (int e = 0; e < E; e++) {
-                            const float delta = scratch[at + 128 * e] - mean[e];
-                            mean[e] += delta * share;
-                            m2[e] += scratch[at + 128 * (E + e)] + delta * delta * cross;
-                        }
-                        n += nb;
-                    }
-                }
-                __syncthreads();
-                cnt = half;
-            }
-            if (in && t.ry == 0)
-#pragma unroll
-                for (int e = 0; e < E; e++) {
-                    cm[v * E + e] = mean[e];
-                    cq[v * E + e] = m2[e];
-                }
+            sm[t.ry * t.nvb + v] = mean;
+            sq[t.ry * t.nvb + v] = m2;
         }
         __syncthreads();
-        const bool whole = units == 1;
-        over_groups(a.groups, a.cg, [&](int g, int lane, int gl) {
-            const float first = g >= 0 ? cm[g * a.cg] : 0.f;
+        const bool whole = u.units == 1;
+        const int lanes_y = min(t.RY, rows), per = lanes_y * cgv;
+        over_groups<BT>(a.groups, per, [&](int g, int lane, int gl) {
+            const float first = g >= 0 ? sm[g * cgv] : 0.f;
+            const float inv = 1.f / ((float)rows * (float)cgv);  // a row lane's mean counts its rows
             float s = 0.f;
-            for (int c = lane; g >= 0 && c < a.cg; c += 1 << gl) s += cm[g * a.cg + c] - first;
-            const float mean = first + sub_sum(s, gl) / (float)a.cg;
+            for (int i = lane; g >= 0 && i < per; i += 1 << gl) {
+                const int y = i / cgv;
+                s += (sm[y * t.nvb + g * cgv + i - y * cgv] - first) * (float)t.count(rows, y);
+            }
+            const float mean = first + sub_sum(s, gl) * inv;
             s = 0.f;
-            for (int c = lane; g >= 0 && c < a.cg; c += 1 << gl) {
-                const float dev = cm[g * a.cg + c] - mean;
-                s += cq[g * a.cg + c] + (float)rows * dev * dev;
+            for (int i = lane; g >= 0 && i < per; i += 1 << gl) {
+                const int y = i / cgv, at = y * t.nvb + g * cgv + i - y * cgv;
+                const float dev = sm[at] - mean;
+                s += sq[at] + (float)(t.count(rows, y) * E) * dev * dev;
             }
             const float m2 = sub_sum(s, gl);
             if (g < 0 || lane != 0) return;
@@ -405,24 +487,12 @@ __global__ __launch_bounds__(256) void k_norm_units(NormArgs a) {
         });
         if (!whole) continue;
         __syncthreads();
-        for (int v0 = 0; v0 < t.nv; v0 += t.nvb) {
-            const int v = v0 + t.cx;
-            if (t.ry >= t.RY || v >= t.nv) continue;
-            float mu[E], rs[E], w[E], b[E];
-#pragma unroll
-            for (int e = 0; e < E; e++) {
-                const int c = v * E + e, g = c / a.cg;
-                mu[e] = gm[g];
-                rs[e] = gr[g];
-                w[e] = a.weight ? a.weight[c] : 1.f;
-                b[e] = a.bias ? a.bias[c] : 0.f;
-            }
-            for (int r = t.ry; r < rows; r += t.RY) {
-                float x[E];
-                load_vec<DT, E>(a.x, (u.r0 + r) * a.xs + v * E, x);
-#pragma unroll
-                for (int e = 0; e < E; e++) x[e] = act_of((x[e] - mu[e]) * rs[e] * w[e] + b[e], a.act);
-                store_as<E>(a.out_dtype, a.out, (u.r0 + r) * a.os + v * E, x);
+        for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
+            if (wide) f.set(a, v, true);
+            const float mu = gm[v / cgv], rs = gr[v / cgv];
+            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+                if (wide || rows > SEG_ROWS * t.RY) x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
+                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, v, mu, rs, f);
             }
         }
     }
@@ -448,26 +518,36 @@ __global__ __launch_bounds__(256) void k_norm_join(NormArgs a, int64_t longs) {
         if (!s.found) continue;  // for the whole workgroup
         const int64_t R = a.R, units = s.units;
         const float size = (float)(s.end - s.begin) * (float)a.cg;
+        // unit i starts in window s.window + i
         auto part = [&](int64_t i) {
-            return a.part + 2 * (unit_place(s.begin + i * R, i == 0 ? 0 : 1, a.R) * a.groups + g);
+            return *reinterpret_cast<const float2*>(a.part + 2 * ((2 * (s.window + i) + (i == 0)) * a.groups + g));
         };
         auto rows = [&](int64_t i) { return (float)min(R, s.end - s.begin - i * R); };
+        // f over the units, four a thread in flight
+        auto each = [&](auto&& f) {
+            constexpr int U = 4;
+            for (int64_t i = threadIdx.x; i < units; i += 256 * U) {
+                float2 v[U];
+#pragma unroll
+                for (int j = 0; j < U; j++) v[j] = part(min(i + 256 * j, units - 1));
+#pragma unroll
+                for (int j = 0; j < U; j++)
+                    if (i + 256 * j < units) f(i + 256 * j, v[j]);
+            }
+        };
         float p = 0.f, q = 0.f;
         if (GRAD) {
-            for (int64_t i = threadIdx.x; i < units; i += 256) {
-                p += part(i)[0];
-                q += part(i)[1];
-            }
+            each([&](int64_t, float2 v) {
+                p += v.x;
+                q += v.y;
+            });
             p = block_sum(p, red) / size;
             q = block_sum(q, red) / size;
         } else {
-            const float first = part(0)[0];
-            for (int64_t i = threadIdx.x; i < units; i += 256) p += rows(i) * (part(i)[0] - first);
+            const float first = part(0).x;
+            each([&](int64_t i, float2 v) { p += rows(i) * (v.x - first); });
             p = first + block_sum(p, red) / (float)(s.end - s.begin);
-            for (int64_t i = threadIdx.x; i < units; i += 256) {
-                const float dev = part(i)[0] - p;
-                q += part(i)[1] + rows(i) * (float)a.cg * dev * dev;
-            }
+            each([&](int64_t i, float2 v) { q += v.y + rows(i) * (float)a.cg * (v.x - p) * (v.x - p); });
             q = 1.f / sqrtf(block_sum(q, red) / size + a.eps);
         }
         if (threadIdx.x == 0) {
@@ -482,272 +562,298 @@ __global__ __launch_bounds__(256) void k_norm_join(NormArgs a, int64_t longs) {
     }
 }
 
-// The second pass over the rows of long segments.
+// Workgroups take the even places first: a long segment has units at those
+// alone, and by turns with empty ones they would fall on every other XCD.
+__device__ inline int64_t place_order(int64_t k, int64_t places) {
+    return k < places / 2 ? 2 * k : 2 * (k - places / 2) + 1;
+}
+
+// The second pass over the rows of longer segments.
 template <int DT, int E>
 __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
-    const Spread t(a.d, E);
-    const Units find(a.off, a.segs, a.m, a.R);
-    for (int64_t k = blockIdx.x; k < a.slots; k += gridDim.x) {
-        const Unit u = find.at(k);
-        if (u.g < 0 || u.units <= 1 || t.ry >= t.RY) continue;
+    const Spread<256> t(a.d, E);
+    const int cgv = a.cg / E;
+    for (int64_t k = blockIdx.x; k < a.places; k += gridDim.x) {
+        const Unit u = wave_place(a.off, a.segs, a.m, a.R, place_order(k, a.places));
+        if (u.r0 >= u.r1 || t.ry >= t.RY) continue;
         const int rows = (int)(u.r1 - u.r0);
         const float* st = a.stat + 2 * (u.begin / a.R) * a.groups;
         for (int v = t.cx; v < t.nv; v += t.nvb) {
-            float mu[E], rs[E], w[E], b[E];
-#pragma unroll
-            for (int e = 0; e < E; e++) {
-                const int c = v * E + e, g = c / a.cg;
-                mu[e] = st[2 * g];
-                rs[e] = st[2 * g + 1];
-                w[e] = a.weight ? a.weight[c] : 1.f;
-                b[e] = a.bias ? a.bias[c] : 0.f;
-            }
-            constexpr int U = 4;
-            for (int r = t.ry; r < rows; r += U * t.RY) {
-                Stored<DT, E> x[U];
-#pragma unroll
-                for (int j = 0; j < U; j++) {
-                    const int rr = r + j * t.RY;
-                    x[j] = rr < rows ? load_stored<DT, E>(a.x, (u.r0 + rr) * a.xs + v * E) : zero_stored<DT, E>();
-                }
-#pragma unroll
-                for (int j = 0; j < U; j++) {
-                    const int rr = r + j * t.RY;
-                    if (rr >= rows) continue;
-                    float f[E];
-                    decode<DT, E>(x[j], f);
-#pragma unroll
-                    for (int e = 0; e < E; e++) f[e] = act_of((f[e] - mu[e]) * rs[e] * w[e] + b[e], a.act);
-                    store_as<E>(a.out_dtype, a.out, (u.r0 + rr) * a.os + v * E, f);
-                }
+            Affine<E> f;
+            f.set(a, v, true);
+            const float mu = st[2 * (v / cgv)], rs = st[2 * (v / cgv) + 1];
+            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+                RowsOf<DT, E> x;
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
+                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, v, mu, rs, f);
             }
         }
     }
 }
 
-// One vector of a row in the gradient: xhat and gamma dz (and dz).
-template <int DT, int E>
-struct GradCols {
-    float mu[E], rs[E], w[E], b[E];
-    __device__ void set(const NormArgs& a, int64_t seg, int v) {
+// Rows in registers are worked on one after another: interleaved by the
+// compiler's scheduler, their decoded values did not fit the registers.
+__device__ inline void one_row_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
+
+// x - mean and dz of one vector of a row, in few steps a value (the chip's
+// vector units, not its memory, bound this: 69 instructions a value took 207
+// us for 300K rows of 128 fp16 channels where memory asks for 48): with wr =
+// w rstd the argument of the activation is z = (x - mean) wr + b.
+template <int DT, int E, int ACT>
+struct GradAt {
+    float mu, rs, wr[E], w[E], b[E];
+    __device__ void set(const Affine<E>& f, float mean, float rstd) {
+        mu = mean;
+        rs = rstd;
 #pragma unroll
         for (int e = 0; e < E; e++) {
-            const int c = v * E + e;
-            const int64_t g = seg * a.groups + c / a.cg;
-            mu[e] = a.mean_in[g];
-            rs[e] = a.rstd_in[g];
-            w[e] = a.weight ? a.weight[c] : 1.f;
-            b[e] = a.bias ? a.bias[c] : 0.f;
+            w[e] = f.w[e];
+            b[e] = f.b[e];
+            wr[e] = w[e] * rs;
         }
     }
-    __device__ void at(const Stored<DT, E>& sx, const Stored<DT, E>& sy, int act, float (&hat)[E], float (&dz)[E]) const {
-        float x[E], y[E];
-        decode<DT, E>(sx, x);
-        decode<DT, E>(sy, y);
+    __device__ void at(const Stored<DT, E>& sx, const Stored<DT, E>& sy, float (&d)[E], float (&dz)[E]) const {
+        float x[E];
+        decode_here<DT, E>(sx, x);
+        decode_here<DT, E>(sy, dz);
 #pragma unroll
-        for (int e = 0; e < E; e++) {
-            hat[e] = (x[e] - mu[e]) * rs[e];
-            dz[e] = act_grad(y[e], x[e], mu[e], rs[e], hat[e], w[e], b[e], act);
+        for (int e = 0; e < E; e++) d[e] = x[e] - mu;
+        if constexpr (ACT == TAURUS_ACT_RELU) {
+            // as act_grad: near the border the side is decided in 64 bits
+            bool near = false, open[E];
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const float t = d[e] * wr[e], z = t + b[e];
+                open[e] = z > 0.f;
+                near |= fabsf(z) <= 0x1p-20f * (fabsf(t) + fabsf(b[e]));
+            }
+            if (near)
+#pragma unroll
+                for (int e = 0; e < E; e++) open[e] = open_exactly(x[e], mu, rs, w[e], b[e]);
+#pragma unroll
+            for (int e = 0; e < E; e++) dz[e] = open[e] ? dz[e] : 0.f;
+        } else if constexpr (ACT == TAURUS_ACT_SILU) {
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                const float z = d[e] * wr[e] + b[e], q = 1.f / (1.f + expf(-z));
+                dz[e] *= q * (1.f + z * (1.f - q));
+            }
         }
     }
-    // dx of the unit's rows, given the group means m1 and m2 of each channel
-    __device__ void write(const NormArgs& a, const Spread& t, int64_t r0, int rows, int v, const float (&m1)[E],
-                          const float (&m2)[E]) const {
-        constexpr int U = 2;
-        for (int r = t.ry; r < rows; r += U * t.RY) {
-            Stored<DT, E> sx[U], sy[U];
+    // dx of SEG_ROWS rows, given the means m1 and m2 of the vector's group:
+    // rstd (w dz - m1 - xhat m2) = wr dz - (rstd m1 + (x - mean) rstd^2 m2)
+    __device__ void store(const NormArgs& a, const RowsOf<DT, E>& x, const RowsOf<DT, E>& y, int64_t r0, int rows,
+                          int r, int RY, int v, float m1, float m2) const {
+        const float k1 = rs * m1, k2 = rs * rs * m2;
 #pragma unroll
-            for (int j = 0; j < U; j++) {
-                const int64_t rr = r0 + min(r + j * t.RY, rows - 1);
-                sx[j] = load_stored<DT, E>(a.x, rr * a.xs + v * E);
-                sy[j] = load_stored<DT, E>(a.dy, rr * a.ds + v * E);
-            }
+        for (int j = 0; j < SEG_ROWS; j++) {
+            const int rr = r + j * RY;
+            if (rr >= rows) continue;
+            float d[E], dz[E];
+            at(x.v[j], y.v[j], d, dz);
 #pragma unroll
-            for (int j = 0; j < U; j++) {
-                const int rr = r + j * t.RY;
-                if (rr >= rows) continue;
-                float hat[E], dz[E];
-                at(sx[j], sy[j], a.act, hat, dz);
-#pragma unroll
-                for (int e = 0; e < E; e++) dz[e] = rs[e] * (dz[e] * w[e] - m1[e] - hat[e] * m2[e]);
-                store_vec<DT, E>(a.out, (r0 + rr) * a.os + v * E, dz);
-            }
+            for (int e = 0; e < E; e++) dz[e] = wr[e] * dz[e] - (k1 + d[e] * k2);
+            store_vec<DT, E>(a.out, (r0 + rr) * a.os + (int64_t)v * E, dz);
+            one_row_at_a_time();
         }
     }
 };
 
 // Sums of dz and dz xhat of each unit: over groups for dx, over channels for
-// dgamma and dbeta (added up over the workgroup's consecutive slots).
-template <int DT, int E>
-__global__ __launch_bounds__(256) void k_norm_units_grad(NormArgs a) {
+// dgamma and dbeta, the latter kept by each thread for its channels over the
+// workgroup's slots (in LDS where it has several vectors of a row).
+template <int DT, int E, int BT, int ACT>
+__global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
     extern __shared__ float lds[];
-    float *ca = lds, *cb = ca + a.d, *ga = cb + a.d, *gb = ga + a.groups;
-    float *ta = gb + a.groups, *tb = ta + a.d, *scratch = tb + a.d;
-    const Spread t(a.d, E);
-    const Units find(a.off, a.segs, a.m, a.R);
-    for (int c = threadIdx.x; c < a.d; c += 256) ta[c] = tb[c] = 0.f;
-    const int64_t k0 = (int64_t)blockIdx.x * a.per_block, k1 = min(k0 + a.per_block, a.slots);
-    for (int64_t k = k0; k < k1; k++) {
-        const Unit u = find.at(k);
-        const int64_t units = u.units;
-        if (u.g < 0 || u.slot >= units) continue;  // for the whole workgroup
+    const Spread<BT> t(a.d, E);
+    const int entries = max(t.nv, BT);
+    float *s1 = lds, *s2 = s1 + entries, *g1 = s2 + entries, *g2 = g1 + a.groups;
+    float *ta = g2 + a.groups, *tb = ta + a.d;  // [d] each
+    const bool wide = t.nv > BT;
+    const int cgv = a.cg / E;
+    Affine<E> f;
+    float dw[E] = {}, db[E] = {};
+    if (!wide) f.set(a, t.cx, true);
+    for (int c = threadIdx.x; c < a.d; c += BT) ta[c] = tb[c] = 0.f;
+    const int64_t k0 = (int64_t)blockIdx.x * a.per_block;
+    for (SlotWalk walk(a, k0, min(k0 + a.per_block, a.slots)); walk.more(); walk.step()) {
+        const Unit u = walk.unit();
+        if (u.g < 0 || u.slot >= u.units) continue;  // for the whole workgroup
         const int rows = (int)(u.r1 - u.r0);
+        RowsOf<DT, E> x, y;
         __syncthreads();
-        for (int v0 = 0; v0 < t.nv; v0 += t.nvb) {
-            const int v = v0 + t.cx;
-            const bool in = t.ry < t.RY && v < t.nv;
-            float sa[E] = {}, sb[E] = {};
-            if (in) {
-                GradCols<DT, E> g;
-                g.set(a, u.g, v);
-                constexpr int U = 4;
-                for (int r = t.ry; r < rows; r += U * t.RY) {
-                    Stored<DT, E> sx[U], sy[U];
+        for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
+            if (wide) f.set(a, v, true);
+            const int64_t g = (int64_t)u.g * a.groups + v / cgv;
+            GradAt<DT, E, ACT> at;
+            at.set(f, a.mean_in[g], a.rstd_in[g]);
+            float sd[E] = {}, sz[E] = {};  // sums of dz (x - mean) and of dz
+            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
+                y.load(a.dy, a.ds, u.r0, rows, r, t.RY, (int64_t)v * E);
 #pragma unroll
-                    for (int j = 0; j < U; j++) {
-                        const int64_t rr = u.r0 + min(r + j * t.RY, rows - 1);
-                        sx[j] = load_stored<DT, E>(a.x, rr * a.xs + v * E);
-                        sy[j] = load_stored<DT, E>(a.dy, rr * a.ds + v * E);
-                    }
-#pragma unroll
-                    for (int j = 0; j < U; j++) {
-                        if (r + j * t.RY >= rows) continue;
-                        float hat[E], dz[E];
-                        g.at(sx[j], sy[j], a.act, hat, dz);
-#pragma unroll
-                        for (int e = 0; e < E; e++) {
-                            sa[e] += dz[e] * hat[e];
-                            sb[e] += dz[e];
-                        }
-                    }
-                }
-            }
-            for (int cnt = t.RY; cnt > 1;) {
-                const int half = (cnt + 1) / 2;
-                if (t.ry >= half && t.ry < cnt) {
-                    const int at = (t.ry - half) * t.nvb + t.cx;
+                for (int j = 0; j < SEG_ROWS; j++) {
+                    if (r + j * t.RY >= rows) continue;
+                    float d[E], dz[E];
+                    at.at(x.v[j], y.v[j], d, dz);
 #pragma unroll
                     for (int e = 0; e < E; e++) {
-                        scratch[at + 128 * e] = sa[e];
-                        scratch[at + 128 * (E + e)] = sb[e];
+                        sd[e] += dz[e] * d[e];
+                        sz[e] += dz[e];
                     }
+                    one_row_at_a_time();
                 }
-                __syncthreads();
-                if (t.ry + half < cnt) {
-                    const int at = t.ry * t.nvb + t.cx;
-#pragma unroll
-                    for (int e = 0; e < E; e++) {
-                        sa[e] += scratch[at + 128 * e];
-                        sb[e] += scratch[at + 128 * (E + e)];
-                    }
-                }
-                __syncthreads();
-                cnt = half;
             }
-            if (in && t.ry == 0)
+            float p = 0.f, q = 0.f;
 #pragma unroll
-                for (int e = 0; e < E; e++) {
-                    const int c = v * E + e;
-                    ca[c] = sa[e];
-                    cb[c] = sb[e];
-                    ta[c] += sa[e];
-                    tb[c] += sb[e];
+            for (int e = 0; e < E; e++) {
+                sd[e] *= at.rs;
+                p += sz[e] * at.w[e];
+                q += sd[e] * at.w[e];
+            }
+            s1[t.ry * t.nvb + v] = p;
+            s2[t.ry * t.nvb + v] = q;
+#pragma unroll
+            for (int e = 0; e < E; e++) {
+                if (wide) {
+                    ta[v * E + e] += sd[e];
+                    tb[v * E + e] += sz[e];
+                } else {
+                    dw[e] += sd[e];
+                    db[e] += sz[e];
                 }
+            }
         }
         if (!a.out) continue;
         __syncthreads();
-        const bool whole = units == 1;
-        const float inv = 1.f / ((float)rows * (float)a.cg);
-        over_groups(a.groups, a.cg, [&](int g, int lane, int gl) {
-            float s1 = 0.f, s2 = 0.f;
-            for (int c = lane; g >= 0 && c < a.cg; c += 1 << gl) {
-                const float w = a.weight ? a.weight[g * a.cg + c] : 1.f;
-                s1 += w * cb[g * a.cg + c];
-                s2 += w * ca[g * a.cg + c];
+        const bool whole = u.units == 1;
+        const int per = min(t.RY, rows) * cgv;
+        over_groups<BT>(a.groups, per, [&](int g, int lane, int gl) {
+            float p = 0.f, q = 0.f;
+            for (int i = lane; g >= 0 && i < per; i += 1 << gl) {
+                const int yy = i / cgv, at = yy * t.nvb + g * cgv + i - yy * cgv;
+                p += s1[at];
+                q += s2[at];
             }
-            s1 = sub_sum(s1, gl);
-            s2 = sub_sum(s2, gl);
+            p = sub_sum(p, gl);
+            q = sub_sum(q, gl);
             if (g < 0 || lane != 0) return;
             if (whole) {
-                ga[g] = s1 * inv;
-                gb[g] = s2 * inv;
+                const float inv = 1.f / ((float)rows * (float)a.cg);
+                g1[g] = p * inv;
+                g2[g] = q * inv;
             } else {
-                const int64_t p = unit_place(u.r0, u.slot, a.R) * a.groups + g;
-                a.part[2 * p] = s1;
-                a.part[2 * p + 1] = s2;
+                const int64_t at = unit_place(u.r0, u.slot, a.R) * a.groups + g;
+                a.part[2 * at] = p;
+                a.part[2 * at + 1] = q;
             }
         });
         if (!whole) continue;
         __syncthreads();
         for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
-            GradCols<DT, E> g;
-            g.set(a, u.g, v);
-            float m1[E], m2[E];
-#pragma unroll
-            for (int e = 0; e < E; e++) {
-                m1[e] = ga[(v * E + e) / a.cg];
-                m2[e] = gb[(v * E + e) / a.cg];
+            if (wide) f.set(a, v, true);
+            const int64_t g = (int64_t)u.g * a.groups + v / cgv;
+            GradAt<DT, E, ACT> at;
+            at.set(f, a.mean_in[g], a.rstd_in[g]);
+            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+                if (wide || rows > SEG_ROWS * t.RY) {
+                    x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
+                    y.load(a.dy, a.ds, u.r0, rows, r, t.RY, (int64_t)v * E);
+                }
+                at.store(a, x, y, u.r0, rows, r, t.RY, v, g1[v / cgv], g2[v / cgv]);
             }
-            g.write(a, t, u.r0, rows, v, m1, m2);
         }
     }
-    if (a.cols) {
-        __syncthreads();
-        float* row = a.cols + (int64_t)blockIdx.x * 2 * a.d;
-        for (int c = threadIdx.x; c < a.d; c += 256) {
-            row[c] = ta[c];
-            row[a.d + c] = tb[c];
+    if (!a.cols) return;
+    // the row lanes' channel sums, in row lane order
+    float* row = a.cols + (int64_t)blockIdx.x * 2 * a.d;
+    if (!wide)
+        for (int e = 0; e < E; e++) {  // one channel of each vector at a time
+            __syncthreads();
+            if (t.ry < t.RY) {
+                s1[t.ry * t.nvb + t.cx] = dw[0];
+                s2[t.ry * t.nvb + t.cx] = db[0];
+            }
+#pragma unroll
+            for (int i = 0; i + 1 < E; i++) {
+                dw[i] = dw[i + 1];
+                db[i] = db[i + 1];
+            }
+            __syncthreads();
+            if (threadIdx.x < (unsigned)t.nvb) {
+                float p = 0.f, q = 0.f;
+                for (int r = 0; r < t.RY; r++) {
+                    p += s1[r * t.nvb + t.cx];
+                    q += s2[r * t.nvb + t.cx];
+                }
+                ta[t.cx * E + e] = p;
+                tb[t.cx * E + e] = q;
+            }
         }
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.d; c += BT) {
+        row[c] = ta[c];
+        row[a.d + c] = tb[c];
     }
 }
 
-template <int DT, int E>
-__global__ __launch_bounds__(256) void k_norm_apply_grad(NormArgs a) {
-    const Spread t(a.d, E);
-    const Units find(a.off, a.segs, a.m, a.R);
-    for (int64_t k = blockIdx.x; k < a.slots; k += gridDim.x) {
-        const Unit u = find.at(k);
-        if (u.g < 0 || u.units <= 1 || u.r0 >= u.r1 || t.ry >= t.RY) continue;
+template <int DT, int E, int ACT>
+__global__ __launch_bounds__(256, 3) void k_norm_apply_grad(NormArgs a) {
+    const Spread<256> t(a.d, E);
+    const int cgv = a.cg / E;
+    for (int64_t k = blockIdx.x; k < a.places; k += gridDim.x) {
+        const Unit u = wave_place(a.off, a.segs, a.m, a.R, place_order(k, a.places));
+        if (u.r0 >= u.r1 || t.ry >= t.RY) continue;
+        const int rows = (int)(u.r1 - u.r0);
         const float* st = a.stat + 2 * (u.begin / a.R) * a.groups;
         for (int v = t.cx; v < t.nv; v += t.nvb) {
-            GradCols<DT, E> g;
-            g.set(a, u.g, v);
-            float m1[E], m2[E];
-#pragma unroll
-            for (int e = 0; e < E; e++) {
-                m1[e] = st[2 * ((v * E + e) / a.cg)];
-                m2[e] = st[2 * ((v * E + e) / a.cg) + 1];
+            Affine<E> f;
+            f.set(a, v, true);
+            const int64_t g = (int64_t)u.g * a.groups + v / cgv;
+            GradAt<DT, E, ACT> at;
+            at.set(f, a.mean_in[g], a.rstd_in[g]);
+            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+                RowsOf<DT, E> x, y;
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
+                y.load(a.dy, a.ds, u.r0, rows, r, t.RY, (int64_t)v * E);
+                at.store(a, x, y, u.r0, rows, r, t.RY, v, st[2 * (v / cgv)], st[2 * (v / cgv) + 1]);
             }
-            g.write(a, t, u.r0, (int)(u.r1 - u.r0), v, m1, m2);
         }
     }
 }
 
 // Column sums of part [rows][2 d] into dgamma (first d) and dbeta: a
-// workgroup takes 16 columns, 16 row lanes each, joined in a fixed order.
-__global__ __launch_bounds__(256) void k_norm_columns(const float* __restrict__ part, int64_t rows, int d,
-                                                      float* __restrict__ dw, float* __restrict__ db) {
-    __shared__ float s[16][17];
+// workgroup takes 16 columns, 64 row lanes each, joined in a fixed order.
+__global__ __launch_bounds__(1024) void k_norm_columns(const float* __restrict__ part, int64_t rows, int d,
+                                                       float* __restrict__ dw, float* __restrict__ db) {
+    __shared__ float s[64][17];
     const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
     const int c = blockIdx.x * 16 + cx;
     const int64_t width = 2 * (int64_t)d;
     float f = 0.f;
     if (c < width) {
         constexpr int U = 8;
-        for (int64_t r = ry; r < rows; r += 16 * U) {
+        for (int64_t r = ry; r < rows; r += 64 * U) {
             float v[U];
 #pragma unroll
-            for (int j = 0; j < U; j++) v[j] = r + 16 * j < rows ? part[(r + 16 * j) * width + c] : 0.f;
+            for (int j = 0; j < U; j++) v[j] = r + 64 * j < rows ? part[(r + 64 * j) * width + c] : 0.f;
 #pragma unroll
             for (int j = 0; j < U; j++) f += v[j];
         }
     }
     s[ry][cx] = f;
     __syncthreads();
+    if (ry < 8) {
+        f = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; j++) f += s[8 * ry + j][cx];
+        s[8 * ry][cx] = f;
+    }
+    __syncthreads();
     if (ry == 0 && c < width) {
         f = 0.f;
 #pragma unroll
-        for (int j = 0; j < 16; j++) f += s[j][cx];
+        for (int j = 0; j < 8; j++) f += s[8 * j][cx];
         if (c < d) {
             if (dw) dw[c] = f;
         } else if (db) {
@@ -758,14 +864,14 @@ __global__ __launch_bounds__(256) void k_norm_columns(const float* __restrict__ 
 
 // ---------------------------------------------------------------- launch ----
 
-// Rows a unit takes: enough units to fill the chip; with many segments, also
-// most segments in one unit (four times their mean length), unless a unit
-// would then be over 256 KB of rows.
+// Rows a unit takes: enough units to fill the chip; with many segments, most
+// segments in one unit (sixteen times their mean length), unless a unit would
+// then be over 256 KB of fp32 rows.
 static int norm_lr(int64_t m, int64_t d, int64_t segs) {
     int lr = 10;
     while (lr > 4 && m >> lr < 2048) lr--;
     if (segs >= 1024)
-        while (lr < 12 && ((int64_t)1 << lr) < 4 * m / segs && (d * 4 << (lr + 1)) <= 256 << 10) lr++;
+        while (lr < 12 && ((int64_t)1 << lr) < 16 * m / segs && (d * 4 << (lr + 1)) <= 256 << 10) lr++;
     return lr;
 }
 // Workgroups of the row walk: at most what the chip holds a few times over,
@@ -826,21 +932,33 @@ static void norm_rows(const NormArgs& a, const RowPlan& r, int64_t blocks, bool 
     else rows_e<DT, 1>(a, r, blocks, grad, s);
 }
 
-template <int DT, int E>
-static void segs_e(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
-    const size_t lds = ((size_t)(grad ? 4 : 2) * a.d + 2 * a.groups + scratch_floats(E)) * 4;
-    const int64_t longs = long_count(a.m, a.segs, a.R);
-    const bool longer = a.m > a.R;  // a segment can take several units
-    if (grad) k_norm_units_grad<DT, E><<<(unsigned)blocks, 256, lds, s>>>(a);
-    else k_norm_units<DT, E><<<grid_for(a.slots), 256, lds, s>>>(a);
+template <int DT, int E, int BT, int ACT>
+static void segs_units(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
+    const size_t lds = ((size_t)2 * std::max(a.d / E, BT) + 2 * a.groups + (grad ? 2 * a.d : 0)) * 4;
+    if (grad) k_norm_units_grad<DT, E, BT, ACT><<<(unsigned)blocks, BT, lds, s>>>(a);
+    else k_norm_units<DT, E, BT><<<(unsigned)blocks, BT, lds, s>>>(a);
     TAURUS_CHECK_LAUNCH();
-    if (!longer || (grad && !a.out)) return;
+}
+template <int DT, int E, int ACT>
+static void segs_act(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
+    // Small segments (up to about 16 vectors a lane of a wave) take a wave
+    // each, without barriers; longer ones four waves.
+    if (a.d / E <= 64 && a.m / a.segs * (a.d / E) <= 1024) segs_units<DT, E, 64, ACT>(a, blocks, grad, s);
+    else segs_units<DT, E, 256, ACT>(a, blocks, grad, s);
+    const int64_t longs = long_count(a.m, a.segs, a.R);
+    if (a.m <= a.R || (grad && !a.out)) return;  // no segment has several units
     if (grad) k_norm_join<true><<<grid_for(longs * a.groups), 256, 0, s>>>(a, longs);
     else k_norm_join<false><<<grid_for(longs * a.groups), 256, 0, s>>>(a, longs);
     TAURUS_CHECK_LAUNCH();
-    if (grad) k_norm_apply_grad<DT, E><<<grid_for(a.slots), 256, 0, s>>>(a);
-    else k_norm_apply<DT, E><<<grid_for(a.slots), 256, 0, s>>>(a);
+    if (grad) k_norm_apply_grad<DT, E, ACT><<<grid_for(a.places), 256, 0, s>>>(a);
+    else k_norm_apply<DT, E><<<grid_for(a.places), 256, 0, s>>>(a);
     TAURUS_CHECK_LAUNCH();
+}
+template <int DT, int E>
+static void segs_e(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
+    if (!grad || a.act == TAURUS_ACT_NONE) segs_act<DT, E, TAURUS_ACT_NONE>(a, blocks, grad, s);
+    else if (a.act == TAURUS_ACT_RELU) segs_act<DT, E, TAURUS_ACT_RELU>(a, blocks, grad, s);
+    else segs_act<DT, E, TAURUS_ACT_SILU>(a, blocks, grad, s);
 }
 template <int DT>
 static void norm_segs(const NormArgs& a, int e, int64_t blocks, bool grad, hipStream_t s) {
@@ -864,7 +982,7 @@ static NormWork norm_work(void* work, int64_t m, int64_t d, int64_t groups, int6
     if (by_segment) {
         w.R = 1 << norm_lr(m, d, segs);
         w.slots = unit_slots(m, segs, w.R);
-        w.per_block = (int)std::max<int64_t>(1, w.slots / 4096);
+        w.per_block = (int)std::max<int64_t>(ceil_div(w.slots, 8192), 1);
         w.blocks = ceil_div(w.slots, w.per_block);
         w.col_rows = w.blocks;
         if (m > w.R) {
@@ -918,6 +1036,7 @@ static void norm_run(NormArgs a, int dtype, int e, bool grad, void* work, int64_
     a.stat = w.stat;
     a.slots = w.slots;
     a.R = w.R;
+    a.places = unit_places(a.m, w.R);
     a.per_block = w.per_block;
     const bool none = a.off && a.segs == 0;  // no segment holds a row: the column sums are zeros
     if (none) {
@@ -931,7 +1050,7 @@ static void norm_run(NormArgs a, int dtype, int e, bool grad, void* work, int64_
         else norm_rows<TAURUS_F16>(a, r, w.blocks, grad, s);
     }
     if (a.cols) {
-        k_norm_columns<<<(unsigned)ceil_div(2 * (int64_t)a.d, 16), 256, 0, s>>>(a.cols, none ? 0 : w.col_rows, a.d,
+        k_norm_columns<<<(unsigned)ceil_div(2 * (int64_t)a.d, 16), 1024, 0, s>>>(a.cols, none ? 0 : w.col_rows, a.d,
                                                                                  dweight, dbias);
         TAURUS_CHECK_LAUNCH();
     }
@@ -970,7 +1089,7 @@ int taurus_group_norm(const void* x, int32_t dtype, int64_t m, int64_t d, int64_
         check_rows(out, out_dtype, m, d, out_stride, "out");
         for (const void* p : {(const void*)weight, (const void*)bias, (const void*)mean, (const void*)rstd})
             if (p) check_ptr(p, 4, "a statistic or weight");
-        const int64_t cols = off ? d : d / groups;
+        const int64_t cols = d / groups;  // a vector lies in one group
         int e = m > 0 ? vec_width(8, dtype, x, cols, x_stride) : 1;
         if (m > 0) e = std::min(e, vec_width(8, out_dtype, out, cols, out_stride));
         NormArgs a{};
@@ -1014,7 +1133,7 @@ int taurus_group_norm_grad(const void* grad, int64_t grad_stride, const void* x,
         }
         for (const void* p : {(const void*)weight, (const void*)bias, (const void*)dweight, (const void*)dbias})
             if (p) check_ptr(p, 4, "a weight or its gradient");
-        const int64_t cols = off ? d : d / groups;
+        const int64_t cols = d / groups;  // a vector lies in one group
         int e = 1;
         if (m > 0) {
             e = std::min(vec_width(8, dtype, x, cols, x_stride), vec_width(8, dtype, grad, cols, grad_stride));

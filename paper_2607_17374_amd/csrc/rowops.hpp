@@ -149,13 +149,23 @@ template <int DT, int E>
 __device__ inline void decode(const Stored<DT, E>& s, float (&f)[E]) {
     if constexpr (DT == TAURUS_F32) {
         __builtin_memcpy(f, &s, sizeof(f));
-    } else {
-        uint16_t h[E];
-        __builtin_memcpy(h, &s, sizeof(h));
+    } else if constexpr (E == 1) {
+        if constexpr (DT == TAURUS_BF16) f[0] = __uint_as_float((uint32_t)s.v[0] << 16);
+        else f[0] = (float)__builtin_bit_cast(_Float16, s.v[0]);
+    } else {  // two values a word, taken from it where they are used
+        uint32_t w[E / 2];
+        __builtin_memcpy(w, &s, sizeof(w));
 #pragma unroll
-        for (int i = 0; i < E; i++) {
-            if constexpr (DT == TAURUS_BF16) f[i] = __uint_as_float((uint32_t)h[i] << 16);
-            else f[i] = (float)__builtin_bit_cast(_Float16, h[i]);
+        for (int i = 0; i < E / 2; i++) {
+            if constexpr (DT == TAURUS_BF16) {
+                f[2 * i] = __uint_as_float(w[i] << 16);
+                f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            } else {
+                typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+                const half2_t h = __builtin_bit_cast(half2_t, w[i]);
+                f[2 * i] = (float)h.x;
+                f[2 * i + 1] = (float)h.y;
+            }
         }
     }
 }
@@ -302,6 +312,25 @@ __device__ inline Long wave_long(const int64_t* __restrict__ off, int64_t parts,
 // its range's first.
 __device__ inline int64_t unit_place(int64_t r0, int slot, int R) { return 2 * (r0 / R) + (slot == 0); }
 inline int64_t unit_places(int64_t m, int R) { return 2 * (m / R + 1); }
+
+// The unit at such a place (none: no rows), for a whole wave: the window's
+// even place is a later unit of the last range that starts before it, the
+// odd one the first unit of the last that starts in it.
+__device__ inline Unit wave_place(const int64_t* __restrict__ off, int64_t parts, int64_t m, int R, int64_t place) {
+    const int64_t w = place >> 1, first = place & 1, before = (w + first) * R;
+    const int64_t g = wave_last(parts, [&](int64_t p) { return (int64_t)off_at(off, p, m) < before; });
+    Unit u;
+    u.g = (int)g;
+    u.begin = off_at(off, g, m);
+    u.end = max((int64_t)off_at(off, g + 1, m), u.begin);
+    u.units = (u.end - u.begin + R - 1) / R;
+    const int64_t i = w - u.begin / R;  // units start in consecutive windows
+    const bool is = u.units > 1 && (first ? i == 0 : i > 0 && i < u.units);
+    u.slot = is ? (int)i : 0;
+    u.r0 = is ? u.begin + i * R : u.end;
+    u.r1 = min(u.r0 + R, u.end);
+    return u;
+}
 
 // Compute units of the current device.
 inline int compute_units() {
