@@ -25,24 +25,32 @@ def _code(dtype, what: str) -> int:
     return _CODE[dtype]
 
 
+# the current stream's handle without a Stream object (4 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _Call:
     """The device and stream of one call.  Tensors made inside belong to the
     stream; when it is not the current one, tensors that come from elsewhere
     are marked as used on it."""
+    __slots__ = ("device", "ptr", "ctx", "stream", "used")
 
     def __init__(self, first: torch.Tensor, stream, what: str):
         if not first.is_cuda:
             raise ValueError(f"{what} must be a device tensor")
         self.device = first.device
-        current = torch.cuda.current_stream(self.device)
-        self.stream = current if stream is None else stream
-        if self.stream.device != self.device:
-            raise ValueError(f"the stream is on {self.stream.device}, {what} on {self.device}")
-        self.foreign = self.stream != current
-        self.ctx = None
-        if self.foreign or torch.cuda.current_device() != self.device.index:
-            self.ctx = torch.cuda.stream(self.stream)
-        self.used: list = []
+        self.ctx = self.stream = self.used = None
+        index = self.device.index
+        self.ptr = _raw_stream(index)
+        if stream is not None:
+            if stream.device != self.device:
+                raise ValueError(f"the stream is on {stream.device}, {what} on {self.device}")
+            if stream.cuda_stream != self.ptr:
+                self.ptr, self.stream, self.used = stream.cuda_stream, stream, []
+                self.ctx = torch.cuda.stream(stream)
+        if self.ctx is None and torch.cuda.current_device() != index:
+            self.ctx = torch.cuda.device(index)
 
     def __enter__(self):
         if self.ctx is not None:
@@ -52,20 +60,21 @@ class _Call:
     def __exit__(self, *exc):
         if self.ctx is not None:
             self.ctx.__exit__(*exc)
-        if self.foreign:
+        if self.used is not None:
             for t in self.used:
                 t.record_stream(self.stream)
 
     def _mine(self, t: torch.Tensor, what: str):
         if t.device != self.device:
             raise ValueError(f"{what} must be on {self.device}, got {t.device}")
-        self.used.append(t)
+        if self.used is not None:
+            self.used.append(t)
 
     def rows(self, t: torch.Tensor, shape, what: str, dtype=None):
         """(pointer, stride) of a row array: [rows][cols], values of a row next
         to one another, rows that do not overlap."""
         self._mine(t, what)
-        if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        if t.dim() != 2 or (shape is not None and t.shape != shape):
             want = "two dimensions" if shape is None else f"shape {tuple(shape)}"
             raise ValueError(f"{what} must have {want}, got shape {tuple(t.shape)}")
         if dtype is not None and t.dtype != dtype:
@@ -85,7 +94,7 @@ class _Call:
         self._mine(t, what)
         if t.dtype != dtype:
             raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-        if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        if t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous with shape {tuple(shape)}, got shape {tuple(t.shape)}")
         return t.data_ptr()
 
@@ -113,10 +122,6 @@ class _Call:
             return None, None
         t = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         return t, t.data_ptr()
-
-    @property
-    def ptr(self) -> int:
-        return self.stream.cuda_stream
 
 
 def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:

@@ -154,7 +154,8 @@ def make_ids(kind, m, n, seed):
     return ids
 
 
-@pytest.mark.parametrize("m", [0, 1, 2, 63, 65, 1000, 1024, 1025, 4099, 40_000])
+@pytest.mark.parametrize("m", [0, 1, 2, 63, 65, 1000, 1024, 1025, 4096, 4097, 40_000, 65_536,
+                               65_537, 300_000])
 @pytest.mark.parametrize("kind", ["uniform", "one", "hubs", "runs", "none"])
 def test_lookup_grad(m, kind):
     n, d, scale = 257, 40, -0.75
@@ -167,6 +168,20 @@ def test_lookup_grad(m, kind):
     assert (out.cpu()[count[:, 0] == 0] == 0).all()
     again = T.lookup_rows_grad(grad.cuda(), ids.cuda(), n, scale)
     assert torch.equal(out, again)  # no order is left to chance
+
+
+@pytest.mark.parametrize("n", [1, 511, 512, 70_001, 1_000_003])
+@pytest.mark.parametrize("m", [100, 1500, 5000, 70_000])
+def test_lookup_grad_tables(n, m):
+    """Tables of one row to many more than there are ids (most rows then are
+    filled with zeros beforehand), ids of one to three sort digits."""
+    note(f"lookup_grad table n={n} m={m}")
+    ids = make_ids("uniform", m, n, n + m)
+    grad = normal((m, 12), F32, n)
+    out = torch.full((n, 12), 5.0, device="cuda")
+    T.lookup_rows_grad(grad.cuda(), ids.cuda(), n, out=out)
+    ref, size, count = grad_reference(grad, ids, n, 1.0)
+    close(out, ref, (count + 2) * U * size, F32, "tables")
 
 
 @pytest.mark.parametrize("din", DTYPES)
