@@ -493,8 +493,8 @@ int taurus_grouped_linear_grad(const void* grad, int64_t grad_stride, const void
  * float[rows or segments][groups], written for the gradient, or both NULL
  * (a segment without rows gets zeros).  segments is ignored when off is NULL.
  */
-int64_t taurus_group_norm_bytes(int64_t m, int64_t d, int64_t groups, int64_t segments, int32_t by_segment,
-                                int32_t grad);
+int64_t taurus_group_norm_bytes(int32_t dtype, int64_t m, int64_t d, int64_t groups, int64_t segments,
+                                int32_t by_segment, int32_t grad);
 int taurus_group_norm(const void* x, int32_t dtype, int64_t m, int64_t d, int64_t x_stride, int64_t groups,
                       const int64_t* off, int64_t segments, const float* weight, const float* bias, float eps,
                       int32_t act, void* out, int32_t out_dtype, int64_t out_stride, float* mean, float* rstd,

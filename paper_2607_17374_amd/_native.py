@@ -119,7 +119,7 @@ for _name, _res, _args in (
         ("taurus_grouped_linear", ctypes.c_int, "pilllplplppilp"),
         ("taurus_grouped_linear_grad_bytes", ctypes.c_int64, "illll"),
         ("taurus_grouped_linear_grad", ctypes.c_int, "plplilllplpplpipplp"),
-        ("taurus_group_norm_bytes", ctypes.c_int64, "llllii"),
+        ("taurus_group_norm_bytes", ctypes.c_int64, "illllii"),
         ("taurus_group_norm", ctypes.c_int, "pillllplppfipilppplp"),
         ("taurus_group_norm_grad", ctypes.c_int, "plplilllplppppiplppplp")):
     SIGNATURES[_name] = (_res, [_ARG[_c] for _c in _args])

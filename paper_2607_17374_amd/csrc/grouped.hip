@@ -85,28 +85,62 @@ struct Tile<TAURUS_F32> {
     static __device__ inline void add_sums(frag a, sums_t& s) { s += (a.x + a.y) + (a.z + a.w); }
 };
 
-// Sixteen bytes at column c of a row of `cols` values, value by value; values
-// past the end (and everything, unless `in`) are zero.
+// The first n values (0 < n < E) leave a piece, the others move down and
+// zeros follow: of a piece that ends at its row's end, what lies past the
+// column it is wanted from.  n is the same for all lanes.
+template <int SZ>
+__device__ inline uint4 drop_values(uint4 v, int n) {
+    if constexpr (SZ == 2) {
+        if (n & 1) {
+            v.x = v.x >> 16 | v.y << 16;
+            v.y = v.y >> 16 | v.z << 16;
+            v.z = v.z >> 16 | v.w << 16;
+            v.w = v.w >> 16;
+        }
+        n >>= 1;
+    }
+    if (n & 1) v = make_uint4(v.y, v.z, v.w, 0);
+    if (n & 2) v = make_uint4(v.z, v.w, 0, 0);
+    return v;
+}
+// One of two pieces, word by word (as a whole it would be chosen by its
+// address, which puts the pieces in memory).
+__device__ inline uint4 pick(bool first, uint4 a, uint4 b) {
+    return make_uint4(first ? a.x : b.x, first ? a.y : b.y, first ? a.z : b.z, first ? a.w : b.w);
+}
+// Sixteen bytes from column c on of a row of `cols` values, at any address of
+// a value: a piece that would pass the row's end is taken from its end
+// backwards, or value by value if the row is shorter than a piece.  Zeros past
+// the end, and for lanes without a row (`in`).
 template <int DT>
 __device__ inline uint4 load_values(const void* __restrict__ base, int64_t row_at, int c, int cols, bool in) {
     constexpr int E = Tile<DT>::E, SZ = type_bytes<DT>;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (!in || c >= cols) return v;
     const char* p = static_cast<const char*>(base) + row_at * SZ;
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (in)
+    if (cols >= E) {
+        const int from = min(c, cols - E);
+        const auto s = load_stored<DT, E>(p, from);
+        v = make_uint4(s.v[0], s.v[1], s.v[2], s.v[3]);
+        return from < c ? drop_values<SZ>(v, E - cols % E) : v;
+    }
+    uint32_t w[4] = {0, 0, 0, 0};  // c is 0
 #pragma unroll
-        for (int e = 0; e < E; e++)
-            if (c + e < cols) {
-                if constexpr (SZ == 4) w[e] = *reinterpret_cast<const uint32_t*>(p + (int64_t)(c + e) * 4);
-                else w[e >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + (int64_t)(c + e) * 2) << (16 * (e & 1));
-            }
+    for (int e = 0; e < E; e++)
+        if (e < cols) {
+            if constexpr (SZ == 4) w[e] = *reinterpret_cast<const uint32_t*>(p + e * 4);
+            else w[e >> 1] |= (uint32_t)*reinterpret_cast<const uint16_t*>(p + e * 2) << (16 * (e & 1));
+        }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Rows of whole 16-byte pieces (AL) go through a buffer resource over the
-// rows that exist: a thread's pieces differ by a fixed number of rows, so it
-// keeps one 32-bit offset, and what lies past the resource's end reads as
-// zeros without a branch.  A piece past its row's end takes the offset
-// OUTSIDE, which stays past every end (tiles span less than 2^31 bytes, at
-// most 128 rows of the widest stride) and wraps for no row of the tile.
+// Rows of whole four-byte words, at least a piece long (AL), go through a
+// buffer resource over the rows that exist: a thread's pieces differ by a
+// fixed number of rows, so it keeps one 32-bit offset, and a piece past the
+// resource's end reads as zeros without a branch (no piece lies across it: a
+// row's last one ends where the row does).  A piece past its row's end
+// takes the offset OUTSIDE, which stays past every end (tiles span less than
+// 2^31 bytes, at most 128 rows of the widest stride) and wraps for no row of
+// the tile.
 constexpr uint32_t OUTSIDE = 0x80000000u;
 __device__ inline __amdgpu_buffer_rsrc_t piece_rsrc(const void* base, int64_t at, int64_t bytes) {
     const char* p = static_cast<const char*>(base) + at;
@@ -117,20 +151,21 @@ __device__ inline uint4 load_buffer(__amdgpu_buffer_rsrc_t rs, uint32_t offset) 
     return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, offset, 0, 0));
 }
 
-// An operand along the contraction: ROWS rows of one stage.
+// An operand along the contraction: ROWS rows of one stage.  Values past the
+// contraction's end are zeros.
 template <int DT, int ROWS, bool AL>
 struct Along {
-    static constexpr int BYTES = ROWS * 128, PER = ROWS * 8 / 256, SZ = type_bytes<DT>;
+    static constexpr int BYTES = ROWS * 128, PER = ROWS * 8 / 256, SZ = type_bytes<DT>, E = Tile<DT>::E;
     static_assert(ROWS * 8 % 256 == 0, "whole pieces per thread");
     const void* base;
     int64_t at0, stride;  // first row's offset, values between rows
     int rows, depth;      // rows that exist (others are zero), contraction length
     __device__ inline void load(int k0, uint4 (&v)[PER]) const {
-        const int r0 = threadIdx.x >> 3, p = threadIdx.x & 7, c = k0 + p * Tile<DT>::E;
+        const int r0 = threadIdx.x >> 3, p = threadIdx.x & 7, c = k0 + p * E;
         if constexpr (AL) {
-            const auto rs = piece_rsrc(base, at0 * SZ, (int64_t)rows * stride * SZ);
+            const auto rs = piece_rsrc(base, at0 * SZ, ((int64_t)(rows - 1) * stride + depth) * SZ);
             const uint32_t row = (uint32_t)stride * SZ;
-            const uint32_t off = c < depth ? (uint32_t)r0 * row + (uint32_t)c * SZ : OUTSIDE;
+            const uint32_t off = c < depth ? (uint32_t)r0 * row + (uint32_t)min(c, depth - E) * SZ : OUTSIDE;
 #pragma unroll
             for (int q = 0; q < PER; q++) v[q] = load_buffer(rs, off + q * 32 * row);
         } else {
@@ -141,9 +176,22 @@ struct Along {
             }
         }
     }
-    static __device__ inline void stage(char* lds, const uint4 (&v)[PER]) {
+    // into LDS; the stage at k0, for the rest of a row that is no whole piece
+    __device__ inline void stage(char* lds, int k0, const uint4 (&v)[PER]) const {
         const int r0 = threadIdx.x >> 3, p = threadIdx.x & 7;
         char* at = lds + r0 * 128 + ((p ^ (r0 & 7)) << 4);  // 32 rows on, the exchange is the same
+        if constexpr (AL) {
+            const int rest = depth % E;
+            if (rest && k0 + Tile<DT>::STAGE > depth) {
+                const bool ends = k0 + p * E == depth - rest;
+#pragma unroll
+                for (int q = 0; q < PER; q++) {
+                    const uint4 d = drop_values<SZ>(v[q], E - rest);
+                    *reinterpret_cast<uint4*>(at + q * 32 * 128) = pick(ends, d, v[q]);
+                }
+                return;
+            }
+        }
 #pragma unroll
         for (int q = 0; q < PER; q++) *reinterpret_cast<uint4*>(at + q * 32 * 128) = v[q];
     }
@@ -154,16 +202,18 @@ struct Along {
     }
 };
 
-// An operand across the contraction: one stage of contraction rows, COLS wide.
+// An operand across the contraction: one stage of contraction rows, COLS
+// wide.  Rows past the contraction's end and columns past a row's end are
+// zeros.
 template <int DT, int COLS, bool AL>
 struct Across {
-    static constexpr int PIECES = COLS / Tile<DT>::E, STEP = 256 / PIECES, SZ = type_bytes<DT>;
+    static constexpr int E = Tile<DT>::E, PIECES = COLS / E, STEP = 256 / PIECES, SZ = type_bytes<DT>;
     static constexpr int PITCH = DT == TAURUS_F32 ? COLS * 4 + 16 : COLS * 2;
     static constexpr int BYTES = Tile<DT>::STAGE * PITCH, PER = Tile<DT>::STAGE / STEP;
     static_assert(256 % PIECES == 0 && Tile<DT>::STAGE % STEP == 0 && STEP % 4 == 0, "whole pieces per thread");
     const void* base;
-    int64_t at0, stride;  // first contraction row's offset at the tile's first column; values between rows
-    int depth, cols;      // contraction rows that exist, columns from the tile's first on
+    int64_t at0, stride;  // first contraction row's offset at its first column; values between rows
+    int depth, cols, c0;  // contraction rows that exist, columns of a row, the tile's first
     // which 32-byte unit of a row holds unit u (16-bit types): the 16 rows
     // 8 a + b (b < 4 or 4 <= b < 8) read together take the row's units twice
     static __device__ inline int unit_of(int k, int u) {
@@ -175,11 +225,12 @@ struct Across {
         else return k * PITCH + unit_of(k, p >> 1) * 32 + (p & 1) * 16;
     }
     __device__ inline void load(int k0, uint4 (&v)[PER]) const {
-        const int k = threadIdx.x / PIECES, p = threadIdx.x % PIECES, c = p * Tile<DT>::E;
+        const int k = threadIdx.x / PIECES, p = threadIdx.x % PIECES, c = c0 + p * E;
         if constexpr (AL) {
-            const auto rs = piece_rsrc(base, (at0 + (int64_t)k0 * stride) * SZ, (int64_t)(depth - k0) * stride * SZ);
+            const auto rs = piece_rsrc(base, (at0 + (int64_t)k0 * stride) * SZ,
+                                       depth > k0 ? ((int64_t)(depth - k0 - 1) * stride + cols) * SZ : 0);
             const uint32_t row = (uint32_t)stride * SZ;
-            const uint32_t off = c < cols ? (uint32_t)k * row + (uint32_t)c * SZ : OUTSIDE;
+            const uint32_t off = c < cols ? (uint32_t)k * row + (uint32_t)min(c, cols - E) * SZ : OUTSIDE;
 #pragma unroll
             for (int q = 0; q < PER; q++) v[q] = load_buffer(rs, off + q * STEP * row);
         } else {
@@ -191,16 +242,28 @@ struct Across {
             }
         }
     }
-    static __device__ inline void stage(char* lds, const uint4 (&v)[PER]) {
+    __device__ inline void stage(char* lds, int, const uint4 (&v)[PER]) const {
         const int k = threadIdx.x / PIECES, p = threadIdx.x % PIECES;
+        if constexpr (AL) {
+            const int rest = cols % E;
+            if (rest && c0 + COLS > cols) {
+                const bool ends = c0 + p * E == cols - rest;
+#pragma unroll
+                for (int q = 0; q < PER; q++) {
+                    const uint4 d = drop_values<SZ>(v[q], E - rest);
+                    *reinterpret_cast<uint4*>(lds + piece_at(k + q * STEP, p)) = pick(ends, d, v[q]);
+                }
+                return;
+            }
+        }
 #pragma unroll
         for (int q = 0; q < PER; q++) *reinterpret_cast<uint4*>(lds + piece_at(k + q * STEP, p)) = v[q];
     }
-    // columns [c0, c0 + 16), matrix step kb
-    static __device__ inline typename Tile<DT>::frag read(const char* lds, int c0, int kb) {
+    // columns [b, b + 16) of the tile, matrix step kb
+    static __device__ inline typename Tile<DT>::frag read(const char* lds, int b, int kb) {
         const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
         if constexpr (DT == TAURUS_F32) {
-            const float* p = reinterpret_cast<const float*>(lds + (kb * 16 + 4 * lk) * PITCH) + c0 + li;
+            const float* p = reinterpret_cast<const float*>(lds + (kb * 16 + 4 * lk) * PITCH) + b + li;
             constexpr int S = PITCH / 4;
             return make_float4(p[0], p[S], p[2 * S], p[3 * S]);
         } else {
@@ -209,7 +272,7 @@ struct Across {
 #pragma unroll
             for (int j = 0; j < 2; j++) {
                 const int k = kb * 32 + 8 * lk + 4 * j + (li >> 2);
-                const char* a = lds + k * PITCH + unit_of(k, c0 >> 4) * 32 + (li & 3) * 8;
+                const char* a = lds + k * PITCH + unit_of(k, b >> 4) * 32 + (li & 3) * 8;
                 h[j] = __builtin_bit_cast(
                     uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(const_cast<char*>(a))));
             }
@@ -269,8 +332,8 @@ __device__ inline void stream_tiles(Tiles& tiles, char* lds, int m0, int n0) {
         const int stages = max((depth + STAGE - 1) / STAGE, 1);  // none: one of zeros
         for (int st = 0; st < stages; st++) {
             __syncthreads();  // the stage before is read
-            OpM::stage(lds, vm);
-            OpN::stage(lds + OpM::BYTES, vn);
+            om.stage(lds, st * STAGE, vm);
+            on.stage(lds + OpM::BYTES, st * STAGE, vn);
             __syncthreads();
             if (st + 1 < stages) {
                 om.load((st + 1) * STAGE, vm);
@@ -304,18 +367,15 @@ __device__ inline void place_of(int64_t b, int64_t slots, int tiles, int64_t& sl
     }
 }
 
-// Four consecutive values of an output row of n columns, at column c; whole:
-// rows are whole vectors of four.
-__device__ inline void put4(void* out, int dtype, int64_t row_at, int c, int n, bool whole, floatx4 v) {
-    if (whole) {
-        if (c < n) {
-            const float f[4] = {v[0], v[1], v[2], v[3]};
-            store_as<4>(dtype, out, row_at + c, f);
-        }
+// Four consecutive values of an output row of n columns, at column c.
+__device__ inline void put4(void* out, int dtype, int64_t row_at, int c, int n, floatx4 v) {
+    if (c + 4 <= n) {
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        store_as<4>(dtype, out, row_at + c, f);
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 4; e++)
+    for (int e = 0; e < 3; e++)
         if (c + e < n) {
             const float f[1] = {v[e]};
             store_as<1>(dtype, out, row_at + c + e, f);
@@ -340,8 +400,16 @@ __device__ inline void put_pair16(void* out, int64_t row_at, int c, int n, bool 
     const auto lo = __builtin_amdgcn_permlane16_swap(pack(v[0], v[1]), pack(w[0], w[1]), false, false);
     const auto hi = __builtin_amdgcn_permlane16_swap(pack(v[2], v[3]), pack(w[2], w[3]), false, false);
     const int at = c + 16 * (lk & 1) + 8 * (lk >> 1);
-    if (in && at < n)
-        *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + row_at + at) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+    if (!in || at >= n) return;
+    uint16_t* p = static_cast<uint16_t*>(out) + row_at + at;
+    const uint32_t z[4] = {(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
+    if (at + 8 <= n) {
+        *reinterpret_cast<typename Raw<16, 2>::type*>(p) = typename Raw<16, 2>::type{z[0], z[1], z[2], z[3]};
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 7; e++)
+        if (at + e < n) p[e] = (uint16_t)(z[e >> 1] >> (16 * (e & 1)));
 }
 
 // ------------------------------------------------------- y = x W, dx = dy W^T
@@ -356,7 +424,7 @@ struct RowsArgs {
     const void* w;
     const float* bias;
     void* y;
-    int y_dtype, whole;  // whole: rows of y are whole vectors of four (1) or, 16-bit, eight (2)
+    int y_dtype;
     int64_t ys, slots;
     int tiles;
 };
@@ -394,7 +462,7 @@ struct RowTiles {
             const int64_t w0 = (int64_t)u.g * a.depth * a.cols;
             om = OpM{a.x, u.r0 * a.xs, a.xs, (int)(u.r1 - u.r0), a.depth};
             if constexpr (WT) on = OpN{a.w, w0 + (int64_t)next_c0 * a.depth, a.depth, min(TN, a.cols - next_c0), a.depth};
-            else on = OpN{a.w, w0 + next_c0, a.cols, a.depth, a.cols - next_c0};
+            else on = OpN{a.w, w0, a.cols, a.depth, a.cols, next_c0};
             b += gridDim.x;
             return true;
         }
@@ -417,7 +485,7 @@ struct RowTiles {
         for (int i = 0; i < MI; i++) {
             const int64_t r = r0 + m0 + 16 * i + li;
             const bool in = r < r1;
-            if (a.whole == 2) {
+            if (a.y_dtype != TAURUS_F32) {
 #pragma unroll
                 for (int j = 0; j < NI; j += 2) {
                     const int c = c0 + n0 + 16 * j;
@@ -429,7 +497,7 @@ struct RowTiles {
             } else if (in) {
 #pragma unroll
                 for (int j = 0; j < NI; j++)
-                    put4(a.y, a.y_dtype, r * a.ys, c0 + n0 + 16 * j + 4 * lk, a.cols, a.whole, acc[i][j]);
+                    put4(a.y, TAURUS_F32, r * a.ys, c0 + n0 + 16 * j + 4 * lk, a.cols, acc[i][j]);
             }
         }
     }
@@ -443,6 +511,10 @@ __global__ __launch_bounds__(256, TN == 64 ? 4 : 3) void k_grouped_rows(RowsArgs
     stream_tiles<DT, typename T::OpM, typename T::OpN, T::MI, T::NI, false>(tiles, lds, m0, n0);
 }
 
+static bool whole_words(int dtype, const void* p, int64_t cols, int64_t stride) {
+    const int64_t sz = dtype_size(dtype);
+    return cols * sz >= 16 && cols * sz % 4 == 0 && stride * sz % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 4 == 0;
+}
 template <int DT, bool WT, int TN>
 static void rows_al(bool al, const RowsArgs& a, hipStream_t s) {
     // as many workgroups as are resident at once
@@ -453,12 +525,10 @@ static void rows_al(bool al, const RowsArgs& a, hipStream_t s) {
 }
 template <int DT, bool WT>
 static void grouped_rows(RowsArgs a, hipStream_t s) {
-    constexpr int E = Tile<DT>::E;
     a.slots = unit_slots(a.m, a.groups, ROW_TILE);
-    const int wrow = WT ? a.depth : a.cols;  // weights' contiguous length
-    const bool al = vec_width(E, DT, a.x, a.depth, a.xs) == E && vec_width(E, DT, a.w, wrow, wrow) == E;
-    const int yv = vec_width(8, a.y_dtype, a.y, a.cols, a.ys);
-    a.whole = yv == 8 && a.y_dtype != TAURUS_F32 ? 2 : yv >= 4;
+    // rows of x and of the weights: whole words, at least a piece long
+    const int wrow = WT ? a.depth : a.cols;
+    const bool al = whole_words(DT, a.x, a.depth, a.xs) && whole_words(DT, a.w, wrow, wrow);
     if (DT == TAURUS_F32 || a.cols <= 64) {
         a.tiles = (int)ceil_div(a.cols, 64);
         rows_al<DT, WT, 64>(al, a, s);
@@ -480,7 +550,7 @@ struct WeightArgs {
     const int64_t* off;
     int64_t groups;
     void* dw;
-    int dw_dtype, whole;
+    int dw_dtype;
     float* db;
     float *part, *part_b;
     int64_t slots;
@@ -523,8 +593,8 @@ struct WeightTiles {
             next_last = u.units <= 1;
             next_place = next_last ? u.g : unit_place(u.r0, u.slot, a.R);
             depth = (int)(u.r1 - u.r0);
-            om = OpM{a.x, u.r0 * a.xs + next_k0, a.xs, depth, a.k - next_k0};
-            on = OpN{a.dy, u.r0 * a.ds + next_c0, a.ds, depth, a.n - next_c0};
+            om = OpM{a.x, u.r0 * a.xs, a.xs, depth, a.k, next_k0};
+            on = OpN{a.dy, u.r0 * a.ds, a.ds, depth, a.n, next_c0};
             b += gridDim.x;
             return true;
         }
@@ -542,7 +612,7 @@ struct WeightTiles {
 #pragma unroll
                 for (int i = 0; i < MI; i++) {
                     const int k = k0 + m0 + 16 * i + li;
-                    if (k < a.k) put4(out, dtype, (place * a.k + k) * a.n, c, a.n, a.whole, acc[i][j]);
+                    if (k < a.k) put4(out, dtype, (place * a.k + k) * a.n, c, a.n, acc[i][j]);
                 }
             if (!sums) continue;  // the same for the whole wave
             if constexpr (DT == TAURUS_F32) {
@@ -552,7 +622,7 @@ struct WeightTiles {
                 const int cc = c0 + n0 + 16 * j + li;
                 if (lk == 0 && cc < a.n) out_b[place * a.n + cc] = v;
             } else if (li == 0) {
-                put4(out_b, TAURUS_F32, place * a.n, c, a.n, false, nsum[j]);
+                put4(out_b, TAURUS_F32, place * a.n, c, a.n, nsum[j]);
             }
         }
     }
@@ -579,24 +649,21 @@ __global__ __launch_bounds__(256) void k_grouped_join(WeightArgs a, int64_t type
         const int64_t size = of_w ? (int64_t)a.k * a.n : a.n;
         const float* part = of_w ? a.part : a.part_b;
         const int64_t at = (int64_t)(of_w ? chunk : chunk - chunks_w) * 128 + v * 4;
-        const bool whole = size % 4 == 0;
+        const bool four = at + 4 <= size;
         float f[4] = {0.f, 0.f, 0.f, 0.f};
         // unit i starts in window t.window + i
         auto unit = [&](int64_t i) { return part + (2 * (t.window + i) + (i == 0)) * size + at; };
         int64_t i = eighth;
-        if (whole && at < size) {
+        if (four) {
             constexpr int U = 4;
             for (; i + 8 * (U - 1) < t.units; i += 8 * U) {
-                float4 x[U];
+                float x[U][4];
 #pragma unroll
-                for (int j = 0; j < U; j++) x[j] = *reinterpret_cast<const float4*>(unit(i + 8 * j));
+                for (int j = 0; j < U; j++) load_vec<TAURUS_F32, 4>(unit(i + 8 * j), 0, x[j]);
 #pragma unroll
-                for (int j = 0; j < U; j++) {
-                    f[0] += x[j].x;
-                    f[1] += x[j].y;
-                    f[2] += x[j].z;
-                    f[3] += x[j].w;
-                }
+                for (int j = 0; j < U; j++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) f[e] += x[j][e];
             }
         }
         for (; i < t.units; i += 8)
@@ -616,7 +683,7 @@ __global__ __launch_bounds__(256) void k_grouped_join(WeightArgs a, int64_t type
             }
             void* out = of_w ? a.dw : (void*)a.db;
             const int dtype = of_w ? a.dw_dtype : (int)TAURUS_F32;
-            if (of_w && a.whole) {
+            if (four) {
                 store_as<4>(dtype, out, t.g * size + at, f);
             } else {
 #pragma unroll
@@ -667,7 +734,6 @@ static void weight_al(bool al, const WeightArgs& a, hipStream_t s) {
 }
 template <int DT>
 static void grouped_weight(WeightArgs a, void* work, hipStream_t s) {
-    constexpr int E = Tile<DT>::E;
     a.R = weight_rows(DT, a.m, a.groups, a.k, a.n);
     const WeightWork w = weight_work(work, DT, a.m, a.groups, a.k, a.n);
     a.part = w.part;
@@ -676,8 +742,7 @@ static void grouped_weight(WeightArgs a, void* work, hipStream_t s) {
     const int tk = weight_tile_k(a.k), tn = weight_tile_n(DT, a.n);
     a.tiles_k = a.dw ? (int)ceil_div(a.k, tk) : 1;  // the first tile holds the sums of dy
     a.tiles_n = (int)ceil_div(a.n, tn);
-    a.whole = a.dw && vec_width(4, a.dw_dtype, a.dw, a.n, a.n) == 4;
-    const bool al = vec_width(E, DT, a.x, a.k, a.xs) == E && vec_width(E, DT, a.dy, a.n, a.ds) == E;
+    const bool al = whole_words(DT, a.x, a.k, a.xs) && whole_words(DT, a.dy, a.n, a.ds);
     if (tk == 64 && tn == 64) weight_al<DT, 64, 64>(al, a, s);
     else if (tn == 64) weight_al<DT, 128, 64>(al, a, s);
     else if constexpr (DT != TAURUS_F32) {
@@ -722,8 +787,8 @@ int taurus_grouped_linear(const void* x, int32_t dtype, int64_t m, int64_t d_in,
         check_rows(out, out_dtype, m, d_out, out_stride, "out");
         check_ptr(weight, dtype_size(dtype), "weight");
         if (bias) check_ptr(bias, 4, "bias");
-        const RowsArgs a{x,  m,  x_stride, (int)d_in, (int)d_out, off,        groups, weight,
-                         bias, out, out_dtype, 0,      out_stride, 0, 0};
+        const RowsArgs a{x,    m,   x_stride,  (int)d_in,  (int)d_out, off, groups, weight,
+                         bias, out, out_dtype, out_stride, 0,          0};
         auto s = static_cast<hipStream_t>(stream);
         if (dtype == TAURUS_F32) grouped_rows<TAURUS_F32, false>(a, s);
         else if (dtype == TAURUS_BF16) grouped_rows<TAURUS_BF16, false>(a, s);
@@ -765,7 +830,7 @@ int taurus_grouped_linear_grad(const void* grad, int64_t grad_stride, const void
         auto s = static_cast<hipStream_t>(stream);
         if (dx && m > 0) {
             const RowsArgs a{grad,    m,  grad_stride, (int)d_out, (int)d_in, off, groups, weight,
-                             nullptr, dx, dtype,       0,          dx_stride, 0,   0};
+                             nullptr, dx, dtype,       dx_stride,  0,         0};
             if (dtype == TAURUS_F32) grouped_rows<TAURUS_F32, true>(a, s);
             else if (dtype == TAURUS_BF16) grouped_rows<TAURUS_BF16, true>(a, s);
             else grouped_rows<TAURUS_F16, true>(a, s);

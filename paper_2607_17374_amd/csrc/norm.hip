@@ -116,23 +116,29 @@ template <int DT, int E, int P, bool WIDE>
 __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a, int lg) {
     __shared__ float red[4];
     const Walk k(a, lg);
-    const int nv = a.cg / E, c0 = k.group * a.cg;
+    const int nv = (a.cg + E - 1) / E, c0 = k.group * a.cg;
+    int at[P], again[P];  // of the lane's vectors: first channel, values the one before has too
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        at[p] = (int)vec_at<E>(k.lane + p * k.L, a.cg);
+        again[p] = k.lane + p * k.L < nv ? vec_again<E>(k.lane + p * k.L, a.cg) : E;
+    }
     float w[P][E], b[P][E];
 #pragma unroll
     for (int p = 0; p < P; p++)
 #pragma unroll
         for (int e = 0; e < E; e++) {
-            const int v = k.lane + p * k.L, c = c0 + v * E + e;
+            const int v = k.lane + p * k.L, c = c0 + at[p] + e;
             w[p][e] = v < nv && a.weight ? a.weight[c] : 1.f;
             b[p][e] = v < nv && a.bias ? a.bias[c] : 0.f;
         }
     Stored<DT, E> next[P];
     auto fetch = [&](int64_t it) {
-        const int64_t at = it / a.groups * a.xs + c0;
+        const int64_t row = it / a.groups * a.xs + c0;
 #pragma unroll
         for (int p = 0; p < P; p++) {
             const int v = k.lane + p * k.L;
-            next[p] = v < nv ? load_stored<DT, E>(a.x, at + v * E) : zero_stored<DT, E>();
+            next[p] = v < nv ? load_stored<DT, E>(a.x, row + at[p]) : zero_stored<DT, E>();
         }
     };
     if (k.sub < k.total) fetch(k.sub);
@@ -146,7 +152,7 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a, int lg) {
 #pragma unroll
         for (int p = 0; p < P; p++)
 #pragma unroll
-            for (int e = 0; e < E; e++) s += x[p][e];
+            for (int e = 0; e < E; e++) s += e >= again[p] ? x[p][e] : 0.f;
         const float mean = lanes_sum<WIDE>(s, lg, red) * inv;
         s = 0.f;
 #pragma unroll
@@ -154,17 +160,17 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormArgs a, int lg) {
 #pragma unroll
             for (int e = 0; e < E; e++) {
                 x[p][e] -= mean;
-                if (k.lane + p * k.L < nv) s += x[p][e] * x[p][e];
+                if (e >= again[p]) s += x[p][e] * x[p][e];
             }
         const float rstd = 1.f / sqrtf(lanes_sum<WIDE>(s, lg, red) * inv + a.eps);
-        const int64_t at = it / a.groups * a.os + c0;
+        const int64_t row = it / a.groups * a.os + c0;
 #pragma unroll
         for (int p = 0; p < P; p++) {
             const int v = k.lane + p * k.L;
             if (v >= nv) continue;
 #pragma unroll
             for (int e = 0; e < E; e++) x[p][e] = act_of(x[p][e] * rstd * w[p][e] + b[p][e], a.act);
-            store_as<E>(a.out_dtype, a.out, at + v * E, x[p]);
+            store_as<E>(a.out_dtype, a.out, row + at[p], x[p]);
         }
         if (a.mean && k.lane == 0) {
             a.mean[it] = mean;
@@ -177,13 +183,19 @@ template <int DT, int E, int P, bool WIDE>
 __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a, int lg) {
     __shared__ float red[4];
     const Walk k(a, lg);
-    const int nv = a.cg / E, c0 = k.group * a.cg;
+    const int nv = (a.cg + E - 1) / E, c0 = k.group * a.cg;
+    int at[P], again[P];  // of the lane's vectors: first channel, values the one before has too
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+        at[p] = (int)vec_at<E>(k.lane + p * k.L, a.cg);
+        again[p] = k.lane + p * k.L < nv ? vec_again<E>(k.lane + p * k.L, a.cg) : E;
+    }
     float w[P][E], b[P][E], dw[P][E], db[P][E];
 #pragma unroll
     for (int p = 0; p < P; p++)
 #pragma unroll
         for (int e = 0; e < E; e++) {
-            const int v = k.lane + p * k.L, c = c0 + v * E + e;
+            const int v = k.lane + p * k.L, c = c0 + at[p] + e;
             w[p][e] = v < nv && a.weight ? a.weight[c] : 1.f;
             b[p][e] = v < nv && a.bias ? a.bias[c] : 0.f;
             dw[p][e] = db[p][e] = 0.f;
@@ -195,8 +207,8 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a, int lg) {
 #pragma unroll
         for (int p = 0; p < P; p++) {
             const int v = k.lane + p * k.L;
-            nx[p] = v < nv ? load_stored<DT, E>(a.x, r * a.xs + c0 + v * E) : zero_stored<DT, E>();
-            ny[p] = v < nv ? load_stored<DT, E>(a.dy, r * a.ds + c0 + v * E) : zero_stored<DT, E>();
+            nx[p] = v < nv ? load_stored<DT, E>(a.x, r * a.xs + c0 + at[p]) : zero_stored<DT, E>();
+            ny[p] = v < nv ? load_stored<DT, E>(a.dy, r * a.ds + c0 + at[p]) : zero_stored<DT, E>();
         }
         nmean = a.mean_in[it];
         nrstd = a.rstd_in[it];
@@ -219,7 +231,7 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a, int lg) {
             for (int e = 0; e < E; e++) {
                 const float hat = (x[p][e] - mean) * rstd;
                 const float dz = act_grad(g[p][e], x[p][e], mean, rstd, hat, w[p][e], b[p][e], a.act);
-                if (k.lane + p * k.L < nv) {
+                if (e >= again[p]) {
                     dw[p][e] += dz * hat;
                     db[p][e] += dz;
                     s1 += dz * w[p][e];
@@ -231,14 +243,14 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a, int lg) {
         s1 = lanes_sum<WIDE>(s1, lg, red) * inv;
         s2 = lanes_sum<WIDE>(s2, lg, red) * inv;
         if (a.out) {
-            const int64_t at = it / a.groups * a.os + c0;
+            const int64_t row = it / a.groups * a.os + c0;
 #pragma unroll
             for (int p = 0; p < P; p++) {
                 const int v = k.lane + p * k.L;
                 if (v >= nv) continue;
 #pragma unroll
                 for (int e = 0; e < E; e++) g[p][e] = rstd * (g[p][e] - s1 - x[p][e] * s2);
-                store_vec<DT, E>(a.out, at + v * E, g[p]);
+                store_vec<DT, E>(a.out, row + at[p], g[p]);
             }
         }
     }
@@ -249,10 +261,11 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a, int lg) {
             const int v = k.lane + p * k.L;
             if (v >= nv) continue;
 #pragma unroll
-            for (int e = 0; e < E; e++) {
-                row[v * E + e] = dw[p][e];
-                row[a.d + v * E + e] = db[p][e];
-            }
+            for (int e = 0; e < E; e++)
+                if (e >= again[p]) {
+                    row[at[p] + e] = dw[p][e];
+                    row[a.d + at[p] + e] = db[p][e];
+                }
         }
     }
 }
@@ -263,11 +276,13 @@ __global__ __launch_bounds__(256) void k_norm_rows_grad(NormArgs a, int lg) {
 // RY rows at a time (threads past the last whole row rest).  Rows of more
 // than BT vectors (WIDE) are taken BT vectors at a time, one row at a time.
 // A vector lies in one group.
-template <int BT>
+template <int BT, int E>
 struct Spread {
-    int nv, nvb, RY, cx, ry;
-    __device__ Spread(int d, int E) {
-        nv = d / E;
+    int nv, nvb, RY, cx, ry, cg, cgv;  // cgv: vectors a group
+    __device__ Spread(const NormArgs& a) {
+        cg = a.cg;
+        cgv = (cg + E - 1) / E;
+        nv = a.groups * cgv;
         nvb = min(nv, BT);
         RY = BT / nvb;
         cx = threadIdx.x % nvb;
@@ -275,6 +290,14 @@ struct Spread {
     }
     // rows of a unit that row lane r takes
     __device__ int count(int rows, int r) const { return (rows - r + RY - 1) / RY; }
+    // vector v's group, first channel, and values that the vector before it
+    // in the group has too (they count there)
+    __device__ int group(int v) const { return v / cgv; }
+    __device__ int channel(int v) const {
+        const int g = v / cgv;
+        return g * cg + (int)vec_at<E>(v - g * cgv, cg);
+    }
+    __device__ int again(int v) const { return vec_again<E>(v % cgv, cg); }
 };
 
 // A workgroup's consecutive slots: the first by search, the others by
@@ -338,11 +361,11 @@ __device__ inline float sub_sum(float v, int gl) {
 template <int E>
 struct Affine {
     float w[E], b[E];
-    __device__ void set(const NormArgs& a, int v, bool in) {
+    __device__ void set(const NormArgs& a, int c) {
 #pragma unroll
         for (int e = 0; e < E; e++) {
-            w[e] = in && a.weight ? a.weight[v * E + e] : 1.f;
-            b[e] = in && a.bias ? a.bias[v * E + e] : 0.f;
+            w[e] = a.weight ? a.weight[c + e] : 1.f;
+            b[e] = a.bias ? a.bias[c + e] : 0.f;
         }
     }
 };
@@ -377,7 +400,7 @@ struct RowsOf {
 };
 
 template <int DT, int E>
-__device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E>& x, int64_t r0, int rows, int r, int RY, int v,
+__device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E>& x, int64_t r0, int rows, int r, int RY, int c,
                                   float mu, float rs, const Affine<E>& f) {
     float w[E];
 #pragma unroll
@@ -390,7 +413,7 @@ __device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E>& x, int
         decode_here<DT, E>(x.v[j], z);
 #pragma unroll
         for (int e = 0; e < E; e++) z[e] = act_of((z[e] - mu) * w[e] + f.b[e], a.act);
-        store_as<E>(a.out_dtype, a.out, (r0 + rr) * a.os + (int64_t)v * E, z);
+        store_as<E>(a.out_dtype, a.out, (r0 + rr) * a.os + c, z);
     }
 }
 
@@ -399,13 +422,13 @@ __device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E>& x, int
 template <int DT, int E, int BT>
 __global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
     extern __shared__ float lds[];
-    const Spread<BT> t(a.d, E);
+    const Spread<BT, E> t(a);
     const int entries = max(t.nv, BT);
     float *sm = lds, *sq = sm + entries, *gm = sq + entries, *gr = gm + a.groups;
     const bool wide = t.nv > BT;
-    const int cgv = a.cg / E;  // vectors a group
+    const int cgv = t.cgv;
     Affine<E> f;
-    if (!wide) f.set(a, t.cx, true);
+    if (!wide) f.set(a, t.channel(t.cx));
     const int64_t k0 = (int64_t)blockIdx.x * a.per_block;
     for (SlotWalk walk(a, k0, min(k0 + a.per_block, a.slots)); walk.more(); walk.step()) {
         const Unit u = walk.unit();
@@ -421,17 +444,18 @@ __global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
         RowsOf<DT, E> x;
         __syncthreads();  // the arrays may still be read for an earlier unit
         for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
+            const int c = t.channel(v), again = t.again(v);
             float n = 0.f, mean = 0.f, m2 = 0.f;
             for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
-                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
                 float s = 0.f, cnt = 0.f;
 #pragma unroll
                 for (int j = 0; j < SEG_ROWS; j++) {
                     float y[E];
                     decode_here<DT, E>(x.v[j], y);
-                    cnt += r + j * t.RY < rows ? (float)E : 0.f;
+                    cnt += r + j * t.RY < rows ? (float)(E - again) : 0.f;
 #pragma unroll
-                    for (int e = 0; e < E; e++) s += y[e];
+                    for (int e = 0; e < E; e++) s += e >= again ? y[e] : 0.f;
                 }
                 const float mb = s / cnt, share = cnt / (n + cnt);
                 float q = 0.f;
@@ -441,7 +465,7 @@ __global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
                     decode_here<DT, E>(x.v[j], y);
                     if (r + j * t.RY < rows)
 #pragma unroll
-                        for (int e = 0; e < E; e++) q += (y[e] - mb) * (y[e] - mb);
+                        for (int e = 0; e < E; e++) q += e >= again ? (y[e] - mb) * (y[e] - mb) : 0.f;
                 }
                 const float delta = mb - mean;
                 mean += delta * share;
@@ -456,18 +480,18 @@ __global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
         const int lanes_y = min(t.RY, rows), per = lanes_y * cgv;
         over_groups<BT>(a.groups, per, [&](int g, int lane, int gl) {
             const float first = g >= 0 ? sm[g * cgv] : 0.f;
-            const float inv = 1.f / ((float)rows * (float)cgv);  // a row lane's mean counts its rows
+            const float inv = 1.f / ((float)rows * (float)a.cg);  // a mean counts the values it is of
             float s = 0.f;
             for (int i = lane; g >= 0 && i < per; i += 1 << gl) {
-                const int y = i / cgv;
-                s += (sm[y * t.nvb + g * cgv + i - y * cgv] - first) * (float)t.count(rows, y);
+                const int y = i / cgv, x = i - y * cgv;
+                s += (sm[y * t.nvb + g * cgv + x] - first) * (float)(t.count(rows, y) * (E - vec_again<E>(x, a.cg)));
             }
             const float mean = first + sub_sum(s, gl) * inv;
             s = 0.f;
             for (int i = lane; g >= 0 && i < per; i += 1 << gl) {
-                const int y = i / cgv, at = y * t.nvb + g * cgv + i - y * cgv;
+                const int y = i / cgv, x = i - y * cgv, at = y * t.nvb + g * cgv + x;
                 const float dev = sm[at] - mean;
-                s += sq[at] + (float)(t.count(rows, y) * E) * dev * dev;
+                s += sq[at] + (float)(t.count(rows, y) * (E - vec_again<E>(x, a.cg))) * dev * dev;
             }
             const float m2 = sub_sum(s, gl);
             if (g < 0 || lane != 0) return;
@@ -488,11 +512,12 @@ __global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
         if (!whole) continue;
         __syncthreads();
         for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
-            if (wide) f.set(a, v, true);
-            const float mu = gm[v / cgv], rs = gr[v / cgv];
+            const int c = t.channel(v);
+            if (wide) f.set(a, c);
+            const float mu = gm[t.group(v)], rs = gr[t.group(v)];
             for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
-                if (wide || rows > SEG_ROWS * t.RY) x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
-                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, v, mu, rs, f);
+                if (wide || rows > SEG_ROWS * t.RY) x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
+                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, c, mu, rs, f);
             }
         }
     }
@@ -571,21 +596,21 @@ __device__ inline int64_t place_order(int64_t k, int64_t places) {
 // The second pass over the rows of longer segments.
 template <int DT, int E>
 __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
-    const Spread<256> t(a.d, E);
-    const int cgv = a.cg / E;
+    const Spread<256, E> t(a);
     for (int64_t k = blockIdx.x; k < a.places; k += gridDim.x) {
         const Unit u = wave_place(a.off, a.segs, a.m, a.R, place_order(k, a.places));
         if (u.r0 >= u.r1 || t.ry >= t.RY) continue;
         const int rows = (int)(u.r1 - u.r0);
         const float* st = a.stat + 2 * (u.begin / a.R) * a.groups;
         for (int v = t.cx; v < t.nv; v += t.nvb) {
+            const int c = t.channel(v);
             Affine<E> f;
-            f.set(a, v, true);
-            const float mu = st[2 * (v / cgv)], rs = st[2 * (v / cgv) + 1];
+            f.set(a, c);
+            const float mu = st[2 * t.group(v)], rs = st[2 * t.group(v) + 1];
             for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
                 RowsOf<DT, E> x;
-                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
-                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, v, mu, rs, f);
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
+                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, c, mu, rs, f);
             }
         }
     }
@@ -643,7 +668,7 @@ struct GradAt {
     // dx of SEG_ROWS rows, given the means m1 and m2 of the vector's group:
     // rstd (w dz - m1 - xhat m2) = wr dz - (rstd m1 + (x - mean) rstd^2 m2)
     __device__ void store(const NormArgs& a, const RowsOf<DT, E>& x, const RowsOf<DT, E>& y, int64_t r0, int rows,
-                          int r, int RY, int v, float m1, float m2) const {
+                          int r, int RY, int c, float m1, float m2) const {
         const float k1 = rs * m1, k2 = rs * rs * m2;
 #pragma unroll
         for (int j = 0; j < SEG_ROWS; j++) {
@@ -653,7 +678,7 @@ struct GradAt {
             at(x.v[j], y.v[j], d, dz);
 #pragma unroll
             for (int e = 0; e < E; e++) dz[e] = wr[e] * dz[e] - (k1 + d[e] * k2);
-            store_vec<DT, E>(a.out, (r0 + rr) * a.os + (int64_t)v * E, dz);
+            store_vec<DT, E>(a.out, (r0 + rr) * a.os + c, dz);
             one_row_at_a_time();
         }
     }
@@ -665,15 +690,14 @@ struct GradAt {
 template <int DT, int E, int BT, int ACT>
 __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
     extern __shared__ float lds[];
-    const Spread<BT> t(a.d, E);
+    const Spread<BT, E> t(a);
     const int entries = max(t.nv, BT);
     float *s1 = lds, *s2 = s1 + entries, *g1 = s2 + entries, *g2 = g1 + a.groups;
     float *ta = g2 + a.groups, *tb = ta + a.d;  // [d] each
     const bool wide = t.nv > BT;
-    const int cgv = a.cg / E;
     Affine<E> f;
     float dw[E] = {}, db[E] = {};
-    if (!wide) f.set(a, t.cx, true);
+    if (!wide) f.set(a, t.channel(t.cx));
     for (int c = threadIdx.x; c < a.d; c += BT) ta[c] = tb[c] = 0.f;
     const int64_t k0 = (int64_t)blockIdx.x * a.per_block;
     for (SlotWalk walk(a, k0, min(k0 + a.per_block, a.slots)); walk.more(); walk.step()) {
@@ -683,14 +707,15 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
         RowsOf<DT, E> x, y;
         __syncthreads();
         for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
-            if (wide) f.set(a, v, true);
-            const int64_t g = (int64_t)u.g * a.groups + v / cgv;
+            const int c = t.channel(v);
+            if (wide) f.set(a, c);
+            const int64_t g = (int64_t)u.g * a.groups + t.group(v);
             GradAt<DT, E, ACT> at;
             at.set(f, a.mean_in[g], a.rstd_in[g]);
             float sd[E] = {}, sz[E] = {};  // sums of dz (x - mean) and of dz
             for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
-                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
-                y.load(a.dy, a.ds, u.r0, rows, r, t.RY, (int64_t)v * E);
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
+                y.load(a.dy, a.ds, u.r0, rows, r, t.RY, c);
 #pragma unroll
                 for (int j = 0; j < SEG_ROWS; j++) {
                     if (r + j * t.RY >= rows) continue;
@@ -704,10 +729,12 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
                     one_row_at_a_time();
                 }
             }
+            const int again = t.again(v);
             float p = 0.f, q = 0.f;
 #pragma unroll
             for (int e = 0; e < E; e++) {
                 sd[e] *= at.rs;
+                if (e < again) continue;
                 p += sz[e] * at.w[e];
                 q += sd[e] * at.w[e];
             }
@@ -716,8 +743,9 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
 #pragma unroll
             for (int e = 0; e < E; e++) {
                 if (wide) {
-                    ta[v * E + e] += sd[e];
-                    tb[v * E + e] += sz[e];
+                    if (e < again) continue;
+                    ta[c + e] += sd[e];
+                    tb[c + e] += sz[e];
                 } else {
                     dw[e] += sd[e];
                     db[e] += sz[e];
@@ -727,7 +755,7 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
         if (!a.out) continue;
         __syncthreads();
         const bool whole = u.units == 1;
-        const int per = min(t.RY, rows) * cgv;
+        const int cgv = t.cgv, per = min(t.RY, rows) * cgv;
         over_groups<BT>(a.groups, per, [&](int g, int lane, int gl) {
             float p = 0.f, q = 0.f;
             for (int i = lane; g >= 0 && i < per; i += 1 << gl) {
@@ -751,16 +779,17 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
         if (!whole) continue;
         __syncthreads();
         for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
-            if (wide) f.set(a, v, true);
-            const int64_t g = (int64_t)u.g * a.groups + v / cgv;
+            const int c = t.channel(v);
+            if (wide) f.set(a, c);
+            const int64_t g = (int64_t)u.g * a.groups + t.group(v);
             GradAt<DT, E, ACT> at;
             at.set(f, a.mean_in[g], a.rstd_in[g]);
             for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
                 if (wide || rows > SEG_ROWS * t.RY) {
-                    x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
-                    y.load(a.dy, a.ds, u.r0, rows, r, t.RY, (int64_t)v * E);
+                    x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
+                    y.load(a.dy, a.ds, u.r0, rows, r, t.RY, c);
                 }
-                at.store(a, x, y, u.r0, rows, r, t.RY, v, g1[v / cgv], g2[v / cgv]);
+                at.store(a, x, y, u.r0, rows, r, t.RY, c, g1[t.group(v)], g2[t.group(v)]);
             }
         }
     }
@@ -786,8 +815,10 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
                     p += s1[r * t.nvb + t.cx];
                     q += s2[r * t.nvb + t.cx];
                 }
-                ta[t.cx * E + e] = p;
-                tb[t.cx * E + e] = q;
+                if (e >= t.again(t.cx)) {
+                    ta[t.channel(t.cx) + e] = p;
+                    tb[t.channel(t.cx) + e] = q;
+                }
             }
         }
     __syncthreads();
@@ -799,24 +830,24 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
 
 template <int DT, int E, int ACT>
 __global__ __launch_bounds__(256, 3) void k_norm_apply_grad(NormArgs a) {
-    const Spread<256> t(a.d, E);
-    const int cgv = a.cg / E;
+    const Spread<256, E> t(a);
     for (int64_t k = blockIdx.x; k < a.places; k += gridDim.x) {
         const Unit u = wave_place(a.off, a.segs, a.m, a.R, place_order(k, a.places));
         if (u.r0 >= u.r1 || t.ry >= t.RY) continue;
         const int rows = (int)(u.r1 - u.r0);
         const float* st = a.stat + 2 * (u.begin / a.R) * a.groups;
         for (int v = t.cx; v < t.nv; v += t.nvb) {
+            const int c = t.channel(v);
             Affine<E> f;
-            f.set(a, v, true);
-            const int64_t g = (int64_t)u.g * a.groups + v / cgv;
+            f.set(a, c);
+            const int64_t g = (int64_t)u.g * a.groups + t.group(v);
             GradAt<DT, E, ACT> at;
             at.set(f, a.mean_in[g], a.rstd_in[g]);
             for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
                 RowsOf<DT, E> x, y;
-                x.load(a.x, a.xs, u.r0, rows, r, t.RY, (int64_t)v * E);
-                y.load(a.dy, a.ds, u.r0, rows, r, t.RY, (int64_t)v * E);
-                at.store(a, x, y, u.r0, rows, r, t.RY, v, st[2 * (v / cgv)], st[2 * (v / cgv) + 1]);
+                x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
+                y.load(a.dy, a.ds, u.r0, rows, r, t.RY, c);
+                at.store(a, x, y, u.r0, rows, r, t.RY, c, st[2 * t.group(v)], st[2 * t.group(v) + 1]);
             }
         }
     }
@@ -889,7 +920,7 @@ struct RowPlan {
 // lanes and vectors a lane for groups of cg channels in vectors of e
 static RowPlan row_plan(int e, int cg) {
     RowPlan r{e, 1, 0, false};
-    const int nv = cg / e;
+    const int nv = (int)ceil_div(cg, e);
     const int most = 16 / e;  // vectors a lane: 16 values
     while (r.lg < 6 && nv > 1 << r.lg) r.lg++;
     while (r.p < most && nv > r.p << r.lg) r.p *= 2;
@@ -934,7 +965,7 @@ static void norm_rows(const NormArgs& a, const RowPlan& r, int64_t blocks, bool 
 
 template <int DT, int E, int BT, int ACT>
 static void segs_units(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
-    const size_t lds = ((size_t)2 * std::max(a.d / E, BT) + 2 * a.groups + (grad ? 2 * a.d : 0)) * 4;
+    const size_t lds = ((size_t)2 * std::max<int64_t>(a.groups * ceil_div(a.cg, E), BT) + 2 * a.groups + (grad ? 2 * a.d : 0)) * 4;
     if (grad) k_norm_units_grad<DT, E, BT, ACT><<<(unsigned)blocks, BT, lds, s>>>(a);
     else k_norm_units<DT, E, BT><<<(unsigned)blocks, BT, lds, s>>>(a);
     TAURUS_CHECK_LAUNCH();
@@ -943,7 +974,8 @@ template <int DT, int E, int ACT>
 static void segs_act(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
     // Small segments (up to about 16 vectors a lane of a wave) take a wave
     // each, without barriers; longer ones four waves.
-    if (a.d / E <= 64 && a.m / a.segs * (a.d / E) <= 1024) segs_units<DT, E, 64, ACT>(a, blocks, grad, s);
+    const int64_t nv = a.groups * ceil_div(a.cg, E);
+    if (nv <= 64 && a.m / a.segs * nv <= 1024) segs_units<DT, E, 64, ACT>(a, blocks, grad, s);
     else segs_units<DT, E, 256, ACT>(a, blocks, grad, s);
     const int64_t longs = long_count(a.m, a.segs, a.R);
     if (a.m <= a.R || (grad && !a.out)) return;  // no segment has several units
@@ -997,16 +1029,15 @@ static NormWork norm_work(void* work, int64_t m, int64_t d, int64_t groups, int6
     w.bytes = c.bytes();
     return w;
 }
-// The gradient's workspace for any alignment of its arrays: fewer lanes a
-// row leave more rows of channel sums, so the narrowest plan counts.
-static int64_t norm_bytes(int64_t m, int64_t d, int64_t groups, int64_t segs, bool by_segment, bool grad) {
-    int64_t most = 0;
-    for (int e = 1; e <= 8; e *= 2) {
-        if (by_segment && e > 1) break;
-        if ((d / groups) % e) continue;
-        most = std::max(most, norm_work(nullptr, m, d, groups, segs, by_segment, grad, row_plan(e, (int)(d / groups)).lg).bytes);
-    }
-    return most;
+// Values of a vector: 16 bytes of a group's channels (half of that where the
+// group is shorter, or one).
+static int norm_vec(int dtype, int64_t cg) {
+    const int e = vec_width(dtype == TAURUS_F32 ? 4 : 8, cg);
+    return e >= 4 ? e : 1;
+}
+static int64_t norm_bytes(int dtype, int64_t m, int64_t d, int64_t groups, int64_t segs, bool by_segment, bool grad) {
+    const int64_t cg = d / groups;
+    return norm_work(nullptr, m, d, groups, segs, by_segment, grad, row_plan(norm_vec(dtype, cg), (int)cg).lg).bytes;
 }
 
 static constexpr int64_t NORM_COLS = 2048;
@@ -1022,13 +1053,10 @@ static void check_norm(int dtype, int64_t m, int64_t d, int64_t groups, const in
     if (act != TAURUS_ACT_NONE && act != TAURUS_ACT_RELU && act != TAURUS_ACT_SILU)
         fail(TAURUS_E_INVALID, "activation %d is none of TAURUS_ACT_*", act);
 }
-static int norm_vec(int e, int dtype) {  // the vectors there are kernels for
-    return e >= 8 && dtype != TAURUS_F32 ? 8 : e >= 4 ? 4 : 1;
-}
-
-static void norm_run(NormArgs a, int dtype, int e, bool grad, void* work, int64_t have, const char* call,
+static void norm_run(NormArgs a, int dtype, bool grad, void* work, int64_t have, const char* call,
                      float* dweight, float* dbias, hipStream_t s) {
-    check_work(work, have, norm_bytes(a.m, a.d, a.groups, a.segs, a.off != nullptr, grad), call);
+    const int e = norm_vec(dtype, a.cg);
+    check_work(work, have, norm_bytes(dtype, a.m, a.d, a.groups, a.segs, a.off != nullptr, grad), call);
     const RowPlan r = a.off ? RowPlan{e, 1, 0, false} : row_plan(e, a.cg);
     const NormWork w = norm_work(work, a.m, a.d, a.groups, a.segs, a.off != nullptr, grad, r.lg);
     a.cols = grad && (dweight || dbias) ? w.cols : nullptr;
@@ -1064,12 +1092,12 @@ using namespace taurus;
 
 extern "C" {
 
-int64_t taurus_group_norm_bytes(int64_t m, int64_t d, int64_t groups, int64_t segments, int32_t by_segment,
+int64_t taurus_group_norm_bytes(int32_t dtype, int64_t m, int64_t d, int64_t groups, int64_t segments, int32_t by_segment,
                                 int32_t grad) {
     int64_t bytes = 0;
     const int rc = guarded_call([&] {
-        check_norm(TAURUS_F32, m, d, groups, nullptr, segments, TAURUS_ACT_NONE);
-        bytes = norm_bytes(m, d, groups, segments, by_segment != 0, grad != 0);
+        check_norm(dtype, m, d, groups, nullptr, segments, TAURUS_ACT_NONE);
+        bytes = norm_bytes(dtype, m, d, groups, segments, by_segment != 0, grad != 0);
         return (int)TAURUS_OK;
     });
     return rc == TAURUS_OK ? bytes : rc;
@@ -1089,9 +1117,6 @@ int taurus_group_norm(const void* x, int32_t dtype, int64_t m, int64_t d, int64_
         check_rows(out, out_dtype, m, d, out_stride, "out");
         for (const void* p : {(const void*)weight, (const void*)bias, (const void*)mean, (const void*)rstd})
             if (p) check_ptr(p, 4, "a statistic or weight");
-        const int64_t cols = d / groups;  // a vector lies in one group
-        int e = m > 0 ? vec_width(8, dtype, x, cols, x_stride) : 1;
-        if (m > 0) e = std::min(e, vec_width(8, out_dtype, out, cols, out_stride));
         NormArgs a{};
         a.x = x;
         a.m = m;
@@ -1110,7 +1135,7 @@ int taurus_group_norm(const void* x, int32_t dtype, int64_t m, int64_t d, int64_
         a.os = out_stride;
         a.mean = mean;
         a.rstd = rstd;
-        norm_run(a, dtype, norm_vec(e, dtype), false, work, work_bytes, "taurus_group_norm", nullptr, nullptr,
+        norm_run(a, dtype, false, work, work_bytes, "taurus_group_norm", nullptr, nullptr,
                  static_cast<hipStream_t>(stream));
         return (int)TAURUS_OK;
     });
@@ -1133,12 +1158,6 @@ int taurus_group_norm_grad(const void* grad, int64_t grad_stride, const void* x,
         }
         for (const void* p : {(const void*)weight, (const void*)bias, (const void*)dweight, (const void*)dbias})
             if (p) check_ptr(p, 4, "a weight or its gradient");
-        const int64_t cols = d / groups;  // a vector lies in one group
-        int e = 1;
-        if (m > 0) {
-            e = std::min(vec_width(8, dtype, x, cols, x_stride), vec_width(8, dtype, grad, cols, grad_stride));
-            if (dx) e = std::min(e, vec_width(8, dtype, dx, cols, dx_stride));
-        }
         NormArgs a{};
         a.x = x;
         a.m = m;
@@ -1157,7 +1176,7 @@ int taurus_group_norm_grad(const void* grad, int64_t grad_stride, const void* x,
         a.ds = grad_stride;
         a.mean_in = mean;
         a.rstd_in = rstd;
-        norm_run(a, dtype, norm_vec(e, dtype), true, work, work_bytes, "taurus_group_norm_grad", dweight, dbias,
+        norm_run(a, dtype, true, work, work_bytes, "taurus_group_norm_grad", dweight, dbias,
                  static_cast<hipStream_t>(stream));
         return (int)TAURUS_OK;
     });

@@ -83,14 +83,14 @@ inline void check_work(const void* work, int64_t have, int64_t need, const char*
              (long long)need);
 }
 
-// Widest vector, of at most `most` values, in which every row of an array
-// can be taken: it divides the row's length and stride, and the address is
-// aligned to it (to 16 bytes, the widest access, for longer vectors).
-inline int vec_width(int most, int dtype, const void* p, int64_t cols, int64_t stride) {
+// Values of the vectors that rows of `cols` values are taken in, at most
+// `most`: rows need not be aligned to them nor a whole number of them.  The
+// chip reads and writes 16 bytes at any address of a value; a row's last
+// vector, when there is a rest, ends at the row's end and covers values of
+// the one before it again (vec_at).
+inline int vec_width(int most, int64_t cols) {
     int e = most;
-    while (e > 1 && (cols % e || stride % e ||
-                     reinterpret_cast<uintptr_t>(p) % (size_t)std::min(16, e * dtype_size(dtype))))
-        e >>= 1;
+    while (e > 1 && e > cols) e >>= 1;
     return e;
 }
 
@@ -101,42 +101,55 @@ inline unsigned grid_for(int64_t blocks) { return (unsigned)std::min(blocks, GRI
 
 // ---------------------------------------------------------------- vectors --
 
-template <int BYTES>
-struct Raw;
-template <>
-struct Raw<2> {
+// BYTES bytes at any multiple of ALIGN
+template <int BYTES, int ALIGN>
+struct Raw {
+    typedef uint32_t type __attribute__((ext_vector_type(BYTES / 4), aligned(ALIGN)));
+};
+template <int ALIGN>
+struct Raw<2, ALIGN> {
     typedef uint16_t type;
 };
 template <>
-struct Raw<4> {
+struct Raw<4, 4> {
     typedef uint32_t type;
 };
 template <>
-struct Raw<8> {
-    typedef uint2 type;
-};
-template <>
-struct Raw<16> {
-    typedef uint4 type;
+struct Raw<4, 2> {
+    typedef uint32_t type __attribute__((aligned(2)));
 };
 template <int DT>
 constexpr int type_bytes = DT == TAURUS_F32 ? 4 : 2;
+
+// First value of vector w of rows of d values (d >= E), and how many of its
+// values the vector before it has too.
+template <int E>
+__host__ __device__ inline int64_t vec_at(int64_t w, int64_t d) {
+    return w * E < d - E ? w * E : d - E;
+}
+template <int E>
+__device__ inline int vec_again(int64_t w, int64_t d) {
+    return (int)(w * E - vec_at<E>(w, d));
+}
 
 // E values of a row as stored
 template <int DT, int E>
 struct Stored {
     static constexpr int BYTES = E * type_bytes<DT>;
     static constexpr int PART = BYTES < 16 ? BYTES : 16, PARTS = BYTES / PART;
-    typedef typename Raw<PART>::type part;
-    part v[PARTS];
+    typedef typename Raw<PART, type_bytes<DT>>::type part;
+    uint32_t v[BYTES >= 4 ? BYTES / 4 : 1];
 };
 template <int DT, int E>
 __device__ inline Stored<DT, E> load_stored(const void* p, int64_t at) {
     typedef Stored<DT, E> S;
-    S s;
+    S s{};
     const auto* q = reinterpret_cast<const typename S::part*>(static_cast<const char*>(p) + at * type_bytes<DT>);
 #pragma unroll
-    for (int i = 0; i < S::PARTS; i++) s.v[i] = q[i];
+    for (int i = 0; i < S::PARTS; i++) {
+        const auto part = q[i];
+        __builtin_memcpy(reinterpret_cast<char*>(&s) + i * S::PART, &part, S::PART);
+    }
     return s;
 }
 template <int DT, int E>
@@ -148,21 +161,19 @@ __device__ inline Stored<DT, E> zero_stored() {
 template <int DT, int E>
 __device__ inline void decode(const Stored<DT, E>& s, float (&f)[E]) {
     if constexpr (DT == TAURUS_F32) {
-        __builtin_memcpy(f, &s, sizeof(f));
+        __builtin_memcpy(f, s.v, sizeof(f));
     } else if constexpr (E == 1) {
-        if constexpr (DT == TAURUS_BF16) f[0] = __uint_as_float((uint32_t)s.v[0] << 16);
-        else f[0] = (float)__builtin_bit_cast(_Float16, s.v[0]);
+        if constexpr (DT == TAURUS_BF16) f[0] = __uint_as_float(s.v[0] << 16);
+        else f[0] = (float)__builtin_bit_cast(_Float16, (uint16_t)s.v[0]);
     } else {  // two values a word, taken from it where they are used
-        uint32_t w[E / 2];
-        __builtin_memcpy(w, &s, sizeof(w));
 #pragma unroll
         for (int i = 0; i < E / 2; i++) {
             if constexpr (DT == TAURUS_BF16) {
-                f[2 * i] = __uint_as_float(w[i] << 16);
-                f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+                f[2 * i] = __uint_as_float(s.v[i] << 16);
+                f[2 * i + 1] = __uint_as_float(s.v[i] & 0xffff0000u);
             } else {
                 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-                const half2_t h = __builtin_bit_cast(half2_t, w[i]);
+                const half2_t h = __builtin_bit_cast(half2_t, s.v[i]);
                 f[2 * i] = (float)h.x;
                 f[2 * i + 1] = (float)h.y;
             }
@@ -177,7 +188,7 @@ __device__ inline void store_vec(void* p, int64_t at, const float (&f)[E]) {
     if constexpr (DT == TAURUS_F32) {
         __builtin_memcpy(&s, f, sizeof(s));
     } else {
-        uint16_t h[E];
+        uint16_t h[E > 1 ? E : 2] = {};
 #pragma unroll
         for (int i = 0; i < E; i++) {
             if constexpr (DT == TAURUS_BF16) h[i] = __builtin_bit_cast(uint16_t, (__bf16)f[i]);
@@ -187,7 +198,11 @@ __device__ inline void store_vec(void* p, int64_t at, const float (&f)[E]) {
     }
     auto* q = reinterpret_cast<typename S::part*>(static_cast<char*>(p) + at * type_bytes<DT>);
 #pragma unroll
-    for (int i = 0; i < S::PARTS; i++) q[i] = s.v[i];
+    for (int i = 0; i < S::PARTS; i++) {
+        typename S::part part;
+        __builtin_memcpy(&part, reinterpret_cast<const char*>(&s) + i * S::PART, S::PART);
+        q[i] = part;
+    }
 }
 // the same with the stored type known at run time (uniform)
 template <int E>

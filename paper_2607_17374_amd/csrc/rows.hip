@@ -27,10 +27,10 @@ namespace taurus {
 // then their values requested together.
 constexpr int LOOKUP_UNROLL = 4;
 template <int TI, int TO, int E>
-__global__ __launch_bounds__(256) void k_lookup(const void* __restrict__ table, int64_t n, int64_t nv, int64_t ts,
+__global__ __launch_bounds__(256) void k_lookup(const void* __restrict__ table, int64_t n, int64_t d, int64_t ts,
                                                 const int32_t* __restrict__ ids, int64_t m, float scale,
                                                 void* __restrict__ out, int64_t os, int lg) {
-    const int64_t rows = 256 >> lg;  // a pass of the workgroup
+    const int64_t rows = 256 >> lg, nv = (d + E - 1) / E;  // rows a pass of the workgroup, vectors a row
     const int64_t lane = threadIdx.x & ((1 << lg) - 1);
     const int64_t step = (int64_t)gridDim.x * rows * LOOKUP_UNROLL;
     for (int64_t first = (int64_t)blockIdx.x * rows * LOOKUP_UNROLL + (threadIdx.x >> lg); first < m; first += step) {
@@ -41,10 +41,11 @@ __global__ __launch_bounds__(256) void k_lookup(const void* __restrict__ table, 
             id[j] = i < m ? (int64_t)ids[i] : -1;
         }
         for (int64_t w = lane; w < nv; w += (int64_t)1 << lg) {
+            const int64_t at = vec_at<E>(w, d);
             Stored<TI, E> v[LOOKUP_UNROLL];
 #pragma unroll
             for (int j = 0; j < LOOKUP_UNROLL; j++)
-                v[j] = (uint64_t)id[j] < (uint64_t)n ? load_stored<TI, E>(table, id[j] * ts + w * E) : zero_stored<TI, E>();
+                v[j] = (uint64_t)id[j] < (uint64_t)n ? load_stored<TI, E>(table, id[j] * ts + at) : zero_stored<TI, E>();
 #pragma unroll
             for (int j = 0; j < LOOKUP_UNROLL; j++) {
                 const int64_t i = first + j * rows;
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(256) void k_lookup(const void* __restrict__ table, 
                 decode<TI, E>(v[j], f);
 #pragma unroll
                 for (int e = 0; e < E; e++) f[e] = (uint64_t)id[j] < (uint64_t)n ? f[e] * scale : 0.f;
-                store_vec<TO, E>(out, i * os + w * E, f);
+                store_vec<TO, E>(out, i * os + at, f);
             }
         }
     }
@@ -68,10 +69,9 @@ static int lanes_lg(int64_t nv, int most) {
 template <int TI, int TO, int E>
 static void lookup_e(const void* table, int64_t n, int64_t d, int64_t ts, const int32_t* ids, int64_t m, float scale,
                      void* out, int64_t os, hipStream_t s) {
-    const int64_t nv = d / E;
-    const int lg = lanes_lg(nv, 8);
+    const int lg = lanes_lg(ceil_div(d, E), 8);
     const int64_t grid = ceil_div(m, (int64_t)(256 >> lg) * LOOKUP_UNROLL);
-    k_lookup<TI, TO, E><<<grid_for(grid), 256, 0, s>>>(table, n, nv, ts, ids, m, scale, out, os, lg);
+    k_lookup<TI, TO, E><<<grid_for(grid), 256, 0, s>>>(table, n, d, ts, ids, m, scale, out, os, lg);
     TAURUS_CHECK_LAUNCH();
 }
 template <int TI, int TO>
@@ -103,13 +103,13 @@ constexpr uint32_t NO_ID = 0xffffffffu;
 struct GradOut {
     void* out;
     int dtype;
-    int64_t stride, n, nv;  // nv: vectors a row
+    int64_t stride, n, d, nv;  // nv: vectors a row
     float scale;
     int accumulate;
 };
 template <int E>
 __device__ inline void grad_write(const GradOut& o, int64_t u, int64_t w, float (&f)[E]) {
-    const int64_t at = u * o.stride + w * E;
+    const int64_t at = u * o.stride + vec_at<E>(w, o.d);
 #pragma unroll
     for (int e = 0; e < E; e++) f[e] *= o.scale;
     if (o.accumulate) {
@@ -119,6 +119,16 @@ __device__ inline void grad_write(const GradOut& o, int64_t u, int64_t w, float 
         else load_vec<TAURUS_F16, E>(o.out, at, old);
 #pragma unroll
         for (int e = 0; e < E; e++) f[e] += old[e];
+        const int again = vec_again<E>(w, o.d);
+        if (again > 0) {  // added to by the vector before: each value once
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if (e >= again) {
+                    const float one[1] = {f[e]};
+                    store_as<1>(o.dtype, o.out, at + e, one);
+                }
+            return;
+        }
     }
     store_as<E>(o.dtype, o.out, at, f);
 }
@@ -129,18 +139,18 @@ template <int E>
 __device__ inline void grad_fill(const GradOut& o, int64_t block, int64_t blocks) {
     const int threads = blockDim.x, lane = threadIdx.x & 63, waves = threads >> 6;
     const float zero[E] = {};
-    if (o.stride == o.nv * E) {
-        const int64_t total = o.n * o.nv;
+    if (o.stride == o.d) {
+        const int64_t total = (o.n * o.d + E - 1) / E;
         for (int64_t i = block * threads * 4 + threadIdx.x; i < total; i += blocks * threads * 4)
 #pragma unroll
             for (int j = 0; j < 4; j++)
-                if (i + j * threads < total) store_as<E>(o.dtype, o.out, (i + j * threads) * E, zero);
+                if (i + j * threads < total) store_as<E>(o.dtype, o.out, vec_at<E>(i + j * threads, o.n * o.d), zero);
         return;
     }
     for (int64_t u = (block * waves + (threadIdx.x >> 6)) * 2; u < o.n; u += blocks * waves * 2)
         for (int64_t w = lane; w < 2 * o.nv; w += 64) {
             const int64_t r = u + (w >= o.nv);
-            if (r < o.n) store_as<E>(o.dtype, o.out, r * o.stride + (w >= o.nv ? w - o.nv : w) * E, zero);
+            if (r < o.n) store_as<E>(o.dtype, o.out, r * o.stride + vec_at<E>(w >= o.nv ? w - o.nv : w, o.d), zero);
         }
 }
 
@@ -174,7 +184,7 @@ __global__ __launch_bounds__(256) void k_grad_small(const void* __restrict__ gra
         float zero[E] = {};
         for (int r = wave; r < rows; r += 4) {
             if ((named[r >> 5] >> (r & 31)) & 1u) continue;
-            for (int64_t w = lane; w < o.nv; w += 64) store_as<E>(o.dtype, o.out, (u0 + r) * o.stride + w * E, zero);
+            for (int64_t w = lane; w < o.nv; w += 64) store_as<E>(o.dtype, o.out, (u0 + r) * o.stride + vec_at<E>(w, o.d), zero);
         }
         return;
     }
@@ -199,7 +209,7 @@ __global__ __launch_bounds__(256) void k_grad_small(const void* __restrict__ gra
         for (; k + (U - 1) * step < n; k += U * step) {
             Stored<TI, E> v[U];
 #pragma unroll
-            for (int j = 0; j < U; j++) v[j] = load_stored<TI, E>(grad, (int64_t)l[k + j * step] * gs + w * E);
+            for (int j = 0; j < U; j++) v[j] = load_stored<TI, E>(grad, (int64_t)l[k + j * step] * gs + vec_at<E>(w, o.d));
 #pragma unroll
             for (int j = 0; j < U; j++) {
                 float x[E];
@@ -210,7 +220,7 @@ __global__ __launch_bounds__(256) void k_grad_small(const void* __restrict__ gra
         }
         for (; k < n; k += step) {
             float x[E];
-            load_vec<TI, E>(grad, (int64_t)l[k] * gs + w * E, x);
+            load_vec<TI, E>(grad, (int64_t)l[k] * gs + vec_at<E>(w, o.d), x);
 #pragma unroll
             for (int e = 0; e < E; e++) f[e] += x[e];
         }
@@ -296,7 +306,7 @@ __device__ inline void grad_clear(const uint32_t* __restrict__ key, int64_t m, c
         while (clear) {
             const int r = __builtin_ctzll(clear);
             clear &= clear - 1;
-            for (int64_t w = lane; w < o.nv; w += 64) store_as<E>(o.dtype, o.out, (u0 + r) * o.stride + w * E, zero);
+            for (int64_t w = lane; w < o.nv; w += 64) store_as<E>(o.dtype, o.out, (u0 + r) * o.stride + vec_at<E>(w, o.d), zero);
         }
     }
 }
@@ -526,7 +536,7 @@ __global__ __launch_bounds__(256) void k_grad_level(const void* __restrict__ row
         grad_clear<E>(key, count, o, blockIdx.x - (gridDim.x - clear_blocks), clear_blocks);
         return;
     }
-    const int64_t nd = o.nv * E;  // row length of `next`
+    const int64_t nd = o.nv * E;  // row length of the later levels, whole vectors
     for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x - clear_blocks) {
         const int64_t b0 = t * groups * T, b1 = min(b0 + (int64_t)groups * T, count);
         const int64_t i0 = min(b0 + (int64_t)group * T, b1), i1 = min(i0 + T, b1);
@@ -539,6 +549,7 @@ __global__ __launch_bounds__(256) void k_grad_level(const void* __restrict__ row
         for (int64_t w0 = 0; w0 < o.nv; w0 += L) {
             const int64_t w = w0 + lane;
             const bool col = w < o.nv;
+            const int64_t wat = first ? vec_at<E>(w, o.d) : w * E;
             uint32_t used0 = NO_ID, used1 = NO_ID;
             GradSums<E> g;
             g.start(k0, before);
@@ -570,7 +581,7 @@ __global__ __launch_bounds__(256) void k_grad_level(const void* __restrict__ row
                 Stored<TI, E> v[U];
 #pragma unroll
                 for (int j = 0; j < U; j++)
-                    v[j] = at[j] >= 0 ? load_stored<TI, E>(rows, at[j] * rs + w * E) : zero_stored<TI, E>();
+                    v[j] = at[j] >= 0 ? load_stored<TI, E>(rows, at[j] * rs + wat) : zero_stored<TI, E>();
 #pragma unroll
                 for (int j = 0; j < U; j++) {
                     if (b + j >= i1) break;
@@ -653,7 +664,8 @@ struct GradWork {
 // entries a group takes of a list
 static int grad_groups(int64_t nv) { return 256 >> lanes_lg(nv, 6); }
 static int grad_tile(int64_t count) { return count <= GRAD_FEW ? TILE_FEW : TILE_MANY; }
-static GradWork grad_work(void* work, int64_t m, int64_t d, int64_t nv) {
+static GradWork grad_work(void* work, int64_t m, int64_t d, int e) {
+    const int64_t nv = ceil_div(d, e);
     GradWork g;
     if (m <= GRAD_SMALL) return g;
     Carve c(work);
@@ -671,7 +683,7 @@ static GradWork grad_work(void* work, int64_t m, int64_t d, int64_t nv) {
         if (tiles <= 1) break;
         GradWork::Level l;
         l.count = count = 2 * tiles;
-        l.rows = c.take<float>(l.count * d);
+        l.rows = c.take<float>(l.count * nv * e);
         l.key = c.take<uint32_t>(l.count);
         l.place = c.take<uint32_t>(l.count);
         g.levels.push_back(l);
@@ -679,17 +691,16 @@ static GradWork grad_work(void* work, int64_t m, int64_t d, int64_t nv) {
     g.bytes = c.bytes();
     return g;
 }
-// for any alignment of the arrays, which decides the vectors
+// for either size of the values, which decides the vectors
 static int64_t grad_bytes(int64_t m, int64_t d) {
-    int64_t most = 0;
-    for (int e = 1; e <= 8 && d % e == 0; e *= 2) most = std::max(most, grad_work(nullptr, m, d, d / e).bytes);
-    return most;
+    return std::max(grad_work(nullptr, m, d, vec_width(4, d)).bytes, grad_work(nullptr, m, d, vec_width(8, d)).bytes);
 }
 
 template <int TI, int E>
 static void grad_e(const void* grad, int64_t gs, const int32_t* ids, int64_t m, int64_t d, GradOut o, void* work,
                    hipStream_t s) {
-    o.nv = d / E;
+    o.d = d;
+    o.nv = ceil_div(d, E);
     if (m <= GRAD_SMALL) {
         const int64_t sums = ceil_div(m, 4), clears = o.accumulate ? 0 : ceil_div(o.n, 256);
         if (sums + clears == 0) return;
@@ -697,7 +708,7 @@ static void grad_e(const void* grad, int64_t gs, const int32_t* ids, int64_t m, 
         TAURUS_CHECK_LAUNCH();
         return;
     }
-    GradWork g = grad_work(work, m, d, o.nv);
+    GradWork g = grad_work(work, m, d, E);
     // Rows without an id: of a table longer than the list, where most rows
     // have none, all are filled beside the sort; else those without are
     // found in the sorted list, beside the sums.
@@ -744,7 +755,7 @@ static void grad_e(const void* grad, int64_t gs, const int32_t* ids, int64_t m, 
         const GradWork::Level from = to;
         to = next(i + 1);
         const int64_t lt = ceil_div(from.count, (int64_t)grad_groups(o.nv) * grad_tile(from.count));
-        k_grad_level<TAURUS_F32, E><<<grid_for(lt), 256, 0, s>>>(from.rows, d, from.key, from.place, from.count, 0, o,
+        k_grad_level<TAURUS_F32, E><<<grid_for(lt), 256, 0, s>>>(from.rows, o.nv * E, from.key, from.place, from.count, 0, o,
                                                                  to.rows, to.key, to.place, lg,
                                                                  grad_tile(from.count), lt, 0);
         TAURUS_CHECK_LAUNCH();
@@ -784,8 +795,7 @@ int taurus_lookup_rows(const void* table, int32_t table_dtype, int64_t n, int64_
         check_rows(table, table_dtype, n, d, table_stride, "table");
         check_rows(out, out_dtype, m, d, out_stride, "out");
         check_ptr(ids, 4, "ids");
-        int e = vec_width(table_dtype == TAURUS_F32 ? 4 : 8, table_dtype, table, d, table_stride);
-        e = std::min(e, vec_width(8, out_dtype, out, d, out_stride));
+        const int e = vec_width(table_dtype == TAURUS_F32 ? 4 : 8, d);
         auto s = static_cast<hipStream_t>(stream);
         if (table_dtype == TAURUS_F32)
             lookup_i<TAURUS_F32>(out_dtype, e, table, n, d, table_stride, ids, m, scale, out, out_stride, s);
@@ -822,9 +832,8 @@ int taurus_lookup_rows_grad(const void* grad, int32_t grad_dtype, int64_t grad_s
         check_rows(out, out_dtype, n, d, out_stride, "out");
         if (m > 0) check_ptr(ids, 4, "ids");
         check_work(work, work_bytes, grad_bytes(m, d), "taurus_lookup_rows_grad");
-        int e = m > 0 ? vec_width(grad_dtype == TAURUS_F32 ? 4 : 8, grad_dtype, grad, d, grad_stride) : 8;
-        e = std::min(e, vec_width(grad_dtype == TAURUS_F32 ? 4 : 8, out_dtype, out, d, out_stride));
-        const GradOut o{out, out_dtype, out_stride, n, 0, scale, accumulate ? 1 : 0};
+        const int e = vec_width(grad_dtype == TAURUS_F32 ? 4 : 8, d);
+        const GradOut o{out, out_dtype, out_stride, n, d, 0, scale, accumulate ? 1 : 0};
         auto s = static_cast<hipStream_t>(stream);
         if (grad_dtype == TAURUS_F32) grad_t<TAURUS_F32>(e, grad, grad_stride, ids, m, d, o, work, s);
         else if (grad_dtype == TAURUS_BF16) grad_t<TAURUS_BF16>(e, grad, grad_stride, ids, m, d, o, work, s);

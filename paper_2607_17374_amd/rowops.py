@@ -280,7 +280,7 @@ def group_norm(x: torch.Tensor, groups: int = 1, weight: Optional[torch.Tensor] 
         L = N.lib()
         nbytes, work, kp = 0, None, None
         if off is not None:  # row by row needs no workspace
-            nbytes = L.taurus_group_norm_bytes(m, d, groups, segs, 1, 0)
+            nbytes = L.taurus_group_norm_bytes(code, m, d, groups, segs, 1, 0)
             work, kp = c.work(nbytes, "taurus_group_norm_bytes")
         N.check(L.taurus_group_norm(xp, code, m, d, xs, groups, fp, segs, wp, bp, eps, act_code, op, out_code, os,
                                     None if mean is None else mean.data_ptr(),
@@ -313,7 +313,7 @@ def group_norm_grad(grad: torch.Tensor, x: torch.Tensor, groups: int, weight: Op
         dw = torch.empty(d, dtype=torch.float32, device=c.device) if "weight" in need else None
         db = torch.empty(d, dtype=torch.float32, device=c.device) if "bias" in need else None
         L = N.lib()
-        nbytes = L.taurus_group_norm_bytes(m, d, groups, segs, int(off is not None), 1)
+        nbytes = L.taurus_group_norm_bytes(code, m, d, groups, segs, int(off is not None), 1)
         work, kp = c.work(nbytes, "taurus_group_norm_bytes")
         N.check(L.taurus_group_norm_grad(
             gp, gs, xp, xs, code, m, d, groups, fp, segs, wp, bp, mp, rp, act_code,

@@ -252,7 +252,7 @@ def ranges(sizes, lead=0):
 LINEAR = [  # type sizes, d_in, d_out
     ([1], 1, 1), ([0, 3, 0], 5, 7), ([1, 1, 1, 1], 16, 4), ([130, 0, 127, 128, 129], 64, 64), ([300], 100, 47),
     ([5, 200, 61], 128, 256), ([77], 33, 130), ([256, 1], 1024, 40), ([40, 40], 200, 129), ([0, 0], 8, 8),
-    ([3] * 150, 24, 20), ([513], 8, 300),
+    ([3] * 150, 24, 20), ([513], 8, 300), ([130, 70], 14, 280), ([90], 15, 9), ([64, 5], 22, 31), ([129], 71, 133),
 ]
 
 

@@ -130,19 +130,19 @@ def test_workspace_sizes():
     for m in (0, 1, 1024):
         assert L.taurus_lookup_rows_grad_bytes(m, 64) == 0
     assert L.taurus_lookup_rows_grad_bytes(1025, 64) >= 8 * 1025
-    # two sorted copies of ids and places, then two sums for every 128 places
-    # (four groups of 64 lanes of 32 places each), 1/64 as many a level
+    # two sorted copies of ids and places, then two sums for every eight
+    # groups of 32 lanes, which take 32 places each; 1/32 as many a level
     m, d = 1 << 20, 128
-    level = 2 * (m // 128) * (4 * d + 8)
+    level = 2 * (m // 256) * (4 * d + 8)
     assert 16 * m + level < L.taurus_lookup_rows_grad_bytes(m, d) < 18 * m + 1.1 * level + (2 << 20)
     assert L.taurus_grouped_linear_grad_bytes(N.F32, 256, 2, 64, 64) == 0
     assert L.taurus_grouped_linear_grad_bytes(N.F32, 257, 2, 64, 64) >= 2 * 2 * 64 * 65 * 4
-    assert L.taurus_group_norm_bytes(10**6, 128, 8, 0, 0, 0) == 0
-    assert L.taurus_group_norm_bytes(10**6, 128, 8, 100, 1, 0) > 0
-    assert L.taurus_group_norm_bytes(10**6, 128, 8, 0, 0, 1) > 0
+    assert L.taurus_group_norm_bytes(N.BF16, 10**6, 128, 8, 0, 0, 0) == 0
+    assert L.taurus_group_norm_bytes(N.BF16, 10**6, 128, 8, 100, 1, 0) > 0
+    assert L.taurus_group_norm_bytes(N.BF16, 10**6, 128, 8, 0, 0, 1) > 0
     for bad in (L.taurus_lookup_rows_grad_bytes(-1, 4), L.taurus_lookup_rows_grad_bytes(4, 0),
                 L.taurus_grouped_linear_grad_bytes(N.F32, 4, 1, 0, 4), L.taurus_grouped_linear_grad_bytes(N.F32, 1 << 31, 1, 4, 4),
-                L.taurus_group_norm_bytes(4, 6, 4, 0, 0, 0), L.taurus_group_norm_bytes(4, 4096, 4, 0, 0, 1)):
+                L.taurus_group_norm_bytes(N.BF16, 4, 6, 4, 0, 0, 0), L.taurus_group_norm_bytes(N.BF16, 4, 4096, 4, 0, 0, 1)):
         assert bad == N.E_INVALID
 
 
