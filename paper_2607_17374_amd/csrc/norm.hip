@@ -52,9 +52,21 @@ struct NormArgs {
     int64_t places;  // units of segments of several units, at most
 };
 
+// 1 / (1 + exp(-z)) to about two units in the last place, by the chip's
+// power of two and reciprocal (one unit each): -z log2(e) as a rounded product
+// and its rest, the rest taken linearly.  (The library's exponential and
+// division take three times the steps; SiLU is then bound by them.)
+__device__ inline float sigmoid(float z) {
+    const float t = -z, hi = t * 1.44269502f;
+    const float lo = __builtin_fmaf(t, 1.44269502f, -hi) + t * 1.92596299e-8f;
+    float e = __builtin_amdgcn_exp2f(hi);
+    // past 2^126 the sum's reciprocal is 0, or near it, whatever the rest
+    e = hi < 126.f ? __builtin_fmaf(e, lo * 0.693147181f, e) : e;
+    return __builtin_amdgcn_rcpf(1.f + e);
+}
 __device__ inline float act_of(float z, int act) {
     if (act == TAURUS_ACT_RELU) return fmaxf(z, 0.f);
-    if (act == TAURUS_ACT_SILU) return z / (1.f + expf(-z));
+    if (act == TAURUS_ACT_SILU) return z * sigmoid(z);
     return z;
 }
 // The sign of (x - mean) rstd w + b in 64 bits.  The conversions stay where
@@ -75,7 +87,7 @@ __device__ inline float act_grad(float dy, float x, float mean, float rstd, floa
             open = open_exactly(x, mean, rstd, w, b);
         return open ? dy : 0.f;
     }
-    const float q = 1.f / (1.f + expf(-z));
+    const float q = sigmoid(z);
     return dy * (q * (1.f + z * (1.f - q)));
 }
 
@@ -370,7 +382,11 @@ struct Affine {
     }
 };
 
-constexpr int SEG_ROWS = 8;  // rows of a vector that a thread has in flight
+// Rows of a vector that a thread has in flight: eight where a wave works by
+// itself, four in a workgroup of four waves, which leaves registers for more
+// of them.
+template <int BT>
+constexpr int seg_rows = BT == 64 ? 8 : 4;
 
 // decode, where it stands: a 16-bit value's fp32 form is cheap, so that the
 // compiler forms it as soon as the value is loaded and keeps both (240
@@ -386,27 +402,27 @@ __device__ inline void decode_here(Stored<DT, E> s, float (&f)[E]) {
     }
     decode<DT, E>(s, f);
 }
-// One vector of SEG_ROWS rows from row r on in steps of RY.
-template <int DT, int E>
+// One vector of ROWS rows from row r on in steps of RY.
+template <int DT, int E, int ROWS>
 struct RowsOf {
-    Stored<DT, E> v[SEG_ROWS];
+    Stored<DT, E> v[ROWS];
     __device__ void load(const void* p, int64_t stride, int64_t r0, int rows, int r, int RY, int64_t c) {
 #pragma unroll
-        for (int j = 0; j < SEG_ROWS; j++) {
+        for (int j = 0; j < ROWS; j++) {
             const int rr = r + j * RY;
             v[j] = rr < rows ? load_stored<DT, E>(p, (r0 + rr) * stride + c) : zero_stored<DT, E>();
         }
     }
 };
 
-template <int DT, int E>
-__device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E>& x, int64_t r0, int rows, int r, int RY, int c,
+template <int DT, int E, int ROWS>
+__device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E, ROWS>& x, int64_t r0, int rows, int r, int RY, int c,
                                   float mu, float rs, const Affine<E>& f) {
     float w[E];
 #pragma unroll
     for (int e = 0; e < E; e++) w[e] = rs * f.w[e];
 #pragma unroll
-    for (int j = 0; j < SEG_ROWS; j++) {
+    for (int j = 0; j < ROWS; j++) {
         const int rr = r + j * RY;
         if (rr >= rows) continue;
         float z[E];
@@ -420,12 +436,13 @@ __device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E>& x, int
 // The statistics of each unit; whole segments are normalised at once, from
 // the registers they were read into where they fit.
 template <int DT, int E, int BT>
-__global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
+__global__ __launch_bounds__(BT, BT == 64 && E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
+    constexpr int ROWS = seg_rows<BT>;
     extern __shared__ float lds[];
     const Spread<BT, E> t(a);
     const int entries = max(t.nv, BT);
     float *sm = lds, *sq = sm + entries, *gm = sq + entries, *gr = gm + a.groups;
-    const bool wide = t.nv > BT;
+    const bool wide = t.nv > BT, ragged = t.cg % E != 0;
     const int cgv = t.cgv;
     Affine<E> f;
     if (!wide) f.set(a, t.channel(t.cx));
@@ -441,31 +458,37 @@ __global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
             }
             continue;
         }
-        RowsOf<DT, E> x;
+        RowsOf<DT, E, ROWS> x;
         __syncthreads();  // the arrays may still be read for an earlier unit
         for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
             const int c = t.channel(v), again = t.again(v);
             float n = 0.f, mean = 0.f, m2 = 0.f;
-            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+            for (int r = t.ry; r < rows; r += ROWS * t.RY) {
                 x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
                 float s = 0.f, cnt = 0.f;
 #pragma unroll
-                for (int j = 0; j < SEG_ROWS; j++) {
+                for (int j = 0; j < ROWS; j++) {
                     float y[E];
                     decode_here<DT, E>(x.v[j], y);
                     cnt += r + j * t.RY < rows ? (float)(E - again) : 0.f;
 #pragma unroll
-                    for (int e = 0; e < E; e++) s += e >= again ? y[e] : 0.f;
+                    for (int e = 0; e < E; e++) {
+                        if (ragged) y[e] = e < again ? 0.f : y[e];
+                        s += y[e];
+                    }
                 }
                 const float mb = s / cnt, share = cnt / (n + cnt);
                 float q = 0.f;
 #pragma unroll
-                for (int j = 0; j < SEG_ROWS; j++) {
+                for (int j = 0; j < ROWS; j++) {
                     float y[E];
                     decode_here<DT, E>(x.v[j], y);
                     if (r + j * t.RY < rows)
 #pragma unroll
-                        for (int e = 0; e < E; e++) q += e >= again ? (y[e] - mb) * (y[e] - mb) : 0.f;
+                        for (int e = 0; e < E; e++) {
+                            if (ragged) y[e] = e < again ? mb : y[e];
+                            q += (y[e] - mb) * (y[e] - mb);
+                        }
                 }
                 const float delta = mb - mean;
                 mean += delta * share;
@@ -515,32 +538,37 @@ __global__ __launch_bounds__(BT, E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
             const int c = t.channel(v);
             if (wide) f.set(a, c);
             const float mu = gm[t.group(v)], rs = gr[t.group(v)];
-            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
-                if (wide || rows > SEG_ROWS * t.RY) x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
-                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, c, mu, rs, f);
+            for (int r = t.ry; r < rows; r += ROWS * t.RY) {
+                if (wide || rows > ROWS * t.RY) x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
+                norm_store<DT, E, ROWS>(a, x, u.r0, rows, r, t.RY, c, mu, rs, f);
             }
         }
     }
 }
 
-__device__ inline float block_sum(float v, float* red) {
+// Sum over T threads: a wave, or the workgroup of four.
+template <int T>
+__device__ inline float team_sum(float v, float* red) {
     for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+    if constexpr (T == 64) return v;
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Joins the units of a longer segment: a workgroup a segment and group.
-// Statistics: means about the first unit's, then the squares.  Gradient:
-// the means of the two sums.
-template <bool GRAD>
+// Joins the units of a longer segment: T threads a segment and group.
+// Statistics: means about the first unit's, then the squares.  Gradient: the
+// means of the two sums.
+template <bool GRAD, int T>
 __global__ __launch_bounds__(256) void k_norm_join(NormArgs a, int64_t longs) {
     __shared__ float red[4];
-    for (int64_t b = blockIdx.x; b < longs * a.groups; b += gridDim.x) {
+    const int lane = threadIdx.x % T;
+    for (int64_t b = (int64_t)blockIdx.x * (256 / T) + threadIdx.x / T; b < longs * a.groups;
+         b += (int64_t)gridDim.x * (256 / T)) {
         const int g = (int)(b % a.groups);
         const Long s = wave_long(a.off, a.segs, a.m, a.R, b / a.groups);
-        if (!s.found) continue;  // for the whole workgroup
+        if (!s.found) continue;  // for the whole team
         const int64_t R = a.R, units = s.units;
         const float size = (float)(s.end - s.begin) * (float)a.cg;
         // unit i starts in window s.window + i
@@ -551,13 +579,13 @@ __global__ __launch_bounds__(256) void k_norm_join(NormArgs a, int64_t longs) {
         // f over the units, four a thread in flight
         auto each = [&](auto&& f) {
             constexpr int U = 4;
-            for (int64_t i = threadIdx.x; i < units; i += 256 * U) {
+            for (int64_t i = lane; i < units; i += T * U) {
                 float2 v[U];
 #pragma unroll
-                for (int j = 0; j < U; j++) v[j] = part(min(i + 256 * j, units - 1));
+                for (int j = 0; j < U; j++) v[j] = part(min(i + T * j, units - 1));
 #pragma unroll
                 for (int j = 0; j < U; j++)
-                    if (i + 256 * j < units) f(i + 256 * j, v[j]);
+                    if (i + T * j < units) f(i + T * j, v[j]);
             }
         };
         float p = 0.f, q = 0.f;
@@ -566,16 +594,16 @@ __global__ __launch_bounds__(256) void k_norm_join(NormArgs a, int64_t longs) {
                 p += v.x;
                 q += v.y;
             });
-            p = block_sum(p, red) / size;
-            q = block_sum(q, red) / size;
+            p = team_sum<T>(p, red) / size;
+            q = team_sum<T>(q, red) / size;
         } else {
             const float first = part(0).x;
             each([&](int64_t i, float2 v) { p += rows(i) * (v.x - first); });
-            p = first + block_sum(p, red) / (float)(s.end - s.begin);
+            p = first + team_sum<T>(p, red) / (float)(s.end - s.begin);
             each([&](int64_t i, float2 v) { q += v.y + rows(i) * (float)a.cg * (v.x - p) * (v.x - p); });
-            q = 1.f / sqrtf(block_sum(q, red) / size + a.eps);
+            q = 1.f / sqrtf(team_sum<T>(q, red) / size + a.eps);
         }
-        if (threadIdx.x == 0) {
+        if (lane == 0) {
             float* st = a.stat + 2 * (s.window * a.groups + g);
             st[0] = p;
             st[1] = q;
@@ -596,6 +624,7 @@ __device__ inline int64_t place_order(int64_t k, int64_t places) {
 // The second pass over the rows of longer segments.
 template <int DT, int E>
 __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
+    constexpr int ROWS = seg_rows<256>;
     const Spread<256, E> t(a);
     for (int64_t k = blockIdx.x; k < a.places; k += gridDim.x) {
         const Unit u = wave_place(a.off, a.segs, a.m, a.R, place_order(k, a.places));
@@ -607,10 +636,10 @@ __global__ __launch_bounds__(256) void k_norm_apply(NormArgs a) {
             Affine<E> f;
             f.set(a, c);
             const float mu = st[2 * t.group(v)], rs = st[2 * t.group(v) + 1];
-            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
-                RowsOf<DT, E> x;
+            for (int r = t.ry; r < rows; r += ROWS * t.RY) {
+                RowsOf<DT, E, ROWS> x;
                 x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
-                norm_store<DT, E>(a, x, u.r0, rows, r, t.RY, c, mu, rs, f);
+                norm_store<DT, E, ROWS>(a, x, u.r0, rows, r, t.RY, c, mu, rs, f);
             }
         }
     }
@@ -660,18 +689,19 @@ struct GradAt {
         } else if constexpr (ACT == TAURUS_ACT_SILU) {
 #pragma unroll
             for (int e = 0; e < E; e++) {
-                const float z = d[e] * wr[e] + b[e], q = 1.f / (1.f + expf(-z));
+                const float z = d[e] * wr[e] + b[e], q = sigmoid(z);
                 dz[e] *= q * (1.f + z * (1.f - q));
             }
         }
     }
-    // dx of SEG_ROWS rows, given the means m1 and m2 of the vector's group:
+    // dx of ROWS rows, given the means m1 and m2 of the vector's group:
     // rstd (w dz - m1 - xhat m2) = wr dz - (rstd m1 + (x - mean) rstd^2 m2)
-    __device__ void store(const NormArgs& a, const RowsOf<DT, E>& x, const RowsOf<DT, E>& y, int64_t r0, int rows,
+    template <int ROWS>
+    __device__ void store(const NormArgs& a, const RowsOf<DT, E, ROWS>& x, const RowsOf<DT, E, ROWS>& y, int64_t r0, int rows,
                           int r, int RY, int c, float m1, float m2) const {
         const float k1 = rs * m1, k2 = rs * rs * m2;
 #pragma unroll
-        for (int j = 0; j < SEG_ROWS; j++) {
+        for (int j = 0; j < ROWS; j++) {
             const int rr = r + j * RY;
             if (rr >= rows) continue;
             float d[E], dz[E];
@@ -688,7 +718,8 @@ struct GradAt {
 // dgamma and dbeta, the latter kept by each thread for its channels over the
 // workgroup's slots (in LDS where it has several vectors of a row).
 template <int DT, int E, int BT, int ACT>
-__global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
+__global__ __launch_bounds__(BT, BT == 64 ? 3 : 4) void k_norm_units_grad(NormArgs a) {
+    constexpr int ROWS = seg_rows<BT>;
     extern __shared__ float lds[];
     const Spread<BT, E> t(a);
     const int entries = max(t.nv, BT);
@@ -704,7 +735,7 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
         const Unit u = walk.unit();
         if (u.g < 0 || u.slot >= u.units) continue;  // for the whole workgroup
         const int rows = (int)(u.r1 - u.r0);
-        RowsOf<DT, E> x, y;
+        RowsOf<DT, E, ROWS> x, y;
         __syncthreads();
         for (int v = t.cx; v < t.nv && t.ry < t.RY; v += t.nvb) {
             const int c = t.channel(v);
@@ -713,11 +744,11 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
             GradAt<DT, E, ACT> at;
             at.set(f, a.mean_in[g], a.rstd_in[g]);
             float sd[E] = {}, sz[E] = {};  // sums of dz (x - mean) and of dz
-            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
+            for (int r = t.ry; r < rows; r += ROWS * t.RY) {
                 x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
                 y.load(a.dy, a.ds, u.r0, rows, r, t.RY, c);
 #pragma unroll
-                for (int j = 0; j < SEG_ROWS; j++) {
+                for (int j = 0; j < ROWS; j++) {
                     if (r + j * t.RY >= rows) continue;
                     float d[E], dz[E];
                     at.at(x.v[j], y.v[j], d, dz);
@@ -784,8 +815,8 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
             const int64_t g = (int64_t)u.g * a.groups + t.group(v);
             GradAt<DT, E, ACT> at;
             at.set(f, a.mean_in[g], a.rstd_in[g]);
-            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
-                if (wide || rows > SEG_ROWS * t.RY) {
+            for (int r = t.ry; r < rows; r += ROWS * t.RY) {
+                if (wide || rows > ROWS * t.RY) {
                     x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
                     y.load(a.dy, a.ds, u.r0, rows, r, t.RY, c);
                 }
@@ -829,7 +860,8 @@ __global__ __launch_bounds__(BT, 3) void k_norm_units_grad(NormArgs a) {
 }
 
 template <int DT, int E, int ACT>
-__global__ __launch_bounds__(256, 3) void k_norm_apply_grad(NormArgs a) {
+__global__ __launch_bounds__(256, 4) void k_norm_apply_grad(NormArgs a) {
+    constexpr int ROWS = seg_rows<256>;
     const Spread<256, E> t(a);
     for (int64_t k = blockIdx.x; k < a.places; k += gridDim.x) {
         const Unit u = wave_place(a.off, a.segs, a.m, a.R, place_order(k, a.places));
@@ -843,8 +875,8 @@ __global__ __launch_bounds__(256, 3) void k_norm_apply_grad(NormArgs a) {
             const int64_t g = (int64_t)u.g * a.groups + t.group(v);
             GradAt<DT, E, ACT> at;
             at.set(f, a.mean_in[g], a.rstd_in[g]);
-            for (int r = t.ry; r < rows; r += SEG_ROWS * t.RY) {
-                RowsOf<DT, E> x, y;
+            for (int r = t.ry; r < rows; r += ROWS * t.RY) {
+                RowsOf<DT, E, ROWS> x, y;
                 x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
                 y.load(a.dy, a.ds, u.r0, rows, r, t.RY, c);
                 at.store(a, x, y, u.r0, rows, r, t.RY, c, st[2 * t.group(v)], st[2 * t.group(v) + 1]);
@@ -897,7 +929,7 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float* __restrict__
 
 // Rows a unit takes: enough units to fill the chip; with many segments, most
 // segments in one unit (sixteen times their mean length), unless a unit would
-// then be over 256 KB of fp32 rows.
+// then be over 256 KB of fp32 rows (one workgroup would be long at work on it).
 static int norm_lr(int64_t m, int64_t d, int64_t segs) {
     int lr = 10;
     while (lr > 4 && m >> lr < 2048) lr--;
@@ -979,8 +1011,15 @@ static void segs_act(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s
     else segs_units<DT, E, 256, ACT>(a, blocks, grad, s);
     const int64_t longs = long_count(a.m, a.segs, a.R);
     if (a.m <= a.R || (grad && !a.out)) return;  // no segment has several units
-    if (grad) k_norm_join<true><<<grid_for(longs * a.groups), 256, 0, s>>>(a, longs);
-    else k_norm_join<false><<<grid_for(longs * a.groups), 256, 0, s>>>(a, longs);
+    // many segments: a wave each and group; few can be of many units each
+    const int64_t teams = longs * a.groups;
+    if (teams >= 1024) {
+        if (grad) k_norm_join<true, 64><<<grid_for(ceil_div(teams, 4)), 256, 0, s>>>(a, longs);
+        else k_norm_join<false, 64><<<grid_for(ceil_div(teams, 4)), 256, 0, s>>>(a, longs);
+    } else {
+        if (grad) k_norm_join<true, 256><<<(unsigned)teams, 256, 0, s>>>(a, longs);
+        else k_norm_join<false, 256><<<(unsigned)teams, 256, 0, s>>>(a, longs);
+    }
     TAURUS_CHECK_LAUNCH();
     if (grad) k_norm_apply_grad<DT, E, ACT><<<grid_for(a.places), 256, 0, s>>>(a);
     else k_norm_apply<DT, E><<<grid_for(a.places), 256, 0, s>>>(a);
