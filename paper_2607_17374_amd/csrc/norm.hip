@@ -435,14 +435,15 @@ __device__ inline void norm_store(const NormArgs& a, const RowsOf<DT, E, ROWS>& 
 
 // The statistics of each unit; whole segments are normalised at once, from
 // the registers they were read into where they fit.
-template <int DT, int E, int BT>
+// RAGGED: groups are no whole number of vectors.
+template <int DT, int E, int BT, bool RAGGED>
 __global__ __launch_bounds__(BT, BT == 64 && E == 8 ? 3 : 4) void k_norm_units(NormArgs a) {
     constexpr int ROWS = seg_rows<BT>;
     extern __shared__ float lds[];
     const Spread<BT, E> t(a);
     const int entries = max(t.nv, BT);
     float *sm = lds, *sq = sm + entries, *gm = sq + entries, *gr = gm + a.groups;
-    const bool wide = t.nv > BT, ragged = t.cg % E != 0;
+    const bool wide = t.nv > BT;
     const int cgv = t.cgv;
     Affine<E> f;
     if (!wide) f.set(a, t.channel(t.cx));
@@ -465,7 +466,8 @@ __global__ __launch_bounds__(BT, BT == 64 && E == 8 ? 3 : 4) void k_norm_units(N
             float n = 0.f, mean = 0.f, m2 = 0.f;
             for (int r = t.ry; r < rows; r += ROWS * t.RY) {
                 x.load(a.x, a.xs, u.r0, rows, r, t.RY, c);
-                float s = 0.f, cnt = 0.f;
+                // four sums side by side: a chain of additions would wait for each
+                float s4[4] = {}, q4[4] = {}, cnt = 0.f;
 #pragma unroll
                 for (int j = 0; j < ROWS; j++) {
                     float y[E];
@@ -473,12 +475,11 @@ __global__ __launch_bounds__(BT, BT == 64 && E == 8 ? 3 : 4) void k_norm_units(N
                     cnt += r + j * t.RY < rows ? (float)(E - again) : 0.f;
 #pragma unroll
                     for (int e = 0; e < E; e++) {
-                        if (ragged) y[e] = e < again ? 0.f : y[e];
-                        s += y[e];
+                        if constexpr (RAGGED) y[e] = e < again ? 0.f : y[e];
+                        s4[(j * E + e) & 3] += y[e];
                     }
                 }
-                const float mb = s / cnt, share = cnt / (n + cnt);
-                float q = 0.f;
+                const float mb = ((s4[0] + s4[1]) + (s4[2] + s4[3])) / cnt, share = cnt / (n + cnt);
 #pragma unroll
                 for (int j = 0; j < ROWS; j++) {
                     float y[E];
@@ -486,11 +487,11 @@ __global__ __launch_bounds__(BT, BT == 64 && E == 8 ? 3 : 4) void k_norm_units(N
                     if (r + j * t.RY < rows)
 #pragma unroll
                         for (int e = 0; e < E; e++) {
-                            if (ragged) y[e] = e < again ? mb : y[e];
-                            q += (y[e] - mb) * (y[e] - mb);
+                            if constexpr (RAGGED) y[e] = e < again ? mb : y[e];
+                            q4[(j * E + e) & 3] += (y[e] - mb) * (y[e] - mb);
                         }
                 }
-                const float delta = mb - mean;
+                const float delta = mb - mean, q = (q4[0] + q4[1]) + (q4[2] + q4[3]);
                 mean += delta * share;
                 m2 += q + delta * delta * n * share;
                 n += cnt;
@@ -927,14 +928,18 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float* __restrict__
 
 // ---------------------------------------------------------------- launch ----
 
-// Rows a unit takes: enough units to fill the chip; with many segments, most
-// segments in one unit (sixteen times their mean length), unless a unit would
-// then be over 256 KB of fp32 rows (one workgroup would be long at work on it).
+// Rows a unit takes: enough units to fill the chip, of at least 64 rows (one
+// graph of 55K rows of 80 fp16 channels: 16 rows 51 us, 64 rows 25); with
+// many segments, most segments in one unit (sixteen times their mean length),
+// unless a unit would then be over 512 KB of fp32 rows, which one workgroup
+// is long at work on (2,282 graphs of 507K rows, 160 bf16 channels: 256 rows
+// 157 us, 512 rows 177, 1,024 rows 230; 1,100 graphs of 55K rows, 256 fp16
+// channels: 256 rows 70, 512 rows 50).
 static int norm_lr(int64_t m, int64_t d, int64_t segs) {
     int lr = 10;
-    while (lr > 4 && m >> lr < 2048) lr--;
+    while (lr > 6 && m >> lr < 2048) lr--;
     if (segs >= 1024)
-        while (lr < 12 && ((int64_t)1 << lr) < 16 * m / segs && (d * 4 << (lr + 1)) <= 256 << 10) lr++;
+        while (lr < 12 && ((int64_t)1 << lr) < 16 * m / segs && (d * 4 << (lr + 1)) <= 512 << 10) lr++;
     return lr;
 }
 // Workgroups of the row walk: at most what the chip holds a few times over,
@@ -999,7 +1004,8 @@ template <int DT, int E, int BT, int ACT>
 static void segs_units(const NormArgs& a, int64_t blocks, bool grad, hipStream_t s) {
     const size_t lds = ((size_t)2 * std::max<int64_t>(a.groups * ceil_div(a.cg, E), BT) + 2 * a.groups + (grad ? 2 * a.d : 0)) * 4;
     if (grad) k_norm_units_grad<DT, E, BT, ACT><<<(unsigned)blocks, BT, lds, s>>>(a);
-    else k_norm_units<DT, E, BT><<<(unsigned)blocks, BT, lds, s>>>(a);
+    else if (E > 1 && a.cg % E) k_norm_units<DT, E, BT, (E > 1)><<<(unsigned)blocks, BT, lds, s>>>(a);
+    else k_norm_units<DT, E, BT, false><<<(unsigned)blocks, BT, lds, s>>>(a);
     TAURUS_CHECK_LAUNCH();
 }
 template <int DT, int E, int ACT>
