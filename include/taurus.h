@@ -403,9 +403,10 @@ int taurus_permute_rows(const void* in, void* out, int64_t n, int64_t row_bytes,
  *     as each has a workspace of its own.
  *   - Pointers are device memory aligned to their element type.  Row arrays
  *     are [rows][stride] with the row's values first, stride >= the row's
- *     length (at most 2^22); 16-byte aligned arrays whose row length and
- *     stride are whole 16-byte pieces are the fast case, any other is
- *     correct.  Outputs must not overlap inputs.
+ *     length (at most 2^22).  Rows need no other alignment: they are read
+ *     and written 16 bytes at a time wherever they start.  (The linear maps
+ *     stage 16-bit rows that are no whole 4-byte words in a slower way.)
+ *     Outputs must not overlap inputs.
  *   - Arithmetic is fp32 (fp32 matrix cores, or 16-bit ones with fp32
  *     accumulation); stored results are rounded to nearest even once.  Sums
  *     run in an order that the sizes, offsets and ids fix: equal calls on

@@ -12,8 +12,9 @@
 // All three are one product of tiles TM x TN with fp32 accumulation.  The
 // contraction runs in stages of 128 bytes a row: the next stage's pieces are
 // on their way from memory to registers while the matrix cores work on this
-// one's in LDS, and go to the other LDS buffer afterwards (one barrier a
-// stage).  An operand whose values lie along the contraction in memory (x
+// one's in LDS (one buffer, two barriers a stage: three or four workgroups a
+// compute unit, which fill each other's waits, were worth more than a second
+// buffer).  An operand whose values lie along the contraction in memory (x
 // and dy in y and dx, W in dx) is staged as rows of eight 16-byte pieces,
 // piece p of row r at p ^ (r mod 8), so that the eight lanes that read
 // together touch all banks.  An operand that lies across it (W in y, both in

@@ -739,6 +739,34 @@ def test_graph_replays(dtype):
             assert torch.equal(a, c) and torch.equal(b, c), (seed, i)
 
 
+def test_far_rows():
+    """Rows far apart in arrays of 2.6e9 values, past what 32 bits hold:
+    linear maps and norms give the dense rows' bits."""
+    note("far rows")
+    m, apart, k, n = 40_001, 65_600, 64, 72
+
+    def far(width):
+        return torch.empty(m * apart, dtype=BF16, device="cuda").view(m, apart)[:, :width]
+    off = ranges([12_000, 0, 1, m - 12_001]).cuda()
+    x, dy = normal((m, k), BF16, 1).cuda(), normal((m, n), BF16, 2).cuda()
+    w = normal((4, k, n), BF16, 3, k ** -0.5).cuda()
+    fx, fdy, out = far(k), far(n), far(n)
+    fx.copy_(x)
+    fdy.copy_(dy)
+    T.grouped_linear(fx, off, w, out=out)
+    y = T.grouped_linear(x, off, w)
+    assert torch.equal(out, y)
+    for got, want in zip(T.grouped_linear_grad(fdy, fx, off, w), T.grouped_linear_grad(dy, x, off, w)):
+        assert torch.equal(got, want)
+    for o in (None, off):
+        _, mean, rstd = T.group_norm(dy, 4, off=o, act="silu", stats=True)
+        want = T.group_norm(dy, 4, off=o, act="silu")
+        assert torch.equal(T.group_norm(fdy, 4, off=o, act="silu", out=out), want)
+        for got, ref in zip(T.group_norm_grad(out, fdy, 4, None, None, mean, rstd, off=o, act="silu"),
+                            T.group_norm_grad(want, dy, 4, None, None, mean, rstd, off=o, act="silu")):
+            assert torch.equal(got, ref)
+
+
 def test_streams():
     """Two streams at once, and the stream argument, give the eager bits."""
     note("streams")
