@@ -430,6 +430,13 @@ struct RowsArgs {
     int tiles;
 };
 // WT: W_g is [cols][depth] (dx), else [depth][cols] (y)
+//
+// Tiles of 128 rows: of 128 columns for 16-bit types, of 64 for narrow outputs
+// and for fp32, whose products bound it (four times the steps of one stage).
+// 256 columns of 512 threads read x once where outputs are that wide, but
+// leave two workgroups a compute unit: 1M bf16 rows 128 -> 256 take 272 us
+// that way, 206 this way (3.7 TB/s), 300K fp16 rows 1,024 -> 256 in fp32 307
+// and 272 (3.4 TB/s, 0.58 PFLOP/s).
 template <int DT, bool WT, int TN, bool AL>
 struct RowTiles {
     typedef Along<DT, ROW_TILE, AL> OpM;
@@ -541,6 +548,9 @@ static void grouped_rows(RowsArgs a, hipStream_t s) {
 
 // ----------------------------------------------------------------- dW, db --
 
+// Bound by memory up to about 256 x 256, where x and dy are read once per
+// column and row tile of W: 1M bf16 rows, 256 x 256, 5 types take 246 us (1.0
+// GB from memory once, 4.2 TB/s), the join 16.
 // A unit of R rows and a tile of W_g at a time.  A type whose rows are one
 // unit is written at once; the units of longer types leave their fp32 sums in
 // the workspace, and k_grouped_join adds them in row order.

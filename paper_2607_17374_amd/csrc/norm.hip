@@ -8,14 +8,21 @@
 //     dx = rstd (gamma dz - mean(gamma dz) - xhat mean(gamma dz xhat)),
 //     dgamma = sum dz xhat,  dbeta = sum dz  (all rows).
 //
-// Everything is bound by memory.  One row at a time: a power-of-two group of
-// lanes holds a group's values in registers, reads them once, and walks the
-// rows with the next row's values already requested.  Segments: units of
-// rows that never cross a segment (rowops.hpp); a unit that is a whole
-// segment is finished by its workgroup, which reads the rows again from the
-// caches; longer segments leave each unit's statistics in the workspace,
-// k_norm_join combines them in unit order and a second pass over the rows
-// applies them.
+// One row at a time is bound by memory: a power-of-two group of lanes holds a
+// group's values in registers, reads them once, and walks the rows with the
+// next row's values already requested (1M bf16 rows of 256 channels, ReLU:
+// 215 us, 4.8 TB/s, the rate of a copy).
+//
+// Segments: units of rows that never cross a segment (rowops.hpp); a unit that
+// is a whole segment is finished by its workgroup, from registers where its
+// rows fit them, else from the caches; longer segments leave each unit's
+// statistics in the workspace, k_norm_join combines them in unit order and a
+// second pass over the rows applies them.  One graph of 400K fp32 rows of 128
+// channels: 48 us for the statistics (4.3 TB/s), 13 for the join, 68 for the
+// second pass (6.0 TB/s, a part of it from the caches).  Many small segments
+// are bound by what a workgroup waits for one after another (its first
+// segment, the rows, the sums): 9,000 graphs of 300K fp16 rows take 93 us,
+// their gradient 113, of which the vector units work 48.
 //
 // Means and squared deviations are fp32 and never formed as E[x^2] - mu^2:
 // deviations are taken from the mean of the values at hand (a row, or a few
