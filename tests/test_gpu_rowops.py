@@ -351,6 +351,26 @@ def test_grouped_linear_grad_long_types(dtype, sizes, k, n):
     assert none is None and none2 is None and torch.equal(db, db2)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,k,n", [(14_000, 72, 300), (66_100, 40, 24), (14_000, 33, 301), (66_100, 301, 17),
+                                   (40_000, 129, 128)])
+def test_grouped_linear_many_tiles(dtype, m, k, n):
+    """More tiles than are resident at once: workgroups take several."""
+    note(f"grouped_linear many tiles {dtype} {m} rows {k} -> {n}")
+    off = ranges([m // 3, 0, 1, m // 5 + 7, m - m // 3 - m // 5 - 8])
+    x, dy = normal((m, k), dtype, 1), normal((m, n), dtype, 2)
+    w, b = normal((5, k, n), dtype, 3, k ** -0.5), normal((5, n), F32, 4)
+    y = T.grouped_linear(x.cuda(), off.cuda(), w.cuda(), b.cuda()).cpu()
+    dx = T.grouped_linear_grad(dy.cuda(), x.cuda(), off.cuda(), w.cuda(), need=("x",))[0].cpu()
+    for g in range(5):
+        r = slice(int(off[g]), int(off[g + 1]))
+        wg, bg = w[g].double(), b[g].double()
+        size = x[r].double().abs() @ wg.abs() + bg.abs()
+        close(y[r], x[r].double() @ wg + bg, 2 * (k + 1) * U * size, dtype, (g, "y"))
+        size = dy[r].double().abs() @ wg.abs().T
+        close(dx[r], dy[r].double() @ wg.T, 2 * (n + 1) * U * size, dtype, (g, "dx"))
+
+
 def test_grouped_linear_differences():
     """dx, dW, db against differences of the 64-bit map along random
     directions: the map is bilinear, so central differences are exact."""
