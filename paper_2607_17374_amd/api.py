@@ -359,6 +359,12 @@ class Layer:
             pass
 
 
+def _check_norm(norm: Optional[dict]) -> None:
+    unknown = set(norm or ()) - {"groups", "weight", "bias", "off", "eps", "act"}
+    if unknown:
+        raise ValueError(f"norm does not know {', '.join(sorted(unknown))}")
+
+
 def _encode(x: torch.Tensor, encoder: dict, stream):
     """The first layer's input rows: vertex v's features (x[v], or scale *
     x[ids[v]]), times its type's weight plus bias, normalised."""
@@ -369,6 +375,7 @@ def _encode(x: torch.Tensor, encoder: dict, stream):
         raise ValueError(f"encoder does not know {', '.join(sorted(enc))}")
     if (off is None) != (weight is None) or (bias is not None and weight is None):
         raise ValueError("the encoder's linear map needs off and weight together")
+    _check_norm(norm)
     h = x if ids is None else lookup_rows(x, ids, scale, stream=stream)
     if weight is not None:
         h = grouped_linear(h, off, weight, bias, stream=stream)
@@ -389,6 +396,8 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     by type, one linear map each: grouped_linear's), ids and scale (x is a
     table, vertex v's row scale * x[ids[v]]: lookup_rows') and norm, each
     optional; offsets must hold every vertex.  Returns (outputs, stats)."""
+    for spec in layers:
+        _check_norm(spec.get("norm"))
     h = x if encoder is None else _encode(x, encoder, stream)
     results, stats = [], []
     plan = Plan(n, row_off, col_dst, chunk, stream=stream)

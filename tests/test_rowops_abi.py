@@ -158,3 +158,18 @@ def test_wrapper_refuses_host_tensors():
         T.lookup_rows_grad(x, ids, 4, accumulate=True)
     with pytest.raises(ValueError, match="need names"):
         T.group_norm_grad(x, x, 1, None, None, x, x, need=("dx",))
+
+
+def test_model_refuses_unknown_encoder_and_norm_keys():
+    x, off = torch.zeros(4, 8), torch.tensor([0, 4])
+
+    def run(layers=(), **kw):
+        T.run_layers(4, off, x, x, list(layers), chunk=4, **kw)
+    with pytest.raises(ValueError, match="norm does not know stats"):
+        run([dict(norm=dict(groups=2, stats=True))])
+    with pytest.raises(ValueError, match="norm does not know out"):
+        run(encoder=dict(norm=dict(out=x)))
+    with pytest.raises(ValueError, match="encoder does not know weights"):
+        run(encoder=dict(weights=x))
+    with pytest.raises(ValueError, match="off and weight together"):
+        run(encoder=dict(off=off))
