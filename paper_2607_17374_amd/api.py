@@ -299,6 +299,9 @@ class Layer:
         """taurus_push_chunk with x = rows [begin, end), on the device or in
         pinned host memory (then it must stay unchanged until the next call)."""
         ptr, on_host = _buf_ptr(x, _TORCH_DTYPE[self.in_dtype], "x")
+        # the library reads that many values behind the pointer
+        if x.numel() < (end - begin) * self.d_in or (x.dim() == 2 and x.shape[1] != self.d_in):
+            raise ValueError(f"x must hold rows [{begin}, {end}) of {self.d_in} values, got shape {tuple(x.shape)}")
         N.check(N.lib().taurus_push_chunk(self._h, begin, end, ptr, on_host), "taurus_push_chunk")
 
     def push_all(self, x: torch.Tensor, order: Optional[Sequence[int]] = None) -> None:
@@ -365,9 +368,9 @@ def _check_norm(norm: Optional[dict]) -> None:
         raise ValueError(f"norm does not know {', '.join(sorted(unknown))}")
 
 
-def _encode(x: torch.Tensor, encoder: dict, stream):
-    """The first layer's input rows: vertex v's features (x[v], or scale *
-    x[ids[v]]), times its type's weight plus bias, normalised."""
+def _encode(x: torch.Tensor, encoder: dict, n: int, d_in: Optional[int], stream):
+    """The first layer's input rows [n][d_in]: vertex v's features (x[v], or
+    scale * x[ids[v]]), times its type's weight plus bias, normalised."""
     enc = dict(encoder)
     ids, scale, norm = enc.pop("ids", None), enc.pop("scale", 1.0), enc.pop("norm", None)
     off, weight, bias = enc.pop("off", None), enc.pop("weight", None), enc.pop("bias", None)
@@ -376,6 +379,10 @@ def _encode(x: torch.Tensor, encoder: dict, stream):
     if (off is None) != (weight is None) or (bias is not None and weight is None):
         raise ValueError("the encoder's linear map needs off and weight together")
     _check_norm(norm)
+    rows, width = (x.shape[0] if ids is None else ids.numel()), (x.shape[-1] if weight is None else weight.shape[-1])
+    if rows != n or (d_in is not None and width != d_in):
+        raise ValueError(f"the encoder gives {rows} rows of {width} values; {n} vertices enter the first layer"
+                         + (f" with {d_in} values each" if d_in is not None else ""))
     h = x if ids is None else lookup_rows(x, ids, scale, stream=stream)
     if weight is not None:
         h = grouped_linear(h, off, weight, bias, stream=stream)
@@ -398,7 +405,7 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     optional; offsets must hold every vertex.  Returns (outputs, stats)."""
     for spec in layers:
         _check_norm(spec.get("norm"))
-    h = x if encoder is None else _encode(x, encoder, stream)
+    h = x if encoder is None else _encode(x, encoder, n, layers[0]["d_in"] if layers else None, stream)
     results, stats = [], []
     plan = Plan(n, row_off, col_dst, chunk, stream=stream)
     for i, spec in enumerate(layers):

@@ -173,3 +173,41 @@ def test_model_refuses_unknown_encoder_and_norm_keys():
         run(encoder=dict(weights=x))
     with pytest.raises(ValueError, match="off and weight together"):
         run(encoder=dict(off=off))
+
+
+def _layer(n, d_in, chunk):
+    """A layer handle that no library call has made."""
+    L = T.Layer.__new__(T.Layer)
+    L._h, L.n, L.d_in, L.chunk, L.in_dtype = ctypes.c_void_p(), n, d_in, chunk, N.F32
+    return L
+
+
+@pytest.mark.parametrize("shape", [(3, 8), (4, 7), (4, 9), (5, 7), (31,), (0, 8)])
+def test_pushed_rows_of_another_shape_are_refused(shape, monkeypatch):
+    """The library reads (end - begin) x d_in values behind the pointer."""
+    monkeypatch.setattr(T.api, "_buf_ptr", lambda t, dtype, what: (1 << 20, 0))
+    with pytest.raises(ValueError, match="rows"):
+        _layer(8, 8, 4).push_chunk(4, 8, torch.zeros(shape))
+    if len(shape) == 2:
+        with pytest.raises(ValueError, match="rows"):
+            _layer(4, 8, 4).push_all(torch.zeros(shape)[:4])
+
+
+def test_pushed_rows_that_fit_reach_the_library(monkeypatch):
+    monkeypatch.setattr(T.api, "_buf_ptr", lambda t, dtype, what: (1 << 20, 0))
+    for x in (torch.zeros(4, 8), torch.zeros(6, 8), torch.zeros(32)):
+        with pytest.raises(T.TaurusError):  # no layer behind the handle
+            _layer(8, 8, 4).push_chunk(4, 8, x)
+
+
+@pytest.mark.parametrize("x,encoder,width", [
+    ((4, 8), dict(ids=torch.zeros(3, dtype=torch.int32)), 8),          # an id a vertex
+    ((3, 8), dict(scale=1.0), 8),                                      # a row a vertex
+    ((4, 8), dict(off=torch.tensor([0, 4]), weight=torch.zeros(1, 8, 6)), 8),
+    ((4, 8), dict(ids=torch.zeros(4, dtype=torch.int32)), 6), ((4, 8), dict(norm=dict(groups=2)), 9),
+])
+def test_model_refuses_an_encoder_of_another_shape(x, encoder, width):
+    """Before any device work: host tensors get no further."""
+    off = torch.tensor([0, 4])
+    with pytest.raises(ValueError, match=r"the encoder gives \d+ rows of \d+ values"):
+        T.run_layers(4, off, off, torch.zeros(x), [dict(d_in=width)], chunk=4, encoder=encoder)
