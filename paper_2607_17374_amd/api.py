@@ -403,6 +403,7 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     by type, one linear map each: grouped_linear's), ids and scale (x is a
     table, vertex v's row scale * x[ids[v]]: lookup_rows') and norm, each
     optional; offsets must hold every vertex.  Returns (outputs, stats)."""
+    layers = list(layers)
     for spec in layers:
         _check_norm(spec.get("norm"))
     h = x if encoder is None else _encode(x, encoder, n, layers[0]["d_in"] if layers else None, stream)

@@ -211,3 +211,50 @@ def test_model_refuses_an_encoder_of_another_shape(x, encoder, width):
     off = torch.tensor([0, 4])
     with pytest.raises(ValueError, match=r"the encoder gives \d+ rows of \d+ values"):
         T.run_layers(4, off, off, torch.zeros(x), [dict(d_in=width)], chunk=4, encoder=encoder)
+
+
+class _FakeRun:
+    """run_layers' parts as a log of what they are asked, without a device."""
+
+    def __init__(self, monkeypatch):
+        self.log = log = []
+
+        class FakeLayer:
+            def __init__(self, n, row_off, col_dst, out, **kw):
+                self.out = out
+
+            def push_all(self, h):
+                log.append("push")
+
+            def finalize(self):
+                log.append("finalize")
+                return {}
+
+            def destroy(self):
+                pass
+
+        class FakePlan:
+            def __init__(self, *a, **kw):
+                pass
+
+            def destroy(self):
+                pass
+
+        def norm(h, out=None, stream=None, **kw):
+            log.append("norm")
+            return h if out is None else out
+        monkeypatch.setattr(T.api, "Layer", FakeLayer)
+        monkeypatch.setattr(T.api, "Plan", FakePlan)
+        monkeypatch.setattr(T.api, "group_norm", norm)
+
+    def synchronize(self):  # the run's stream
+        self.log.append("wait")
+
+    def __call__(self, layers):
+        return T.run_layers(4, None, None, torch.zeros(4, 8), layers, chunk=4, stream=self)
+
+
+def test_model_takes_layers_of_any_iterable(monkeypatch):
+    run = _FakeRun(monkeypatch)
+    outs, stats = run(dict(d_in=8, d_out=8) for _ in range(3))
+    assert len(outs) == len(stats) == 3 and run.log == ["push", "finalize"] * 3
