@@ -402,7 +402,8 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     layer's input from x: a dict with off, weight and bias (vertices grouped
     by type, one linear map each: grouped_linear's), ids and scale (x is a
     table, vertex v's row scale * x[ids[v]]: lookup_rows') and norm, each
-    optional; offsets must hold every vertex.  Returns (outputs, stats)."""
+    optional; offsets must hold every vertex.  Returns (outputs, stats); the
+    outputs are complete."""
     layers = list(layers)
     for spec in layers:
         _check_norm(spec.get("norm"))
@@ -412,18 +413,20 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     for i, spec in enumerate(layers):
         spec = dict(spec)
         norm = spec.pop("norm", None)
-        given = outs[i] if outs is not None else None
-        dtype = _TORCH_DTYPE[spec.get("out_dtype", N.F32)]
-        out = given if given is not None and norm is None else torch.empty((n, spec["d_out"]), dtype=dtype,
-                                                                           device=x.device)
+        shape, dtype = (n, spec["d_out"]), _TORCH_DTYPE[spec.get("out_dtype", N.F32)]
+        result = outs[i] if outs is not None and outs[i] is not None else torch.empty(shape, dtype=dtype,
+                                                                                      device=x.device)
+        out = result if norm is None else torch.empty(shape, dtype=dtype, device=result.device)
         L = Layer(n, row_off, col_dst, out=out, chunk=chunk, stream=stream, profile=profile, plan=plan, **spec)
         L.push_all(h)
         stats.append(L.finalize())
         L.destroy()
         if norm is not None:
-            out = group_norm(out, out=given, stream=stream, **norm)
+            out = group_norm(out, out=result, stream=stream, **norm)
         results.append(out)
         h = out
+    if layers and norm is not None:  # the norm is only enqueued; finalize leaves a layer's rows complete
+        (torch.cuda.current_stream(result.device) if stream is None else stream).synchronize()
     if plan is not None:
         plan.destroy()
     return results, stats

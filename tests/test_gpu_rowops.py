@@ -925,3 +925,26 @@ def test_encoder_and_norms_in_a_model():
         T.run_layers(n, row_off, col_dst, table.cuda(), layers, chunk=1024, encoder=dict(enc, foo=1))
     with pytest.raises(ValueError, match="together"):
         T.run_layers(n, row_off, col_dst, table.cuda(), layers, chunk=1024, encoder=dict(weight=w.cuda()))
+
+
+def test_model_on_a_stream_of_its_own():
+    """A model whose last layer is normalised, run on another stream than the
+    current one, is complete when it returns and gives the same bits."""
+    note("model on a stream of its own")
+    n, d = 200_003, 64
+    g = torch.Generator().manual_seed(1)
+    src, dst = (torch.randint(0, n, (4 * n,), generator=g, dtype=torch.int32).cuda() for _ in range(2))
+    row_off, col_dst = T.build_csr(n, src, dst)
+    x = normal((n, d), F32, 2).cuda()
+    off = torch.arange(0, n + 1, n // 7).cuda()
+    off[-1] = n
+    layers = [dict(agg=N.SAGE_MEAN, d_in=d, d_out=d, weight_cat=normal((d, 2 * d), F32, 3, 0.2).numpy(), bias=None,
+                   layer=i + 1, norm=dict(groups=4, off=off, act="silu")) for i in range(2)]
+    enc = dict(norm=dict(groups=1, act="relu"))
+    want, _ = T.run_layers(n, row_off, col_dst, x, layers, chunk=65536, encoder=enc)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    got, _ = T.run_layers(n, row_off, col_dst, x, layers, chunk=65536, encoder=enc, stream=s)
+    assert s.query()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

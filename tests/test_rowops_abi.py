@@ -241,7 +241,7 @@ class _FakeRun:
                 pass
 
         def norm(h, out=None, stream=None, **kw):
-            log.append("norm")
+            log.append("norm" if out is not None else "norm into memory of its stream")
             return h if out is None else out
         monkeypatch.setattr(T.api, "Layer", FakeLayer)
         monkeypatch.setattr(T.api, "Plan", FakePlan)
@@ -258,3 +258,15 @@ def test_model_takes_layers_of_any_iterable(monkeypatch):
     run = _FakeRun(monkeypatch)
     outs, stats = run(dict(d_in=8, d_out=8) for _ in range(3))
     assert len(outs) == len(stats) == 3 and run.log == ["push", "finalize"] * 3
+
+
+def test_model_waits_for_a_last_norm(monkeypatch):
+    """Outputs are complete when the model returns, as finalize leaves them,
+    and are the current stream's memory on whichever stream it ran."""
+    layer = dict(d_in=8, d_out=8)
+    run = _FakeRun(monkeypatch)
+    run([dict(layer, norm=dict(groups=2)), layer])
+    assert run.log == ["push", "finalize", "norm", "push", "finalize"]
+    run.log.clear()
+    run([layer, dict(layer, norm=dict(groups=2))])
+    assert run.log == ["push", "finalize"] * 2 + ["norm", "wait"]
