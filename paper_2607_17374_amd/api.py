@@ -425,8 +425,8 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
             out = group_norm(out, out=result, stream=stream, **norm)
         results.append(out)
         h = out
-    if layers and norm is not None:  # the norm is only enqueued; finalize leaves a layer's rows complete
-        (torch.cuda.current_stream(result.device) if stream is None else stream).synchronize()
     if plan is not None:
         plan.destroy()
+    if layers and norm is not None:  # the norm is only enqueued; finalize leaves a layer's rows complete
+        (torch.cuda.current_stream(result.device) if stream is None else stream).synchronize()
     return results, stats
