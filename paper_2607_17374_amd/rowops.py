@@ -80,9 +80,7 @@ class _Call:
         if dtype is not None and t.dtype != dtype:
             raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
         m, d = t.shape
-        stride = t.stride(0)
-        if m <= 1:
-            stride = max(stride, d)
+        stride = t.stride(0) if m > 1 else d
         if (d > 1 and m > 0 and t.stride(1) != 1) or stride < d:
             raise ValueError(f"{what}: the values of a row must lie next to one another and rows must not overlap")
         return t.data_ptr(), max(stride, 1)

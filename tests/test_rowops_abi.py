@@ -270,3 +270,13 @@ def test_model_waits_for_a_last_norm(monkeypatch):
     run.log.clear()
     run([layer, dict(layer, norm=dict(groups=2))])
     assert run.log == ["push", "finalize"] * 2 + ["norm", "wait"]
+
+
+def test_one_row_of_a_wide_array():
+    """Nothing lies between the rows of an array of one row (or none)."""
+    c = T.rowops._Call.__new__(T.rowops._Call)
+    c.device, c.used = torch.device("cpu"), None
+    wide = torch.zeros(1, (1 << 22) + 8)
+    for t, d in ((wide[:, :16], 16), (wide[:0, :16], 16), (wide[:, 5:6], 1), (torch.zeros(3, 4)[1:2], 4)):
+        pointer, stride = c.rows(t, None, "x")
+        assert (pointer, stride) == (t.data_ptr(), d)
