@@ -1114,7 +1114,8 @@ static void norm_run(NormArgs a, int dtype, bool grad, void* work, int64_t have,
     check_work(work, have, norm_bytes(dtype, a.m, a.d, a.groups, a.segs, a.off != nullptr, grad), call);
     const RowPlan r = a.off ? RowPlan{e, 1, 0, false} : row_plan(e, a.cg);
     const NormWork w = norm_work(work, a.m, a.d, a.groups, a.segs, a.off != nullptr, grad, r.lg);
-    a.cols = grad && (dweight || dbias) ? w.cols : nullptr;
+    const bool sums = dweight || dbias;  // of columns: the gradient alone has them
+    a.cols = sums ? w.cols : nullptr;
     a.part = w.part;
     a.stat = w.stat;
     a.slots = w.slots;
@@ -1132,7 +1133,7 @@ static void norm_run(NormArgs a, int dtype, bool grad, void* work, int64_t have,
         else if (dtype == TAURUS_BF16) norm_rows<TAURUS_BF16>(a, r, w.blocks, grad, s);
         else norm_rows<TAURUS_F16>(a, r, w.blocks, grad, s);
     }
-    if (a.cols) {
+    if (sums) {  // also of no rows, which may have no workspace
         k_norm_columns<<<(unsigned)ceil_div(2 * (int64_t)a.d, 16), 1024, 0, s>>>(a.cols, none ? 0 : w.col_rows, a.d,
                                                                                  dweight, dbias);
         TAURUS_CHECK_LAUNCH();

@@ -709,6 +709,22 @@ def test_relu_border_is_exact():
         assert torch.equal(db.cpu().double(), (z > 0).double().sum(0))
 
 
+@pytest.mark.parametrize("m", [1, 5, 63, 64, 500])
+def test_norm_grad_of_no_segments_writes_zeros(m):
+    """No segment holds a row: the weights' gradients are zeros, written also
+    where the call needs no workspace."""
+    note(f"group_norm_grad of no segments m={m}")
+    L, x, off = N.lib(), torch.ones(m, 16, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    dw, db = (torch.full((16,), float("nan"), device="cuda") for _ in range(2))
+    nbytes = L.taurus_group_norm_bytes(N.F32, m, 16, 4, 0, 1, 1)
+    work = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+    N.check(L.taurus_group_norm_grad(x.data_ptr(), 16, x.data_ptr(), 16, N.F32, m, 16, 4, off.data_ptr(), 0, None, None,
+                                     None, None, N.ACT_NONE, None, 16, dw.data_ptr(), db.data_ptr(),
+                                     work.data_ptr() if nbytes else None, nbytes,
+                                     torch.cuda.current_stream().cuda_stream), "taurus_group_norm_grad")
+    assert (dw == 0).all() and (db == 0).all()
+
+
 # ------------------------------------------------- streams, graphs, refusals --
 
 def everything(t):
