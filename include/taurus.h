@@ -45,7 +45,7 @@ typedef enum { TAURUS_F32 = 0, TAURUS_BF16 = 1, TAURUS_F16 = 2 } taurus_dtype;
 typedef enum {
     TAURUS_ACT_NONE = 0,
     TAURUS_ACT_RELU = 1, /* max(z, 0), as the layers' (a NaN becomes 0)                  */
-    TAURUS_ACT_SILU = 2  /* z / (1 + exp(-z))                                            */
+    TAURUS_ACT_SILU = 2  /* z / (1 + exp(-z)), at infinities its limits z and 0          */
 } taurus_activation;
 
 /* Eviction policies of a budgeted layer (desc.eviction).  The paper's

@@ -59,21 +59,34 @@ struct NormArgs {
     int64_t places;  // units of segments of several units, at most
 };
 
-// 1 / (1 + exp(-z)) to about two units in the last place, by the chip's
-// power of two and reciprocal (one unit each): -z log2(e) as a rounded product
-// and its rest, the rest taken linearly.  (The library's exponential and
-// division take three times the steps; SiLU is then bound by them.)
+// 1 / (1 + exp(-z)) for |z| <= SIGMOID_END by the chip's power of two and
+// reciprocal (one unit in the last place each): with t = -z and h = t log2(e)
+// rounded, exp(t) is 2^h times the exponential of t - h ln 2, taken linearly
+// (ln 2 in two parts).  Right to about three units in the last place above z =
+// -87.3; below, where it passes under the least normal value, it may be 0.
+// (The library's exponential and division take three times the steps; SiLU is
+// then bound by them.)
+constexpr float SIGMOID_END = 88.7f;
 __device__ inline float sigmoid(float z) {
-    const float t = -z, hi = t * 1.44269502f;
-    const float lo = __builtin_fmaf(t, 1.44269502f, -hi) + t * 1.92596299e-8f;
-    float e = __builtin_amdgcn_exp2f(hi);
-    // past 2^126 the sum's reciprocal is 0, or near it, whatever the rest
-    e = hi < 126.f ? __builtin_fmaf(e, lo * 0.693147181f, e) : e;
-    return __builtin_amdgcn_rcpf(1.f + e);
+    const float t = -z, h = t * 1.44269502f;  // |h| < 128: the power is finite
+    const float rest = __builtin_fmaf(h, 1.90465421e-9f, __builtin_fmaf(h, -0.693147182f, t));
+    const float e = __builtin_amdgcn_exp2f(h);
+    return __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(e, rest, e));
+}
+// Arguments past its ends are held there (NaN stays): above, the sigmoid is 1
+// and SiLU's slope too; below, SiLU and its slope are less than 2^-119 from 0.
+__device__ inline float silu(float z) {
+    const float c = __builtin_elementwise_maximum(z, -SIGMOID_END);
+    return c * sigmoid(__builtin_elementwise_minimum(c, SIGMOID_END));
+}
+__device__ inline float silu_slope(float z) {
+    const float c = __builtin_elementwise_minimum(__builtin_elementwise_maximum(z, -SIGMOID_END), SIGMOID_END);
+    const float q = sigmoid(c);
+    return q * (1.f + c * (1.f - q));
 }
 __device__ inline float act_of(float z, int act) {
     if (act == TAURUS_ACT_RELU) return fmaxf(z, 0.f);
-    if (act == TAURUS_ACT_SILU) return z * sigmoid(z);
+    if (act == TAURUS_ACT_SILU) return silu(z);
     return z;
 }
 // The sign of (x - mean) rstd w + b in 64 bits.  The conversions stay where
@@ -94,8 +107,7 @@ __device__ inline float act_grad(float dy, float x, float mean, float rstd, floa
             open = open_exactly(x, mean, rstd, w, b);
         return open ? dy : 0.f;
     }
-    const float q = sigmoid(z);
-    return dy * (q * (1.f + z * (1.f - q)));
+    return dy * silu_slope(z);
 }
 
 // ---------------------------------------------------------- row by row ----
@@ -697,8 +709,7 @@ struct GradAt {
         } else if constexpr (ACT == TAURUS_ACT_SILU) {
 #pragma unroll
             for (int e = 0; e < E; e++) {
-                const float z = d[e] * wr[e] + b[e], q = sigmoid(z);
-                dz[e] *= q * (1.f + z * (1.f - q));
+                dz[e] *= silu_slope(d[e] * wr[e] + b[e]);
             }
         }
     }

@@ -725,6 +725,49 @@ def test_norm_grad_of_no_segments_writes_zeros(m):
     assert (dw == 0).all() and (db == 0).all()
 
 
+SILU_AT = [0.0, 1e-30, -1e-30, 0.5, -0.5, 1.0, -1.0, 8.0, -8.0, 17.0, -17.0, 60.0, -60.0, 87.0, -87.0, 87.6, -87.6, 88.5,
+           -88.5, 95.0, -95.0, 200.0, -200.0, 1e30, -1e30, 2.5e38, -2.5e38, 3.4e38, -3.4e38, float("inf"), -float("inf")]
+
+
+@pytest.mark.parametrize("off", [None, [0, 3]])
+def test_silu_at_any_argument(off):
+    """With weights of zero the argument is the bias.  The sigmoid q is within
+    8 U of itself (power of two, sum, reciprocal, each rounded); under
+    z = -87.3 it passes below the least normal fp32 value 2^-126 and may be 0,
+    so that z q is off by less than 89 x 2^-126 < 2^-119.  The slope
+    q (1 + z (1 - q)) varies with q by at most 1 + |z|, from z = 20 on not at
+    all: there q is 1.  Both have limits at infinity: z and 1, 0 and 0."""
+    note(f"silu at any argument {off}")
+    z = torch.tensor(SILU_AT)
+    d, m = z.numel(), 3
+    x, zero = normal((m, d), F32, 1).cuda(), torch.zeros(d, device="cuda")
+    off = None if off is None else torch.tensor(off, device="cuda")
+    y, mean, rstd = T.group_norm(x, 1, zero, z.cuda(), off=off, act="silu", stats=True)
+    dx, dw, db = T.group_norm_grad(torch.ones_like(x), x, 1, zero, z.cuda(), mean, rstd, off=off, act="silu")
+    zd = z.double().clamp(-1e300, 1e300)
+    q = torch.sigmoid(zd)
+    ref, slope = zd * q, q * (1 + zd * (1 - q))
+    top = torch.isinf(z) & (z > 0)
+    assert (y.cpu()[:, top] == float("inf")).all()
+    near = 16 * U * ref[~top].abs() + 2.0 ** -119
+    for r in range(m):
+        close(y[r][~top.cuda()], ref[~top], near, F32, "silu")
+    close(db, m * slope, m * (8 * U * q * (1 + zd.abs().clamp(max=20)) + 8 * U * slope.abs() + 2.0 ** -119), F32, "slope")
+    assert (dx == 0).all() and torch.isfinite(dw).all()
+
+
+@pytest.mark.parametrize("off", [None, [0, 40]])
+def test_silu_of_arguments_past_fp32(off):
+    """Arguments that overflow fp32 to infinity: z above, 0 below."""
+    note(f"silu past fp32 {off}")
+    x = normal((40, 16), F32, 1)
+    w = torch.full((16,), 3e38)
+    y = T.group_norm(x.cuda(), 1, w.cuda(), off=None if off is None else torch.tensor(off, device="cuda"), act="silu").cpu()
+    z = norm_reference(x, 1, w, None, None if off is None else torch.tensor(off), 1e-5, "none")["z"]
+    assert (y[z > 4e38] == float("inf")).all() and (y[z < -1e3] == 0).all() and not torch.isnan(y).any()
+    assert (z > 4e38).any() and (z < -4e38).any()
+
+
 # ------------------------------------------------- streams, graphs, refusals --
 
 def everything(t):
