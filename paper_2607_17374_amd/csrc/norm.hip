@@ -714,11 +714,12 @@ struct GradAt {
         }
     }
     // dx of ROWS rows, given the means m1 and m2 of the vector's group:
-    // rstd (w dz - m1 - xhat m2) = wr dz - (rstd m1 + (x - mean) rstd^2 m2)
+    // rstd (w dz - m1 - xhat m2) = wr dz - (rstd m1 + xhat (rstd m2));
+    // rstd^2 alone would pass fp32 where eps is 0 and values lie close together
     template <int ROWS>
     __device__ void store(const NormArgs& a, const RowsOf<DT, E, ROWS>& x, const RowsOf<DT, E, ROWS>& y, int64_t r0, int rows,
                           int r, int RY, int c, float m1, float m2) const {
-        const float k1 = rs * m1, k2 = rs * rs * m2;
+        const float k1 = rs * m1, k2 = rs * m2;
 #pragma unroll
         for (int j = 0; j < ROWS; j++) {
             const int rr = r + j * RY;
@@ -726,7 +727,7 @@ struct GradAt {
             float d[E], dz[E];
             at(x.v[j], y.v[j], d, dz);
 #pragma unroll
-            for (int e = 0; e < E; e++) dz[e] = wr[e] * dz[e] - (k1 + d[e] * k2);
+            for (int e = 0; e < E; e++) dz[e] = wr[e] * dz[e] - (k1 + d[e] * rs * k2);
             store_vec<DT, E>(a.out, (r0 + rr) * a.os + c, dz);
             one_row_at_a_time();
         }

@@ -768,6 +768,27 @@ def test_silu_of_arguments_past_fp32(off):
     assert (z > 4e38).any() and (z < -4e38).any()
 
 
+@pytest.mark.parametrize("sizes", [[40], [300], [3] * 30])
+@pytest.mark.parametrize("scale", [1e-20, 1e-12, 1e12])
+def test_norm_grad_of_any_spread(sizes, scale):
+    """rstd from 1e-12 to 1e20 (eps may be 0): its square alone passes fp32."""
+    note(f"group_norm_grad spread {scale} {sizes[:3]}")
+    off, groups, d = ranges(sizes), 2, 24
+    m = int(off[-1])
+    x = normal((m, d), F32, 1, scale)
+    w, b, dy = normal((d,), F32, 2), normal((d,), F32, 3), normal((m, d), F32, 4)
+    ref = norm_reference(x, groups, w, b, off, 0.0, "none")
+    mean, rstd = ref["mean"].float(), ref["rstd"].float()
+    for o, mu, rs in ((off, mean, rstd), (None, mean.repeat_interleave(torch.tensor(sizes), 0),
+                                          rstd.repeat_interleave(torch.tensor(sizes), 0))):
+        dx, dw, db = T.group_norm_grad(dy.cuda(), x.cuda(), groups, w.cuda(), b.cuda(), mu.cuda(), rs.cuda(),
+                                       off=None if o is None else o.cuda())
+        rdx, tdx, rdw, tw, rdb, tb, _ = norm_grad_reference(x, dy, groups, w, b, mu, rs, o, "none")
+        close(dx, rdx, tdx, F32, "dx")
+        close(dw, rdw, tw, F32, "dweight")
+        close(db, rdb, tb, F32, "dbias")
+
+
 # ------------------------------------------------- streams, graphs, refusals --
 
 def everything(t):
