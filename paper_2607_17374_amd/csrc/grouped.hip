@@ -767,14 +767,21 @@ __global__ __launch_bounds__(256) void k_grouped_join(WeightArgs a, int64_t type
 
 // Rows a unit of dW takes: every unit of a long type writes and reads a copy
 // of W, so as few units as fill the chip's 256 compute units once, ranges
-// that end inside a unit counted in; at least 256 rows.
+// that end inside a unit counted in; at least 256 rows.  At most 8,192, so
+// that one long type among short ones does not end by itself (60 types of 700K
+// bf16 rows, 1,024 -> 320: 4,096 rows 1.09 ms, 8,192 1.08, 16,384 1.27, no end
+// 1.64), or as many more as keep all units' copies, two places a window of R
+// rows, at a quarter of the bytes of x and dy: 8 k n m / R <= m (k + n) size /
+// 4 (one type of 300K bf16 rows, 4,096 -> 4,096: 8,192 rows take 5.0 GB and
+// 19.7 ms, 32,768 rows 1.3 GB and 18 ms).
 static int weight_tile_k(int64_t k) { return k <= 64 ? 64 : 128; }
 static int weight_tile_n(int dtype, int64_t n) { return dtype == TAURUS_F32 || n <= 64 ? 64 : 128; }
 static int weight_rows(int dtype, int64_t m, int64_t groups, int64_t k, int64_t n) {
     const int64_t tiles = ceil_div(k, weight_tile_k(k)) * ceil_div(n, weight_tile_n(dtype, n));
     const int64_t resident = 256 * (weight_tile_k(k) * weight_tile_n(dtype, n) == 128 * 128 ? 3 : 4);
     const int64_t units = std::max<int64_t>(resident / tiles - std::min(groups, resident), 1);
-    return (int)std::min<int64_t>(std::max<int64_t>(ceil_div(ceil_div(m, units), 64) * 64, 256), 8192);
+    const int64_t most = std::max<int64_t>(ceil_div(32 * k * n, (k + n) * dtype_size(dtype) * 64) * 64, 8192);
+    return (int)std::min<int64_t>(std::max<int64_t>(ceil_div(ceil_div(m, units), 64) * 64, 256), most);
 }
 struct WeightWork {
     float *part, *part_b;

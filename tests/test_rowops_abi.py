@@ -280,3 +280,17 @@ def test_one_row_of_a_wide_array():
     for t, d in ((wide[:, :16], 16), (wide[:0, :16], 16), (wide[:, 5:6], 1), (torch.zeros(3, 4)[1:2], 4)):
         pointer, stride = c.rows(t, None, "x")
         assert (pointer, stride) == (t.data_ptr(), d)
+
+
+@pytest.mark.parametrize("dtype,size", [(N.F32, 4), (N.BF16, 2)])
+@pytest.mark.parametrize("m", [300, 9_000, 100_000, 1_000_000, 30_000_000])
+@pytest.mark.parametrize("k,n", [(1, 1), (64, 64), (256, 256), (1024, 1024), (1024, 320), (4096, 4096), (16384, 8192),
+                                 (65536, 65536)])
+def test_weight_gradient_workspace_is_bounded(dtype, size, m, k, n):
+    """The sums of long types' units take at most a quarter of what x and dy
+    do, or a pair of 128 x 128 tiles for each of 1,024 workgroups, and twice
+    the weight's gradient and its bias's in fp32."""
+    pair = 2 * (k + 1) * n * 4  # dW and db, two places of a window of rows
+    for groups in (1, 5, 60, 2000):
+        bound = max(m * (k + n) * size / 4 * (1 + 1 / k), 1024 * 2 * 128 * (128 + 1) * 4) + pair + 512
+        assert N.lib().taurus_grouped_linear_grad_bytes(dtype, m, groups, k, n) <= bound
