@@ -224,6 +224,37 @@ def test_lookup_grad_accumulates(dtype, m):
     assert (wide[:, d:] == 3.0).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [3, 7, 12, 20, 257])
+@pytest.mark.parametrize("m", [60, 3000])
+def test_lookup_grad_accumulates_to_any_width(dtype, d, m):
+    """A row's last vector covers values of the one before it: each value is
+    added to once."""
+    note(f"lookup_grad accumulate {dtype} d={d} m={m}")
+    n = 41
+    ids = make_ids("uniform", m, n, d)
+    grad, old = normal((m, d), dtype, 8), normal((n, d), dtype, 9)
+    out = strided(old, 3, 1)
+    T.lookup_rows_grad(grad.cuda(), ids.cuda(), n, 2.0, out=out, accumulate=True)
+    ref, size, count = grad_reference(grad, ids, n, 2.0)
+    total = ref + old.double()
+    close(out, total, (count + 2) * U * size + U * total.abs(), dtype, "accumulate")
+
+
+@pytest.mark.parametrize("n,d", [(70_001, 2), (3_000_017, 1)])
+def test_lookup_grad_of_millions(n, d):
+    """Over 4,194,304 ids: the sort's tiles are grouped."""
+    m = 4_300_003
+    note(f"lookup_grad of millions m={m} n={n} d={d}")
+    ids = make_ids("uniform", m, n, 1)
+    ids[:1_000_000] = n // 2  # one id of many tiles
+    grad = normal((m, d), F32, 2)
+    out = T.lookup_rows_grad(grad.cuda(), ids.cuda(), n, 0.5)
+    ref, size, count = grad_reference(grad, ids, n, 0.5)
+    close(out, ref, (count + 2) * U * size, F32, "millions")
+    assert torch.equal(out, T.lookup_rows_grad(grad.cuda(), ids.cuda(), n, 0.5))
+
+
 def test_lookup_grad_special_values():
     """An id's infinities and NaN stay in its own row, those of padded places
     reach none."""
@@ -349,6 +380,38 @@ def test_grouped_linear_grad_long_types(dtype, sizes, k, n):
     assert none is None and none2 is None and torch.equal(dw, dw2)
     none, none2, db2 = T.grouped_linear_grad(ys, xs, off.cuda(), w.cuda(), need=("bias",))
     assert none is None and none2 is None and torch.equal(db, db2)
+
+
+WEIGHT = [  # type sizes, d_in, d_out
+    ([9_000, 0, 17_000, 1] + [40, 0, 333, 65] * 14, 1024, 320),  # more tiles than workgroups, long types among short
+    ([299_223, 0, 777], 24, 40),                                 # units of more than 256 rows
+    ([40_000], 2048, 2048),                                      # units of more than 8,192 rows
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(WEIGHT)))
+def test_grouped_linear_grad_many_units(dtype, case):
+    """Workgroups that take several tiles of several units."""
+    sizes, k, n = WEIGHT[case]
+    off, g = ranges(sizes), len(sizes)
+    m = int(off[-1])
+    note(f"grouped_linear_grad many units {dtype} m={m} types={g} {k} -> {n}")
+    x, dy = normal((m, k), dtype, 1).cuda(), normal((m, n), dtype, 2).cuda()
+    w = torch.zeros(g, k, n, dtype=dtype, device="cuda")
+    wd = [dtype, F32][case % 2]
+    _, dw, db = T.grouped_linear_grad(dy, x, off.cuda(), w, need=("weight", "bias"), weight_dtype=wd)
+    for i in range(g):
+        r = slice(int(off[i]), int(off[i + 1]))
+        xd, yd = x[r].double(), dy[r].double()
+        xt = xd.t().contiguous()
+        tol = 2 * (sizes[i] + 1) * U
+        for got, ref, size, out in ((dw[i], xt @ yd, xt.abs() @ yd.abs(), wd), (db[i], yd.sum(0), yd.abs().sum(0), F32)):
+            bound = tol * size + HALF[out] * (ref.abs() + tol * size) + TINY[out]
+            assert ((got.double() - ref).abs() <= bound).all(), (i, sizes[i])
+    _, dw2, _ = T.grouped_linear_grad(dy, x, off.cuda(), w, need=("weight",), weight_dtype=wd)
+    _, _, db2 = T.grouped_linear_grad(dy, x, off.cuda(), w, need=("bias",))
+    assert torch.equal(dw, dw2) and torch.equal(db, db2)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -787,6 +850,236 @@ def test_norm_grad_of_any_spread(sizes, scale):
         close(dx, rdx, tdx, F32, "dx")
         close(dw, rdw, tw, F32, "dweight")
         close(db, rdb, tb, F32, "dbias")
+
+
+# ---------------------------------------------- norms held to their own sums --
+
+def norm_vectors(dtype, cg):
+    """Values of a vector, and vectors, of a group of cg channels."""
+    e = next(v for v in ([4, 1] if dtype == F32 else [8, 4, 1]) if cg >= v)
+    return e, -(-cg // e)
+
+
+def norm_truth(x, groups, w, b, off, eps, act):
+    """Group norm in 64 bits on the device, every segment at once, with
+    tolerances from the additions that a value passes.
+
+    A row by itself: a lane adds its values, at most 16, one after another;
+    the lanes of a wave join in 6 steps, of four waves in 2 more.  Segments:
+    a thread adds up to eight rows of a vector in four chains of at most 16,
+    joins them, and joins what it has of one batch of rows after another
+    (four roundings each); then up to 64 lanes go through a group's threads,
+    and a long segment's units are added by a wave or four.  A mean is off by
+    the additions' depth, the squares by theirs and, where means of parts
+    are joined, by twice the means' error times the spread."""
+    x = x.cuda()
+    m, d = x.shape
+    cg = d // groups
+    e, cgv = norm_vectors(x.dtype, cg)
+    xd = x.double()
+    W = torch.ones(d, dtype=torch.float64, device="cuda") if w is None else w.double().cuda()
+    B = torch.zeros(d, dtype=torch.float64, device="cuda") if b is None else b.double().cuda()
+    if off is None:
+        seg, count = torch.arange(m, device="cuda"), torch.ones(m, dtype=torch.int64, device="cuda")
+        first, end = 0, m
+    else:
+        first, end = int(off[0]), int(off[-1])
+        count = (off[1:] - off[:-1]).cuda()
+        seg = torch.repeat_interleave(torch.arange(count.numel(), device="cuda"), count)
+    xg = xd[first:end].view(-1, groups, cg)
+
+    def per_segment(v):  # sums of [rows][groups] over a segment's rows
+        return torch.zeros(count.numel(), groups, dtype=torch.float64, device="cuda").index_add_(0, seg, v)
+    size = (count.clamp(min=1) * cg).double().unsqueeze(1)
+    mean = per_segment(xg.sum(2)) / size
+    var = per_segment(((xg - mean[seg].unsqueeze(2)) ** 2).sum(2)) / size
+    rstd = (var + eps) ** -0.5
+    sizes = per_segment(xg.abs().sum(2)) / size
+    top = torch.zeros(count.numel(), groups, dtype=torch.float64, device="cuda")
+    top.scatter_reduce_(0, seg.unsqueeze(1).expand(-1, groups), xg.abs().amax(2), "amax")
+    nv = groups * cgv
+    longest = int(count.max()) if count.numel() else 0
+    if off is None:
+        depth = min(cg, 16) + 6 + 2
+        em = (depth + 3) * U * sizes
+        ev = (depth + 5) * U * var + em ** 2
+    else:
+        ry = max(1, (64 if nv <= 64 else 256) // nv)          # rows side by side, at least
+        rows = min(longest, 4096)                             # of a unit, at most
+        batches = -(-rows // (4 * ry))
+        joins = -(-(min(ry if nv <= 64 else 256 // min(nv, 256), rows) * 4 * cgv) // 64) + 6
+        units = 0 if longest <= 64 else -(-(-(-longest // 64)) // 64) + 8
+        em = U * (16 + 3) * sizes + U * (4 * (batches - 1) + 2 * (joins + 3) + 2 * (units + 3) * (units > 0)) * top
+        ev = (16 + 4 * batches + joins + units + 12) * U * var + 4 * em * var.sqrt() + 4 * em ** 2
+    trel = 0.5 * (ev + U * (var + eps)) * rstd ** 2 + 5 * U
+    hat = (xg - mean[seg].unsqueeze(2)) * rstd[seg].unsqueeze(2)
+    eh = (rstd * em)[seg].unsqueeze(2) + hat.abs() * (trel[seg].unsqueeze(2) + 3 * U)
+    t = hat.reshape(-1, d) * W
+    z, tz = t + B, eh.reshape(-1, d) * W.abs()
+    tz = tz + 3 * U * (z.abs() + B.abs() + t.abs())
+    if act == "relu":
+        y, ty = z.clamp(min=0), tz
+    elif act == "silu":
+        y = z * torch.sigmoid(z)
+        ty = 1.1 * tz + 16 * U * y.abs()
+    else:
+        y, ty = z, tz
+    return dict(y=y, ty=ty, mean=mean, em=em, rstd=rstd, trel=trel, seg=seg, count=count, rows=slice(first, end), nv=nv,
+                longest=longest)
+
+
+def norm_grad_truth(x, dy, groups, w, b, mean, rstd, off, act, ref):
+    """The gradients at the given statistics, likewise."""
+    x, dy = x.cuda(), dy.cuda()
+    m, d = x.shape
+    cg = d // groups
+    e, cgv = norm_vectors(x.dtype, cg)
+    seg, count, r = ref["seg"], ref["count"], ref["rows"]
+    W = torch.ones(d, dtype=torch.float64, device="cuda") if w is None else w.double().cuda()
+    B = torch.zeros(d, dtype=torch.float64, device="cuda") if b is None else b.double().cuda()
+    mu, rs = mean.double()[seg].unsqueeze(2), rstd.double()[seg].unsqueeze(2)
+    hat = (x[r].double().view(-1, groups, cg) - mu) * rs
+    h, y = hat.reshape(-1, d), dy[r].double()
+    z = h * W + B
+    ez = 4 * U * ((h * W).abs() + B.abs())
+    if act == "relu":
+        dz, edz = torch.where(z > 0, y, 0.0), torch.zeros_like(y)
+    elif act == "silu":
+        q = torch.sigmoid(z)
+        dz = y * q * (1 + z * (1 - q))
+        edz = y.abs() * (0.5 * ez + 8 * U * q * (1 + z.abs().clamp(max=20)) + 8 * U)
+    else:
+        dz, edz = y, torch.zeros_like(y)
+    nv, longest = ref["nv"], ref["longest"]
+    if off is None:
+        lanes = min(64, 1 << max(0, (cgv - 1).bit_length())) if cg <= 1024 else 256
+        per = 256 // lanes
+        depth = min(cg, 16) + 6 + 2
+        blocks = min(-(-m * groups // (8 * per)), 1024)
+        column = -(-m * groups // max(1, (blocks * per // groups) * groups)) + -(-blocks * per // groups // 64) + 20
+    else:
+        wave = nv <= 64
+        ry, ry_most = max(1, (64 if wave else 256) // nv), max(1, 256 // nv)
+        rows = -(-min(longest, 4096) // ry)                   # a thread's of a unit
+        slots = -(-(m // 64 + count.numel()) // 4096)         # a workgroup's
+        joins = -(-(min(ry_most, longest) * cgv) // 64) + 6
+        units = 0 if longest <= 64 else -(-(-(-longest // 64)) // 64) + 8
+        depth = rows + e + joins + units
+        column = slots * rows + ry_most + 64 + 20
+    eh = 3 * U * h.abs()
+    dw, db = (dz * h).sum(0), dz.sum(0)
+    tw = (edz * h.abs() + dz.abs() * eh).sum(0) + (column + 4) * U * (dz * h).abs().sum(0)
+    tb = edz.sum(0) + column * U * dz.abs().sum(0)
+    gz, egz = (dz * W).view(-1, groups, cg), (edz * W.abs() + U * (dz * W).abs()).view(-1, groups, cg)
+
+    def averages(v):
+        total = torch.zeros(count.numel(), groups, dtype=torch.float64, device="cuda").index_add_(0, seg, v.sum(2))
+        return (total / (count.clamp(min=1) * cg).double().unsqueeze(1))[seg].unsqueeze(2)
+    s1, s2 = averages(gz), averages(gz * hat)
+    e1 = averages(egz) + (depth + 3) * U * averages(gz.abs())
+    e2 = averages(egz * hat.abs()) + (depth + 7) * U * averages((gz * hat).abs())
+    dx = (rs * (gz - s1 - hat * s2)).reshape(-1, d)
+    tdx = (rs * (egz + e1 + hat.abs() * e2 + 8 * U * (gz.abs() + s1.abs() + (hat * s2).abs()))).reshape(-1, d)
+    return dx, tdx, dw, tw, db, tb
+
+
+def near(got, ref, tol, dtype, what):
+    """close, on the device."""
+    got = got.double()
+    bound = tol + HALF[dtype] * (ref.abs() + tol) + TINY[dtype]
+    bad = ~((got - ref).abs() <= bound)
+    assert not bad.any(), (what, int(bad.sum()), float(((got - ref).abs() / bound)[bad].max()), bad.nonzero()[:4].tolist())
+
+
+def check_norm(x, dy, groups, w, b, off, act):
+    """Forward and gradients against the 64-bit forms; rows outside stay."""
+    d = x.shape[1]
+    dev = (lambda t: None if t is None else t.cuda())
+    xs, ys, wd, bd, od = x.cuda(), dy.cuda(), dev(w), dev(b), dev(off)
+    ref = norm_truth(x, groups, w, b, off, 1e-5, act)
+    r = ref["rows"]
+    out = torch.full_like(xs, 9.0)
+    y, mean, rstd = T.group_norm(xs, groups, wd, bd, off=od, act=act, out=out, stats=True)
+    held = ref["count"] > 0
+    near(mean[held], ref["mean"][held], ref["em"][held], F32, "mean")
+    near(rstd[held], ref["rstd"][held], (ref["trel"] * ref["rstd"])[held], F32, "rstd")
+    assert (mean[~held] == 0).all() and (rstd[~held] == 0).all()
+    near(y[r], ref["y"], ref["ty"], x.dtype, "y")
+    assert (y[:r.start] == 9.0).all() and (y[r.stop:] == 9.0).all()
+    dx, dw, db = T.group_norm_grad(ys, xs, groups, wd, bd, mean, rstd, off=od, act=act)
+    rdx, tdx, rdw, tw, rdb, tb = norm_grad_truth(x, dy, groups, w, b, mean, rstd, off, act, ref)
+    near(dx[r], rdx, tdx, x.dtype, "dx")
+    near(dw, rdw, tw, F32, "dweight")
+    near(db, rdb, tb, F32, "dbias")
+    again = T.group_norm_grad(ys, xs, groups, wd, bd, mean, rstd, off=od, act=act)
+    assert torch.equal(again[0][r], dx[r]) and torch.equal(again[1], dw) and torch.equal(again[2], db)
+
+
+def norm_inputs(m, d, dtype, seed):
+    x = normal((m, d), dtype, seed, 2.0) + normal((d,), dtype, seed + 1)
+    return x, normal((m, d), dtype, seed + 2), normal((d,), F32, seed + 3), normal((d,), F32, seed + 4)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(NORM_ROWS)))
+def test_norm_rows_held_to_their_depth(dtype, case):
+    m, groups, cg = NORM_ROWS[case]
+    note(f"group_norm depth rows {dtype} m={m} groups={groups} cg={cg}")
+    x, dy, w, b = norm_inputs(m, groups * cg, dtype, case)
+    check_norm(x, dy, groups, w, b, None, ["silu", "none", "relu"][case % 3])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(NORM_SEGS)))
+def test_norm_segments_held_to_their_depth(dtype, case):
+    sizes, groups, cg = NORM_SEGS[case]
+    note(f"group_norm depth segments {dtype} segs={len(sizes)} groups={groups} cg={cg}")
+    off = ranges(sizes)
+    x, dy, w, b = norm_inputs(int(off[-1]), groups * cg, dtype, case)
+    check_norm(x, dy, groups, w, b, off, ["none", "relu", "silu"][case % 3])
+
+
+def segment_sizes(count, sizes, long, seed):
+    """count segments of the given sizes, a few long ones among them."""
+    g = torch.Generator().manual_seed(seed)
+    s = torch.tensor(sizes)[torch.randint(0, len(sizes), (count,), generator=g)]
+    s[torch.randperm(count, generator=g)[:len(long)]] = torch.tensor(long, dtype=torch.int64)
+    return s.tolist()
+
+
+MANY = [  # segments, sizes, long ones, groups, channels a group
+    (9_000, [0, 0, 1, 2, 3, 5, 30], [129, 200, 256, 257, 400] * 20, 2, 12),    # a wave a slot, several slots each
+    (9_000, [0, 1, 7, 63, 64, 65], [], 1, 5),
+    (5_000, [0, 1, 2, 5, 9], [300, 1000, 77], 4, 160),                         # four waves a slot
+    (4_300, [0, 1, 1, 2], [90, 65], 1, 2048),                                  # rows wider than a workgroup
+    (24, [200, 130, 90, 65], [], 64, 4),                                       # 1,536 joins
+    (1_023, [130, 90, 200], [], 2, 8),                                         # 2,046 joins of a few units each
+    (3, [1], [70_000, 200_000, 30_000], 2, 8),                                 # units of 128 rows
+    (2, [600_000], [], 1, 8),                                                  # units of 512 rows
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_norm_of_many_and_long_segments(dtype, case):
+    """More slots than workgroups, more joins than 1,024, longer units."""
+    count, sizes, long, groups, cg = MANY[case]
+    off = ranges(segment_sizes(count, sizes, long, case), lead=5)
+    m = int(off[-1]) + 3
+    note(f"group_norm many {dtype} m={m} segs={count} groups={groups} cg={cg}")
+    x, dy, w, b = norm_inputs(m, groups * cg, dtype, case)
+    for t in (x, dy):
+        t[:5], t[m - 3:] = float("nan"), float("nan")
+    check_norm(x, dy, groups, w, b, off, ["relu", "silu", "none"][case % 3])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,groups,cg", [(140_001, 1, 64), (9_001, 1, 2048), (30_011, 40, 5), (1_100_003, 1, 7)])
+def test_norm_of_many_rows(dtype, m, groups, cg):
+    """More rows than the launch has lanes for: each takes several."""
+    note(f"group_norm many rows {dtype} m={m} groups={groups} cg={cg}")
+    x, dy, w, b = norm_inputs(m, groups * cg, dtype, 3)
+    check_norm(x, dy, groups, w, b, None, "silu")
 
 
 # ------------------------------------------------- streams, graphs, refusals --
