@@ -997,18 +997,15 @@ static void rows_launch(const NormArgs& a, int lg, int64_t blocks, bool grad, hi
 }
 template <int DT, int E>
 static void rows_e(const NormArgs& a, const RowPlan& r, int64_t blocks, bool grad, hipStream_t s) {
-    if (r.wide) {  // groups of over 1,024 channels
-        if constexpr (E == 1) return rows_launch<DT, E, 8, true>(a, r.lg, blocks, grad, s);
-        else return rows_launch<DT, E, 8 / E, true>(a, r.lg, blocks, grad, s);
-    }
-    if (r.p == 1) return rows_launch<DT, E, 1, false>(a, r.lg, blocks, grad, s);
-    if constexpr (E <= 8) {
+    // shorter vectors are those of groups under 16 bytes (norm_vec): one a lane
+    if constexpr (E * type_bytes<DT> == 16) {
+        if (r.wide) return rows_launch<DT, E, 8 / E, true>(a, r.lg, blocks, grad, s);  // groups of over 1,024 channels
         if (r.p == 2) return rows_launch<DT, E, 2, false>(a, r.lg, blocks, grad, s);
+        if constexpr (E == 4) {
+            if (r.p == 4) return rows_launch<DT, E, 4, false>(a, r.lg, blocks, grad, s);
+        }
     }
-    if constexpr (E <= 4) {
-        if (r.p == 4) return rows_launch<DT, E, 4, false>(a, r.lg, blocks, grad, s);
-    }
-    if constexpr (E == 1) rows_launch<DT, E, 16, false>(a, r.lg, blocks, grad, s);
+    rows_launch<DT, E, 1, false>(a, r.lg, blocks, grad, s);
 }
 template <int DT>
 static void norm_rows(const NormArgs& a, const RowPlan& r, int64_t blocks, bool grad, hipStream_t s) {
