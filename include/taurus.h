@@ -492,7 +492,8 @@ int taurus_grouped_linear_grad(const void* grad, int64_t grad_stride, const void
  * x: [m][x_stride] of dtype; weight, bias: float[d], or NULL for 1 and 0;
  * act: taurus_activation; out: [m][out_stride] of out_dtype; mean, rstd:
  * float[rows or segments][groups], written for the gradient, or both NULL
- * (a segment without rows gets zeros).  segments is ignored when off is NULL.
+ * (a segment without rows gets zeros).  segments is not used when off is NULL
+ * (it must still not be negative).
  */
 int64_t taurus_group_norm_bytes(int32_t dtype, int64_t m, int64_t d, int64_t groups, int64_t segments,
                                 int32_t by_segment, int32_t grad);
@@ -506,7 +507,7 @@ int taurus_group_norm(const void* x, int32_t dtype, int64_t m, int64_t d, int64_
  * [grad_stride] of dtype, at the mean and rstd the forward call wrote:
  *     dx [m][dx_stride] of dtype, dweight and dbias float[d]; each may be
  * NULL and is then not written.  ReLU passes gradient where its argument,
- * formed exactly from x, mean, rstd, weight and bias, is positive.  Rows
+ * formed from x, mean, rstd, weight and bias in 64 bits, is positive.  Rows
  * outside the segments add nothing to dweight and dbias.
  */
 int taurus_group_norm_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int32_t dtype,

@@ -11,18 +11,18 @@
 // One row at a time is bound by memory: a power-of-two group of lanes holds a
 // group's values in registers, reads them once, and walks the rows with the
 // next row's values already requested (1M bf16 rows of 256 channels, ReLU:
-// 215 us, 4.8 TB/s, the rate of a copy).
+// 219 us, 4.7 TB/s, the rate of a copy).
 //
 // Segments: units of rows that never cross a segment (rowops.hpp); a unit that
 // is a whole segment is finished by its workgroup, from registers where its
 // rows fit them, else from the caches; longer segments leave each unit's
 // statistics in the workspace, k_norm_join combines them in unit order and a
 // second pass over the rows applies them.  One graph of 400K fp32 rows of 128
-// channels: 48 us for the statistics (4.3 TB/s), 13 for the join, 68 for the
+// channels: 47 us for the statistics (4.4 TB/s), 14 for the join, 68 for the
 // second pass (6.0 TB/s, a part of it from the caches).  Many small segments
 // are bound by what a workgroup waits for one after another (its first
-// segment, the rows, the sums): 9,000 graphs of 300K fp16 rows take 93 us,
-// their gradient 113, of which the vector units work 48.
+// segment, the rows, the sums): 9,000 graphs of 300K fp16 rows take 94 us,
+// their gradient 115, of which the vector units work 48.
 //
 // Means and squared deviations are fp32 and never formed as E[x^2] - mu^2:
 // deviations are taken from the mean of the values at hand (a row, or a few
@@ -89,22 +89,23 @@ __device__ inline float act_of(float z, int act) {
     if (act == TAURUS_ACT_SILU) return silu(z);
     return z;
 }
-// The sign of (x - mean) rstd w + b in 64 bits.  The conversions stay where
-// they are: taken out of a loop they hold two registers a value.
-__device__ inline bool open_exactly(float x, float mean, float rstd, float w, float b) {
+// The sign of (x - mean) rstd w + b in 64-bit arithmetic (whose own roundings
+// are within 2^-51 of its terms).  The conversions stay where they are: taken
+// out of a loop they hold two registers a value.
+__device__ inline bool open_in_64(float x, float mean, float rstd, float w, float b) {
     asm volatile("" : "+v"(mean), "+v"(rstd), "+v"(w), "+v"(b));
     return ((double)x - (double)mean) * (double)rstd * (double)w + (double)b > 0.0;
 }
-// dy act'(z).  Which side of ReLU's border z lies on is decided by the sign
-// of z's exact value: where rounding could change it (the four roundings of
-// z are within 2^-21 of its terms) z is formed again in 64 bits.
+// dy act'(z).  Which side of ReLU's border z lies on is decided as 64-bit
+// arithmetic decides it: where rounding could change the sign (the four
+// roundings of z are within 2^-21 of its terms) z is formed again in 64 bits.
 __device__ inline float act_grad(float dy, float x, float mean, float rstd, float hat, float w, float b, int act) {
     if (act == TAURUS_ACT_NONE) return dy;
     const float t = hat * w, z = t + b;
     if (act == TAURUS_ACT_RELU) {
         bool open = z > 0.f;
         if (fabsf(z) <= 0x1p-20f * (fabsf(t) + fabsf(b)))
-            open = open_exactly(x, mean, rstd, w, b);
+            open = open_in_64(x, mean, rstd, w, b);
         return open ? dy : 0.f;
     }
     return dy * silu_slope(z);
@@ -703,7 +704,7 @@ struct GradAt {
             }
             if (near)
 #pragma unroll
-                for (int e = 0; e < E; e++) open[e] = open_exactly(x[e], mu, rs, w[e], b[e]);
+                for (int e = 0; e < E; e++) open[e] = open_in_64(x[e], mu, rs, w[e], b[e]);
 #pragma unroll
             for (int e = 0; e < E; e++) dz[e] = open[e] ? dz[e] : 0.f;
         } else if constexpr (ACT == TAURUS_ACT_SILU) {
@@ -951,9 +952,10 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float* __restrict__
 // graph of 55K rows of 80 fp16 channels: 16 rows 51 us, 64 rows 25); with
 // many segments, most segments in one unit (sixteen times their mean length),
 // unless a unit would then be over 512 KB of fp32 rows, which one workgroup
-// is long at work on (2,282 graphs of 507K rows, 160 bf16 channels: 256 rows
-// 157 us, 512 rows 177, 1,024 rows 230; 1,100 graphs of 55K rows, 256 fp16
-// channels: 256 rows 70, 512 rows 50).
+// is long at work on (2,282 graphs of 507K rows, 160 bf16 channels, SiLU: 256
+// rows 158 us, 512 rows 176, 1,024 rows 230; 1,100 graphs of 55K rows, 256 fp16
+// channels: 256 rows 71, 512 rows 50; 512 rows is what this border takes of
+// either, so that it costs the first some and gains the second more).
 static int norm_lr(int64_t m, int64_t d, int64_t segs) {
     int lr = 10;
     while (lr > 6 && m >> lr < 2048) lr--;
@@ -1077,7 +1079,9 @@ static NormWork norm_work(void* work, int64_t m, int64_t d, int64_t groups, int6
         w.slots = unit_slots(m, segs, w.R);
         // a workgroup finds its first segment by search and leaves a row of
         // channel sums: a gradient over 9,000 graphs of 300K rows of 128 fp16
-        // channels takes 129 us with one slot each, 121 with three
+        // channels (9,292 slots), call after call, takes 141 us with one slot
+        // each, 133 with two, 127 with three, 142 with five (forward: 92,
+        // 101, 99, 117)
         w.per_block = (int)std::max<int64_t>(ceil_div(w.slots, 4096), 1);
         w.blocks = ceil_div(w.slots, w.per_block);
         w.col_rows = w.blocks;

@@ -814,7 +814,10 @@ __global__ __launch_bounds__(RS_THREADS) void k_radix_offsets(uint32_t* __restri
 // Few tiles: one launch instead of those three.  A workgroup takes 16 digits,
 // 16 tile lanes each; every tile's count is replaced by the number of the
 // digit's items in the tiles before it, and the scatter scans the totals.
-// (1M keys and values, two passes: 79 -> 62 us.)
+// (CSR builds of edges in random order: 1M, 256 tiles, 225 -> 166 us, 4.2M,
+// 1,024 tiles, 352 -> 296; gradients of 1M looked-up ids 163 -> 146, of 4.2M
+// 321 -> 313.  Of 2,048 and 4,096 tiles the gradients are slower this way, 551
+// -> 558 and 932 -> 976, and the build of 4,096 tiles, 847 -> 881.)
 constexpr int64_t RADIX_FEW = 1024;
 template <int DBITS>
 __global__ __launch_bounds__(RS_THREADS) void k_radix_columns(uint32_t* __restrict__ hist, int64_t nblocks,

@@ -316,7 +316,8 @@ __device__ inline void grad_clear(const uint32_t* __restrict__ key, int64_t m, c
 
 // The sort of at most GRAD_ONE ids in one workgroup: ids and places pass
 // through LDS eight bits at a time (a stable radix sort as of large arrays,
-// whose launches cost more than the work of so few; 1,001 ids 9 us).
+// whose launches cost more than the work of so few; 2,048 ids of a table of
+// 100K rows, three passes beside its zeros: 18 us).
 constexpr int GRAD_ONE = 4096;
 template <int E>
 __global__ __launch_bounds__(1024) void k_grad_sort_one(const int32_t* __restrict__ ids, int m, GradOut o, int bits,
