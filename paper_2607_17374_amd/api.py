@@ -369,8 +369,9 @@ def _check_norm(norm: Optional[dict]) -> None:
 
 
 def _encode(x: torch.Tensor, encoder: dict, n: int, d_in: Optional[int], stream):
-    """The first layer's input rows [n][d_in]: vertex v's features (x[v], or
-    scale * x[ids[v]]), times its type's weight plus bias, normalised."""
+    """The first layer's input, at least n rows of d_in values: vertex v's
+    features (x[v], or scale * x[ids[v]]), times its type's weight plus bias,
+    normalised."""
     enc = dict(encoder)
     ids, scale, norm = enc.pop("ids", None), enc.pop("scale", 1.0), enc.pop("norm", None)
     off, weight, bias = enc.pop("off", None), enc.pop("weight", None), enc.pop("bias", None)
@@ -380,7 +381,7 @@ def _encode(x: torch.Tensor, encoder: dict, n: int, d_in: Optional[int], stream)
         raise ValueError("the encoder's linear map needs off and weight together")
     _check_norm(norm)
     rows, width = (x.shape[0] if ids is None else ids.numel()), (x.shape[-1] if weight is None else weight.shape[-1])
-    if rows != n or (d_in is not None and width != d_in):
+    if rows < n or (d_in is not None and width != d_in):
         raise ValueError(f"the encoder gives {rows} rows of {width} values; {n} vertices enter the first layer"
                          + (f" with {d_in} values each" if d_in is not None else ""))
     h = x if ids is None else lookup_rows(x, ids, scale, stream=stream)

@@ -213,6 +213,14 @@ def test_model_refuses_an_encoder_of_another_shape(x, encoder, width):
         T.run_layers(4, off, off, torch.zeros(x), [dict(d_in=width)], chunk=4, encoder=encoder)
 
 
+def test_model_takes_an_encoder_with_rows_behind_the_vertices():
+    """Padded ids or rows get past the check of shapes; the layers read n."""
+    off = torch.tensor([0, 4])
+    for x, encoder in (((9, 8), dict(ids=torch.zeros(6, dtype=torch.int32))), ((6, 8), dict(norm=dict(groups=2)))):
+        with pytest.raises(ValueError, match="device tensor"):
+            T.run_layers(4, off, off, torch.zeros(x), [dict(d_in=8)], chunk=4, encoder=encoder)
+
+
 class _FakeRun:
     """run_layers' parts as a log of what they are asked, without a device."""
 
