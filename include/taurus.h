@@ -41,12 +41,21 @@ typedef enum {
 
 typedef enum { TAURUS_F32 = 0, TAURUS_BF16 = 1, TAURUS_F16 = 2 } taurus_dtype;
 
-/* Activations of taurus_group_norm. */
+/* Activations of taurus_group_norm (the first three) and taurus_linear. */
 typedef enum {
     TAURUS_ACT_NONE = 0,
     TAURUS_ACT_RELU = 1, /* max(z, 0), as the layers' (a NaN becomes 0)                  */
-    TAURUS_ACT_SILU = 2  /* z / (1 + exp(-z)), at infinities its limits z and 0          */
+    TAURUS_ACT_SILU = 2, /* z / (1 + exp(-z)), at infinities its limits z and 0          */
+    TAURUS_ACT_GELU = 3, /* z (1 + erf(z / sqrt(2))) / 2, likewise                       */
+    TAURUS_ACT_GELU_TANH = 4 /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2        */
 } taurus_activation;
+
+/* Norms of a row around taurus_residual_norm's sum. */
+typedef enum {
+    TAURUS_NORM_NONE = 0,
+    TAURUS_NORM_LAYER = 1, /* (v - mean) / sqrt(mean square deviation + eps)             */
+    TAURUS_NORM_RMS = 2    /* v / sqrt(mean square + eps)                                */
+} taurus_norm_kind;
 
 /* Eviction policies of a budgeted layer (desc.eviction).  The paper's
  * policy evicts the partial states with the fewest pending messages
@@ -515,6 +524,117 @@ int taurus_group_norm_grad(const void* grad, int64_t grad_stride, const void* x,
                            const float* weight, const float* bias, const float* mean, const float* rstd,
                            int32_t act, void* dx, int64_t dx_stride, float* dweight, float* dbias, void* work,
                            int64_t work_bytes, void* stream);
+
+/*
+ * Linear map of rows with an activation and a residual:
+ *     z[r] = x[r] weight + bias,   out[r] = act(z[r]) + residual[r].
+ * x: [m][x_stride] of dtype, rows of d_in values; weight: [d_in][d_out] of
+ * dtype, contiguous; bias: float[d_out] or NULL; residual: [m]
+ * [residual_stride] of out_dtype, or NULL; act: taurus_activation; out: [m]
+ * [out_stride] of out_dtype; pre: [m][pre_stride] of dtype, receives z for
+ * the gradient, or NULL (out comes from the unrounded z).  1 <= d_in, d_out
+ * <= 2^20.  The contraction of few rows is cut into parts whose fp32 sums wait
+ * in work.
+ */
+int64_t taurus_linear_bytes(int32_t dtype, int64_t m, int64_t d_in, int64_t d_out);
+int taurus_linear(const void* x, int32_t dtype, int64_t m, int64_t d_in, int64_t x_stride, const void* weight,
+                  int64_t d_out, const float* bias, const void* residual, int64_t residual_stride, int32_t act,
+                  void* out, int32_t out_dtype, int64_t out_stride, void* pre, int64_t pre_stride, void* work,
+                  int64_t work_bytes, void* stream);
+
+/*
+ * Gradients of taurus_linear, from grad = d(loss)/d(out), [m][grad_stride] of
+ * dtype, at the z that pre holds (not read where act is TAURUS_ACT_NONE).
+ * With dz = grad act'(z):
+ *     dx      = dz weight^T                 [m][dx_stride] of dtype
+ *     dweight = sum over rows of x[r]^T dz[r]  [d_in][d_out] of dweight_dtype
+ *     dbias   = sum over rows of dz[r]      float[d_out]
+ * Each may be NULL and is then not computed.  The residual's gradient is grad
+ * itself.  For dx and dweight dz is rounded to dtype, as the matrix cores take
+ * it; dbias adds it unrounded.  act'(0) of ReLU is 0.
+ */
+int64_t taurus_linear_grad_bytes(int32_t dtype, int64_t m, int64_t d_in, int64_t d_out, int32_t act);
+int taurus_linear_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int32_t dtype,
+                       int64_t m, int64_t d_in, int64_t d_out, const void* weight, const void* pre,
+                       int64_t pre_stride, int32_t act, void* dx, int64_t dx_stride, void* dweight,
+                       int32_t dweight_dtype, float* dbias, void* work, int64_t work_bytes, void* stream);
+
+/*
+ * Norms after and before a block, with its gate and the residual sum.  With f
+ * the block's output and x the residual stream, rows of d channels (1 <= d <=
+ * 8192),
+ *     p = post(f),   y = x + scale * gate * p,   h = pre(y),
+ * post and pre: taurus_norm_kind over a row, times weight plus bias (float[d]
+ * each, or NULL for 1 and 0).  gate: float[d] for all rows if off is NULL, or
+ * [segments][d], row r of segment s (off[s] <= r < off[s + 1]) taking row s;
+ * NULL: 1 (off then says which rows there are).  segments is not used when off
+ * is NULL.  f, h: [m][stride] of dtype; x, y: of x_dtype, dtype itself or
+ * fp32; h (not written, and may be NULL, if pre is TAURUS_NORM_NONE) comes
+ * from the unrounded y.  stats: 16-byte aligned float[m][4], or NULL: for the
+ * gradient post's mean and (var + eps)^-1/2, then pre's (0 where there is no
+ * norm; the mean of an RMS norm is 0).
+ */
+int taurus_residual_norm(const void* x, int32_t x_dtype, int64_t x_stride, const void* f, int32_t dtype,
+                         int64_t f_stride, int64_t m, int64_t d, float scale, const float* gate, const int64_t* off,
+                         int64_t segments, int32_t post, const float* post_weight, const float* post_bias,
+                         float post_eps, int32_t pre, const float* pre_weight, const float* pre_bias, float pre_eps,
+                         void* y, int64_t y_stride, void* h, int64_t h_stride, float* stats, void* stream);
+
+/*
+ * Gradients of taurus_residual_norm, from grad_y = d(loss)/dy by the ways that
+ * y takes besides h (of y_dtype; NULL: none) and grad_h = d(loss)/dh (of
+ * dtype; with a norm pre only, and then needed), at the y and stats that the
+ * forward call wrote: dx of y_dtype, df of dtype, dgate float of gate's shape,
+ * dpost_weight, dpost_bias, dpre_weight and dpre_bias float[d]; each may be
+ * NULL and is then not written.  A segment without rows gets zeros in dgate;
+ * rows outside the segments add to no sum.
+ */
+int64_t taurus_residual_norm_grad_bytes(int32_t dtype, int64_t m, int64_t d, int64_t segments, int32_t by_segment);
+int taurus_residual_norm_grad(const void* grad_y, int64_t grad_y_stride, const void* grad_h, int64_t grad_h_stride,
+                              const void* y, int32_t y_dtype, int64_t y_stride, const void* f, int32_t dtype,
+                              int64_t f_stride, int64_t m, int64_t d, float scale, const float* gate,
+                              const int64_t* off, int64_t segments, int32_t post, const float* post_weight,
+                              const float* post_bias, int32_t pre, const float* pre_weight, const float* stats,
+                              void* dx, int64_t dx_stride, void* df, int64_t df_stride, float* dgate,
+                              float* dpost_weight, float* dpost_bias, float* dpre_weight, float* dpre_bias,
+                              void* work, int64_t work_bytes, void* stream);
+
+/*
+ * Log probabilities of labels, entropy and the likeliest classes.  With the
+ * scaled logits l = scale * x[r] (scale > 0, finite) over c classes (1 <= c <=
+ * 2^22), M their largest, S = sum of e^(l - M) and log p_j = (l_j - M) - log S,
+ *     logp[r]    = log p_y, y = labels[r]  (0 if y is outside [0, c): -1 pads)
+ *     entropy[r] = -sum over j of p_j log p_j
+ *     stats[r]   = M, log S                float[m][2], for the gradient
+ *     top_ids[r], top_logp[r]              int32, float[m][top]: the `top` (at
+ *                  most 64 and c) classes of the largest logits and their log
+ *                  probabilities, largest first, of equal ones the lower class
+ * logp (with labels, int32[m]), stats and entropy may be NULL.  A logit of -inf
+ * is a masked class, of probability 0 and never an alternative: where fewer
+ * than `top` are left, ids are -1 and log probabilities -inf.  A row of masked
+ * classes only has log probability -inf (of any label in range), entropy 0 and
+ * stats -inf, 0.  A row with a NaN or an infinite l has NaN and ids -1.
+ */
+int64_t taurus_label_log_probs_bytes(int32_t dtype, int64_t m, int64_t c, int32_t top);
+int taurus_label_log_probs(const void* x, int32_t dtype, int64_t m, int64_t c, int64_t x_stride,
+                           const int32_t* labels, float scale, int32_t top, float* logp, float* stats,
+                           float* entropy, float* top_logp, int32_t* top_ids, void* work, int64_t work_bytes,
+                           void* stream);
+
+/*
+ * Gradient of taurus_label_log_probs, from grad_logp = d(loss)/d(logp) (with
+ * labels; both may be NULL) and grad_entropy = d(loss)/d(entropy) (with
+ * entropy; both may be NULL), float[m], at the stats and entropy that the
+ * forward call wrote:
+ *     dx[r][j] = scale * (grad_logp[r] * ([j = y] - p_j)
+ *                         - grad_entropy[r] * p_j * (log p_j + entropy[r])).
+ * dx: [m][dx_stride] of dtype.  A label outside [0, c) adds nothing; a row of
+ * masked classes only has zeros.  The alternatives have no gradient.
+ */
+int taurus_label_log_probs_grad(const void* x, int32_t dtype, int64_t m, int64_t c, int64_t x_stride,
+                                const int32_t* labels, float scale, const float* stats, const float* entropy,
+                                const float* grad_logp, const float* grad_entropy, void* dx, int64_t dx_stride,
+                                void* stream);
 
 /*
  * A plan holds the per-graph structures that layers over one graph and chunk

@@ -10,3 +10,5 @@ from .api import (build_csr, Layer, Plan, hash_u64, run_layers, reorder, reorder
                   permute_rows)
 from .rowops import (lookup_rows, lookup_rows_grad, grouped_linear, grouped_linear_grad, group_norm,  # noqa: F401
                      group_norm_grad)
+from .blockops import (linear, linear_grad, residual_norm, residual_norm_grad, ResidualNormGrad, label_log_probs,  # noqa: F401
+                       label_log_probs_grad, LabelLogProbs)

@@ -17,7 +17,8 @@ OK, E_INVALID, E_OOM, E_DEVICE, E_STATE, E_INCOMPLETE, E_BUDGET = 0, -1, -2, -3,
 F32, BF16, F16 = 0, 1, 2
 SAGE_MEAN, GCN_SYM, GIN_SUM, GAT_ATT, GIN_MLP = 0, 1, 2, 3, 4
 EVICT_PENDING, EVICT_RANDOM, EVICT_FIFO, EVICT_LRU = 0, 1, 2, 3
-ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 NOALLOC_SCRATCH_BYTES, NOALLOC_MAX_EDGES = 32 << 20, 1 << 20
 
 STATUS_NAMES = {OK: "OK", E_INVALID: "E_INVALID", E_OOM: "E_OOM", E_DEVICE: "E_DEVICE",
@@ -121,7 +122,17 @@ for _name, _res, _args in (
         ("taurus_grouped_linear_grad", ctypes.c_int, "plplilllplpplpipplp"),
         ("taurus_group_norm_bytes", ctypes.c_int64, "illllii"),
         ("taurus_group_norm", ctypes.c_int, "pillllplppfipilppplp"),
-        ("taurus_group_norm_grad", ctypes.c_int, "plplilllplppppiplppplp")):
+        ("taurus_group_norm_grad", ctypes.c_int, "plplilllplppppiplppplp"),
+        ("taurus_linear_bytes", ctypes.c_int64, "illl"),
+        ("taurus_linear", ctypes.c_int, "pilllplpplipilplplp"),
+        ("taurus_linear_grad_bytes", ctypes.c_int64, "illli"),
+        ("taurus_linear_grad", ctypes.c_int, "plplilllppliplpipplp"),
+        ("taurus_residual_norm", ctypes.c_int, "pilpilllfpplippfippfplplpp"),
+        ("taurus_residual_norm_grad_bytes", ctypes.c_int64, "illli"),
+        ("taurus_residual_norm_grad", ctypes.c_int, "plplpilpilllfpplippippplplpppppplp"),
+        ("taurus_label_log_probs_bytes", ctypes.c_int64, "illi"),
+        ("taurus_label_log_probs", ctypes.c_int, "pilllpfipppppplp"),
+        ("taurus_label_log_probs_grad", ctypes.c_int, "pilllpfppppplp")):
     SIGNATURES[_name] = (_res, [_ARG[_c] for _c in _args])
 
 _lib = None

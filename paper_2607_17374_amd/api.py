@@ -14,6 +14,7 @@ import numpy as np
 import torch
 
 from . import _native as N
+from .blockops import check_norm_args, label_log_probs, linear, residual_norm
 from .rowops import group_norm, grouped_linear, lookup_rows
 
 _TORCH_DTYPE = {N.F32: torch.float32, N.BF16: torch.bfloat16, N.F16: torch.float16}
@@ -390,9 +391,51 @@ def _encode(x: torch.Tensor, encoder: dict, n: int, d_in: Optional[int], stream)
     return h if norm is None else group_norm(h, stream=stream, **norm)
 
 
+def _check_blocks(layers: list, stream_dtype) -> None:
+    """The layers' norms and residual blocks fit what enters them (stream_dtype:
+    the first layer's input)."""
+    for spec in layers:
+        _check_norm(spec.get("norm"))
+        block = spec.get("residual")
+        out_dtype = _TORCH_DTYPE[spec.get("out_dtype", N.F32)]
+        if block is None:
+            stream_dtype = out_dtype
+            continue
+        unknown = set(block) - {"scale", "gate", "off", "post", "pre"}
+        if unknown:
+            raise ValueError(f"residual does not know {', '.join(sorted(unknown))}")
+        check_norm_args(block.get("post"), "post")
+        check_norm_args(block.get("pre"), "pre")
+        if spec.get("norm") is not None:
+            raise ValueError("a layer has a norm or a residual, whose post is the norm of its output")
+        if spec["d_in"] != spec["d_out"]:
+            raise ValueError(f"a layer of {spec['d_in']} to {spec['d_out']} values has no residual")
+        if stream_dtype not in (out_dtype, torch.float32):
+            raise ValueError(f"the residual stream is {stream_dtype}, the layer's output {out_dtype}")
+
+
+def _answer(h: torch.Tensor, head: dict, stream):
+    """Log probabilities of the classes of rows h."""
+    head = dict(head)
+    maps = list(head.pop("linear", ()))
+    for i, m in enumerate(maps):  # logits in fp32: 16 bits would make equal ones of different
+        h = linear(h, stream=stream, out_dtype=torch.float32 if i + 1 == len(maps) else None, **m)
+    return label_log_probs(h, head.pop("labels", None), stream=stream, **head)
+
+
+def _check_head(head: dict) -> None:
+    unknown = set(head) - {"linear", "labels", "scale", "top", "entropy"}
+    if unknown:
+        raise ValueError(f"head does not know {', '.join(sorted(unknown))}")
+    for m in head.get("linear", ()):
+        unknown = set(m) - {"weight", "bias", "act"}
+        if unknown or "weight" not in m:
+            raise ValueError("head's linear maps have weight, bias and act, got " + ", ".join(sorted(m)))
+
+
 def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Tensor, layers: list,
                *, chunk: int, stream=None, profile: bool = False, outs: Optional[list] = None,
-               encoder: Optional[dict] = None):
+               encoder: Optional[dict] = None, head: Optional[dict] = None):
     """Layer-wise inference: layer l's output is layer l+1's input.
 
     ``layers`` holds dicts with keys agg, d_in, d_out, weight_cat, bias,
@@ -403,31 +446,61 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     layer's input from x: a dict with off, weight and bias (vertices grouped
     by type, one linear map each: grouped_linear's), ids and scale (x is a
     table, vertex v's row scale * x[ids[v]]: lookup_rows') and norm, each
-    optional; offsets must hold every vertex.  Returns (outputs, stats); the
-    outputs are complete."""
+    optional; offsets must hold every vertex.
+
+    A layer's residual makes a block of it: a dict of residual_norm's scale,
+    gate, off, post and pre.  The rows that entered the block before (the first
+    layer's input, or what the layer before put out) are the stream x, the
+    layer's output is f; y = x + scale * gate * post(f) is the layer's output
+    and the stream of the next block, and the next layer takes pre(y) (y
+    without pre).  Offsets must hold every vertex.  The stream has the layers'
+    out_dtype or fp32.
+
+    head answers with classes: a dict of linear (a list of dicts of linear's
+    weight, bias and act, applied one after another to the last layer's rows,
+    after its block's pre; none: the rows are the logits) and
+    label_log_probs' labels, scale, top and entropy, each optional.  Its
+    LabelLogProbs follows the layers' outputs.
+
+    Returns (outputs, stats); the outputs are complete."""
     layers = list(layers)
-    for spec in layers:
-        _check_norm(spec.get("norm"))
+    _check_blocks(layers, x.dtype)
+    if head is not None:
+        head = dict(head, linear=list(head.get("linear", ())))
+        _check_head(head)
     h = x if encoder is None else _encode(x, encoder, n, layers[0]["d_in"] if layers else None, stream)
     results, stats = [], []
+    block, norm, rows = None, None, h[:n]  # rows: the residual stream
     plan = Plan(n, row_off, col_dst, chunk, stream=stream)
     for i, spec in enumerate(layers):
         spec = dict(spec)
-        norm = spec.pop("norm", None)
+        norm, block = spec.pop("norm", None), spec.pop("residual", None)
         shape, dtype = (n, spec["d_out"]), _TORCH_DTYPE[spec.get("out_dtype", N.F32)]
-        result = outs[i] if outs is not None and outs[i] is not None else torch.empty(shape, dtype=dtype,
-                                                                                      device=x.device)
-        out = result if norm is None else torch.empty(shape, dtype=dtype, device=result.device)
+        result = outs[i] if outs is not None and outs[i] is not None else torch.empty(
+            shape, dtype=dtype if block is None else rows.dtype, device=x.device)
+        out = result if norm is None and block is None else torch.empty(shape, dtype=dtype, device=result.device)
         L = Layer(n, row_off, col_dst, out=out, chunk=chunk, stream=stream, profile=profile, plan=plan, **spec)
         L.push_all(h)
         stats.append(L.finalize())
         L.destroy()
         if norm is not None:
             out = group_norm(out, out=result, stream=stream, **norm)
+        h = None
+        if block is not None:
+            out, h = residual_norm(rows, out, out=result, stream=stream, **block)
         results.append(out)
-        h = out
+        rows = out
+        h = out if h is None else h
     if plan is not None:
         plan.destroy()
-    if layers and norm is not None:  # the norm is only enqueued; finalize leaves a layer's rows complete
-        (torch.cuda.current_stream(result.device) if stream is None else stream).synchronize()
+    if head is not None:
+        answer = _answer(h[:n], head, stream)
+        if stream is not None:  # made on that stream, handed to the current one
+            for t in answer:
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream(t.device))
+        results.append(answer)
+    if norm is not None or block is not None or head is not None:
+        # these are only enqueued; finalize leaves a layer's rows complete
+        (torch.cuda.current_stream(h.device) if stream is None else stream).synchronize()
     return results, stats

@@ -1,0 +1,494 @@
+// Linear maps of rows with an activation and a residual in the epilogue, and
+// their gradients, on the matrix cores:
+//     z = x W + b,  out = act(z) + residual
+//     dz = dy act'(z),  dx = dz W^T,  dW = x^T dz,  db = sum over rows of dz
+//
+// Each is one product of tiles (product.hpp) whose epilogue works on the fp32
+// sums in registers, so that nothing but the result goes to memory.  Products
+// with fewer tiles than the chip takes at once are cut along the contraction
+// too: every part leaves fp32 sums in the workspace, and k_linear_join adds
+// them in order and does the epilogue.  With an activation, dz is formed once,
+// rounded to x's type (what the matrix cores take; fp32 stays), by the pass
+// that adds its columns for db before that rounding.
+#include "act.hpp"
+#include "columns.hpp"
+#include "product.hpp"
+
+namespace taurus {
+
+constexpr int64_t LINEAR_WIDTH = (int64_t)1 << 20;
+
+// What becomes of the sums of a product: of forward calls all of it, of
+// gradients the store alone.
+struct Epilogue {
+    const float* bias;     // or null
+    const void* residual;  // of out's type, or null
+    int64_t residual_stride;
+    void* out;
+    int out_dtype;
+    int64_t out_stride;
+    void* pre;  // z in the operands' type, or null
+    int64_t pre_stride;
+};
+// Values c .. c + E - 1 of row r, c + E <= cols.
+template <int DT, int ACT, int E>
+__device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E]) {
+    if (e.bias) {
+        float b[E];
+        load_vec<TAURUS_F32, E>(e.bias, c, b);
+#pragma unroll
+        for (int i = 0; i < E; i++) v[i] += b[i];
+    }
+    if (e.pre) store_vec<DT, E>(e.pre, r * e.pre_stride + c, v);
+#pragma unroll
+    for (int i = 0; i < E; i++) v[i] = activation<ACT>(v[i]);
+    if (e.residual) {
+        float f[E];
+        const int64_t at = r * e.residual_stride + c;
+        if (e.out_dtype == TAURUS_F32) load_vec<TAURUS_F32, E>(e.residual, at, f);
+        else if (e.out_dtype == TAURUS_BF16) load_vec<TAURUS_BF16, E>(e.residual, at, f);
+        else load_vec<TAURUS_F16, E>(e.residual, at, f);
+#pragma unroll
+        for (int i = 0; i < E; i++) v[i] += f[i];
+    }
+    store_as<E>(e.out_dtype, e.out, r * e.out_stride + c, v);
+}
+// four consecutive values of a row of `cols`
+template <int DT, int ACT>
+__device__ inline void finish4(const Epilogue& e, int64_t r, int c, int cols, floatx4 v) {
+    if (c + 4 <= cols) {
+        float f[4] = {v[0], v[1], v[2], v[3]};
+        finish<DT, ACT, 4>(e, r, c, f);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; i++)
+        if (c + i < cols) {
+            float f[1] = {v[i]};
+            finish<DT, ACT, 1>(e, r, c + i, f);
+        }
+}
+
+// A product out [rows][cols] of `depth` terms, of operands `m` (rows of out)
+// and `n` (columns).
+enum { PRODUCT_Y, PRODUCT_DX, PRODUCT_DW };
+struct ProductArgs {
+    const void *m, *n;
+    int64_t ms, ns;  // values between rows of the operands in memory
+    int64_t rows, cols, depth;
+    Epilogue e;
+    float* part;      // parts' sums [splits][rows][cols], or null
+    int64_t per;      // terms of a part, whole stages
+    int64_t row_tiles;
+    int col_tiles, splits;
+};
+template <int KIND, int DT, int TM, int TN, bool AL>
+struct ProductOps {
+    typedef std::conditional_t<KIND == PRODUCT_DW, Across<DT, TM, AL>, Along<DT, TM, AL>> OpM;
+    typedef std::conditional_t<KIND == PRODUCT_DX, Along<DT, TN, AL>, Across<DT, TN, AL>> OpN;
+};
+template <int KIND, int DT, int TM, int TN, bool AL, int ACT>
+struct ProductTiles {
+    typedef ProductOps<KIND, DT, TM, TN, AL> Ops;
+    typedef typename Ops::OpM OpM;
+    typedef typename Ops::OpN OpN;
+    static constexpr int WN = TN / 64, WM = 4 / WN, MI = TM / WM / 16, NI = 4;
+    const ProductArgs& a;
+    int64_t b;
+    int m0, n0;
+    int64_t r0 = 0, next_r0 = 0;
+    int64_t c0 = 0, next_c0 = 0;
+    int split = 0, next_split = 0;
+    __device__ ProductTiles(const ProductArgs& a_, int m0_, int n0_) : a(a_), b(blockIdx.x), m0(m0_), n0(n0_) {}
+    __device__ bool enter(int) { return false; }
+    __device__ bool seek(OpM& om, OpN& on, int& depth) {
+        r0 = next_r0;
+        c0 = next_c0;
+        split = next_split;
+        const int64_t slots = a.row_tiles * a.splits;
+        if (b >= slots * a.col_tiles) return false;
+        int64_t slot;
+        int tile;
+        place_of(b, slots, a.col_tiles, slot, tile);
+        b += gridDim.x;
+        next_split = (int)(slot / a.row_tiles);
+        next_r0 = (slot - next_split * a.row_tiles) * TM;
+        next_c0 = (int64_t)tile * TN;
+        const int64_t k0 = next_split * a.per;
+        depth = (int)(next_split + 1 < a.splits ? a.per : a.depth - k0);
+        if constexpr (KIND == PRODUCT_DW) om = OpM{a.m, k0 * a.ms, a.ms, depth, (int)a.rows, (int)next_r0};
+        else om = OpM{a.m, next_r0 * a.ms + k0, a.ms, (int)min((int64_t)TM, a.rows - next_r0), depth};
+        if constexpr (KIND == PRODUCT_DX)
+            on = OpN{a.n, next_c0 * a.ns + k0, a.ns, (int)min((int64_t)TN, a.cols - next_c0), depth};
+        else on = OpN{a.n, k0 * a.ns, a.ns, depth, (int)a.cols, (int)next_c0};
+        return true;
+    }
+    __device__ void done(floatx4 (&acc)[MI][NI], typename Tile<DT>::sums_t (&)[1]) {
+        const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < MI; i++) {
+            const int64_t r = r0 + m0 + 16 * i + li;
+            if (r >= a.rows) continue;
+#pragma unroll
+            for (int j = 0; j < NI; j++) {
+                const int c = (int)c0 + n0 + 16 * j + 4 * lk;
+                if (a.part) put4(a.part, TAURUS_F32, (split * a.rows + r) * a.cols, c, (int)a.cols, acc[i][j]);
+                else finish4<DT, ACT>(a.e, r, c, (int)a.cols, acc[i][j]);
+            }
+        }
+    }
+};
+template <int KIND, int DT, int TM, int TN, bool AL, int ACT>
+__global__ __launch_bounds__(256, TM * TN == 128 * 128 ? 3 : 4) void k_linear(ProductArgs a) {
+    typedef ProductTiles<KIND, DT, TM, TN, AL, ACT> T;
+    __shared__ __align__(16) char lds[T::OpM::BYTES + T::OpN::BYTES];
+    const int wave = threadIdx.x >> 6, m0 = wave / T::WN * T::MI * 16, n0 = wave % T::WN * 64;
+    T tiles(a, m0, n0);
+    stream_tiles<DT, typename T::OpM, typename T::OpN, T::MI, T::NI, false>(tiles, lds, m0, n0);
+}
+
+// The parts' sums added in order, then the epilogue: a thread four values.
+template <int DT, int ACT>
+__global__ __launch_bounds__(256) void k_linear_join(ProductArgs a) {
+    const int64_t vecs = (a.cols + 3) / 4, n = a.rows * vecs;
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / vecs;
+        const int c = (int)(i - r * vecs) * 4;
+        floatx4 v{0.f, 0.f, 0.f, 0.f};
+        const float* p = a.part + r * a.cols + c;
+        const int64_t step = a.rows * a.cols;
+        if (c + 4 <= a.cols) {
+            for (int s = 0; s < a.splits; s++) {
+                float f[4];
+                load_vec<TAURUS_F32, 4>(p, s * step, f);
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] += f[e];
+            }
+        } else {
+            for (int s = 0; s < a.splits; s++)
+#pragma unroll
+                for (int e = 0; e < 3; e++)
+                    if (c + e < a.cols) v[e] += p[s * step + e];
+        }
+        finish4<DT, ACT>(a.e, r, c, (int)a.cols, v);
+    }
+}
+
+// ---------------------------------------------------------- dz and its sums --
+
+// dz = dy act'(z), stored in the operands' type, and each workgroup's sums of
+// its rows' columns, before that rounding.  A workgroup takes 64 vectors of
+// columns and every fourth row of its range a thread; without dz (no
+// activation) the sums alone.
+struct SlopeArgs {
+    const void *dy, *z;
+    int64_t ds, zs, rows, per;  // per: rows of a workgroup
+    int cols;
+    void* dz;
+    int64_t dzs;
+    float* part;  // [row blocks][cols], or null
+};
+template <int DT, int E, int ACT>
+__global__ __launch_bounds__(256) void k_linear_slope(SlopeArgs a) {
+    __shared__ float sums[3][64 * E];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t w = (int64_t)blockIdx.y * 64 + lane;
+    const bool in = w * E < a.cols;
+    const int64_t c = vec_at<E>(in ? w : 0, a.cols);
+    const int64_t r0 = (int64_t)blockIdx.x * a.per, r1 = min(r0 + a.per, a.rows);
+    float f[E] = {};
+    if (in)
+        for (int64_t r = r0 + wave; r < r1; r += 4) {
+            float g[E];
+            load_vec<DT, E>(a.dy, r * a.ds + c, g);
+            if constexpr (ACT != TAURUS_ACT_NONE) {
+                float z[E];
+                load_vec<DT, E>(a.z, r * a.zs + c, z);
+#pragma unroll
+                for (int e = 0; e < E; e++)
+                    g[e] = ACT == TAURUS_ACT_RELU ? (z[e] > 0.f ? g[e] : 0.f) : g[e] * activation_slope<ACT>(z[e]);
+                store_vec<DT, E>(a.dz, r * a.dzs + c, g);
+            }
+#pragma unroll
+            for (int e = 0; e < E; e++) f[e] += g[e];
+        }
+    if (!a.part) return;
+    if (wave > 0)
+#pragma unroll
+        for (int e = 0; e < E; e++) sums[wave - 1][e * 64 + lane] = f[e];
+    __syncthreads();
+    if (wave == 0 && in) {
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            for (int i = 0; i < 3; i++) f[e] += sums[i][e * 64 + lane];
+        const int again = vec_again<E>(w, a.cols);
+#pragma unroll
+        for (int e = 0; e < E; e++)
+            if (e >= again) a.part[(int64_t)blockIdx.x * a.cols + c + e] = f[e];
+    }
+}
+
+// ---------------------------------------------------------------- launches --
+
+// Rows whose memory the stages read through buffer resources.
+static bool whole_words(int dtype, const void* p, int64_t cols, int64_t stride) {
+    const int64_t sz = dtype_size(dtype);
+    return cols * sz >= 16 && cols * sz % 4 == 0 && stride * sz % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 4 == 0;
+}
+
+// How a product is cut.
+struct ProductPlan {
+    int tm, tn;
+    int64_t row_tiles, per;
+    int col_tiles, splits;
+    int64_t part;  // fp32 sums of the workspace
+};
+static ProductPlan product_plan(int dtype, bool al, int64_t rows, int64_t cols, int64_t depth) {
+    ProductPlan p{};
+    const int stage = dtype == TAURUS_F32 ? 32 : 64;
+    p.tm = 128;
+    p.tn = dtype == TAURUS_F32 || !al || cols <= 64 ? 64 : 128;
+    if (ceil_div(rows, p.tm) * ceil_div(cols, p.tn) < 512) p.tn = 64;
+    p.row_tiles = ceil_div(rows, p.tm);
+    p.col_tiles = (int)ceil_div(cols, p.tn);
+    const int64_t tiles = p.row_tiles * p.col_tiles, resident = 256 * (p.tm * p.tn == 128 * 128 ? 3 : 4);
+    const int64_t stages = ceil_div(depth, stage);
+    // as many parts as fill the chip, of at least four stages
+    int64_t splits = std::max<int64_t>(1, std::min(resident / std::max<int64_t>(tiles, 1), stages / 4));
+    const int64_t each = ceil_div(stages, splits);
+    p.splits = (int)ceil_div(std::max<int64_t>(stages, 1), std::max<int64_t>(each, 1));
+    p.per = std::max<int64_t>(each, 1) * stage;
+    // a part is at least a piece long: less is left to the part before it
+    if (p.splits > 1 && depth - (p.splits - 1) * p.per < 8) p.splits--;
+    p.part = p.splits > 1 ? p.splits * rows * cols : 0;
+    return p;
+}
+template <int KIND, int DT, int TM, int TN, bool AL, int ACT>
+static void product_launch(const ProductArgs& a, hipStream_t s) {
+    const int64_t tiles = a.row_tiles * a.col_tiles * a.splits;
+    const int64_t resident = (int64_t)(TM * TN == 128 * 128 ? 3 : 4) * compute_units();
+    k_linear<KIND, DT, TM, TN, AL, ACT><<<(unsigned)std::min(tiles, resident), 256, 0, s>>>(a);
+    TAURUS_CHECK_LAUNCH();
+}
+template <int KIND, int DT, int ACT>
+static void product_tiles(const ProductArgs& a, const ProductPlan& p, bool al, hipStream_t s) {
+    if (!al) return product_launch<KIND, DT, 128, 64, false, ACT>(a, s);
+    if constexpr (DT != TAURUS_F32) {
+        if (p.tn == 128) return product_launch<KIND, DT, 128, 128, true, ACT>(a, s);
+    }
+    product_launch<KIND, DT, 128, 64, true, ACT>(a, s);
+}
+template <int KIND, int DT>
+static void product(ProductArgs a, float* part, int act, hipStream_t s) {
+    const int64_t m_width = KIND == PRODUCT_DW ? a.rows : a.depth, n_width = KIND == PRODUCT_DX ? a.depth : a.cols;
+    const bool al = whole_words(DT, a.m, m_width, a.ms) && whole_words(DT, a.n, n_width, a.ns);
+    const ProductPlan p = product_plan(DT, al, a.rows, a.cols, a.depth);
+    a.part = p.splits > 1 ? part : nullptr;
+    a.per = p.per;
+    a.row_tiles = p.row_tiles;
+    a.col_tiles = p.col_tiles;
+    a.splits = p.splits;
+    if (p.splits > 1) {  // the sums alone: one kernel for all activations
+        product_tiles<KIND, DT, TAURUS_ACT_NONE>(a, p, al, s);
+        const unsigned grid = grid_for(std::min<int64_t>(ceil_div(a.rows * ceil_div(a.cols, 4), 256), 4096));
+        if constexpr (KIND == PRODUCT_Y) {
+            with_act(act, [&](auto c) { k_linear_join<DT, decltype(c)::value><<<grid, 256, 0, s>>>(a); });
+        } else {
+            k_linear_join<DT, TAURUS_ACT_NONE><<<grid, 256, 0, s>>>(a);
+        }
+        TAURUS_CHECK_LAUNCH();
+    } else if constexpr (KIND == PRODUCT_Y) {
+        with_act(act, [&](auto c) { product_tiles<KIND, DT, decltype(c)::value>(a, p, al, s); });
+    } else {
+        product_tiles<KIND, DT, TAURUS_ACT_NONE>(a, p, al, s);
+    }
+}
+template <int KIND>
+static void product_of(int dtype, const ProductArgs& a, float* part, int act, hipStream_t s) {
+    if (dtype == TAURUS_F32) product<KIND, TAURUS_F32>(a, part, act, s);
+    else if (dtype == TAURUS_BF16) product<KIND, TAURUS_BF16>(a, part, act, s);
+    else product<KIND, TAURUS_F16>(a, part, act, s);
+}
+
+// Row blocks of the slope pass, each of which leaves a row of column sums: as
+// many as give the chip eight workgroups a compute unit, of at least 32 rows.
+static int64_t slope_blocks(int dtype, int64_t rows, int64_t cols) {
+    const int64_t wide = ceil_div(cols, 64 * (dtype == TAURUS_F32 ? 4 : 8));
+    return std::max<int64_t>(1, std::min(ceil_div(rows, 32), ceil_div(2048, wide)));
+}
+struct LinearWork {
+    float *part = nullptr, *sums = nullptr;
+    void* dz = nullptr;
+    int64_t dz_stride = 0, blocks = 0, bytes = 0;
+};
+// whether rows are whole words is known at the call: room for both
+static int64_t part_values(int dtype, int64_t rows, int64_t cols, int64_t depth) {
+    return std::max(product_plan(dtype, true, rows, cols, depth).part, product_plan(dtype, false, rows, cols, depth).part);
+}
+static int64_t forward_bytes(int dtype, int64_t m, int64_t d_in, int64_t d_out) {
+    Carve c;
+    c.take<float>(part_values(dtype, m, d_out, d_in));
+    return c.bytes();
+}
+static LinearWork gradient_work(void* work, int dtype, int64_t m, int64_t d_in, int64_t d_out, int act) {
+    LinearWork w;
+    Carve c(work);
+    w.blocks = slope_blocks(dtype, m, d_out);
+    w.sums = c.take<float>(w.blocks * d_out);
+    if (act != TAURUS_ACT_NONE) {
+        w.dz_stride = (d_out + 7) & ~(int64_t)7;
+        w.dz = c.take<char>(m * w.dz_stride * dtype_size(dtype));
+    }
+    w.part = c.take<float>(std::max(part_values(dtype, m, d_in, d_out), part_values(dtype, d_in, d_out, m)));
+    w.bytes = c.bytes();
+    return w;
+}
+static void check_linear(int dtype, int64_t m, int64_t d_in, int64_t d_out, int act) {
+    check_dtype(dtype, "x");
+    check_count(m, 0, ROWS_MAX, "the number of rows");
+    check_count(d_in, 1, LINEAR_WIDTH, "the input width");
+    check_count(d_out, 1, LINEAR_WIDTH, "the output width");
+    if (!known_act(act)) fail(TAURUS_E_INVALID, "activation %d is none of TAURUS_ACT_*", act);
+}
+
+}  // namespace taurus
+
+// ------------------------------------------------------------------ C ABI --
+
+using namespace taurus;
+
+extern "C" {
+
+int64_t taurus_linear_bytes(int32_t dtype, int64_t m, int64_t d_in, int64_t d_out) {
+    int64_t bytes = 0;
+    const int rc = guarded_call([&] {
+        check_linear(dtype, m, d_in, d_out, TAURUS_ACT_NONE);
+        bytes = forward_bytes(dtype, m, d_in, d_out);
+        return (int)TAURUS_OK;
+    });
+    return rc == TAURUS_OK ? bytes : rc;
+}
+
+int taurus_linear(const void* x, int32_t dtype, int64_t m, int64_t d_in, int64_t x_stride, const void* weight,
+                  int64_t d_out, const float* bias, const void* residual, int64_t residual_stride, int32_t act,
+                  void* out, int32_t out_dtype, int64_t out_stride, void* pre, int64_t pre_stride, void* work,
+                  int64_t work_bytes, void* stream) {
+    return guarded_call([&] {
+        check_linear(dtype, m, d_in, d_out, act);
+        check_dtype(out_dtype, "out");
+        if (m == 0) return (int)TAURUS_OK;
+        check_rows(x, dtype, m, d_in, x_stride, "x");
+        check_ptr(weight, dtype_size(dtype), "weight");
+        if (bias) check_ptr(bias, 4, "bias");
+        if (residual) check_rows(residual, out_dtype, m, d_out, residual_stride, "residual");
+        check_rows(out, out_dtype, m, d_out, out_stride, "out");
+        if (pre) check_rows(pre, dtype, m, d_out, pre_stride, "pre");
+        check_work(work, work_bytes, forward_bytes(dtype, m, d_in, d_out), "taurus_linear");
+        ProductArgs a{};
+        a.m = x;
+        a.n = weight;
+        a.ms = x_stride;
+        a.ns = d_out;
+        a.rows = m;
+        a.cols = d_out;
+        a.depth = d_in;
+        a.e = Epilogue{bias, residual, residual_stride, out, out_dtype, out_stride, pre, pre_stride};
+        product_of<PRODUCT_Y>(dtype, a, static_cast<float*>(work), act, static_cast<hipStream_t>(stream));
+        return (int)TAURUS_OK;
+    });
+}
+
+int64_t taurus_linear_grad_bytes(int32_t dtype, int64_t m, int64_t d_in, int64_t d_out, int32_t act) {
+    int64_t bytes = 0;
+    const int rc = guarded_call([&] {
+        check_linear(dtype, m, d_in, d_out, act);
+        bytes = gradient_work(nullptr, dtype, m, d_in, d_out, act).bytes;
+        return (int)TAURUS_OK;
+    });
+    return rc == TAURUS_OK ? bytes : rc;
+}
+
+int taurus_linear_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int32_t dtype,
+                       int64_t m, int64_t d_in, int64_t d_out, const void* weight, const void* pre,
+                       int64_t pre_stride, int32_t act, void* dx, int64_t dx_stride, void* dweight,
+                       int32_t dweight_dtype, float* dbias, void* work, int64_t work_bytes, void* stream) {
+    return guarded_call([&] {
+        check_linear(dtype, m, d_in, d_out, act);
+        if (dweight) check_dtype(dweight_dtype, "dweight");
+        if (!dx && !dweight && !dbias) return (int)TAURUS_OK;
+        check_rows(grad, dtype, m, d_out, grad_stride, "grad");
+        if (act != TAURUS_ACT_NONE) check_rows(pre, dtype, m, d_out, pre_stride, "pre");
+        if (dx) {
+            check_rows(dx, dtype, m, d_in, dx_stride, "dx");
+            if (m > 0) check_ptr(weight, dtype_size(dtype), "weight");
+        }
+        if (dweight) {
+            check_rows(x, dtype, m, d_in, x_stride, "x");
+            check_ptr(dweight, dtype_size(dweight_dtype), "dweight");
+        }
+        if (dbias) check_ptr(dbias, 4, "dbias");
+        check_work(work, work_bytes, gradient_work(nullptr, dtype, m, d_in, d_out, act).bytes, "taurus_linear_grad");
+        const LinearWork w = gradient_work(work, dtype, m, d_in, d_out, act);
+        auto s = static_cast<hipStream_t>(stream);
+        const void* dz = grad;
+        int64_t dzs = grad_stride;
+        if (act != TAURUS_ACT_NONE || dbias) {
+            SlopeArgs a{grad, pre, grad_stride, pre_stride, m, ceil_div(m, w.blocks), (int)d_out, w.dz, w.dz_stride,
+                        dbias ? w.sums : nullptr};
+            auto go = [&](auto dt, auto e) {
+                constexpr int DT = decltype(dt)::value, E = decltype(e)::value;
+                const dim3 grid((unsigned)w.blocks, (unsigned)ceil_div(d_out, 64 * E));
+                with_act(act, [&](auto c) { k_linear_slope<DT, E, decltype(c)::value><<<grid, 256, 0, s>>>(a); });
+                TAURUS_CHECK_LAUNCH();
+            };
+            auto go_e = [&](auto dt) {
+                if (d_out >= 8 && dtype != TAURUS_F32) go(dt, std::integral_constant<int, 8>{});
+                else if (d_out >= 4) go(dt, std::integral_constant<int, 4>{});
+                else go(dt, std::integral_constant<int, 1>{});
+            };
+            if (dtype == TAURUS_F32) go_e(std::integral_constant<int, TAURUS_F32>{});
+            else if (dtype == TAURUS_BF16) go_e(std::integral_constant<int, TAURUS_BF16>{});
+            else go_e(std::integral_constant<int, TAURUS_F16>{});
+            if (dbias) {
+                ColumnSums j{};
+                j.add(w.sums, d_out, w.blocks, d_out, dbias);
+                join_columns(j, s);
+            }
+            if (act != TAURUS_ACT_NONE) {
+                dz = w.dz;
+                dzs = w.dz_stride;
+            }
+        }
+        if (dx && m > 0) {
+            ProductArgs a{};
+            a.m = dz;
+            a.n = weight;
+            a.ms = dzs;
+            a.ns = d_out;
+            a.rows = m;
+            a.cols = d_in;
+            a.depth = d_out;
+            a.e.out = dx;
+            a.e.out_dtype = dtype;
+            a.e.out_stride = dx_stride;
+            product_of<PRODUCT_DX>(dtype, a, w.part, TAURUS_ACT_NONE, s);
+        }
+        if (dweight) {
+            ProductArgs a{};
+            a.m = x;
+            a.n = dz;
+            a.ms = x_stride;
+            a.ns = dzs;
+            a.rows = d_in;
+            a.cols = d_out;
+            a.depth = m;
+            a.e.out = dweight;
+            a.e.out_dtype = dweight_dtype;
+            a.e.out_stride = d_out;
+            product_of<PRODUCT_DW>(dtype, a, w.part, TAURUS_ACT_NONE, s);
+        }
+        return (int)TAURUS_OK;
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,660 @@
+// Norms after and before a block, fused with its gate and the residual sum, and
+// their gradients.  With f the block's output and x the residual stream, rows of
+// d channels,
+//     p = post(f),  y = x + scale gate p,  h = pre(y),
+// post and pre being nothing, layer norm or RMS norm with weight and bias,
+//     n(v) = (v - mu) rstd w + b,   rstd = (mean of (v - mu)^2 + eps)^-1/2,
+// (mu = 0 for RMS), and gate one row of d or a row for each segment of rows.
+// With vhat = (v - mu) rstd and g = dn w, the gradient of a norm is
+//     dv = rstd (g - mean of g [layer] - vhat mean of (g vhat)),
+// so that with dh and dy' = d(loss)/dy from elsewhere
+//     dy = dy' + pre's gradient of dh,  dx = dy,  dp = scale gate dy,
+//     df = post's gradient of dp,  dgate = scale sum of dy p,
+// and the weights' gradients are sums over rows of dn vhat and dn.
+//
+// One pass each way, bound by memory: a row lies in the registers of a team, up
+// to eight values a lane (lanes of a wave up to 512 channels, then 4, 8 or 16
+// waves), with the channels' parameters beside it, and statistics are two
+// passes over registers.  The gradient's column sums stay in registers too; a
+// workgroup leaves one row of them, k_join_columns adds those.  Rows of a
+// segment are cut into units (rowops.hpp), whose gate gradients are written at
+// once, or joined where a segment has several.
+#include "columns.hpp"
+#include "lanes.hpp"
+#include "rowops.hpp"
+
+namespace taurus {
+
+constexpr int64_t RESNORM_MOST = 8192;
+
+struct NormOf {
+    int kind;
+    const float *w, *b;
+    float eps;
+};
+struct ResnormArgs {
+    const void *x, *f;
+    int64_t m, xs, fs;
+    int d;
+    float scale;
+    const float* gate;
+    const int64_t* off;
+    int64_t segs;
+    NormOf post, pre;
+    void *y, *h;
+    int64_t ys, hs;
+    float4* stats;
+    // gradient
+    const void *dh, *dy;
+    int64_t dhs, dys;
+    void *dx, *df;
+    int64_t dxs, dfs;
+    float *dgate, *gate_part, *cols;  // cols [workgroups][sums][d]
+    int sums;                         // column sums a workgroup leaves
+    int at_gate, at_post_w, at_post_b, at_pre_w, at_pre_b;  // which of them, or -1
+    // work
+    int R;
+    int64_t slots, per;  // a worker takes `per` consecutive slots
+};
+
+// The units of a worker's slots, one after another (rowops.hpp: range g owns
+// the slots from off[g] / R + g on).  Without offsets all rows are one range.
+struct UnitWalk {
+    const ResnormArgs& a;
+    int64_t k, end, g, b, e;
+    __device__ UnitWalk(const ResnormArgs& a_, int64_t worker) : a(a_) {
+        k = worker * a.per;
+        end = min(k + a.per, a.slots);
+        g = 0;
+        b = 0;
+        e = a.m;
+        if (a.off && k < end) {
+            g = wave_last(a.segs, [&](int64_t p) { return (int64_t)(off_at(a.off, p, a.m) / (uint32_t)a.R) + p <= k; });
+            bounds();
+        }
+    }
+    __device__ void bounds() {
+        b = off_at(a.off, g, a.m);
+        e = max((int64_t)off_at(a.off, g + 1, a.m), b);
+    }
+    // the next unit: its rows (none for slots without), whether it is its
+    // segment's first, and whether the segment's only one
+    __device__ bool next(int64_t& r0, int64_t& r1, bool& first, bool& only, int64_t& seg) {
+        if (k >= end) return false;
+        if (a.off && g + 1 < a.segs && k >= e / a.R + g + 1) {
+            g++;
+            bounds();
+        }
+        const int64_t slot = k - (b / a.R + g);
+        k++;
+        seg = g;
+        first = slot == 0;
+        only = e - b <= a.R;
+        r0 = min(b + max(slot, (int64_t)0) * a.R, e);
+        r1 = slot < 0 ? r0 : min(r0 + a.R, e);
+        return true;
+    }
+};
+
+// Sums over a team: 2^lg lanes, or all waves of the workgroup (WAVES > 0)
+// through LDS; the same order everywhere.
+template <int WAVES>
+struct Team {
+    int lg;
+    float2* room;  // [2][WAVES]
+    int turn = 0;
+    __device__ Team(int lg_, float2* room_) : lg(lg_), room(room_) {}
+    __device__ float2 sum(float2 v) {
+        if constexpr (WAVES == 0) {
+            return {lanes_sum(v.x, lg), lanes_sum(v.y, lg)};
+        } else {
+            v = {lanes_sum(v.x, 6), lanes_sum(v.y, 6)};
+            float2* at = room + turn * WAVES;  // the other half is still being read
+            turn ^= 1;
+            if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
+            __syncthreads();
+            float2 s{0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < WAVES; i++) {
+                s.x += at[i].x;
+                s.y += at[i].y;
+            }
+            return s;
+        }
+    }
+};
+
+// What a lane holds of a row: P vectors of E values.
+template <int E, int P>
+struct Cols {
+    int64_t at[P];  // first column
+    bool in[P];     // whether there is one
+    int again[P];   // its values that the vector before has too
+    __device__ Cols(int lane, int lanes, int d) {
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int64_t w = lane + (int64_t)p * lanes;
+            in[p] = w * E < d;
+            at[p] = in[p] ? vec_at<E>(w, d) : 0;
+            again[p] = in[p] ? vec_again<E>(w, d) : E;
+        }
+    }
+    __device__ bool counts(int p, int e) const { return e >= again[p]; }
+};
+template <int E, int P>
+struct Values {
+    float v[P][E];
+    template <int DT>
+    __device__ void load(const void* base, int64_t row_at, const Cols<E, P>& c) {
+#pragma unroll
+        for (int p = 0; p < P; p++) load_vec<DT, E>(base, row_at + c.at[p], v[p]);
+    }
+    template <int DT>
+    __device__ void store(void* base, int64_t row_at, const Cols<E, P>& c, bool write) const {
+#pragma unroll
+        for (int p = 0; p < P; p++)
+            if (write && c.in[p]) store_vec<DT, E>(base, row_at + c.at[p], v[p]);
+    }
+    __device__ void parameter(const float* base, float otherwise, const Cols<E, P>& c) {
+        if (base) {
+            load<TAURUS_F32>(base, 0, c);
+        } else {
+#pragma unroll
+            for (int p = 0; p < P; p++)
+#pragma unroll
+                for (int e = 0; e < E; e++) v[p][e] = otherwise;
+        }
+    }
+    __device__ void zero() { parameter(nullptr, 0.f, Cols<E, P>(0, 1, 1)); }
+};
+#define EACH                      \
+    _Pragma("unroll") for (int p = 0; p < P; p++) _Pragma("unroll") for (int e = 0; e < E; e++)
+
+// mean and rstd of a row, for a team
+template <int WAVES, int E, int P>
+__device__ inline float2 moments(Team<WAVES>& team, const Values<E, P>& x, const Cols<E, P>& c, int kind, float eps,
+                                 float inv_d) {
+    float mean = 0.f;
+    if (kind == TAURUS_NORM_LAYER) {
+        float s = 0.f;
+        EACH s += c.counts(p, e) ? x.v[p][e] : 0.f;
+        mean = team.sum({s, 0.f}).x * inv_d;
+    }
+    float q = 0.f;
+    EACH {
+        const float dev = c.counts(p, e) ? x.v[p][e] - mean : 0.f;
+        q = __builtin_fmaf(dev, dev, q);
+    }
+    const float var = team.sum({q, 0.f}).x * inv_d;
+    return {mean, 1.f / sqrtf(var + eps)};
+}
+
+template <int WAVES>
+struct Workers {
+    static constexpr int THREADS = WAVES ? WAVES * 64 : 256;
+    // workers of a workgroup: its waves, or itself
+    static constexpr int PER_BLOCK = WAVES ? 1 : 4;
+};
+
+// FT the block's type, ST the stream's
+template <int FT, int ST, int E, int P, int WAVES>
+__global__ __launch_bounds__(Workers<WAVES>::THREADS) void k_resnorm(ResnormArgs a, int lg) {
+    __shared__ float2 room[2 * (WAVES ? WAVES : 1)];
+    const int lanes = WAVES ? WAVES * 64 : 1 << lg, lane = WAVES ? threadIdx.x : threadIdx.x & (lanes - 1);
+    const int team_at = WAVES ? 0 : (threadIdx.x & 63) >> lg, teams = WAVES ? 1 : 64 >> lg;
+    Team<WAVES> team(lg, room);
+    const Cols<E, P> c(lane, lanes, a.d);
+    const float inv_d = 1.f / (float)a.d;
+    Values<E, P> w1, b1, w2, b2, gate;
+    w1.parameter(a.post.w, 1.f, c);
+    b1.parameter(a.post.b, 0.f, c);
+    w2.parameter(a.pre.w, 1.f, c);
+    b2.parameter(a.pre.b, 0.f, c);
+    gate.parameter(a.off ? nullptr : a.gate, 1.f, c);
+    EACH gate.v[p][e] *= a.scale;
+    UnitWalk walk(a, WAVES ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
+    int64_t r0, r1, seg, gate_of = -1;
+    bool first, only;
+    while (walk.next(r0, r1, first, only, seg)) {
+        if (a.off && a.gate && seg != gate_of && r0 < r1) {
+            gate_of = seg;
+            gate.template load<TAURUS_F32>(a.gate, seg * a.d, c);
+            EACH gate.v[p][e] *= a.scale;
+        }
+        for (int64_t at = r0; at < r1; at += teams) {
+            const bool in = at + team_at < r1;
+            const int64_t r = in ? at + team_at : r1 - 1;
+            Values<E, P> f, y;
+            f.template load<FT>(a.f, r * a.fs, c);
+            y.template load<ST>(a.x, r * a.xs, c);
+            float2 s1{0.f, 0.f}, s2{0.f, 0.f};
+            if (a.post.kind != TAURUS_NORM_NONE) {
+                s1 = moments(team, f, c, a.post.kind, a.post.eps, inv_d);
+                EACH f.v[p][e] = (f.v[p][e] - s1.x) * s1.y * w1.v[p][e] + b1.v[p][e];
+            }
+            EACH y.v[p][e] = __builtin_fmaf(gate.v[p][e], f.v[p][e], y.v[p][e]);
+            y.template store<ST>(a.y, r * a.ys, c, in);
+            if (a.pre.kind != TAURUS_NORM_NONE) {
+                s2 = moments(team, y, c, a.pre.kind, a.pre.eps, inv_d);
+                EACH y.v[p][e] = (y.v[p][e] - s2.x) * s2.y * w2.v[p][e] + b2.v[p][e];
+                y.template store<FT>(a.h, r * a.hs, c, in);
+            }
+            if (a.stats && in && lane == 0) a.stats[r] = make_float4(s1.x, s1.y, s2.x, s2.y);
+        }
+    }
+}
+
+// A worker's column sums of one kind: its teams' in order, into the
+// workgroup's row (`waves` workers a workgroup).
+template <int E, int P, int WAVES>
+__device__ inline void put_sums(float* lds, const Values<E, P>& v, const Cols<E, P>& c, int d, int lg, float* out) {
+    if constexpr (WAVES > 0) {
+        EACH if (c.counts(p, e)) out[c.at[p] + e] = v.v[p][e];
+    } else {
+        const int team = threadIdx.x >> lg, teams = 256 >> lg;
+        EACH if (c.counts(p, e)) lds[team * d + c.at[p] + e] = v.v[p][e];
+        __syncthreads();
+        for (int i = threadIdx.x; i < d; i += 256) {
+            float s = 0.f;
+            for (int t = 0; t < teams; t++) s += lds[t * d + i];
+            out[i] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// HOLD: the channels' parameters stay in registers
+template <int FT, int ST, int E, int P, int WAVES, bool HOLD>
+__global__ __launch_bounds__(Workers<WAVES>::THREADS) void k_resnorm_grad(ResnormArgs a, int lg) {
+    __shared__ float2 room[2 * (WAVES ? WAVES : 1)];
+    extern __shared__ float lds[];
+    const int lanes = WAVES ? WAVES * 64 : 1 << lg, lane = WAVES ? threadIdx.x : threadIdx.x & (lanes - 1);
+    const int team_at = WAVES ? 0 : (threadIdx.x & 63) >> lg, teams = WAVES ? 1 : 64 >> lg;
+    Team<WAVES> team(lg, room);
+    const Cols<E, P> c(lane, lanes, a.d);
+    const float inv_d = 1.f / (float)a.d;
+    const bool post = a.post.kind != TAURUS_NORM_NONE, pre = a.pre.kind != TAURUS_NORM_NONE;
+    const bool centre1 = a.post.kind == TAURUS_NORM_LAYER, centre2 = a.pre.kind == TAURUS_NORM_LAYER;
+    Values<E, P> w1, b1, w2, gate, to_gate, to_w1, to_b1, to_w2, to_b2;
+    if constexpr (HOLD) {
+        w1.parameter(a.post.w, 1.f, c);
+        b1.parameter(a.post.b, 0.f, c);
+        w2.parameter(a.pre.w, 1.f, c);
+        gate.parameter(a.off ? nullptr : a.gate, 1.f, c);
+    }
+    to_gate.zero();
+    to_w1.zero();
+    to_b1.zero();
+    to_w2.zero();
+    to_b2.zero();
+    UnitWalk walk(a, WAVES ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
+    int64_t r0, r1, seg, gate_of = -1;
+    bool first, only;
+    while (walk.next(r0, r1, first, only, seg)) {
+        if constexpr (HOLD)
+            if (a.off && a.gate && seg != gate_of && r0 < r1) {
+                gate_of = seg;
+                gate.template load<TAURUS_F32>(a.gate, seg * a.d, c);
+            }
+        for (int64_t at = r0; at < r1; at += teams) {
+            const bool in = at + team_at < r1;
+            const int64_t r = in ? at + team_at : r1 - 1;
+            Values<E, P> f, y, dy, dh;
+            float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (post || pre) st = a.stats[r];
+            f.template load<FT>(a.f, r * a.fs, c);
+            if (pre) {
+                y.template load<ST>(a.y, r * a.ys, c);
+                dh.template load<FT>(a.dh, r * a.dhs, c);
+            }
+            if (a.dy) dy.template load<ST>(a.dy, r * a.dys, c);
+            else dy.zero();
+            if (pre) {
+                if constexpr (!HOLD) w2.parameter(a.pre.w, 1.f, c);
+                float2 s{0.f, 0.f};
+                EACH {
+                    const float hat = (y.v[p][e] - st.z) * st.w, d = dh.v[p][e], g = d * w2.v[p][e];
+                    y.v[p][e] = hat;
+                    dh.v[p][e] = g;
+                    if (c.counts(p, e)) {
+                        s.x += g;
+                        s.y += g * hat;
+                    }
+                    if (in) {
+                        to_w2.v[p][e] += d * hat;
+                        to_b2.v[p][e] += d;
+                    }
+                }
+                s = team.sum(s);
+                const float m1 = centre2 ? s.x * inv_d : 0.f, m2 = s.y * inv_d;
+                EACH dy.v[p][e] += st.w * (dh.v[p][e] - m1 - y.v[p][e] * m2);
+            }
+            dy.template store<ST>(a.dx, r * a.dxs, c, in && a.dx);
+            if constexpr (!HOLD) {
+                w1.parameter(a.post.w, 1.f, c);
+                b1.parameter(a.post.b, 0.f, c);
+                gate.parameter(a.gate ? a.gate + (a.off ? seg * a.d : 0) : nullptr, 1.f, c);
+            }
+            float2 s{0.f, 0.f};
+            EACH {
+                const float hat = post ? (f.v[p][e] - st.x) * st.y : f.v[p][e];
+                const float n = hat * w1.v[p][e] + b1.v[p][e], d = dy.v[p][e] * a.scale;
+                const float dp = d * gate.v[p][e], g = dp * w1.v[p][e];
+                f.v[p][e] = hat;
+                dy.v[p][e] = g;
+                if (c.counts(p, e)) {
+                    s.x += g;
+                    s.y += g * hat;
+                }
+                if (in) {
+                    to_gate.v[p][e] += d * n;
+                    to_w1.v[p][e] += dp * hat;
+                    to_b1.v[p][e] += dp;
+                }
+            }
+            if (a.df) {
+                if (post) {
+                    s = team.sum(s);
+                    const float m1 = centre1 ? s.x * inv_d : 0.f, m2 = s.y * inv_d;
+                    EACH dy.v[p][e] = st.y * (dy.v[p][e] - m1 - f.v[p][e] * m2);
+                }
+                dy.template store<FT>(a.df, r * a.dfs, c, in);
+            }
+        }
+        if (a.off && a.dgate && (r0 < r1 || (only && first))) {  // the unit's gate gradient: its teams' sums
+            float* out = only ? a.dgate + seg * a.d : a.gate_part + unit_place(r0, first ? 0 : 1, a.R) * a.d;
+            EACH {
+                float v = to_gate.v[p][e];
+                if constexpr (WAVES == 0)  // lanes of the same column in the wave's teams
+                    for (int o = lanes; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+                if (team_at == 0 && c.counts(p, e)) out[c.at[p] + e] = v;
+                to_gate.v[p][e] = 0.f;
+            }
+        }
+    }
+    float* out = a.cols + (int64_t)blockIdx.x * a.sums * a.d;
+    if (a.at_gate >= 0) put_sums<E, P, WAVES>(lds, to_gate, c, a.d, lg, out + a.at_gate * a.d);
+    if (a.at_post_w >= 0) put_sums<E, P, WAVES>(lds, to_w1, c, a.d, lg, out + a.at_post_w * a.d);
+    if (a.at_post_b >= 0) put_sums<E, P, WAVES>(lds, to_b1, c, a.d, lg, out + a.at_post_b * a.d);
+    if (a.at_pre_w >= 0) put_sums<E, P, WAVES>(lds, to_w2, c, a.d, lg, out + a.at_pre_w * a.d);
+    if (a.at_pre_b >= 0) put_sums<E, P, WAVES>(lds, to_b2, c, a.d, lg, out + a.at_pre_b * a.d);
+}
+
+// Segments of several units: their gate gradients added in row order, a
+// workgroup 256 columns of one.
+__global__ __launch_bounds__(256) void k_resnorm_gates(ResnormArgs a, int64_t longs, int chunks) {
+    for (int64_t i = blockIdx.x; i < longs * chunks; i += gridDim.x) {
+        const Long t = wave_long(a.off, a.segs, a.m, a.R, i / chunks);
+        const int64_t c = i % chunks * 256 + threadIdx.x;
+        if (!t.found || c >= a.d) continue;
+        float s = 0.f;
+        for (int64_t u = 0; u < t.units; u++) s += a.gate_part[unit_place(t.begin + u * a.R, u ? 1 : 0, a.R) * a.d + c];
+        a.dgate[t.g * a.d + c] = s;
+    }
+}
+
+// ---------------------------------------------------------------- launches --
+
+struct ResnormPlan {
+    int e, p, lg, waves;
+    int R;
+    int64_t slots, per, blocks, places;
+};
+static ResnormPlan resnorm_plan(int dtype, int64_t m, int64_t d, int64_t segs, bool by_segment, bool grad) {
+    ResnormPlan p{};
+    const int e = vec_width(dtype == TAURUS_F32 ? 4 : 8, d);
+    p.e = e >= 4 ? e : 1;
+    const int64_t vecs = ceil_div(d, p.e);
+    const int most = p.e == 1 ? 1 : 8 / p.e;  // eight values a lane
+    p.p = 1;
+    while (p.p < most && vecs > 8 * p.p) p.p *= 2;
+    while (p.lg < 6 && vecs > (int64_t)p.p << p.lg) p.lg++;
+    if (vecs > (int64_t)p.p << p.lg) {
+        p.waves = 4;
+        while (vecs > (int64_t)p.p * 64 * p.waves) p.waves *= 2;
+        if (grad && p.waves == 16) {  // sums of sixteen values a lane instead
+            p.waves = 8;
+            p.p *= 2;
+        }
+    }
+    const int64_t teams = p.waves ? 1 : 64 >> p.lg, per_block = p.waves ? 1 : 4;
+    // workers that the chip holds at once, of at least four rows a team
+    const int64_t resident = p.waves ? 256 * 16 / p.waves : 256 * 16;
+    const int64_t workers = std::max<int64_t>(1, std::min(resident, ceil_div(m, teams * (grad ? 4 : 1))));
+    if (by_segment) {
+        p.R = (int)std::max<int64_t>(32, ceil_div(m, 4 * workers));
+        p.slots = segs > 0 ? unit_slots(m, segs, p.R) : 0;
+    } else {
+        p.R = (int)std::max<int64_t>(ceil_div(m, workers), 1);
+        p.slots = ceil_div(m, p.R);
+    }
+    p.per = std::max<int64_t>(1, ceil_div(p.slots, workers));
+    p.blocks = std::max<int64_t>(1, ceil_div(ceil_div(p.slots, p.per), per_block));
+    p.places = by_segment && m > p.R ? unit_places(m, p.R) : 0;
+    return p;
+}
+struct ResnormWork {
+    float *cols = nullptr, *gates = nullptr;
+    int64_t bytes = 0;
+};
+static ResnormWork resnorm_work(void* work, const ResnormPlan& p, int64_t d) {
+    ResnormWork w;
+    Carve c(work);
+    w.cols = c.take<float>(p.blocks * ColumnSums::MOST * d);
+    w.gates = c.take<float>(p.places * d);
+    w.bytes = c.bytes();
+    return w;
+}
+template <int FT, int ST, int E, int P, int WAVES>
+static void resnorm_launch(const ResnormArgs& a, const ResnormPlan& p, bool grad, hipStream_t s) {
+    constexpr int THREADS = Workers<WAVES>::THREADS;
+    if (!grad) {
+        if constexpr (E * P <= 8) k_resnorm<FT, ST, E, P, WAVES><<<(unsigned)p.blocks, THREADS, 0, s>>>(a, p.lg);
+    } else if constexpr (WAVES != 16) {
+        const size_t lds = WAVES ? 0 : (size_t)(256 >> p.lg) * a.d * 4;
+        k_resnorm_grad<FT, ST, E, P, WAVES, E * P <= 8><<<(unsigned)p.blocks, THREADS, lds, s>>>(a, p.lg);
+    }
+    TAURUS_CHECK_LAUNCH();
+}
+template <int FT, int ST, int E, int P>
+static void resnorm_waves(const ResnormArgs& a, const ResnormPlan& p, bool grad, hipStream_t s) {
+    if constexpr (E * P > 8) return resnorm_launch<FT, ST, E, P, 8>(a, p, grad, s);  // the gradient of the longest rows
+    else {
+        if (!p.waves) return resnorm_launch<FT, ST, E, P, 0>(a, p, grad, s);
+        if constexpr (E * P == 8) {
+            if (p.waves == 4) resnorm_launch<FT, ST, E, P, 4>(a, p, grad, s);
+            else if (p.waves == 8) resnorm_launch<FT, ST, E, P, 8>(a, p, grad, s);
+            else resnorm_launch<FT, ST, E, P, 16>(a, p, grad, s);
+        }
+    }
+}
+template <int FT, int ST>
+static void resnorm_types(const ResnormArgs& a, const ResnormPlan& p, bool grad, hipStream_t s) {
+    if constexpr (FT != TAURUS_F32) {
+        if (p.e == 8) {
+            if (p.p == 1) resnorm_waves<FT, ST, 8, 1>(a, p, grad, s);
+            else resnorm_waves<FT, ST, 8, 2>(a, p, grad, s);
+            return;
+        }
+    }
+    if (p.e == 1) return resnorm_waves<FT, ST, 1, 1>(a, p, grad, s);
+    if (p.p == 1) return resnorm_waves<FT, ST, 4, 1>(a, p, grad, s);
+    if constexpr (FT == TAURUS_F32) {
+        if (p.p == 2) resnorm_waves<FT, ST, 4, 2>(a, p, grad, s);
+        else resnorm_waves<FT, ST, 4, 4>(a, p, grad, s);
+    }
+}
+static void resnorm(const ResnormArgs& a, const ResnormPlan& p, int dtype, int stream_dtype, bool grad, hipStream_t s) {
+    if (dtype == TAURUS_F32) resnorm_types<TAURUS_F32, TAURUS_F32>(a, p, grad, s);
+    else if (dtype == TAURUS_BF16) {
+        if (stream_dtype == TAURUS_F32) resnorm_types<TAURUS_BF16, TAURUS_F32>(a, p, grad, s);
+        else resnorm_types<TAURUS_BF16, TAURUS_BF16>(a, p, grad, s);
+    } else {
+        if (stream_dtype == TAURUS_F32) resnorm_types<TAURUS_F16, TAURUS_F32>(a, p, grad, s);
+        else resnorm_types<TAURUS_F16, TAURUS_F16>(a, p, grad, s);
+    }
+}
+static void check_resnorm(int dtype, int stream_dtype, int64_t m, int64_t d, const int64_t* off, int64_t segs,
+                          const float* gate) {
+    check_dtype(dtype, "f");
+    check_dtype(stream_dtype, "x");
+    if (stream_dtype != dtype && stream_dtype != TAURUS_F32)
+        fail(TAURUS_E_INVALID, "x has f's type or fp32, not type %d with %d", stream_dtype, dtype);
+    check_count(m, 0, ROWS_MAX, "the number of rows");
+    check_count(d, 1, RESNORM_MOST, "the number of channels");
+    if (off) {
+        check_count(segs, 0, ROWS_MAX, "the number of segments");
+        check_ptr(off, 8, "off");
+    }
+    if (gate) check_ptr(gate, 4, "gate");
+}
+static NormOf norm_of(int kind, const float* w, const float* b, float eps, const char* what) {
+    if (kind != TAURUS_NORM_NONE && kind != TAURUS_NORM_LAYER && kind != TAURUS_NORM_RMS)
+        fail(TAURUS_E_INVALID, "%s: norm %d is none of TAURUS_NORM_*", what, kind);
+    if (kind == TAURUS_NORM_NONE) return NormOf{kind, nullptr, nullptr, 0.f};
+    if (!(eps >= 0.f) || eps == INFINITY) fail(TAURUS_E_INVALID, "%s: eps %g is not in [0, inf)", what, (double)eps);
+    if (w) check_ptr(w, 4, what);
+    if (b) check_ptr(b, 4, what);
+    return NormOf{kind, w, b, eps};
+}
+static int64_t resnorm_bytes(int dtype, int64_t m, int64_t d, int64_t segs, bool by_segment) {
+    return resnorm_work(nullptr, resnorm_plan(dtype, m, d, segs, by_segment, true), d).bytes;
+}
+
+}  // namespace taurus
+
+// ------------------------------------------------------------------ C ABI --
+
+using namespace taurus;
+
+extern "C" {
+
+int taurus_residual_norm(const void* x, int32_t x_dtype, int64_t x_stride, const void* f, int32_t dtype,
+                         int64_t f_stride, int64_t m, int64_t d, float scale, const float* gate, const int64_t* off,
+                         int64_t segments, int32_t post, const float* post_weight, const float* post_bias,
+                         float post_eps, int32_t pre, const float* pre_weight, const float* pre_bias, float pre_eps,
+                         void* y, int64_t y_stride, void* h, int64_t h_stride, float* stats, void* stream) {
+    return guarded_call([&] {
+        check_resnorm(dtype, x_dtype, m, d, off, segments, gate);
+        ResnormArgs a{};
+        a.post = norm_of(post, post_weight, post_bias, post_eps, "post");
+        a.pre = norm_of(pre, pre_weight, pre_bias, pre_eps, "pre");
+        if (m == 0 || (off && segments == 0)) return (int)TAURUS_OK;
+        check_rows(x, x_dtype, m, d, x_stride, "x");
+        check_rows(f, dtype, m, d, f_stride, "f");
+        check_rows(y, x_dtype, m, d, y_stride, "y");
+        if (pre != TAURUS_NORM_NONE) check_rows(h, dtype, m, d, h_stride, "h");
+        if (stats) check_ptr(stats, 16, "stats");
+        const ResnormPlan p = resnorm_plan(dtype, m, d, segments, off != nullptr, false);
+        a.x = x;
+        a.f = f;
+        a.m = m;
+        a.xs = x_stride;
+        a.fs = f_stride;
+        a.d = (int)d;
+        a.scale = scale;
+        a.gate = gate;
+        a.off = off;
+        a.segs = segments;
+        a.y = y;
+        a.h = h;
+        a.ys = y_stride;
+        a.hs = h_stride;
+        a.stats = reinterpret_cast<float4*>(stats);
+        a.R = p.R;
+        a.slots = p.slots;
+        a.per = p.per;
+        resnorm(a, p, dtype, x_dtype, false, static_cast<hipStream_t>(stream));
+        return (int)TAURUS_OK;
+    });
+}
+
+int64_t taurus_residual_norm_grad_bytes(int32_t dtype, int64_t m, int64_t d, int64_t segments, int32_t by_segment) {
+    int64_t bytes = 0;
+    const int rc = guarded_call([&] {
+        check_resnorm(dtype, TAURUS_F32, m, d, nullptr, 0, nullptr);
+        if (by_segment) check_count(segments, 0, ROWS_MAX, "the number of segments");
+        bytes = resnorm_bytes(dtype, m, d, segments, by_segment != 0);
+        return (int)TAURUS_OK;
+    });
+    return rc == TAURUS_OK ? bytes : rc;
+}
+
+int taurus_residual_norm_grad(const void* grad_y, int64_t grad_y_stride, const void* grad_h, int64_t grad_h_stride,
+                              const void* y, int32_t y_dtype, int64_t y_stride, const void* f, int32_t dtype,
+                              int64_t f_stride, int64_t m, int64_t d, float scale, const float* gate,
+                              const int64_t* off, int64_t segments, int32_t post, const float* post_weight,
+                              const float* post_bias, int32_t pre, const float* pre_weight, const float* stats,
+                              void* dx, int64_t dx_stride, void* df, int64_t df_stride, float* dgate,
+                              float* dpost_weight, float* dpost_bias, float* dpre_weight, float* dpre_bias,
+                              void* work, int64_t work_bytes, void* stream) {
+    return guarded_call([&] {
+        check_resnorm(dtype, y_dtype, m, d, off, segments, gate);
+        ResnormArgs a{};
+        a.post = norm_of(post, post_weight, post_bias, 0.f, "post");
+        a.pre = norm_of(pre, pre_weight, nullptr, 0.f, "pre");
+        const bool has_post = post != TAURUS_NORM_NONE, has_pre = pre != TAURUS_NORM_NONE;
+        if ((dpost_weight || dpost_bias) && !has_post) fail(TAURUS_E_INVALID, "gradients of a norm after the block that there is not");
+        if ((dpre_weight || dpre_bias) && !has_pre) fail(TAURUS_E_INVALID, "gradients of a norm before the block that there is not");
+        if (dgate && !gate) fail(TAURUS_E_INVALID, "the gradient of a gate that there is not");
+        if (grad_h && !has_pre) fail(TAURUS_E_INVALID, "a gradient of h, which there is not");
+        if (grad_y) check_rows(grad_y, y_dtype, m, d, grad_y_stride, "grad_y");
+        check_rows(f, dtype, m, d, f_stride, "f");
+        if (has_pre) {
+            check_rows(grad_h, dtype, m, d, grad_h_stride, "grad_h");
+            check_rows(y, y_dtype, m, d, y_stride, "y");
+        }
+        if ((has_post || has_pre) && m > 0) check_ptr(stats, 16, "stats");
+        if (dx) check_rows(dx, y_dtype, m, d, dx_stride, "dx");
+        if (df) check_rows(df, dtype, m, d, df_stride, "df");
+        if (dgate) check_ptr(dgate, 4, "dgate");
+        for (float* p : {dpost_weight, dpost_bias, dpre_weight, dpre_bias})
+            if (p) check_ptr(p, 4, "the gradient of a norm's weight or bias");
+        check_work(work, work_bytes, resnorm_bytes(dtype, m, d, segments, off != nullptr), "taurus_residual_norm_grad");
+        const ResnormPlan p = resnorm_plan(dtype, m, d, segments, off != nullptr, true);
+        const ResnormWork w = resnorm_work(work, p, d);
+        a.f = f;
+        a.m = m;
+        a.fs = f_stride;
+        a.d = (int)d;
+        a.scale = scale;
+        a.gate = gate;
+        a.off = off;
+        a.segs = segments;
+        a.y = const_cast<void*>(y);
+        a.ys = y_stride;
+        a.stats = reinterpret_cast<float4*>(const_cast<float*>(stats));
+        a.dh = grad_h;
+        a.dhs = grad_h_stride;
+        a.dy = grad_y;
+        a.dys = grad_y_stride;
+        a.dx = dx;
+        a.dxs = dx_stride;
+        a.df = df;
+        a.dfs = df_stride;
+        a.dgate = off ? dgate : nullptr;
+        a.gate_part = w.gates;
+        a.cols = w.cols;
+        a.R = p.R;
+        a.slots = p.slots;
+        a.per = p.per;
+        float* const outs[] = {off ? nullptr : dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias};
+        int* const places[] = {&a.at_gate, &a.at_post_w, &a.at_post_b, &a.at_pre_w, &a.at_pre_b};
+        ColumnSums j{};
+        for (int i = 0; i < ColumnSums::MOST; i++) *places[i] = outs[i] ? a.sums++ : -1;
+        for (int i = 0; i < ColumnSums::MOST; i++)
+            if (outs[i]) j.add(w.cols + *places[i] * d, a.sums * d, p.blocks, d, outs[i]);
+        auto s = static_cast<hipStream_t>(stream);
+        resnorm(a, p, dtype, y_dtype, true, s);
+        if (a.dgate && p.places) {
+            const int64_t longs = long_count(m, segments, p.R);
+            const int chunks = (int)ceil_div(d, 256);
+            k_resnorm_gates<<<grid_for(longs * chunks), 256, 0, s>>>(a, longs, chunks);
+            TAURUS_CHECK_LAUNCH();
+        }
+        join_columns(j, s);
+        return (int)TAURUS_OK;
+    });
+}
+
+}  // extern "C"
