@@ -10,78 +10,11 @@
 // them in order and does the epilogue.  With an activation, dz is formed once,
 // rounded to x's type (what the matrix cores take; fp32 stays), by the pass
 // that adds its columns for db before that rounding.
-#include "act.hpp"
 #include "columns.hpp"
-#include "product.hpp"
+#include "linear.hpp"
 
 namespace taurus {
 
-constexpr int64_t LINEAR_WIDTH = (int64_t)1 << 20;
-
-// What becomes of the sums of a product: of forward calls all of it, of
-// gradients the store alone.
-struct Epilogue {
-    const float* bias;     // or null
-    const void* residual;  // of out's type, or null
-    int64_t residual_stride;
-    void* out;
-    int out_dtype;
-    int64_t out_stride;
-    void* pre;  // z in the operands' type, or null
-    int64_t pre_stride;
-};
-// Values c .. c + E - 1 of row r, c + E <= cols.
-template <int DT, int ACT, int E>
-__device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E]) {
-    if (e.bias) {
-        float b[E];
-        load_vec<TAURUS_F32, E>(e.bias, c, b);
-#pragma unroll
-        for (int i = 0; i < E; i++) v[i] += b[i];
-    }
-    if (e.pre) store_vec<DT, E>(e.pre, r * e.pre_stride + c, v);
-#pragma unroll
-    for (int i = 0; i < E; i++) v[i] = activation<ACT>(v[i]);
-    if (e.residual) {
-        float f[E];
-        const int64_t at = r * e.residual_stride + c;
-        if (e.out_dtype == TAURUS_F32) load_vec<TAURUS_F32, E>(e.residual, at, f);
-        else if (e.out_dtype == TAURUS_BF16) load_vec<TAURUS_BF16, E>(e.residual, at, f);
-        else load_vec<TAURUS_F16, E>(e.residual, at, f);
-#pragma unroll
-        for (int i = 0; i < E; i++) v[i] += f[i];
-    }
-    store_as<E>(e.out_dtype, e.out, r * e.out_stride + c, v);
-}
-// four consecutive values of a row of `cols`
-template <int DT, int ACT>
-__device__ inline void finish4(const Epilogue& e, int64_t r, int c, int cols, floatx4 v) {
-    if (c + 4 <= cols) {
-        float f[4] = {v[0], v[1], v[2], v[3]};
-        finish<DT, ACT, 4>(e, r, c, f);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 3; i++)
-        if (c + i < cols) {
-            float f[1] = {v[i]};
-            finish<DT, ACT, 1>(e, r, c + i, f);
-        }
-}
-
-// A product out [rows][cols] of `depth` terms, of operands `m` (rows of out)
-// and `n` (columns).
-enum { PRODUCT_Y, PRODUCT_DX, PRODUCT_DW };
-struct ProductArgs {
-    const void *m, *n;
-    int64_t ms, ns;  // values between rows of the operands in memory
-    int64_t rows, cols, depth;
-    Epilogue e;
-    float* part;      // parts' sums [splits][rows][cols], or null
-    int64_t per;      // terms of a part, whole stages
-    int64_t row_tiles;
-    int col_tiles, splits;
-};
 template <int KIND, int DT, int TM, int TN, bool AL>
 struct ProductOps {
     typedef std::conditional_t<KIND == PRODUCT_DW, Across<DT, TM, AL>, Along<DT, TM, AL>> OpM;
@@ -280,6 +213,7 @@ static void product_tiles(const ProductArgs& a, const ProductPlan& p, bool al, h
 }
 template <int KIND, int DT>
 static void product(ProductArgs a, float* part, int act, hipStream_t s) {
+    if (wide_takes(KIND, DT, a)) return wide_product(KIND, DT, a, part, act, s);
     const int64_t m_width = KIND == PRODUCT_DW ? a.rows : a.depth, n_width = KIND == PRODUCT_DX ? a.depth : a.cols;
     const bool al = whole_words(DT, a.m, m_width, a.ms) && whole_words(DT, a.n, n_width, a.ns);
     const ProductPlan p = product_plan(DT, al, a.rows, a.cols, a.depth);
@@ -323,7 +257,8 @@ struct LinearWork {
 };
 // whether rows are whole words is known at the call: room for both
 static int64_t part_values(int dtype, int64_t rows, int64_t cols, int64_t depth) {
-    return std::max(product_plan(dtype, true, rows, cols, depth).part, product_plan(dtype, false, rows, cols, depth).part);
+    return std::max(std::max(product_plan(dtype, true, rows, cols, depth).part, product_plan(dtype, false, rows, cols, depth).part),
+                    wide_part(rows, cols, depth));
 }
 static int64_t forward_bytes(int dtype, int64_t m, int64_t d_in, int64_t d_out) {
     Carve c;

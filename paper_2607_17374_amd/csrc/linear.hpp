@@ -1,0 +1,132 @@
+// What the products of the linear maps share (linear.hip, linear_wide.hip):
+// their arguments and what becomes of their sums.
+#pragma once
+
+#include "act.hpp"
+#include "product.hpp"
+
+namespace taurus {
+
+constexpr int64_t LINEAR_WIDTH = (int64_t)1 << 20;
+
+// What becomes of the sums of a product: of forward calls all of it, of
+// gradients the store alone.
+struct Epilogue {
+    const float* bias;     // or null
+    const void* residual;  // of out's type, or null
+    int64_t residual_stride;
+    void* out;
+    int out_dtype;
+    int64_t out_stride;
+    void* pre;  // z in the operands' type, or null
+    int64_t pre_stride;
+};
+// Values c .. c + E - 1 of row r, c + E <= cols.
+template <int DT, int ACT, int E>
+__device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E]) {
+    if (e.bias) {
+        float b[E];
+        load_vec<TAURUS_F32, E>(e.bias, c, b);
+#pragma unroll
+        for (int i = 0; i < E; i++) v[i] += b[i];
+    }
+    if (e.pre) store_vec<DT, E>(e.pre, r * e.pre_stride + c, v);
+#pragma unroll
+    for (int i = 0; i < E; i++) v[i] = activation<ACT>(v[i]);
+    if (e.residual) {
+        float f[E];
+        const int64_t at = r * e.residual_stride + c;
+        if (e.out_dtype == TAURUS_F32) load_vec<TAURUS_F32, E>(e.residual, at, f);
+        else if (e.out_dtype == TAURUS_BF16) load_vec<TAURUS_BF16, E>(e.residual, at, f);
+        else load_vec<TAURUS_F16, E>(e.residual, at, f);
+#pragma unroll
+        for (int i = 0; i < E; i++) v[i] += f[i];
+    }
+    store_as<E>(e.out_dtype, e.out, r * e.out_stride + c, v);
+}
+// four consecutive values of a row of `cols`
+template <int DT, int ACT>
+__device__ inline void finish4(const Epilogue& e, int64_t r, int c, int cols, floatx4 v) {
+    if (c + 4 <= cols) {
+        float f[4] = {v[0], v[1], v[2], v[3]};
+        finish<DT, ACT, 4>(e, r, c, f);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; i++)
+        if (c + i < cols) {
+            float f[1] = {v[i]};
+            finish<DT, ACT, 1>(e, r, c + i, f);
+        }
+}
+
+// Two blocks of 16 columns of row r, values c + 4 lk of each in v and w, for
+// columns in whole eights; `in`: whether there is the row.  All lanes take part
+// (put_pair16).
+template <int DT, int ACT>
+__device__ inline void finish_pair(const Epilogue& e, int64_t r, int c, int cols, bool in, floatx4 v, floatx4 w) {
+    const int at = c + 4 * ((threadIdx.x & 63) >> 4);
+    const bool has_v = at < cols, has_w = at + 16 < cols;
+    auto add = [&](floatx4& x, const float (&f)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[i] += f[i];
+    };
+    if (e.bias) {
+        float f[4];
+        if (has_v) {
+            load_vec<TAURUS_F32, 4>(e.bias, at, f);
+            add(v, f);
+        }
+        if (has_w) {
+            load_vec<TAURUS_F32, 4>(e.bias, at + 16, f);
+            add(w, f);
+        }
+    }
+    if (e.pre) put_pair16<DT>(e.pre, r * e.pre_stride, c, cols, in, v, w);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        v[i] = activation<ACT>(v[i]);
+        w[i] = activation<ACT>(w[i]);
+    }
+    if (e.residual) {
+        auto take = [&](int col, floatx4& x) {
+            float f[4];
+            const int64_t from = r * e.residual_stride + col;
+            if (e.out_dtype == TAURUS_F32) load_vec<TAURUS_F32, 4>(e.residual, from, f);
+            else if (e.out_dtype == TAURUS_BF16) load_vec<TAURUS_BF16, 4>(e.residual, from, f);
+            else load_vec<TAURUS_F16, 4>(e.residual, from, f);
+            add(x, f);
+        };
+        if (in && has_v) take(at, v);
+        if (in && has_w) take(at + 16, w);
+    }
+    const int64_t row = r * e.out_stride;
+    if (e.out_dtype == TAURUS_BF16) put_pair16<TAURUS_BF16>(e.out, row, c, cols, in, v, w);
+    else if (e.out_dtype == TAURUS_F16) put_pair16<TAURUS_F16>(e.out, row, c, cols, in, v, w);
+    else if (in) {
+        put4(e.out, TAURUS_F32, row, at, cols, v);
+        put4(e.out, TAURUS_F32, row, at + 16, cols, w);
+    }
+}
+
+// A product out [rows][cols] of `depth` terms, of operands `m` (rows of out)
+// and `n` (columns).
+enum { PRODUCT_Y, PRODUCT_DX, PRODUCT_DW };
+struct ProductArgs {
+    const void *m, *n;
+    int64_t ms, ns;  // values between rows of the operands in memory
+    int64_t rows, cols, depth;
+    Epilogue e;
+    float* part;      // parts' sums [splits][rows][cols], or null
+    int64_t per;      // terms of a part, whole stages
+    int64_t row_tiles;
+    int col_tiles, splits;
+};
+
+// Large products of 16-bit operands (linear_wide.hip).  Whether one is taken,
+// and the fp32 values it leaves in the workspace.
+bool wide_takes(int kind, int dtype, const ProductArgs& a);
+int64_t wide_part(int64_t rows, int64_t cols, int64_t depth);
+void wide_product(int kind, int dtype, ProductArgs a, float* part, int act, hipStream_t s);
+
+}  // namespace taurus

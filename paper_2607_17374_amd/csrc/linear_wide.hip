@@ -1,0 +1,318 @@
+// Large products of 16-bit operands (linear.hpp): tiles of 256 x 256, the
+// contraction in stages of 64.
+//
+// Eight waves of 128 x 64 values share a compute unit, two a SIMD.  They work in
+// two groups of four, half a step apart: while one group's matrix instructions
+// run, the other reads its next operands from LDS, and a barrier hands over.  A
+// stage is four such steps (32 of the contraction by 64 rows).  Stages go from
+// memory straight into LDS, in two buffers of 64 KB: the next stage's pieces
+// are asked for in the first two steps of this one, when the last wave has read
+// the buffer that they go to, and waited for in its last step.
+//
+// The layouts in LDS are those of product.hpp.  A wave's load fills 1 KB in lane
+// order, so the exchange is made in the addresses that the lanes read from.
+// Rows and columns past the edge are read from inside it (what they give is not
+// stored); of the contraction's last stage, lanes past its end leave out the
+// load and write zeros.
+#include "linear.hpp"
+
+namespace taurus {
+
+constexpr int WIDE = 256, WIDE_STAGE = 64, WIDE_BYTES = 256 * 128;  // of an operand's stage
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// A resource over everything from p on: addresses are checked by the caller.
+__device__ inline u32x4 far_rsrc(const char* p) {
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at),
+                 (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)), 0xffffffffu, 0x00020000u};
+}
+// 16 bytes a lane from the resource's start + offset to LDS at `to` + 16 lane.
+// Counted by vmcnt; the compiler does not know that LDS is written, so the
+// reader waits and meets a barrier (asm with a memory clobber) first.
+__device__ inline void load_to_lds(u32x4 rs, uint32_t offset, uint32_t to) {
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, 0 offen lds"
+        :
+        : "s"(to), "v"(offset), "s"(rs)
+        : "memory");
+}
+__device__ inline void zero_to_lds(char* lds, uint32_t to) {
+    *reinterpret_cast<uint4*>(lds + to + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
+}
+
+// One operand of a tile: how its stages come to LDS and are read.  `at` is the
+// first row's (Along) or the first contraction row's (Across) address.
+template <int DT>
+struct WideAlong {
+    const char* at;
+    uint32_t offset[4];
+    int depth, col;  // of this lane's pieces in a stage
+    __device__ WideAlong(const void* base, int64_t stride, int64_t first, int64_t rows, int64_t k0, int depth_)
+        : depth(depth_) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        at = static_cast<const char*>(base) + (first * stride + k0) * 2;
+        const int p = (lane & 7) ^ (lane >> 3);
+        col = p * 8;
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const int64_t row = min((int64_t)(q * 8 + wave) * 8 + (lane >> 3), rows - 1 - first);
+            offset[q] = (uint32_t)(row * stride * 2) + p * 16;
+        }
+    }
+    __device__ const char* stage(int t) const { return at + (int64_t)t * WIDE_STAGE * 2; }
+    __device__ bool holds(int t, int) const { return t * WIDE_STAGE + col < depth; }
+    // rows [r0, r0 + 16), matrix step kb
+    static __device__ inline uint4 read(const char* lds, int r0, int kb) { return Along<DT, WIDE, true>::read(lds, r0, kb); }
+};
+template <int DT>
+struct WideAcross {
+    typedef Across<DT, 128, true> Half;  // the same exchange of 32-byte units
+    const char* at;
+    int64_t step;
+    uint32_t offset[4];
+    int depth, row;
+    __device__ WideAcross(const void* base, int64_t stride, int64_t first, int64_t cols, int64_t k0, int depth_)
+        : step(stride * 2), depth(depth_) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        at = static_cast<const char*>(base) + (k0 * stride + first) * 2;
+        row = wave * 2 + (lane >> 5);
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const int k = q * 16 + row;
+            const int64_t c = min((int64_t)unit_of(k, (lane & 31) >> 1) * 16 + (lane & 1) * 8, cols - 8 - first);
+            offset[q] = (uint32_t)(k * step) + (uint32_t)c * 2;
+        }
+    }
+    static __device__ inline int unit_of(int k, int u) { return u ^ ((k & 3) | (((k >> 3) & 1) << 2)); }
+    __device__ const char* stage(int t) const { return at + (int64_t)t * WIDE_STAGE * step; }
+    __device__ bool holds(int t, int q) const { return t * WIDE_STAGE + q * 16 + row < depth; }
+    static __device__ inline uint4 read(const char* lds, int b, int kb) {
+        const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+        const int k = kb * 32 + 8 * lk + (li >> 2);
+        const char* a = lds + k * 512 + unit_of(k, b >> 4) * 32 + (li & 3) * 8;
+        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(const_cast<char*>(a))));
+        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(const_cast<char*>(a + 2048))));
+        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+};
+template <class Op>
+__device__ inline void bring(const Op& op, int t, char* lds, uint32_t to) {
+    const u32x4 rs = far_rsrc(op.stage(t));
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const uint32_t start = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    if ((t + 1) * WIDE_STAGE <= op.depth) {
+#pragma unroll
+        for (int q = 0; q < 4; q++) load_to_lds(rs, op.offset[q], start + to + (q * 8 + wave) * 1024);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const uint32_t at = to + (q * 8 + wave) * 1024;
+            if (op.holds(t, q)) load_to_lds(rs, op.offset[q], start + at);
+            else zero_to_lds(lds, at);
+        }
+    }
+}
+
+// The tiles that fill the chip a whole number of times are a workgroup's each;
+// those of the last, partial round are cut along the contraction into parts
+// that fill it too, whose sums k_wide_join adds.
+struct WideArgs {
+    ProductArgs p;
+    uint32_t whole, cut;  // tiles taken whole, tiles cut into p.splits parts
+};
+// Consecutive workgroups go round the chip's eight XCDs; an XCD takes
+// consecutive tiles of an order that goes down eight row tiles before it moves
+// to the next column, so that the workgroups on it at one time share both
+// operands in its L2.
+constexpr int64_t WIDE_TILES = (int64_t)1 << 22;  // of a launch of 512 threads a tile, below 2^32
+struct WidePlace {
+    int64_t row, col;
+};
+__device__ inline uint32_t wide_turn(uint32_t b, uint32_t n) {  // the b-th workgroup's turn among n
+    const uint32_t each = n / 8, more = n % 8, x = b % 8;
+    return x * each + min(x, more) + b / 8;
+}
+__device__ inline WidePlace wide_place(const WideArgs& a, uint32_t tile) {
+    const uint32_t cols = (uint32_t)a.p.col_tiles, first = tile / (8 * cols) * 8, in = tile - first * cols;
+    const uint32_t tall = min(8u, (uint32_t)a.p.row_tiles - first);
+    return {first + in % tall, in / tall};
+}
+
+template <int KIND, int DT, int ACT>
+__global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
+    typedef std::conditional_t<KIND == PRODUCT_DW, WideAcross<DT>, WideAlong<DT>> OpM;
+    typedef std::conditional_t<KIND == PRODUCT_DX, WideAlong<DT>, WideAcross<DT>> OpN;
+    __shared__ __align__(1024) char lds[4 * WIDE_BYTES];
+    const bool cut = blockIdx.x >= a.whole;
+    uint32_t tile, part = 0;
+    if (cut) {
+        const uint32_t i = wide_turn(blockIdx.x - a.whole, a.cut * a.p.splits);
+        part = i / a.cut;
+        tile = a.whole + i % a.cut;
+    } else {
+        tile = wide_turn(blockIdx.x, a.whole);
+    }
+    const WidePlace at = wide_place(a, tile);
+    const int64_t r0 = at.row * WIDE, c0 = at.col * WIDE, k0 = part * a.p.per;
+    const int depth = (int)(cut && (int)part + 1 < a.p.splits ? a.p.per : a.p.depth - k0);
+    const OpM om(a.p.m, a.p.ms, r0, a.p.rows, k0, depth);
+    const OpN on(a.p.n, a.p.ns, c0, a.p.cols, k0, depth);
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), group = wave >> 2;
+    const int m0 = group * 128, n0 = (wave & 3) * 64;
+    const int stages = (depth + WIDE_STAGE - 1) / WIDE_STAGE;
+
+    floatx4 acc[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    bring(om, 0, lds, 0);
+    bring(on, 0, lds, WIDE_BYTES);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // the second group is half a step behind: it meets one barrier more here,
+    // the first one more at the end
+    if (group == 1) asm volatile("s_barrier" ::: "memory");
+    for (int t = 0; t < stages; t++) {
+        const char* mine = lds + (t & 1) * 2 * WIDE_BYTES;
+        const uint32_t next = (uint32_t)((t + 1) & 1) * 2 * WIDE_BYTES;
+        const bool more = t + 1 < stages;
+        uint4 fn[4];
+#pragma unroll
+        for (int step = 0; step < 4; step++) {
+            const int kb = step >> 1, half = step & 1;
+            uint4 fm[4];
+            if (half == 0)
+#pragma unroll
+                for (int j = 0; j < 4; j++) fn[j] = OpN::read(mine + WIDE_BYTES, n0 + 16 * j, kb);
+#pragma unroll
+            for (int i = 0; i < 4; i++) fm[i] = OpM::read(mine, m0 + 64 * half + 16 * i, kb);
+            if (step == 0 && more) bring(om, t + 1, lds, next);
+            if (step == 1 && more) bring(on, t + 1, lds, next + WIDE_BYTES);
+            // all reads of this step are done before the barrier: past the last
+            // one's, the other group may ask for what overwrites them
+            if (step == 3) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) acc[4 * half + i][j] = mfma16<DT>(fn[j], fm[i], acc[4 * half + i][j]);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_barrier" ::: "memory");
+        }
+    }
+    if (group == 0) asm volatile("s_barrier" ::: "memory");
+
+    const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
+    float* sums = cut ? a.p.part + (int64_t)(part * a.cut + tile - a.whole) * (WIDE * WIDE) : nullptr;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const int mr = m0 + 16 * i + li;
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            if (cut) {
+                float* out = sums + mr * WIDE + n0 + 16 * j + 4 * lk;
+                *reinterpret_cast<floatx4*>(out) = acc[i][j];
+                *reinterpret_cast<floatx4*>(out + 16) = acc[i][j + 1];
+            } else {
+                finish_pair<DT, ACT>(a.p.e, r0 + mr, (int)c0 + n0 + 16 * j, (int)a.p.cols, r0 + mr < a.p.rows, acc[i][j],
+                                     acc[i][j + 1]);
+            }
+        }
+    }
+}
+
+// The parts of the cut tiles added in order, then the epilogue: a thread four
+// values, a workgroup four rows of a tile.
+template <int DT, int ACT>
+__global__ __launch_bounds__(256) void k_wide_join(WideArgs a) {
+    const uint32_t i = blockIdx.x / 64;
+    const WidePlace at = wide_place(a, a.whole + i);
+    const int row = (int)(blockIdx.x % 64) * 4 + (threadIdx.x >> 6), col = (threadIdx.x & 63) * 4;
+    const int64_t r = at.row * WIDE + row;
+    const int c = (int)at.col * WIDE + col;
+    if (r >= a.p.rows || c >= a.p.cols) return;
+    const float* p = a.p.part + (int64_t)i * (WIDE * WIDE) + row * WIDE + col;
+    floatx4 v{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.p.splits; s++) v += *reinterpret_cast<const floatx4*>(p + (int64_t)s * a.cut * (WIDE * WIDE));
+    finish4<DT, ACT>(a.p.e, r, c, (int)a.p.cols, v);
+}
+
+// ---------------------------------------------------------------- launches --
+
+struct WidePlan {
+    int64_t whole, cut, per;
+    int splits;
+};
+// A part's sums are written and read, about 0.1 us for the whole chip; a stage
+// takes about 0.9 us: cutting r tiles of s stages into p parts costs about 0.9
+// s / p + 0.1 r p, least at 3 sqrt(s / r) parts.
+static WidePlan wide_plan(int64_t rows, int64_t cols, int64_t depth) {
+    const int64_t tiles = ceil_div(rows, WIDE) * ceil_div(cols, WIDE), stages = ceil_div(depth, WIDE_STAGE);
+    constexpr int64_t CUS = 256;  // of the chip; a workgroup fills one
+    const int64_t rest = tiles % CUS;
+    WidePlan p{tiles, 0, stages * WIDE_STAGE, 1};
+    if (!rest || stages < 4) return p;
+    const int64_t best = (int64_t)(3.0 * sqrt((double)stages / (double)rest));
+    const int64_t parts = std::min(std::min(CUS / rest, stages / 2), best);
+    if (parts < 2) return p;
+    const int64_t each = ceil_div(stages, parts);
+    p.whole = tiles - rest;
+    p.cut = rest;
+    p.per = each * WIDE_STAGE;
+    p.splits = (int)ceil_div(stages, each);
+    return p;
+}
+bool wide_takes(int kind, int dtype, const ProductArgs& a) {
+    if (dtype == TAURUS_F32) return false;
+    auto whole = [](const void* p, int64_t width, int64_t stride) {
+        return width % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+    };
+    const int64_t m_width = kind == PRODUCT_DW ? a.rows : a.depth, n_width = kind == PRODUCT_DX ? a.depth : a.cols;
+    return whole(a.m, m_width, a.ms) && whole(a.n, n_width, a.ns) && a.cols % 8 == 0 && a.rows >= 256 && a.cols >= 256 &&
+           a.depth >= 256 && ceil_div(a.rows, WIDE) * ceil_div(a.cols, WIDE) <= WIDE_TILES;
+}
+int64_t wide_part(int64_t rows, int64_t cols, int64_t depth) {
+    const WidePlan p = wide_plan(rows, cols, depth);
+    return p.cut * p.splits * WIDE * WIDE;
+}
+template <int KIND, int DT>
+static void wide_launch(const WideArgs& a, int act, hipStream_t s) {
+    auto go = [&](auto c) {
+        constexpr int ACT = decltype(c)::value;
+        k_linear_wide<KIND, DT, ACT><<<a.whole + a.cut * a.p.splits, 512, 0, s>>>(a);
+        TAURUS_CHECK_LAUNCH();
+        if (a.cut) {
+            k_wide_join<DT, ACT><<<a.cut * 64, 256, 0, s>>>(a);
+            TAURUS_CHECK_LAUNCH();
+        }
+    };
+    if constexpr (KIND == PRODUCT_Y) with_act(act, go);
+    else go(std::integral_constant<int, TAURUS_ACT_NONE>{});
+}
+void wide_product(int kind, int dtype, ProductArgs p, float* part, int act, hipStream_t s) {
+    const WidePlan plan = wide_plan(p.rows, p.cols, p.depth);
+    p.part = part;
+    p.per = plan.per;
+    p.splits = plan.splits;
+    p.row_tiles = ceil_div(p.rows, WIDE);
+    p.col_tiles = (int)ceil_div(p.cols, WIDE);
+    const WideArgs a{p, (uint32_t)plan.whole, (uint32_t)plan.cut};
+    auto of = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (kind == PRODUCT_Y) wide_launch<PRODUCT_Y, DT>(a, act, s);
+        else if (kind == PRODUCT_DX) wide_launch<PRODUCT_DX, DT>(a, act, s);
+        else wide_launch<PRODUCT_DW, DT>(a, act, s);
+    };
+    if (dtype == TAURUS_BF16) of(std::integral_constant<int, TAURUS_BF16>{});
+    else of(std::integral_constant<int, TAURUS_F16>{});
+}
+
+}  // namespace taurus
