@@ -15,10 +15,17 @@
 // One pass each way, bound by memory: a row lies in the registers of a team, up
 // to eight values a lane (lanes of a wave up to 512 channels, then 4, 8 or 16
 // waves), with the channels' parameters beside it, and statistics are two
-// passes over registers.  The gradient's column sums stay in registers too; a
-// workgroup leaves one row of them, k_join_columns adds those.  Rows of a
-// segment are cut into units (rowops.hpp), whose gate gradients are written at
-// once, or joined where a segment has several.
+// passes over registers.  A worker (a wave of teams, or a workgroup that is
+// one) takes consecutive rows, as many as the others, and has the next ones
+// under way while it works on these.
+//
+// The gradient's column sums stay in registers too.  The gate is the same for
+// all rows of a segment, so that with A = sum of dy fhat and B = sum of dy over
+// a worker's rows of one,
+//     dgate = scale (w A + b B),   dw += scale gate A,   db += scale gate B.
+// A workgroup leaves one row of sums, k_join_columns adds those.  A segment
+// that lies within a worker's rows has its gate's gradient written at once; of
+// others each worker leaves its part in the workspace, for k_resnorm_gates.
 #include "columns.hpp"
 #include "lanes.hpp"
 #include "rowops.hpp"
@@ -44,54 +51,52 @@ struct ResnormArgs {
     void *y, *h;
     int64_t ys, hs;
     float4* stats;
-    // gradient
+    // gradient: arrays that there are not are a row's length of workspace, with
+    // a stride of 0
     const void *dh, *dy;
-    int64_t dhs, dys;
+    int64_t dhs, dys, stats_stride;
+    bool has_dy;
     void *dx, *df;
     int64_t dxs, dfs;
     float *dgate, *gate_part, *cols;  // cols [workgroups][sums][d]
     int sums;                         // column sums a workgroup leaves
     int at_gate, at_post_w, at_post_b, at_pre_w, at_pre_b;  // which of them, or -1
-    // work
-    int R;
-    int64_t slots, per;  // a worker takes `per` consecutive slots
+    int64_t per;  // rows of a worker
 };
 
-// The units of a worker's slots, one after another (rowops.hpp: range g owns
-// the slots from off[g] / R + g on).  Without offsets all rows are one range.
-struct UnitWalk {
+// A worker's rows, segment by segment.  Without offsets all rows are one
+// segment.  Whatever the offsets hold, rows go up and stay the worker's.
+struct Piece {
+    int64_t r0, r1, seg;
+    bool begins, ends;  // whether the segment does, here
+};
+struct SegmentWalk {
     const ResnormArgs& a;
-    int64_t k, end, g, b, e;
-    __device__ UnitWalk(const ResnormArgs& a_, int64_t worker) : a(a_) {
-        k = worker * a.per;
-        end = min(k + a.per, a.slots);
-        g = 0;
-        b = 0;
-        e = a.m;
-        if (a.off && k < end) {
-            g = wave_last(a.segs, [&](int64_t p) { return (int64_t)(off_at(a.off, p, a.m) / (uint32_t)a.R) + p <= k; });
-            bounds();
+    int64_t from, to;  // the worker's rows
+    int64_t r, g = -1, e = 0;
+    __device__ SegmentWalk(const ResnormArgs& a_, int64_t worker)
+        : a(a_), from(min(worker * a_.per, a_.m)), to(min(from + a_.per, a_.m)), r(from) {}
+    __device__ bool next(Piece& p) {
+        if (r >= to || (a.off && a.segs == 0)) return false;
+        if (!a.off) {
+            p = Piece{r, to, 0, false, false};
+            r = to;
+            return true;
         }
-    }
-    __device__ void bounds() {
-        b = off_at(a.off, g, a.m);
-        e = max((int64_t)off_at(a.off, g + 1, a.m), b);
-    }
-    // the next unit: its rows (none for slots without), whether it is its
-    // segment's first, and whether the segment's only one
-    __device__ bool next(int64_t& r0, int64_t& r1, bool& first, bool& only, int64_t& seg) {
-        if (k >= end) return false;
-        if (a.off && g + 1 < a.segs && k >= e / a.R + g + 1) {
-            g++;
-            bounds();
+        int64_t b = e;
+        if (g >= 0 && g + 1 < a.segs) e = max((int64_t)off_at(a.off, ++g + 1, a.m), b);
+        if (g < 0 || e <= r) {  // the first, or empty ones between: the last segment that begins at r or before
+            g = wave_last(a.segs, [&](int64_t q) { return (int64_t)off_at(a.off, q, a.m) <= r; });
+            b = off_at(a.off, g, a.m);
+            e = max((int64_t)off_at(a.off, g + 1, a.m), b);
         }
-        const int64_t slot = k - (b / a.R + g);
-        k++;
-        seg = g;
-        first = slot == 0;
-        only = e - b <= a.R;
-        r0 = min(b + max(slot, (int64_t)0) * a.R, e);
-        r1 = slot < 0 ? r0 : min(r0 + a.R, e);
+        r = max(r, b);  // rows before the first segment
+        if (r >= min(e, to)) {
+            r = to;
+            return false;
+        }
+        p = Piece{r, min(e, to), g, b >= from, e <= to};
+        r = p.r1;
         return true;
     }
 };
@@ -106,9 +111,9 @@ struct Team {
     __device__ Team(int lg_, float2* room_) : lg(lg_), room(room_) {}
     __device__ float2 sum(float2 v) {
         if constexpr (WAVES == 0) {
-            return {lanes_sum(v.x, lg), lanes_sum(v.y, lg)};
+            return lanes_sum2(v, lg);
         } else {
-            v = {lanes_sum(v.x, 6), lanes_sum(v.y, 6)};
+            v = lanes_sum2(v, 6);
             float2* at = room + turn * WAVES;  // the other half is still being read
             turn ^= 1;
             if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = v;
@@ -125,37 +130,39 @@ struct Team {
 };
 
 // What a lane holds of a row: P vectors of E values.
-template <int E, int P>
+template <int E, int P, bool WHOLE>
 struct Cols {
     int64_t at[P];  // first column
     bool in[P];     // whether there is one
-    int again[P];   // its values that the vector before has too
+    int again[P];   // its values that the vector before has too (WHOLE: all vectors are there, and no values are)
     __device__ Cols(int lane, int lanes, int d) {
 #pragma unroll
         for (int p = 0; p < P; p++) {
             const int64_t w = lane + (int64_t)p * lanes;
-            in[p] = w * E < d;
+            in[p] = WHOLE || w * E < d;
             at[p] = in[p] ? vec_at<E>(w, d) : 0;
             again[p] = in[p] ? vec_again<E>(w, d) : E;
         }
     }
-    __device__ bool counts(int p, int e) const { return e >= again[p]; }
+    __device__ bool counts(int p, int e) const { return WHOLE || e >= again[p]; }
+    __device__ float counted(int p, int e, float v) const { return counts(p, e) ? v : 0.f; }
 };
 template <int E, int P>
 struct Values {
     float v[P][E];
-    template <int DT>
-    __device__ void load(const void* base, int64_t row_at, const Cols<E, P>& c) {
+    template <int DT, bool WHOLE>
+    __device__ void load(const void* base, int64_t row_at, const Cols<E, P, WHOLE>& c) {
 #pragma unroll
         for (int p = 0; p < P; p++) load_vec<DT, E>(base, row_at + c.at[p], v[p]);
     }
-    template <int DT>
-    __device__ void store(void* base, int64_t row_at, const Cols<E, P>& c, bool write) const {
+    template <int DT, bool WHOLE>
+    __device__ void store(void* base, int64_t row_at, const Cols<E, P, WHOLE>& c, bool write) const {
 #pragma unroll
         for (int p = 0; p < P; p++)
             if (write && c.in[p]) store_vec<DT, E>(base, row_at + c.at[p], v[p]);
     }
-    __device__ void parameter(const float* base, float otherwise, const Cols<E, P>& c) {
+    template <bool WHOLE>
+    __device__ void parameter(const float* base, float otherwise, const Cols<E, P, WHOLE>& c) {
         if (base) {
             load<TAURUS_F32>(base, 0, c);
         } else {
@@ -165,45 +172,75 @@ struct Values {
                 for (int e = 0; e < E; e++) v[p][e] = otherwise;
         }
     }
-    __device__ void zero() { parameter(nullptr, 0.f, Cols<E, P>(0, 1, 1)); }
+    __device__ void zero() {
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+            for (int e = 0; e < E; e++) v[p][e] = 0.f;
+    }
+    template <int DT>
+    __device__ void take(const Stored<DT, E> (&s)[P]) {
+#pragma unroll
+        for (int p = 0; p < P; p++) decode<DT, E>(s[p], v[p]);
+    }
 };
+template <int DT, int E, int P, bool WHOLE>
+__device__ inline void fetch(Stored<DT, E> (&s)[P], const void* base, int64_t row_at, const Cols<E, P, WHOLE>& c) {
+#pragma unroll
+    for (int p = 0; p < P; p++) s[p] = load_stored<DT, E>(base, row_at + c.at[p]);
+}
 #define EACH                      \
     _Pragma("unroll") for (int p = 0; p < P; p++) _Pragma("unroll") for (int e = 0; e < E; e++)
 
 // mean and rstd of a row, for a team
-template <int WAVES, int E, int P>
-__device__ inline float2 moments(Team<WAVES>& team, const Values<E, P>& x, const Cols<E, P>& c, int kind, float eps,
+template <int WAVES, int E, int P, bool WHOLE>
+__device__ inline float2 moments(Team<WAVES>& team, const Values<E, P>& x, const Cols<E, P, WHOLE>& c, int kind, float eps,
                                  float inv_d) {
     float mean = 0.f;
     if (kind == TAURUS_NORM_LAYER) {
         float s = 0.f;
-        EACH s += c.counts(p, e) ? x.v[p][e] : 0.f;
+        EACH s += c.counted(p, e, x.v[p][e]);
         mean = team.sum({s, 0.f}).x * inv_d;
     }
     float q = 0.f;
     EACH {
-        const float dev = c.counts(p, e) ? x.v[p][e] - mean : 0.f;
+        const float dev = c.counted(p, e, x.v[p][e] - mean);
         q = __builtin_fmaf(dev, dev, q);
     }
     const float var = team.sum({q, 0.f}).x * inv_d;
     return {mean, 1.f / sqrtf(var + eps)};
 }
 
+// Workers of a workgroup: its four waves, each of 64 / 2^lg teams, or itself.
 template <int WAVES>
 struct Workers {
     static constexpr int THREADS = WAVES ? WAVES * 64 : 256;
-    // workers of a workgroup: its waves, or itself
-    static constexpr int PER_BLOCK = WAVES ? 1 : 4;
+    int lanes, lane, team, teams;
+    int64_t worker;
+    __device__ explicit Workers(int lg) {
+        if constexpr (WAVES > 0) {
+            lanes = WAVES * 64;
+            lane = threadIdx.x;
+            team = 0;
+            teams = 1;
+            worker = blockIdx.x;
+        } else {
+            lanes = 1 << lg;
+            lane = threadIdx.x & (lanes - 1);
+            team = (threadIdx.x & 63) >> lg;
+            teams = 64 >> lg;
+            worker = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+        }
+    }
 };
 
 // FT the block's type, ST the stream's
-template <int FT, int ST, int E, int P, int WAVES>
+template <int FT, int ST, int E, int P, int WAVES, bool WHOLE>
 __global__ __launch_bounds__(Workers<WAVES>::THREADS) void k_resnorm(ResnormArgs a, int lg) {
     __shared__ float2 room[2 * (WAVES ? WAVES : 1)];
-    const int lanes = WAVES ? WAVES * 64 : 1 << lg, lane = WAVES ? threadIdx.x : threadIdx.x & (lanes - 1);
-    const int team_at = WAVES ? 0 : (threadIdx.x & 63) >> lg, teams = WAVES ? 1 : 64 >> lg;
+    const Workers<WAVES> k(lg);
     Team<WAVES> team(lg, room);
-    const Cols<E, P> c(lane, lanes, a.d);
+    const Cols<E, P, WHOLE> c(k.lane, k.lanes, a.d);
     const float inv_d = 1.f / (float)a.d;
     Values<E, P> w1, b1, w2, b2, gate;
     w1.parameter(a.post.w, 1.f, c);
@@ -212,21 +249,32 @@ __global__ __launch_bounds__(Workers<WAVES>::THREADS) void k_resnorm(ResnormArgs
     b2.parameter(a.pre.b, 0.f, c);
     gate.parameter(a.off ? nullptr : a.gate, 1.f, c);
     EACH gate.v[p][e] *= a.scale;
-    UnitWalk walk(a, WAVES ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
-    int64_t r0, r1, seg, gate_of = -1;
-    bool first, only;
-    while (walk.next(r0, r1, first, only, seg)) {
-        if (a.off && a.gate && seg != gate_of && r0 < r1) {
-            gate_of = seg;
-            gate.template load<TAURUS_F32>(a.gate, seg * a.d, c);
+    SegmentWalk walk(a, k.worker);
+    Piece now;
+    if (!walk.next(now)) return;  // the same for all of the team
+    Stored<FT, E> next_f[P];
+    Stored<ST, E> next_x[P];
+    // rows are consecutive over segments: the next ones are known before the
+    // next segment is
+    auto bring = [&](int64_t at) {
+        const int64_t r = min(at + k.team, walk.to - 1);
+        fetch<FT>(next_f, a.f, r * a.fs, c);
+        fetch<ST>(next_x, a.x, r * a.xs, c);
+    };
+    bring(now.r0);
+    bool have = true;
+    while (have) {
+        if (a.off && a.gate) {
+            gate.template load<TAURUS_F32>(a.gate, now.seg * a.d, c);
             EACH gate.v[p][e] *= a.scale;
         }
-        for (int64_t at = r0; at < r1; at += teams) {
-            const bool in = at + team_at < r1;
-            const int64_t r = in ? at + team_at : r1 - 1;
+        for (int64_t at = now.r0; at < now.r1; at += k.teams) {
+            const int64_t r = at + k.team;
+            const bool in = r < now.r1;
             Values<E, P> f, y;
-            f.template load<FT>(a.f, r * a.fs, c);
-            y.template load<ST>(a.x, r * a.xs, c);
+            f.template take<FT>(next_f);
+            y.template take<ST>(next_x);
+            bring(min(at + k.teams, now.r1));
             float2 s1{0.f, 0.f}, s2{0.f, 0.f};
             if (a.post.kind != TAURUS_NORM_NONE) {
                 s1 = moments(team, f, c, a.post.kind, a.post.eps, inv_d);
@@ -239,15 +287,16 @@ __global__ __launch_bounds__(Workers<WAVES>::THREADS) void k_resnorm(ResnormArgs
                 EACH y.v[p][e] = (y.v[p][e] - s2.x) * s2.y * w2.v[p][e] + b2.v[p][e];
                 y.template store<FT>(a.h, r * a.hs, c, in);
             }
-            if (a.stats && in && lane == 0) a.stats[r] = make_float4(s1.x, s1.y, s2.x, s2.y);
+            if (a.stats && in && k.lane == 0) a.stats[r] = make_float4(s1.x, s1.y, s2.x, s2.y);
         }
+        have = walk.next(now);
     }
 }
 
 // A worker's column sums of one kind: its teams' in order, into the
-// workgroup's row (`waves` workers a workgroup).
-template <int E, int P, int WAVES>
-__device__ inline void put_sums(float* lds, const Values<E, P>& v, const Cols<E, P>& c, int d, int lg, float* out) {
+// workgroup's row.
+template <int WAVES, int E, int P, bool WHOLE>
+__device__ inline void put_sums(float* lds, const Values<E, P>& v, const Cols<E, P, WHOLE>& c, int d, int lg, float* out) {
     if constexpr (WAVES > 0) {
         EACH if (c.counts(p, e)) out[c.at[p] + e] = v.v[p][e];
     } else {
@@ -263,95 +312,108 @@ __device__ inline void put_sums(float* lds, const Values<E, P>& v, const Cols<E,
     }
 }
 
-// HOLD: the channels' parameters stay in registers
-template <int FT, int ST, int E, int P, int WAVES, bool HOLD>
-__global__ __launch_bounds__(Workers<WAVES>::THREADS) void k_resnorm_grad(ResnormArgs a, int lg) {
+// What the gradient reads of a row, as stored.
+template <int FT, int ST, int E, int P, bool WHOLE>
+struct GradRow {
+    Stored<FT, E> f[P], dh[P];
+    Stored<ST, E> y[P], dy[P];
+    float4 st;
+    // what there is not is read from somewhere (ResnormArgs), without a branch:
+    // one would keep the loads from being under way over a round of the loop
+    __device__ void load(const ResnormArgs& a, int64_t r, const Cols<E, P, WHOLE>& c) {
+        st = a.stats[r * a.stats_stride];
+        fetch<FT>(f, a.f, r * a.fs, c);
+        fetch<ST>(y, a.y, r * a.ys, c);
+        fetch<FT>(dh, a.dh, r * a.dhs, c);
+        fetch<ST>(dy, a.dy, r * a.dys, c);
+    }
+};
+
+// HOLD: up to eight values a lane; the channels' parameters stay in registers
+// and the next row is under way.  OFF: a gate's row for each segment.
+template <int FT, int ST, int E, int P, int WAVES, bool HOLD, bool OFF, bool WHOLE>
+__global__ __launch_bounds__(Workers<WAVES>::THREADS, WAVES ? 1 : 3) void k_resnorm_grad(ResnormArgs a, int lg) {
     __shared__ float2 room[2 * (WAVES ? WAVES : 1)];
     extern __shared__ float lds[];
-    const int lanes = WAVES ? WAVES * 64 : 1 << lg, lane = WAVES ? threadIdx.x : threadIdx.x & (lanes - 1);
-    const int team_at = WAVES ? 0 : (threadIdx.x & 63) >> lg, teams = WAVES ? 1 : 64 >> lg;
+    const Workers<WAVES> k(lg);
     Team<WAVES> team(lg, room);
-    const Cols<E, P> c(lane, lanes, a.d);
+    const Cols<E, P, WHOLE> c(k.lane, k.lanes, a.d);
     const float inv_d = 1.f / (float)a.d;
     const bool post = a.post.kind != TAURUS_NORM_NONE, pre = a.pre.kind != TAURUS_NORM_NONE;
     const bool centre1 = a.post.kind == TAURUS_NORM_LAYER, centre2 = a.pre.kind == TAURUS_NORM_LAYER;
-    Values<E, P> w1, b1, w2, gate, to_gate, to_w1, to_b1, to_w2, to_b2;
-    if constexpr (HOLD) {
+    // gate times scale; A and B of the segment under way
+    Values<E, P> w1, w2, gate, sum_a, sum_b, to_w1, to_b1, to_w2, to_b2;
+    auto take_gate = [&](int64_t seg) {
+        gate.parameter(a.gate ? a.gate + (OFF ? seg * a.d : 0) : nullptr, 1.f, c);
+        EACH gate.v[p][e] *= a.scale;
+    };
+    auto parameters = [&](int64_t seg) {
         w1.parameter(a.post.w, 1.f, c);
-        b1.parameter(a.post.b, 0.f, c);
         w2.parameter(a.pre.w, 1.f, c);
-        gate.parameter(a.off ? nullptr : a.gate, 1.f, c);
-    }
-    to_gate.zero();
+        take_gate(seg);
+    };
+    sum_a.zero();
+    sum_b.zero();
     to_w1.zero();
     to_b1.zero();
     to_w2.zero();
     to_b2.zero();
-    UnitWalk walk(a, WAVES ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6));
-    int64_t r0, r1, seg, gate_of = -1;
-    bool first, only;
-    while (walk.next(r0, r1, first, only, seg)) {
-        if constexpr (HOLD)
-            if (a.off && a.gate && seg != gate_of && r0 < r1) {
-                gate_of = seg;
-                gate.template load<TAURUS_F32>(a.gate, seg * a.d, c);
+    SegmentWalk walk(a, k.worker);
+    Piece now;
+    bool have = walk.next(now);
+    GradRow<FT, ST, E, P, WHOLE> row;
+    if (HOLD && have) {
+        parameters(now.seg);
+        row.load(a, min(now.r0 + k.team, walk.to - 1), c);
+    }
+    while (have) {
+        for (int64_t at = now.r0; at < now.r1; at += k.teams) {
+            const int64_t r = at + k.team;
+            const bool in = r < now.r1;
+            if constexpr (!HOLD) row.load(a, min(r, walk.to - 1), c);
+            Values<E, P> f, dy;
+            const float4 st = row.st;
+            f.template take<FT>(row.f);
+            dy.template take<ST>(row.dy);
+            if (!a.has_dy) dy.zero();
+            Values<E, P> hat2, dh;
+            hat2.template take<ST>(row.y);
+            dh.template take<FT>(row.dh);
+            if constexpr (HOLD) {  // rows are consecutive over segments
+                row.load(a, min(min(at + k.teams, now.r1) + k.team, walk.to - 1), c);
+            } else {
+                parameters(now.seg);
             }
-        for (int64_t at = r0; at < r1; at += teams) {
-            const bool in = at + team_at < r1;
-            const int64_t r = in ? at + team_at : r1 - 1;
-            Values<E, P> f, y, dy, dh;
-            float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (post || pre) st = a.stats[r];
-            f.template load<FT>(a.f, r * a.fs, c);
             if (pre) {
-                y.template load<ST>(a.y, r * a.ys, c);
-                dh.template load<FT>(a.dh, r * a.dhs, c);
-            }
-            if (a.dy) dy.template load<ST>(a.dy, r * a.dys, c);
-            else dy.zero();
-            if (pre) {
-                if constexpr (!HOLD) w2.parameter(a.pre.w, 1.f, c);
                 float2 s{0.f, 0.f};
                 EACH {
-                    const float hat = (y.v[p][e] - st.z) * st.w, d = dh.v[p][e], g = d * w2.v[p][e];
-                    y.v[p][e] = hat;
-                    dh.v[p][e] = g;
-                    if (c.counts(p, e)) {
-                        s.x += g;
-                        s.y += g * hat;
-                    }
-                    if (in) {
-                        to_w2.v[p][e] += d * hat;
-                        to_b2.v[p][e] += d;
-                    }
+                    const float hat = (hat2.v[p][e] - st.z) * st.w, g = dh.v[p][e] * w2.v[p][e];
+                    hat2.v[p][e] = hat;
+                    s.x += c.counted(p, e, g);
+                    s.y += c.counted(p, e, g * hat);
+                }
+                if (in) EACH {
+                    to_w2.v[p][e] = __builtin_fmaf(dh.v[p][e], hat2.v[p][e], to_w2.v[p][e]);
+                    to_b2.v[p][e] += dh.v[p][e];
                 }
                 s = team.sum(s);
                 const float m1 = centre2 ? s.x * inv_d : 0.f, m2 = s.y * inv_d;
-                EACH dy.v[p][e] += st.w * (dh.v[p][e] - m1 - y.v[p][e] * m2);
+                EACH dy.v[p][e] += st.w * (dh.v[p][e] * w2.v[p][e] - m1 - hat2.v[p][e] * m2);
             }
             dy.template store<ST>(a.dx, r * a.dxs, c, in && a.dx);
-            if constexpr (!HOLD) {
-                w1.parameter(a.post.w, 1.f, c);
-                b1.parameter(a.post.b, 0.f, c);
-                gate.parameter(a.gate ? a.gate + (a.off ? seg * a.d : 0) : nullptr, 1.f, c);
-            }
             float2 s{0.f, 0.f};
             EACH {
                 const float hat = post ? (f.v[p][e] - st.x) * st.y : f.v[p][e];
-                const float n = hat * w1.v[p][e] + b1.v[p][e], d = dy.v[p][e] * a.scale;
-                const float dp = d * gate.v[p][e], g = dp * w1.v[p][e];
+                const float g = dy.v[p][e] * gate.v[p][e] * w1.v[p][e];
                 f.v[p][e] = hat;
-                dy.v[p][e] = g;
-                if (c.counts(p, e)) {
-                    s.x += g;
-                    s.y += g * hat;
-                }
-                if (in) {
-                    to_gate.v[p][e] += d * n;
-                    to_w1.v[p][e] += dp * hat;
-                    to_b1.v[p][e] += dp;
-                }
+                s.x += c.counted(p, e, g);
+                s.y += c.counted(p, e, g * hat);
             }
+            if (in) EACH {
+                sum_a.v[p][e] = __builtin_fmaf(dy.v[p][e], f.v[p][e], sum_a.v[p][e]);
+                sum_b.v[p][e] += dy.v[p][e];
+            }
+            EACH dy.v[p][e] *= gate.v[p][e] * w1.v[p][e];
             if (a.df) {
                 if (post) {
                     s = team.sum(s);
@@ -361,35 +423,89 @@ __global__ __launch_bounds__(Workers<WAVES>::THREADS) void k_resnorm_grad(Resnor
                 dy.template store<FT>(a.df, r * a.dfs, c, in);
             }
         }
-        if (a.off && a.dgate && (r0 < r1 || (only && first))) {  // the unit's gate gradient: its teams' sums
-            float* out = only ? a.dgate + seg * a.d : a.gate_part + unit_place(r0, first ? 0 : 1, a.R) * a.d;
-            EACH {
-                float v = to_gate.v[p][e];
-                if constexpr (WAVES == 0)  // lanes of the same column in the wave's teams
-                    for (int o = lanes; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-                if (team_at == 0 && c.counts(p, e)) out[c.at[p] + e] = v;
-                to_gate.v[p][e] = 0.f;
+        const Piece done = now;
+        have = walk.next(now);
+        if constexpr (OFF) {  // the segment's sums over the worker's teams
+            if (a.dgate) {
+                float* out = a.gate_part + (2 * k.worker + (done.begins ? 1 : 0)) * a.d;
+                if (done.begins && done.ends) out = a.dgate + done.seg * a.d;
+                Values<E, P> b1;
+                b1.parameter(a.post.b, 0.f, c);
+                EACH {
+                    float v = a.scale * (w1.v[p][e] * sum_a.v[p][e] + b1.v[p][e] * sum_b.v[p][e]);
+                    if constexpr (WAVES == 0) v = groups_sum(v, lg);
+                    if (k.team == 0 && c.counts(p, e)) out[c.at[p] + e] = v;
+                }
             }
+            EACH {
+                to_w1.v[p][e] += gate.v[p][e] * sum_a.v[p][e];
+                to_b1.v[p][e] += gate.v[p][e] * sum_b.v[p][e];
+            }
+            sum_a.zero();
+            sum_b.zero();
+            if (HOLD && have) take_gate(now.seg);
         }
     }
     float* out = a.cols + (int64_t)blockIdx.x * a.sums * a.d;
-    if (a.at_gate >= 0) put_sums<E, P, WAVES>(lds, to_gate, c, a.d, lg, out + a.at_gate * a.d);
-    if (a.at_post_w >= 0) put_sums<E, P, WAVES>(lds, to_w1, c, a.d, lg, out + a.at_post_w * a.d);
-    if (a.at_post_b >= 0) put_sums<E, P, WAVES>(lds, to_b1, c, a.d, lg, out + a.at_post_b * a.d);
-    if (a.at_pre_w >= 0) put_sums<E, P, WAVES>(lds, to_w2, c, a.d, lg, out + a.at_pre_w * a.d);
-    if (a.at_pre_b >= 0) put_sums<E, P, WAVES>(lds, to_b2, c, a.d, lg, out + a.at_pre_b * a.d);
+    if constexpr (!OFF) {
+        if (!HOLD || walk.from >= walk.to) parameters(0);
+        if (a.at_gate >= 0) {
+            Values<E, P> b1;
+            b1.parameter(a.post.b, 0.f, c);
+            EACH b1.v[p][e] = a.scale * (w1.v[p][e] * sum_a.v[p][e] + b1.v[p][e] * sum_b.v[p][e]);
+            put_sums<WAVES>(lds, b1, c, a.d, lg, out + a.at_gate * a.d);
+        }
+        EACH {
+            to_w1.v[p][e] = gate.v[p][e] * sum_a.v[p][e];
+            to_b1.v[p][e] = gate.v[p][e] * sum_b.v[p][e];
+        }
+    }
+    if (a.at_post_w >= 0) put_sums<WAVES>(lds, to_w1, c, a.d, lg, out + a.at_post_w * a.d);
+    if (a.at_post_b >= 0) put_sums<WAVES>(lds, to_b1, c, a.d, lg, out + a.at_post_b * a.d);
+    if (a.at_pre_w >= 0) put_sums<WAVES>(lds, to_w2, c, a.d, lg, out + a.at_pre_w * a.d);
+    if (a.at_pre_b >= 0) put_sums<WAVES>(lds, to_b2, c, a.d, lg, out + a.at_pre_b * a.d);
 }
 
-// Segments of several units: their gate gradients added in row order, a
-// workgroup 256 columns of one.
-__global__ __launch_bounds__(256) void k_resnorm_gates(ResnormArgs a, int64_t longs, int chunks) {
-    for (int64_t i = blockIdx.x; i < longs * chunks; i += gridDim.x) {
-        const Long t = wave_long(a.off, a.segs, a.m, a.R, i / chunks);
-        const int64_t c = i % chunks * 256 + threadIdx.x;
-        if (!t.found || c >= a.d) continue;
-        float s = 0.f;
-        for (int64_t u = 0; u < t.units; u++) s += a.gate_part[unit_place(t.begin + u * a.R, u ? 1 : 0, a.R) * a.d + c];
-        a.dgate[t.g * a.d + c] = s;
+// Gate gradients that no worker has written: zeros of segments without rows,
+// and the parts of those that several workers hold, in row order.  The first
+// of these workers leaves its part in its second place, the others in their
+// first.  A wave a segment; or, where there are few segments, which can be
+// long, a workgroup 16 columns of one, 64 row lanes each.
+template <bool FEW>
+__global__ __launch_bounds__(FEW ? 1024 : 256) void k_resnorm_gates(ResnormArgs a) {
+    __shared__ float lanes[FEW ? 64 : 1][17];
+    const int64_t step = FEW ? gridDim.x : (int64_t)gridDim.x * 4;
+    for (int64_t s = FEW ? blockIdx.x : (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); s < a.segs; s += step) {
+        const int64_t b = off_at(a.off, s, a.m), e = max((int64_t)off_at(a.off, s + 1, a.m), b);
+        const int64_t first = b / a.per, last = e > b ? (e - 1) / a.per : first;
+        if (e > b && first == last) continue;  // the same for the team
+        const int64_t parts = e > b ? last - first + 1 : 0;
+        auto part = [&](int64_t i) { return a.gate_part + (2 * (first + i) + (i == 0)) * a.d; };
+        if constexpr (FEW) {
+            const int cx = threadIdx.x & 15, ry = threadIdx.x >> 4;
+            const int c = blockIdx.y * 16 + cx;
+            float f = 0.f;
+            if (c < a.d)
+                for (int64_t i = ry; i < parts; i += 64) f += part(i)[c];
+            __syncthreads();  // the sums before are read
+            lanes[ry][cx] = f;
+            __syncthreads();
+            if (ry == 0 && c < a.d) {
+                for (int i = 1; i < 64; i++) f += lanes[i][cx];
+                a.dgate[s * a.d + c] = f;
+            }
+        } else {
+            for (int c = threadIdx.x & 63; c < a.d; c += 64) {
+                float f = 0.f;
+                int64_t i = 0;
+                for (; i + 4 <= parts; i += 4) {
+                    const float v0 = part(i)[c], v1 = part(i + 1)[c], v2 = part(i + 2)[c], v3 = part(i + 3)[c];
+                    f = (((f + v0) + v1) + v2) + v3;
+                }
+                for (; i < parts; i++) f += part(i)[c];
+                a.dgate[s * a.d + c] = f;
+            }
+        }
     }
 }
 
@@ -397,10 +513,9 @@ __global__ __launch_bounds__(256) void k_resnorm_gates(ResnormArgs a, int64_t lo
 
 struct ResnormPlan {
     int e, p, lg, waves;
-    int R;
-    int64_t slots, per, blocks, places;
+    int64_t per, blocks, places;
 };
-static ResnormPlan resnorm_plan(int dtype, int64_t m, int64_t d, int64_t segs, bool by_segment, bool grad) {
+static ResnormPlan resnorm_plan(int dtype, int64_t m, int64_t d, bool by_segment, bool grad) {
     ResnormPlan p{};
     const int e = vec_width(dtype == TAURUS_F32 ? 4 : 8, d);
     p.e = e >= 4 ? e : 1;
@@ -419,18 +534,11 @@ static ResnormPlan resnorm_plan(int dtype, int64_t m, int64_t d, int64_t segs, b
     }
     const int64_t teams = p.waves ? 1 : 64 >> p.lg, per_block = p.waves ? 1 : 4;
     // workers that the chip holds at once, of at least four rows a team
-    const int64_t resident = p.waves ? 256 * 16 / p.waves : 256 * 16;
+    const int64_t resident = p.waves ? 256 * 16 / p.waves : 256 * (grad ? 12 : 16);
     const int64_t workers = std::max<int64_t>(1, std::min(resident, ceil_div(m, teams * (grad ? 4 : 1))));
-    if (by_segment) {
-        p.R = (int)std::max<int64_t>(32, ceil_div(m, 4 * workers));
-        p.slots = segs > 0 ? unit_slots(m, segs, p.R) : 0;
-    } else {
-        p.R = (int)std::max<int64_t>(ceil_div(m, workers), 1);
-        p.slots = ceil_div(m, p.R);
-    }
-    p.per = std::max<int64_t>(1, ceil_div(p.slots, workers));
-    p.blocks = std::max<int64_t>(1, ceil_div(ceil_div(p.slots, p.per), per_block));
-    p.places = by_segment && m > p.R ? unit_places(m, p.R) : 0;
+    p.per = std::max<int64_t>(1, ceil_div(m, workers));
+    p.blocks = std::max<int64_t>(1, ceil_div(ceil_div(m, p.per), per_block));
+    p.places = grad && by_segment ? 2 * ceil_div(m, p.per) : 0;
     return p;
 }
 struct ResnormWork {
@@ -445,26 +553,29 @@ static ResnormWork resnorm_work(void* work, const ResnormPlan& p, int64_t d) {
     w.bytes = c.bytes();
     return w;
 }
-template <int FT, int ST, int E, int P, int WAVES>
+template <int FT, int ST, int E, int P, int WAVES, bool WHOLE>
 static void resnorm_launch(const ResnormArgs& a, const ResnormPlan& p, bool grad, hipStream_t s) {
     constexpr int THREADS = Workers<WAVES>::THREADS;
     if (!grad) {
-        if constexpr (E * P <= 8) k_resnorm<FT, ST, E, P, WAVES><<<(unsigned)p.blocks, THREADS, 0, s>>>(a, p.lg);
+        if constexpr (E * P <= 8) k_resnorm<FT, ST, E, P, WAVES, WHOLE><<<(unsigned)p.blocks, THREADS, 0, s>>>(a, p.lg);
     } else if constexpr (WAVES != 16) {
         const size_t lds = WAVES ? 0 : (size_t)(256 >> p.lg) * a.d * 4;
-        k_resnorm_grad<FT, ST, E, P, WAVES, E * P <= 8><<<(unsigned)p.blocks, THREADS, lds, s>>>(a, p.lg);
+        if (a.off) k_resnorm_grad<FT, ST, E, P, WAVES, E * P <= 8, true, WHOLE><<<(unsigned)p.blocks, THREADS, lds, s>>>(a, p.lg);
+        else k_resnorm_grad<FT, ST, E, P, WAVES, E * P <= 8, false, WHOLE><<<(unsigned)p.blocks, THREADS, lds, s>>>(a, p.lg);
     }
     TAURUS_CHECK_LAUNCH();
 }
 template <int FT, int ST, int E, int P>
 static void resnorm_waves(const ResnormArgs& a, const ResnormPlan& p, bool grad, hipStream_t s) {
-    if constexpr (E * P > 8) return resnorm_launch<FT, ST, E, P, 8>(a, p, grad, s);  // the gradient of the longest rows
+    if constexpr (E * P > 8) return resnorm_launch<FT, ST, E, P, 8, false>(a, p, grad, s);  // the gradient of the longest rows
     else {
-        if (!p.waves) return resnorm_launch<FT, ST, E, P, 0>(a, p, grad, s);
+        // rows of whole vectors, as many as the team's lanes hold
+        const bool whole = a.d == (E * P) << p.lg;
+        if (!p.waves) return whole ? resnorm_launch<FT, ST, E, P, 0, true>(a, p, grad, s) : resnorm_launch<FT, ST, E, P, 0, false>(a, p, grad, s);
         if constexpr (E * P == 8) {
-            if (p.waves == 4) resnorm_launch<FT, ST, E, P, 4>(a, p, grad, s);
-            else if (p.waves == 8) resnorm_launch<FT, ST, E, P, 8>(a, p, grad, s);
-            else resnorm_launch<FT, ST, E, P, 16>(a, p, grad, s);
+            if (p.waves == 4) resnorm_launch<FT, ST, E, P, 4, false>(a, p, grad, s);
+            else if (p.waves == 8) resnorm_launch<FT, ST, E, P, 8, false>(a, p, grad, s);
+            else resnorm_launch<FT, ST, E, P, 16, false>(a, p, grad, s);
         }
     }
 }
@@ -517,8 +628,8 @@ static NormOf norm_of(int kind, const float* w, const float* b, float eps, const
     if (b) check_ptr(b, 4, what);
     return NormOf{kind, w, b, eps};
 }
-static int64_t resnorm_bytes(int dtype, int64_t m, int64_t d, int64_t segs, bool by_segment) {
-    return resnorm_work(nullptr, resnorm_plan(dtype, m, d, segs, by_segment, true), d).bytes;
+static int64_t resnorm_bytes(int dtype, int64_t m, int64_t d, bool by_segment) {
+    return resnorm_work(nullptr, resnorm_plan(dtype, m, d, by_segment, true), d).bytes;
 }
 
 }  // namespace taurus
@@ -545,7 +656,7 @@ int taurus_residual_norm(const void* x, int32_t x_dtype, int64_t x_stride, const
         check_rows(y, x_dtype, m, d, y_stride, "y");
         if (pre != TAURUS_NORM_NONE) check_rows(h, dtype, m, d, h_stride, "h");
         if (stats) check_ptr(stats, 16, "stats");
-        const ResnormPlan p = resnorm_plan(dtype, m, d, segments, off != nullptr, false);
+        const ResnormPlan p = resnorm_plan(dtype, m, d, off != nullptr, false);
         a.x = x;
         a.f = f;
         a.m = m;
@@ -561,8 +672,6 @@ int taurus_residual_norm(const void* x, int32_t x_dtype, int64_t x_stride, const
         a.ys = y_stride;
         a.hs = h_stride;
         a.stats = reinterpret_cast<float4*>(stats);
-        a.R = p.R;
-        a.slots = p.slots;
         a.per = p.per;
         resnorm(a, p, dtype, x_dtype, false, static_cast<hipStream_t>(stream));
         return (int)TAURUS_OK;
@@ -574,7 +683,7 @@ int64_t taurus_residual_norm_grad_bytes(int32_t dtype, int64_t m, int64_t d, int
     const int rc = guarded_call([&] {
         check_resnorm(dtype, TAURUS_F32, m, d, nullptr, 0, nullptr);
         if (by_segment) check_count(segments, 0, ROWS_MAX, "the number of segments");
-        bytes = resnorm_bytes(dtype, m, d, segments, by_segment != 0);
+        bytes = resnorm_bytes(dtype, m, d, by_segment != 0);
         return (int)TAURUS_OK;
     });
     return rc == TAURUS_OK ? bytes : rc;
@@ -610,8 +719,8 @@ int taurus_residual_norm_grad(const void* grad_y, int64_t grad_y_stride, const v
         if (dgate) check_ptr(dgate, 4, "dgate");
         for (float* p : {dpost_weight, dpost_bias, dpre_weight, dpre_bias})
             if (p) check_ptr(p, 4, "the gradient of a norm's weight or bias");
-        check_work(work, work_bytes, resnorm_bytes(dtype, m, d, segments, off != nullptr), "taurus_residual_norm_grad");
-        const ResnormPlan p = resnorm_plan(dtype, m, d, segments, off != nullptr, true);
+        check_work(work, work_bytes, resnorm_bytes(dtype, m, d, off != nullptr), "taurus_residual_norm_grad");
+        const ResnormPlan p = resnorm_plan(dtype, m, d, off != nullptr, true);
         const ResnormWork w = resnorm_work(work, p, d);
         a.f = f;
         a.m = m;
@@ -624,10 +733,25 @@ int taurus_residual_norm_grad(const void* grad_y, int64_t grad_y_stride, const v
         a.y = const_cast<void*>(y);
         a.ys = y_stride;
         a.stats = reinterpret_cast<float4*>(const_cast<float*>(stats));
+        a.stats_stride = 1;
         a.dh = grad_h;
         a.dhs = grad_h_stride;
         a.dy = grad_y;
         a.dys = grad_y_stride;
+        a.has_dy = grad_y != nullptr;
+        if (!a.has_dy) {
+            a.dy = w.cols;
+            a.dys = 0;
+        }
+        if (!has_pre) {
+            a.y = w.cols;
+            a.dh = w.cols;
+            a.ys = a.dhs = 0;
+        }
+        if (!has_pre && !has_post) {
+            a.stats = reinterpret_cast<float4*>(w.cols);
+            a.stats_stride = 0;
+        }
         a.dx = dx;
         a.dxs = dx_stride;
         a.df = df;
@@ -635,8 +759,6 @@ int taurus_residual_norm_grad(const void* grad_y, int64_t grad_y_stride, const v
         a.dgate = off ? dgate : nullptr;
         a.gate_part = w.gates;
         a.cols = w.cols;
-        a.R = p.R;
-        a.slots = p.slots;
         a.per = p.per;
         float* const outs[] = {off ? nullptr : dgate, dpost_weight, dpost_bias, dpre_weight, dpre_bias};
         int* const places[] = {&a.at_gate, &a.at_post_w, &a.at_post_b, &a.at_pre_w, &a.at_pre_b};
@@ -646,10 +768,9 @@ int taurus_residual_norm_grad(const void* grad_y, int64_t grad_y_stride, const v
             if (outs[i]) j.add(w.cols + *places[i] * d, a.sums * d, p.blocks, d, outs[i]);
         auto s = static_cast<hipStream_t>(stream);
         resnorm(a, p, dtype, y_dtype, true, s);
-        if (a.dgate && p.places) {
-            const int64_t longs = long_count(m, segments, p.R);
-            const int chunks = (int)ceil_div(d, 256);
-            k_resnorm_gates<<<grid_for(longs * chunks), 256, 0, s>>>(a, longs, chunks);
+        if (a.dgate && segments > 0) {
+            if (segments <= 256) k_resnorm_gates<true><<<dim3((unsigned)segments, (unsigned)ceil_div(d, 16)), 1024, 0, s>>>(a);
+            else k_resnorm_gates<false><<<(unsigned)std::min<int64_t>(ceil_div(segments, 4), 65536), 256, 0, s>>>(a);
             TAURUS_CHECK_LAUNCH();
         }
         join_columns(j, s);
