@@ -26,16 +26,19 @@ constexpr float LOWEST = -200.f;
 struct Sums {
     float m, s, t;
 };
-// (l - m), e^ of it; m = -inf (nothing but masked classes so far) counts as 0
-__device__ inline void add_logit(Sums& a, float l, float ref) {
-    const float d = __builtin_elementwise_maximum(l - ref, LOWEST), e = exp_of(d);
+// e^d for d <= 0 as the chip's power of two of d log2(e): the product's rounding
+// makes it off by |d| 1.2e-7 of itself, at most 5e-8 of the sum's 1
+__device__ inline float exp_to_sum(float d) { return __builtin_amdgcn_exp2f(d * 1.44269502f); }
+// l - m and e^ of it; m = -inf (nothing but masked classes so far) counts as 0
+__device__ inline void add_logit(Sums& a, float x, float scale, float ref) {
+    const float d = __builtin_elementwise_maximum(__builtin_fmaf(x, scale, -ref), LOWEST), e = exp_to_sum(d);
     a.s += e;
     a.t = __builtin_fmaf(e, d, a.t);
 }
 __device__ inline float reference(float m) { return m == -INFINITY ? 0.f : m; }
 // moves the sums to a larger maximum
 __device__ inline void raise(Sums& a, float m) {
-    const float d = a.m == -INFINITY ? 0.f : __builtin_elementwise_maximum(a.m - m, LOWEST), e = exp_of(d);
+    const float d = a.m == -INFINITY ? 0.f : __builtin_elementwise_maximum(a.m - m, LOWEST), e = exp_to_sum(d);
     a.t = e * __builtin_fmaf(d, a.s, a.t);
     a.s *= e;
     a.m = m;
@@ -60,19 +63,19 @@ struct LabelArgs {
     float* part_v;       // [m][parts][top]
     int32_t* part_id;
 };
-// A row's results but the alternatives, by one lane, and log S (NaN: the row
-// has no distribution).
+// A row with a NaN or an infinite logit has no distribution.
+__device__ inline bool bad_row(const Sums& a) { return __builtin_isnan(a.s + a.t) || a.m == INFINITY; }
 __device__ inline float log_sum_of(const Sums& a) { return a.s == 0.f ? 0.f : logf(a.s); }
 template <int DT>
 __device__ inline void put_row(const LabelArgs& a, int64_t r, const Sums& s) {
     const bool none = s.s == 0.f;
-    const float log_s = log_sum_of(s), nan = s.s + s.t;  // NaN if either is
-    const bool bad = __builtin_isnan(nan);
+    const bool bad = bad_row(s);
+    const float log_s = log_sum_of(s), nan = __builtin_nanf("");
     if (a.stats) {
         a.stats[2 * r] = bad ? nan : s.m;
         a.stats[2 * r + 1] = bad ? nan : log_s;
     }
-    if (a.entropy) a.entropy[r] = none ? 0.f : log_s - s.t / s.s;
+    if (a.entropy) a.entropy[r] = bad ? nan : none ? 0.f : log_s - s.t / s.s;
     if (a.logp) {
         const int64_t y = a.labels[r];
         float v = 0.f;
@@ -85,78 +88,189 @@ __device__ inline void put_row(const LabelArgs& a, int64_t r, const Sums& s) {
     }
 }
 __device__ inline void put_top(const LabelArgs& a, int64_t r, int i, const Sums& s, float v, int id) {
-    const float nan = s.s + s.t;
-    const bool bad = __builtin_isnan(nan);
-    a.top_logp[r * a.top + i] = bad ? nan : id < 0 ? -INFINITY : (v * a.scale - s.m) - log_sum_of(s);
+    const bool bad = bad_row(s);
+    a.top_logp[r * a.top + i] = bad ? __builtin_nanf("") : id < 0 ? -INFINITY : (v * a.scale - s.m) - log_sum_of(s);
     a.top_ids[r * a.top + i] = bad ? -1 : id;
 }
 
 // ------------------------------------------------------- rows in registers --
 
-// P vectors a lane, 2^lg lanes a row.  The alternatives are found one after
-// another: the largest value left, then the lowest class that has it.
+// A lane's values of a row: P vectors of E.  -inf where there is none.
+template <int E, int P>
+struct RowValues {
+    float v[P][E];
+    int lane, lg;
+    int64_t c;
+    __device__ int at(int p) const { return (int)vec_at<E>(lane + ((int64_t)p << lg), c); }
+    template <int DT>
+    __device__ void load(const void* x, int64_t row_at) {
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int64_t w = lane + ((int64_t)p << lg);
+            if (w * E < c) load_vec<DT, E>(x, row_at + vec_at<E>(w, c), v[p]);
+        }
+#pragma unroll
+        for (int p = 0; p < P; p++) {
+            const int64_t w = lane + ((int64_t)p << lg);
+            const int again = w * E < c ? vec_again<E>(w, c) : E;
+#pragma unroll
+            for (int e = 0; e < E; e++) v[p][e] = e < again ? -INFINITY : v[p][e];
+        }
+    }
+    __device__ float most() const {
+        float m = -INFINITY;
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+            for (int e = 0; e < E; e++) m = fmaxf(m, v[p][e]);
+        return m;
+    }
+};
+__device__ inline bool taken(float x, float scale) { return x * scale > -INFINITY; }
+
+// The alternatives one after another: the largest value left, then the lowest
+// class that has it.
+template <int E, int P>
+__device__ inline void top_in_turn(const LabelArgs& a, int64_t r, bool write, const Sums& s, RowValues<E, P>& x) {
+    for (int i = 0; i < a.top; i++) {
+        const float best = lanes_max(x.most(), x.lg);
+        int id = INT32_MAX;
+#pragma unroll
+        for (int p = P - 1; p >= 0; p--)
+#pragma unroll
+            for (int e = E - 1; e >= 0; e--)
+                if (x.v[p][e] == best) id = x.at(p) + e;
+        id = lanes_min(id, x.lg);
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+            for (int e = 0; e < E; e++)
+                if (x.at(p) + e == id) x.v[p][e] = -INFINITY;
+        if (write) put_top(a, r, i, s, best, taken(best, a.scale) ? id : -1);
+    }
+}
+
+// Whole numbers in the order of the values (zeros of both signs are equal),
+// above ORDER_NONE but for -inf, which has that; and with the class behind it, of
+// equal values the lower one first.
+constexpr uint32_t ORDER_NONE = 0x007fffffu;
+__device__ inline uint32_t order_of(float v) {
+    const uint32_t bits = __float_as_uint(v + 0.f);
+    return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+}
+__device__ inline uint2 key_of(float v, int id) { return make_uint2(~(uint32_t)id, order_of(v)); }
+__device__ inline float value_of(uint2 k) { return __uint_as_float(k.y & 0x80000000u ? k.y & 0x7fffffffu : ~k.y); }
+__device__ inline int class_of(uint2 k) { return (int)~k.x; }
+__device__ inline uint64_t whole_key(uint2 k) { return (uint64_t)k.y << 32 | k.x; }
+
+// All at once, for at least 16 lanes a row and up to 16 alternatives: of the
+// largest values of 16 lanes the top-th is at most the top-th of the row.  The
+// few values from there on go to a list in LDS, a lane one, and each counts
+// those before it.  False (for the whole wave) where a list has over 16.
+constexpr int TOP_LIST = 16;
+template <int N, typename F>
+__device__ inline void rotations(F&& f) {  // f(constant i) for i = 1 .. N
+    if constexpr (N > 0) {
+        rotations<N - 1>(f);
+        f(std::integral_constant<int, N>{});
+    }
+}
+template <int DT, int E, int P>
+__device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const Sums& s, const RowValues<E, P>& x,
+                                   uint2* list) {
+    const float mine = x.most();
+    int above = 0;
+    rotations<15>([&](auto i) {
+        above += __uint_as_float(lane_move<0x120 + decltype(i)::value>(__float_as_uint(mine))) > mine;
+    });
+    // the least of the lane values that have fewer than `top` above them; rows
+    // of 16 lanes by themselves, the largest of theirs
+    float least = above < a.top ? mine : INFINITY;
+    least = lanes_of<4>(least, [](float p, float q) { return fminf(p, q); });
+    if (x.lg > 4) least = lane_step<4>(least, [](float p, float q) { return fmaxf(p, q); });
+    if (x.lg > 5) least = lane_step<5>(least, [](float p, float q) { return fmaxf(p, q); });
+    uint32_t some = 0;  // which of this lane's values, the first in the highest bit
+#pragma unroll
+    for (int p = 0; p < P; p++)
+#pragma unroll
+        for (int e = 0; e < E; e++) some = 2 * some + (x.v[p][e] >= least && x.v[p][e] > -INFINITY);
+    const int n = __popc(some);
+    int upto = n;  // over the row's lanes up to this one
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+        const int v = __shfl_up(upto, o, 16);
+        if ((x.lane & 15) >= o) upto += v;
+    }
+    if (x.lg > 4) {
+        const int v = __shfl(upto, (threadIdx.x & 63 & ~31) + 15, 64);
+        if (x.lane & 16) upto += v;
+    }
+    if (x.lg > 5) {
+        const int v = __shfl(upto, 31, 64);
+        if (x.lane & 32) upto += v;
+    }
+    const int count = __shfl(upto, (threadIdx.x & 63) | ((1 << x.lg) - 1), 64);
+    if (__any(count > TOP_LIST)) return false;
+    uint2* to = list + ((threadIdx.x & 63) >> x.lg) * TOP_LIST;
+    if (x.lane < TOP_LIST) to[x.lane] = make_uint2(0, 0);  // below every key
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    int place = upto - n;
+    while (some) {
+        const int i = P * E - 32 + __clz(some);  // the first left
+        some &= ~(1u << (P * E - 1 - i));
+        const int id = (int)vec_at<E>(x.lane + ((int64_t)(i / E) << x.lg), x.c) + i % E;
+        float v[1];
+        load_vec<DT, 1>(a.x, r * a.xs + id, v);
+        to[place++] = key_of(v[0], id);
+    }
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    const uint2 key = to[x.lane & (TOP_LIST - 1)];
+    const uint64_t whole = (uint64_t)key.y << 32 | key.x;
+    int rank = 0;
+    rotations<15>([&](auto i) {
+        constexpr int CTRL = 0x120 + decltype(i)::value;
+        rank += ((uint64_t)lane_move<CTRL>(key.y) << 32 | lane_move<CTRL>(key.x)) > whole;
+    });
+    if (in && x.lane < TOP_LIST) {
+        const float v = value_of(key);
+        if (whole && rank < a.top) put_top(a, r, rank, s, v, taken(v, a.scale) ? class_of(key) : -1);
+        if (x.lane >= count && x.lane < a.top) put_top(a, r, x.lane, s, -INFINITY, -1);  // too few unmasked
+    }
+    __builtin_amdgcn_wave_barrier();
+    return true;
+}
+
+// P vectors a lane, 2^lg lanes a row.
 template <int DT, int E, int P>
 __global__ __launch_bounds__(256) void k_labels_rows(LabelArgs a, int lg) {
+    __shared__ uint2 lists[4][4 * TOP_LIST];
     const int lane = threadIdx.x & ((1 << lg) - 1);
     const int64_t step = (int64_t)gridDim.x * (256 >> lg);
     // all lanes of a wave go round together: rows past the last are repeated
     for (int64_t r0 = (int64_t)blockIdx.x * (256 >> lg); r0 < a.m; r0 += step) {
         const int64_t mine = r0 + (threadIdx.x >> lg), r = min(mine, a.m - 1);
-        float x[P][E];
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int64_t w = lane + ((int64_t)p << lg);
-            if (w * E < a.c) load_vec<DT, E>(a.x, r * a.xs + vec_at<E>(w, a.c), x[p]);
-        }
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int64_t w = lane + ((int64_t)p << lg);
-            const int again = w * E < a.c ? vec_again<E>(w, a.c) : E;
-#pragma unroll
-            for (int e = 0; e < E; e++)
-                if (e < again) x[p][e] = -INFINITY;
-        }
-        Sums s{-INFINITY, 0.f, 0.f};
-#pragma unroll
-        for (int p = 0; p < P; p++)
-#pragma unroll
-            for (int e = 0; e < E; e++) s.m = fmaxf(s.m, x[p][e] * a.scale);
-        s.m = lanes_max(s.m, lg);
+        const bool in = mine < a.m;
+        RowValues<E, P> x;
+        x.lane = lane;
+        x.lg = lg;
+        x.c = a.c;
+        x.template load<DT>(a.x, r * a.xs);
+        Sums s{lanes_max(x.most() * a.scale, lg), 0.f, 0.f};
         const float ref = reference(s.m);
 #pragma unroll
         for (int p = 0; p < P; p++)
 #pragma unroll
-            for (int e = 0; e < E; e++) add_logit(s, x[p][e] * a.scale, ref);
-        s.s = lanes_sum(s.s, lg);
-        s.t = lanes_sum(s.t, lg);
-        const bool write = mine < a.m && lane == 0;
-        if (write) put_row<DT>(a, r, s);
-        for (int i = 0; i < a.top; i++) {
-            float best = -INFINITY;
-#pragma unroll
-            for (int p = 0; p < P; p++)
-#pragma unroll
-                for (int e = 0; e < E; e++) best = fmaxf(best, x[p][e]);
-            best = lanes_max(best, lg);
-            int id = INT32_MAX;
-#pragma unroll
-            for (int p = P - 1; p >= 0; p--) {
-                const int at = (int)vec_at<E>(lane + ((int64_t)p << lg), a.c);
-#pragma unroll
-                for (int e = E - 1; e >= 0; e--)
-                    if (x[p][e] == best) id = at + e;
-            }
-            id = lanes_min(id, lg);
-            const bool some = best * a.scale > -INFINITY;
-#pragma unroll
-            for (int p = 0; p < P; p++) {
-                const int at = (int)vec_at<E>(lane + ((int64_t)p << lg), a.c);
-#pragma unroll
-                for (int e = 0; e < E; e++)
-                    if (at + e == id) x[p][e] = -INFINITY;
-            }
-            if (write) put_top(a, r, i, s, best, some ? id : -1);
-        }
+            for (int e = 0; e < E; e++) add_logit(s, x.v[p][e], a.scale, ref);
+        const float2 st = lanes_sum2({s.s, s.t}, lg);
+        s.s = st.x;
+        s.t = st.y;
+        if (in && lane == 0) put_row<DT>(a, r, s);
+        if (!a.top) continue;
+        if constexpr (E * P == 16)
+            if (lg >= 4 && a.top <= TOP_LIST && top_at_once<DT, E, P>(a, r, in, s, x, lists[threadIdx.x >> 6])) continue;
+        top_in_turn<E, P>(a, r, in && lane == 0, s, x);
     }
 }
 
@@ -195,83 +309,219 @@ struct TopList {
     }
 };
 
-// A team (a wave, or the workgroup) a part of a row.
+// Values that wait in a wave's lanes, N each: in order (ORDER_NONE for those
+// that are no alternatives), and their classes.
+template <int N>
+struct Waiting {
+    uint32_t o[N];
+    int id[N];
+    __device__ void put(int i, float v, int jd, bool is) {
+        o[i] = is ? max(order_of(v), ORDER_NONE) : ORDER_NONE;
+        id[i] = jd;
+    }
+    __device__ int count(uint32_t from) const {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; i++) n += __popcll(__ballot(o[i] >= from));
+        return n;
+    }
+    // The keys from `from` on to `room`, `places` of them from the base-th.
+    __device__ void gather(uint32_t from, uint2* room, int base, int places) const {
+        int n = -base;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const bool mine = o[i] >= from;
+            const uint64_t all = __ballot(mine);
+            const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+            if (mine && at >= 0 && at < places) room[at] = make_uint2(~(uint32_t)id[i], o[i]);
+            n += __popcll(all);
+        }
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    }
+};
+constexpr int ROOM = 128;  // keys that a wave ranks at once
+// Adds to the list the values from `from` on, 64 at a time (in one piece of
+// code: a short launch waits for every further one).
+template <int N>
+__device__ inline void offer_from(TopList& list, const Waiting<N>& x, uint32_t from, uint2* room) {
+    const int lane = threadIdx.x & 63, n = x.count(from);
+    for (int base = 0; base < n; base += 64) {
+        x.gather(from, room, base, 64);
+        const bool in = lane < n - base;
+        const uint2 key = room[lane];
+        list.offer(in ? value_of(key) : -INFINITY, in ? class_of(key) : 0);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+// The list of the waiting values alone, all at once.  Of the largest of the 64
+// lanes the top-th is at most the top-th of all; where more than ROOM values are
+// that large, halving finds a number that fewer reach.  These each count those
+// before them.  `room` is the wave's.
+template <int N>
+__device__ inline TopList top_of_wave(const Waiting<N>& x, int top, uint2* room) {
+    TopList list(top);
+    const int lane = threadIdx.x & 63;
+    uint32_t mine = x.o[0];
+#pragma unroll
+    for (int i = 1; i < N; i++) mine = max(mine, x.o[i]);
+    int above = 0;
+#pragma unroll 4
+    for (int i = 0; i < 64; i++) above += (uint32_t)__builtin_amdgcn_readlane((int)mine, i) > mine;
+    auto least_of = [](uint32_t p, uint32_t q) { return min(p, q); };
+    auto most_of = [](uint32_t p, uint32_t q) { return max(p, q); };
+    uint32_t from = (uint32_t)__builtin_amdgcn_readfirstlane(
+        (int)max(lanes_of<6>(above < top ? mine : 0xffffffffu, least_of), ORDER_NONE + 1));
+    int n = x.count(from);
+    if (n > ROOM) {
+        uint32_t past = (uint32_t)__builtin_amdgcn_readfirstlane((int)lanes_of<6>(mine, most_of)) + 1;  // none reaches it
+        while (n > ROOM && past - from > 1) {
+            const uint32_t mid = from + (past - from) / 2;
+            const int c = x.count(mid);
+            if (c >= top) {
+                from = mid;
+                n = c;
+            } else {
+                past = mid;
+            }
+        }
+        if (n > ROOM) {  // equal values
+            offer_from(list, x, from, room);
+            return list;
+        }
+    }
+    x.gather(from, room, 0, ROOM);
+    const uint2 none = make_uint2(0, 0), a = lane < n ? room[lane] : none, b = lane + 64 < n ? room[lane + 64] : none;
+    const uint64_t ka = whole_key(a), kb = whole_key(b);
+    int ra = 0, rb = 0;
+#pragma unroll 1
+    for (int i = 0; i < n; i++) {
+        const uint64_t other = whole_key(room[i]);
+        ra += other > ka;
+        rb += other > kb;
+    }
+    __builtin_amdgcn_wave_barrier();
+    if (lane < n && ra < 64) room[ra] = a;
+    if (lane + 64 < n && rb < 64) room[rb] = b;
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+    if (lane < n && lane < top) {
+        const uint2 k = room[lane];
+        list.v = value_of(k);
+        list.id = class_of(k);
+    }
+    __builtin_amdgcn_wave_barrier();
+    list.last = lane_value(list.v, top - 1);
+    list.last_id = __builtin_amdgcn_readlane(list.id, top - 1);
+    return list;
+}
+// The lists of a workgroup's four waves, one behind another in LDS.
+struct Lists4 {
+    uint2 k[4 * TOP_MOST];
+    __device__ void put(int wave, const TopList& list) {
+        const int lane = threadIdx.x & 63;
+        if (lane < list.top) k[wave * list.top + lane] = list.id < 0 ? make_uint2(0, ORDER_NONE) : key_of(list.v, list.id);
+    }
+    __device__ TopList all(int top, uint2* room) const {
+        Waiting<4> x;
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int at = i * 64 + (threadIdx.x & 63);
+            const uint2 key = at < 4 * top ? k[at] : make_uint2(0, ORDER_NONE);
+            x.o[i] = key.y;
+            x.id[i] = class_of(key);
+        }
+        return top_of_wave(x, top, room);
+    }
+};
+struct Sums4 {
+    float v[4][3];
+    __device__ void put(int wave, const Sums& s) {
+        v[wave][0] = s.m;
+        v[wave][1] = s.s;
+        v[wave][2] = s.t;
+    }
+    __device__ Sums all() const {
+        Sums s{v[0][0], v[0][1], v[0][2]};
+        for (int i = 1; i < 4; i++) join(s, Sums{v[i][0], v[i][1], v[i][2]});
+        return s;
+    }
+    static __device__ void join(Sums& s, Sums o) {
+        const float m = fmaxf(s.m, o.m);
+        raise(s, m);
+        raise(o, m);
+        s.s += o.s;
+        s.t += o.t;
+    }
+};
+
+// A team (a wave, or the workgroup of four) a part of a row.
 template <int DT, int E, int TEAM, bool TOP>
 __global__ __launch_bounds__(256) void k_labels_stream(LabelArgs a) {
-    constexpr int TEAMS = 256 / TEAM, WAVES = TEAM / 64, U = 4;
-    __shared__ float sums[WAVES > 1 ? WAVES : 1][3];
-    __shared__ float list_v[WAVES > 1 ? WAVES : 1][64];
-    __shared__ int list_id[WAVES > 1 ? WAVES : 1][64];
-    const int tid = threadIdx.x % TEAM, wave = tid >> 6, lane = threadIdx.x & 63;
+    constexpr int TEAMS = 256 / TEAM, U = 16 / E;
+    __shared__ Sums4 sums;
+    __shared__ Lists4 lists;
+    __shared__ uint2 room[4][ROOM];
+    const int tid = threadIdx.x % TEAM, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t items = a.m * a.parts;
     for (int64_t item = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM; item < items;
          item += (int64_t)gridDim.x * TEAMS) {
-        const int64_t r = item / a.parts, part = item - r * a.parts;
+        // one part a row, or few items
+        const int64_t r = a.parts == 1 ? item : (uint32_t)item / (uint32_t)a.parts, part = item - r * a.parts;
         // the part's classes, a whole number of vectors but for the row's last
         const int64_t w0 = part * a.per, w1 = min(w0 + a.per, (a.c + E - 1) / E);
         Sums s{-INFINITY, 0.f, 0.f};
         TopList list(a.top);
         for (int64_t w = w0; w < w1; w += TEAM * U) {
-            float x[U][E];
+            float x[U * E];
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 const int64_t v = w + u * TEAM + tid;
-                if (v < w1) load_vec<DT, E>(a.x, r * a.xs + vec_at<E>(v, a.c), x[u]);
+                float f[E];
+                if (v < w1) load_vec<DT, E>(a.x, r * a.xs + vec_at<E>(v, a.c), f);
+#pragma unroll
+                for (int e = 0; e < E; e++) x[u * E + e] = f[e];
             }
-            float most = -INFINITY, best[U];
+            float best = -INFINITY;
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 const int64_t v = w + u * TEAM + tid;
                 const int again = v < w1 ? vec_again<E>(v, a.c) : E;
-                best[u] = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < E; e++) {
-                    if (e < again) x[u][e] = -INFINITY;
-                    best[u] = fmaxf(best[u], x[u][e]);
+                    x[u * E + e] = e < again ? -INFINITY : x[u * E + e];
+                    best = fmaxf(best, x[u * E + e]);
                 }
-                most = fmaxf(most, best[u] * a.scale);
             }
+            const float most = best * a.scale;
             if (most > s.m) raise(s, most);
             const float ref = reference(s.m);
 #pragma unroll
-            for (int u = 0; u < U; u++)
-#pragma unroll
-                for (int e = 0; e < E; e++) add_logit(s, x[u][e] * a.scale, ref);
+            for (int i = 0; i < U * E; i++) add_logit(s, x[i], a.scale, ref);
             if constexpr (TOP) {
+                const bool first = w == w0;
+                if (!first && !__ballot(best >= list.last && best > -INFINITY)) continue;
+                Waiting<U * E> wait;
 #pragma unroll
                 for (int u = 0; u < U; u++) {
-                    if (!__ballot(best[u] >= list.last && best[u] > -INFINITY)) continue;
                     const int at = (int)vec_at<E>(w + u * TEAM + tid, a.c);
 #pragma unroll
-                    for (int e = 0; e < E; e++)
-                        list.offer(x[u][e] * a.scale > -INFINITY ? x[u][e] : -INFINITY, at + e);
+                    for (int e = 0; e < E; e++) wait.put(u * E + e, x[u * E + e], at + e, taken(x[u * E + e], a.scale));
                 }
+                // later values equal to the last are of higher classes, or not
+                if (first) list = top_of_wave(wait, a.top, room[wave]);
+                else offer_from(list, wait, max(order_of(list.last), ORDER_NONE + 1), room[wave]);
             }
         }
         s = lanes_joined(s, 6);
-        if constexpr (WAVES > 1) {
+        if constexpr (TEAM == 256) {
             __syncthreads();  // the item before is read
-            if (lane == 0) {
-                sums[wave][0] = s.m;
-                sums[wave][1] = s.s;
-                sums[wave][2] = s.t;
-            }
-            if constexpr (TOP) {
-                list_v[wave][lane] = list.v;
-                list_id[wave][lane] = list.id;
-            }
+            if (lane == 0) sums.put(wave, s);
+            if constexpr (TOP) lists.put(wave, list);
             __syncthreads();
             if (wave > 0) continue;
-            for (int i = 1; i < WAVES; i++) {
-                Sums o{sums[i][0], sums[i][1], sums[i][2]};
-                const float m = fmaxf(s.m, o.m);
-                raise(s, m);
-                raise(o, m);
-                s.s += o.s;
-                s.t += o.t;
-                if constexpr (TOP)
-                    list.offer(lane < a.top ? list_v[i][lane] : -INFINITY, list_id[i][lane]);
-            }
+            s = sums.all();
+            if constexpr (TOP) list = lists.all(a.top, room[0]);
         }
         if (a.parts > 1) {
             if (lane == 0) {
@@ -291,31 +541,43 @@ __global__ __launch_bounds__(256) void k_labels_stream(LabelArgs a) {
     }
 }
 
-// The parts of a row joined, a wave a row.
+// The parts of a row joined, a workgroup a row.
 template <int DT>
-__global__ __launch_bounds__(64) void k_labels_join(LabelArgs a) {
-    const int lane = threadIdx.x;
+__global__ __launch_bounds__(256) void k_labels_join(LabelArgs a) {
+    __shared__ Sums4 sums;
+    __shared__ Lists4 lists;
+    __shared__ uint2 room[4][ROOM];
+    constexpr int N = 8;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     for (int64_t r = blockIdx.x; r < a.m; r += gridDim.x) {
         Sums s{-INFINITY, 0.f, 0.f};
-        for (int64_t i = lane; i < a.parts; i += 64) {
+        for (int64_t i = threadIdx.x; i < a.parts; i += 256) {
             const float* p = a.part_sums + (r * a.parts + i) * 3;
-            Sums o{p[0], p[1], p[2]};
-            const float m = fmaxf(s.m, o.m);
-            raise(s, m);
-            raise(o, m);
-            s.s += o.s;
-            s.t += o.t;
+            Sums4::join(s, Sums{p[0], p[1], p[2]});
         }
         s = lanes_joined(s, 6);
-        if (lane == 0) put_row<DT>(a, r, s);
-        if (!a.top) continue;
         TopList list(a.top);
         const int64_t n = a.parts * a.top, at = r * n;
-        for (int64_t i = 0; i < n; i += 64) {
-            const bool in = i + lane < n;
-            const float v = in ? a.part_v[at + i + lane] : -INFINITY;
-            list.offer(v, in ? a.part_id[at + i + lane] : 0);
+        for (int64_t i = 0; i < n; i += 256 * N) {
+            Waiting<N> x;
+#pragma unroll
+            for (int k = 0; k < N; k++) {
+                const int64_t j = i + k * 256 + threadIdx.x;
+                const int id = j < n ? a.part_id[at + j] : -1;
+                x.put(k, j < n ? a.part_v[at + j] : 0.f, id, id >= 0);
+            }
+            if (i == 0) list = top_of_wave(x, a.top, room[wave]);
+            else offer_from(list, x, max(order_of(list.last), ORDER_NONE + 1), room[wave]);
         }
+        __syncthreads();  // the row before is read
+        if (lane == 0) sums.put(wave, s);
+        lists.put(wave, list);
+        __syncthreads();
+        if (wave > 0) continue;
+        s = sums.all();
+        if (lane == 0) put_row<DT>(a, r, s);
+        if (!a.top) continue;
+        list = lists.all(a.top, room[0]);
         if (lane < a.top) put_top(a, r, lane, s, list.v, list.id);
     }
 }
@@ -437,7 +699,7 @@ static void labels_e(const LabelArgs& a, const LabelPlan& p, hipStream_t s) {
         }
         TAURUS_CHECK_LAUNCH();
         if (a.parts > 1) {
-            k_labels_join<DT><<<(unsigned)std::min<int64_t>(a.m, 8192), 64, 0, s>>>(a);
+            k_labels_join<DT><<<(unsigned)std::min<int64_t>(a.m, 8192), 256, 0, s>>>(a);
             TAURUS_CHECK_LAUNCH();
         }
     }
