@@ -605,7 +605,8 @@ int taurus_residual_norm_grad(const void* grad_y, int64_t grad_y_stride, const v
  * 2^22), M their largest, S = sum of e^(l - M) and log p_j = (l_j - M) - log S,
  *     logp[r]    = log p_y, y = labels[r]  (0 if y is outside [0, c): -1 pads)
  *     entropy[r] = -sum over j of p_j log p_j
- *     stats[r]   = M, log S                float[m][2], for the gradient
+ *     stats[r]   = M, log S                float[m][2], 8-byte aligned, for the
+ *                                          gradient
  *     top_ids[r], top_logp[r]              int32, float[m][top]: the `top` (at
  *                  most 64 and c) classes of the largest logits and their log
  *                  probabilities, largest first, of equal ones the lower class

@@ -63,56 +63,58 @@ struct LabelArgs {
     float* part_v;       // [m][parts][top]
     int32_t* part_id;
 };
-// A row with a NaN or an infinite logit has no distribution.
-__device__ inline bool bad_row(const Sums& a) { return __builtin_isnan(a.s + a.t) || a.m == INFINITY; }
-__device__ inline float log_sum_of(const Sums& a) { return a.s == 0.f ? 0.f : logf(a.s); }
-template <int DT>
-__device__ inline void put_row(const LabelArgs& a, int64_t r, const Sums& s) {
-    const bool none = s.s == 0.f;
-    const bool bad = bad_row(s);
-    const float log_s = log_sum_of(s), nan = __builtin_nanf("");
-    if (a.stats) {
-        a.stats[2 * r] = bad ? nan : s.m;
-        a.stats[2 * r + 1] = bad ? nan : log_s;
+// What a row's results come from.  A row with a NaN or an infinite logit has no
+// distribution.
+struct Row {
+    float most, log_s, spread;  // M, log S, T / S
+    bool bad, none;             // no distribution; nothing but masked classes
+    __device__ explicit Row(const Sums& a)
+        : most(a.m), bad(__builtin_isnan(a.s + a.t) || a.m == INFINITY), none(a.s == 0.f) {
+        log_s = none ? 0.f : logf(a.s);
+        spread = none ? 0.f : a.t / a.s;
     }
-    if (a.entropy) a.entropy[r] = bad ? nan : none ? 0.f : log_s - s.t / s.s;
-    if (a.logp) {
-        const int64_t y = a.labels[r];
-        float v = 0.f;
-        if (y >= 0 && y < a.c) {
-            float x[1];
-            load_vec<DT, 1>(a.x, r * a.xs + y, x);
-            v = bad ? nan : none ? -INFINITY : (x[0] * a.scale - s.m) - log_s;
-        }
-        a.logp[r] = v;
+    // log probability of a class of logit x
+    __device__ float logp(float x, float scale) const {
+        return bad ? __builtin_nanf("") : none ? -INFINITY : (x * scale - most) - log_s;
     }
-}
-__device__ inline void put_top(const LabelArgs& a, int64_t r, int i, const Sums& s, float v, int id) {
-    const bool bad = bad_row(s);
-    a.top_logp[r * a.top + i] = bad ? __builtin_nanf("") : id < 0 ? -INFINITY : (v * a.scale - s.m) - log_sum_of(s);
-    a.top_ids[r * a.top + i] = bad ? -1 : id;
-}
+    // all but the alternatives, by one lane; x: the label's logit
+    __device__ void put(const LabelArgs& a, int64_t r, bool known, float x) const {
+        const float nan = __builtin_nanf("");
+        if (a.stats) *reinterpret_cast<float2*>(a.stats + 2 * r) = make_float2(bad ? nan : most, bad ? nan : log_s);
+        if (a.entropy) a.entropy[r] = bad ? nan : log_s - spread;
+        if (a.logp) a.logp[r] = known ? logp(x, a.scale) : 0.f;
+    }
+    template <int DT>
+    __device__ void put(const LabelArgs& a, int64_t r) const {
+        const int64_t y = a.logp ? a.labels[r] : -1;
+        const bool known = y >= 0 && y < a.c;
+        float x[1] = {0.f};
+        if (known) load_vec<DT, 1>(a.x, r * a.xs + y, x);
+        put(a, r, known, x[0]);
+    }
+    // the i-th alternative (id -1: there is none)
+    __device__ void put_top(const LabelArgs& a, int64_t r, int i, float x, int id) const {
+        a.top_logp[r * a.top + i] = bad ? __builtin_nanf("") : id < 0 ? -INFINITY : logp(x, a.scale);
+        a.top_ids[r * a.top + i] = bad ? -1 : id;
+    }
+};
 
 // ------------------------------------------------------- rows in registers --
 
-// A lane's values of a row: P vectors of E.  -inf where there is none.
-template <int E, int P>
+// A lane's values of a row: P vectors of E, 2^LG lanes a row.  -inf where there
+// is none, and for a value that the vector before has too.
+template <int E, int P, int LG>
 struct RowValues {
     float v[P][E];
-    int lane, lg;
+    int lane;
     int64_t c;
-    __device__ int at(int p) const { return (int)vec_at<E>(lane + ((int64_t)p << lg), c); }
+    __device__ int at(int p) const { return (int)vec_at<E>(lane + (p << LG), c); }
     template <int DT>
-    __device__ void load(const void* x, int64_t row_at) {
+    __device__ void take(const Stored<DT, E> (&s)[P]) {
 #pragma unroll
         for (int p = 0; p < P; p++) {
-            const int64_t w = lane + ((int64_t)p << lg);
-            if (w * E < c) load_vec<DT, E>(x, row_at + vec_at<E>(w, c), v[p]);
-        }
-#pragma unroll
-        for (int p = 0; p < P; p++) {
-            const int64_t w = lane + ((int64_t)p << lg);
-            const int again = w * E < c ? vec_again<E>(w, c) : E;
+            decode<DT, E>(s[p], v[p]);
+            const int w = lane + (p << LG), again = w * E < c ? vec_again<E>(w, c) : E;
 #pragma unroll
             for (int e = 0; e < E; e++) v[p][e] = e < again ? -INFINITY : v[p][e];
         }
@@ -125,28 +127,40 @@ struct RowValues {
             for (int e = 0; e < E; e++) m = fmaxf(m, v[p][e]);
         return m;
     }
+    // the row in LDS, by class
+    __device__ void lay_out(float* row) const {
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+            for (int e = 0; e < E; e++) row[(lane + (p << LG)) * E + e] = v[p][e];
+    }
+    // where it has class i: the last vector ends where the row does
+    __device__ int place(int i) const {
+        const int last = (int)((c - 1) / E) * E;
+        return i < last ? i : last + i - (int)(c - E);
+    }
 };
 __device__ inline bool taken(float x, float scale) { return x * scale > -INFINITY; }
 
 // The alternatives one after another: the largest value left, then the lowest
 // class that has it.
-template <int E, int P>
-__device__ inline void top_in_turn(const LabelArgs& a, int64_t r, bool write, const Sums& s, RowValues<E, P>& x) {
+template <int E, int P, int LG>
+__device__ inline void top_in_turn(const LabelArgs& a, int64_t r, bool write, const Row& row, RowValues<E, P, LG>& x) {
     for (int i = 0; i < a.top; i++) {
-        const float best = lanes_max(x.most(), x.lg);
+        const float best = lanes_of<LG>(x.most(), [](float p, float q) { return fmaxf(p, q); });
         int id = INT32_MAX;
 #pragma unroll
         for (int p = P - 1; p >= 0; p--)
 #pragma unroll
             for (int e = E - 1; e >= 0; e--)
                 if (x.v[p][e] == best) id = x.at(p) + e;
-        id = lanes_min(id, x.lg);
+        id = lanes_of<LG>(id, [](int p, int q) { return min(p, q); });
 #pragma unroll
         for (int p = 0; p < P; p++)
 #pragma unroll
             for (int e = 0; e < E; e++)
                 if (x.at(p) + e == id) x.v[p][e] = -INFINITY;
-        if (write) put_top(a, r, i, s, best, taken(best, a.scale) ? id : -1);
+        if (write) row.put_top(a, r, i, best, taken(best, a.scale) ? id : -1);
     }
 }
 
@@ -175,9 +189,9 @@ __device__ inline void rotations(F&& f) {  // f(constant i) for i = 1 .. N
         f(std::integral_constant<int, N>{});
     }
 }
-template <int DT, int E, int P>
-__device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const Sums& s, const RowValues<E, P>& x,
-                                   uint2* list) {
+template <int E, int P, int LG>
+__device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const Row& row,
+                                   const RowValues<E, P, LG>& x, const float* laid_out, uint2* list) {
     const float mine = x.most();
     int above = 0;
     rotations<15>([&](auto i) {
@@ -185,33 +199,34 @@ __device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const
     });
     // the least of the lane values that have fewer than `top` above them; rows
     // of 16 lanes by themselves, the largest of theirs
-    float least = above < a.top ? mine : INFINITY;
-    least = lanes_of<4>(least, [](float p, float q) { return fminf(p, q); });
-    if (x.lg > 4) least = lane_step<4>(least, [](float p, float q) { return fmaxf(p, q); });
-    if (x.lg > 5) least = lane_step<5>(least, [](float p, float q) { return fmaxf(p, q); });
+    float least = lanes_of<4>(above < a.top ? mine : INFINITY, [](float p, float q) { return fminf(p, q); });
+    if constexpr (LG > 4) least = lane_step<4>(least, [](float p, float q) { return fmaxf(p, q); });
+    if constexpr (LG > 5) least = lane_step<5>(least, [](float p, float q) { return fmaxf(p, q); });
     uint32_t some = 0;  // which of this lane's values, the first in the highest bit
 #pragma unroll
     for (int p = 0; p < P; p++)
 #pragma unroll
         for (int e = 0; e < E; e++) some = 2 * some + (x.v[p][e] >= least && x.v[p][e] > -INFINITY);
+    auto add = [](int p, int q) { return p + q; };
     const int n = __popc(some);
-    int upto = n;  // over the row's lanes up to this one
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) {
-        const int v = __shfl_up(upto, o, 16);
-        if ((x.lane & 15) >= o) upto += v;
+    int upto = n;  // over the lanes up to this one: moved up in 16 by 1, 2, 4, 8
+    upto += (int)lane_move<0x111>((uint32_t)upto);
+    upto += (int)lane_move<0x112>((uint32_t)upto);
+    upto += (int)lane_move<0x114>((uint32_t)upto);
+    upto += (int)lane_move<0x118>((uint32_t)upto);
+    int count = lanes_of<4>(n, add);
+    if constexpr (LG > 4) {
+        const int both = lane_step<4>(count, add);
+        if (x.lane & 16) upto += both - count;
+        count = both;
     }
-    if (x.lg > 4) {
-        const int v = __shfl(upto, (threadIdx.x & 63 & ~31) + 15, 64);
-        if (x.lane & 16) upto += v;
+    if constexpr (LG > 5) {
+        const int both = lane_step<5>(count, add);
+        if (x.lane & 32) upto += both - count;
+        count = both;
     }
-    if (x.lg > 5) {
-        const int v = __shfl(upto, 31, 64);
-        if (x.lane & 32) upto += v;
-    }
-    const int count = __shfl(upto, (threadIdx.x & 63) | ((1 << x.lg) - 1), 64);
     if (__any(count > TOP_LIST)) return false;
-    uint2* to = list + ((threadIdx.x & 63) >> x.lg) * TOP_LIST;
+    uint2* to = list + ((threadIdx.x & 63) >> LG) * TOP_LIST;
     if (x.lane < TOP_LIST) to[x.lane] = make_uint2(0, 0);  // below every key
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
@@ -219,58 +234,81 @@ __device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const
     while (some) {
         const int i = P * E - 32 + __clz(some);  // the first left
         some &= ~(1u << (P * E - 1 - i));
-        const int id = (int)vec_at<E>(x.lane + ((int64_t)(i / E) << x.lg), x.c) + i % E;
-        float v[1];
-        load_vec<DT, 1>(a.x, r * a.xs + id, v);
-        to[place++] = key_of(v[0], id);
+        const int w = x.lane + ((i / E) << LG), id = (int)vec_at<E>(w, x.c) + i % E;
+        to[place++] = key_of(laid_out[w * E + i % E], id);
     }
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     const uint2 key = to[x.lane & (TOP_LIST - 1)];
-    const uint64_t whole = (uint64_t)key.y << 32 | key.x;
+    const uint64_t whole = whole_key(key);
     int rank = 0;
     rotations<15>([&](auto i) {
         constexpr int CTRL = 0x120 + decltype(i)::value;
-        rank += ((uint64_t)lane_move<CTRL>(key.y) << 32 | lane_move<CTRL>(key.x)) > whole;
+        rank += whole_key(make_uint2(lane_move<CTRL>(key.x), lane_move<CTRL>(key.y))) > whole;
     });
     if (in && x.lane < TOP_LIST) {
         const float v = value_of(key);
-        if (whole && rank < a.top) put_top(a, r, rank, s, v, taken(v, a.scale) ? class_of(key) : -1);
-        if (x.lane >= count && x.lane < a.top) put_top(a, r, x.lane, s, -INFINITY, -1);  // too few unmasked
+        if (whole && rank < a.top) row.put_top(a, r, rank, v, taken(v, a.scale) ? class_of(key) : -1);
+        if (x.lane >= count && x.lane < a.top) row.put_top(a, r, x.lane, -INFINITY, -1);  // too few unmasked
     }
     __builtin_amdgcn_wave_barrier();
     return true;
 }
 
-// P vectors a lane, 2^lg lanes a row.
-template <int DT, int E, int P>
-__global__ __launch_bounds__(256) void k_labels_rows(LabelArgs a, int lg) {
-    __shared__ uint2 lists[4][4 * TOP_LIST];
-    const int lane = threadIdx.x & ((1 << lg) - 1);
-    const int64_t step = (int64_t)gridDim.x * (256 >> lg);
+// P vectors a lane, 2^LG lanes a row.  The next rows are on their way while the
+// wave works on these; what it reads of a row by class (the label, the
+// alternatives) it reads from LDS.
+template <int DT, int E, int P, int LG>
+__global__ __launch_bounds__(256, 4) void k_labels_rows(LabelArgs a) {
+    __shared__ uint2 lists[4][LG >= 4 ? (64 >> LG) * TOP_LIST : 1];
+    __shared__ __align__(16) float rows[4][64 * P * E];
+    const int wave = threadIdx.x >> 6;
+    float* laid_out = rows[wave] + ((threadIdx.x & 63) >> LG << LG) * P * E;
+    RowValues<E, P, LG> x;
+    x.lane = threadIdx.x & ((1 << LG) - 1);
+    x.c = a.c;
+    const int64_t step = (int64_t)gridDim.x * (256 >> LG);
+    Stored<DT, E> next[P];
+    int next_y = -1;
+    auto bring = [&](int64_t r) {
+        r = min(r, a.m - 1);
+#pragma unroll
+        for (int p = 0; p < P; p++) next[p] = load_stored<DT, E>(a.x, r * a.xs + x.at(p));
+        if (a.logp) next_y = a.labels[r];
+    };
     // all lanes of a wave go round together: rows past the last are repeated
-    for (int64_t r0 = (int64_t)blockIdx.x * (256 >> lg); r0 < a.m; r0 += step) {
-        const int64_t mine = r0 + (threadIdx.x >> lg), r = min(mine, a.m - 1);
-        const bool in = mine < a.m;
-        RowValues<E, P> x;
-        x.lane = lane;
-        x.lg = lg;
-        x.c = a.c;
-        x.template load<DT>(a.x, r * a.xs);
-        Sums s{lanes_max(x.most() * a.scale, lg), 0.f, 0.f};
+    int64_t r = (int64_t)blockIdx.x * (256 >> LG) + (threadIdx.x >> LG);
+    bring(r);
+    for (int64_t r0 = (int64_t)blockIdx.x * (256 >> LG); r0 < a.m; r0 += step, r += step) {
+        const bool in = r < a.m;
+        const int y = next_y;
+        x.template take<DT>(next);
+        bring(r + step);
+        x.lay_out(laid_out);
+        auto more = [](float p, float q) { return fmaxf(p, q); };
+        auto add = [](float p, float q) { return p + q; };
+        Sums s{lanes_of<LG>(x.most() * a.scale, more), 0.f, 0.f};
         const float ref = reference(s.m);
 #pragma unroll
         for (int p = 0; p < P; p++)
 #pragma unroll
             for (int e = 0; e < E; e++) add_logit(s, x.v[p][e], a.scale, ref);
-        const float2 st = lanes_sum2({s.s, s.t}, lg);
-        s.s = st.x;
-        s.t = st.y;
-        if (in && lane == 0) put_row<DT>(a, r, s);
-        if (!a.top) continue;
-        if constexpr (E * P == 16)
-            if (lg >= 4 && a.top <= TOP_LIST && top_at_once<DT, E, P>(a, r, in, s, x, lists[threadIdx.x >> 6])) continue;
-        top_in_turn<E, P>(a, r, in && lane == 0, s, x);
+        s.s = lanes_of<LG>(s.s, add);
+        s.t = lanes_of<LG>(s.t, add);
+        const Row row(s);
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+        if (in && x.lane == 0) {
+            const bool known = y >= 0 && y < a.c;
+            row.put(a, r, known, laid_out[known ? x.place(y) : 0]);
+        }
+        if (a.top) {
+            bool done = false;
+            if constexpr (LG >= 4)
+                done = a.top <= TOP_LIST && top_at_once<E, P, LG>(a, r, in, row, x, laid_out, lists[wave]);
+            if (!done) top_in_turn<E, P, LG>(a, r, in && x.lane == 0, row, x);
+        }
+        __builtin_amdgcn_wave_barrier();  // the row is read before the next one's is written
     }
 }
 
@@ -535,8 +573,9 @@ __global__ __launch_bounds__(256) void k_labels_stream(LabelArgs a) {
                 a.part_id[item * a.top + lane] = list.id;
             }
         } else {
-            if (lane == 0) put_row<DT>(a, r, s);
-            if (TOP && lane < a.top) put_top(a, r, lane, s, list.v, list.id);
+            const Row row(s);
+            if (lane == 0) row.template put<DT>(a, r);
+            if (TOP && lane < a.top) row.put_top(a, r, lane, list.v, list.id);
         }
     }
 }
@@ -575,10 +614,11 @@ __global__ __launch_bounds__(256) void k_labels_join(LabelArgs a) {
         __syncthreads();
         if (wave > 0) continue;
         s = sums.all();
-        if (lane == 0) put_row<DT>(a, r, s);
+        const Row row(s);
+        if (lane == 0) row.template put<DT>(a, r);
         if (!a.top) continue;
         list = lists.all(a.top, room[0]);
-        if (lane < a.top) put_top(a, r, lane, s, list.v, list.id);
+        if (lane < a.top) row.put_top(a, r, lane, list.v, list.id);
     }
 }
 
@@ -677,13 +717,29 @@ static LabelWork label_work(void* work, const LabelPlan& p, int64_t m, int64_t t
 template <int DT, int E>
 static void labels_e(const LabelArgs& a, const LabelPlan& p, hipStream_t s) {
     if (!p.stream) {
-        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.m, 256 >> p.lg), 16384);
-        auto go = [&](auto n) {
-            if constexpr (E * decltype(n)::value <= 16) k_labels_rows<DT, E, decltype(n)::value><<<grid, 256, 0, s>>>(a, p.lg);
+        // as many workgroups as are resident
+        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.m, 256 >> p.lg), 4 * compute_units());
+        auto go = [&](auto n, auto lg) {
+            constexpr int P = decltype(n)::value, LG = decltype(lg)::value;
+            if constexpr (E * P == 16 || LG == 0) k_labels_rows<DT, E, P, LG><<<grid, 256, 0, s>>>(a);
         };
-        if (p.p == 1) go(std::integral_constant<int, 1>{});
-        else if (p.p == 2) go(std::integral_constant<int, 2>{});
-        else if (p.p == 4) go(std::integral_constant<int, 4>{});
+        auto go_p = [&](auto lg) {
+            if constexpr (E == 8 || E == 4) {
+                if (p.p * E == 16) return go(std::integral_constant<int, 16 / E>{}, lg);
+            }
+            // rows of so few classes are one lane's
+            if (p.p == 1) go(std::integral_constant<int, 1>{}, lg);
+            else if constexpr (E < 8) go(std::integral_constant<int, 2>{}, lg);
+        };
+        switch (p.lg) {
+            case 0: go_p(std::integral_constant<int, 0>{}); break;
+            case 1: go_p(std::integral_constant<int, 1>{}); break;
+            case 2: go_p(std::integral_constant<int, 2>{}); break;
+            case 3: go_p(std::integral_constant<int, 3>{}); break;
+            case 4: go_p(std::integral_constant<int, 4>{}); break;
+            case 5: go_p(std::integral_constant<int, 5>{}); break;
+            default: go_p(std::integral_constant<int, 6>{}); break;
+        }
         TAURUS_CHECK_LAUNCH();
         return;
     }
@@ -775,7 +831,7 @@ int taurus_label_log_probs(const void* x, int32_t dtype, int64_t m, int64_t c, i
             check_ptr(logp, 4, "logp");
             check_ptr(labels, 4, "labels");
         }
-        if (stats) check_ptr(stats, 4, "stats");
+        if (stats) check_ptr(stats, 8, "stats");
         if (entropy) check_ptr(entropy, 4, "entropy");
         if (top > 0) {
             check_ptr(top_logp, 4, "top_logp");
