@@ -71,7 +71,7 @@ struct Row {
     __device__ explicit Row(const Sums& a)
         : most(a.m), bad(__builtin_isnan(a.s + a.t) || a.m == INFINITY), none(a.s == 0.f) {
         log_s = none ? 0.f : logf(a.s);
-        spread = none ? 0.f : a.t / a.s;
+        spread = none ? 0.f : a.t * __builtin_amdgcn_rcpf(a.s);  // S is in [1, c]
     }
     // log probability of a class of logit x
     __device__ float logp(float x, float scale) const {
@@ -202,11 +202,12 @@ __device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const
     float least = lanes_of<4>(above < a.top ? mine : INFINITY, [](float p, float q) { return fminf(p, q); });
     if constexpr (LG > 4) least = lane_step<4>(least, [](float p, float q) { return fmaxf(p, q); });
     if constexpr (LG > 5) least = lane_step<5>(least, [](float p, float q) { return fmaxf(p, q); });
+    least = fmaxf(least, -3.40282347e38f);  // not the masked ones
     uint32_t some = 0;  // which of this lane's values, the first in the highest bit
 #pragma unroll
     for (int p = 0; p < P; p++)
 #pragma unroll
-        for (int e = 0; e < E; e++) some = 2 * some + (x.v[p][e] >= least && x.v[p][e] > -INFINITY);
+        for (int e = 0; e < E; e++) some = some + some + (x.v[p][e] >= least);
     auto add = [](int p, int q) { return p + q; };
     const int n = __popc(some);
     int upto = n;  // over the lanes up to this one: moved up in 16 by 1, 2, 4, 8
@@ -242,10 +243,9 @@ __device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const
     const uint2 key = to[x.lane & (TOP_LIST - 1)];
     const uint64_t whole = whole_key(key);
     int rank = 0;
-    rotations<15>([&](auto i) {
-        constexpr int CTRL = 0x120 + decltype(i)::value;
-        rank += whole_key(make_uint2(lane_move<CTRL>(key.x), lane_move<CTRL>(key.y))) > whole;
-    });
+    for (int i = 0; __any(i < count); i += 4)  // those behind a list's end are below every key
+#pragma unroll
+        for (int k = 0; k < 4; k++) rank += whole_key(to[i + k]) > whole;
     if (in && x.lane < TOP_LIST) {
         const float v = value_of(key);
         if (whole && rank < a.top) row.put_top(a, r, rank, v, taken(v, a.scale) ? class_of(key) : -1);
@@ -270,19 +270,24 @@ __global__ __launch_bounds__(256, 4) void k_labels_rows(LabelArgs a) {
     const int64_t step = (int64_t)gridDim.x * (256 >> LG);
     Stored<DT, E> next[P];
     int next_y = -1;
-    auto bring = [&](int64_t r) {
-        r = min(r, a.m - 1);
-#pragma unroll
-        for (int p = 0; p < P; p++) next[p] = load_stored<DT, E>(a.x, r * a.xs + x.at(p));
-        if (a.logp) next_y = a.labels[r];
-    };
     // all lanes of a wave go round together: rows past the last are repeated
     int64_t r = (int64_t)blockIdx.x * (256 >> LG) + (threadIdx.x >> LG);
+    const char* at = static_cast<const char*>(a.x) + min(r, a.m - 1) * a.xs * type_bytes<DT>;
+    const int64_t step_bytes = step * a.xs * type_bytes<DT>;
+    uint32_t vec[P];
+#pragma unroll
+    for (int p = 0; p < P; p++) vec[p] = (uint32_t)x.at(p) * type_bytes<DT>;
+    auto bring = [&](int64_t r) {
+#pragma unroll
+        for (int p = 0; p < P; p++) next[p] = load_stored<DT, E>(at + vec[p], 0);
+        if (a.logp) next_y = a.labels[min(r, a.m - 1)];
+    };
     bring(r);
     for (int64_t r0 = (int64_t)blockIdx.x * (256 >> LG); r0 < a.m; r0 += step, r += step) {
         const bool in = r < a.m;
         const int y = next_y;
         x.template take<DT>(next);
+        if (r + step < a.m) at += step_bytes;
         bring(r + step);
         x.lay_out(laid_out);
         auto more = [](float p, float q) { return fmaxf(p, q); };
