@@ -60,55 +60,6 @@ __device__ inline void finish4(const Epilogue& e, int64_t r, int c, int cols, fl
         }
 }
 
-// Two blocks of 16 columns of row r, values c + 4 lk of each in v and w, for
-// columns in whole eights; `in`: whether there is the row.  All lanes take part
-// (put_pair16).
-template <int DT, int ACT>
-__device__ inline void finish_pair(const Epilogue& e, int64_t r, int c, int cols, bool in, floatx4 v, floatx4 w) {
-    const int at = c + 4 * ((threadIdx.x & 63) >> 4);
-    const bool has_v = at < cols, has_w = at + 16 < cols;
-    auto add = [&](floatx4& x, const float (&f)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) x[i] += f[i];
-    };
-    if (e.bias) {
-        float f[4];
-        if (has_v) {
-            load_vec<TAURUS_F32, 4>(e.bias, at, f);
-            add(v, f);
-        }
-        if (has_w) {
-            load_vec<TAURUS_F32, 4>(e.bias, at + 16, f);
-            add(w, f);
-        }
-    }
-    if (e.pre) put_pair16<DT>(e.pre, r * e.pre_stride, c, cols, in, v, w);
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-        v[i] = activation<ACT>(v[i]);
-        w[i] = activation<ACT>(w[i]);
-    }
-    if (e.residual) {
-        auto take = [&](int col, floatx4& x) {
-            float f[4];
-            const int64_t from = r * e.residual_stride + col;
-            if (e.out_dtype == TAURUS_F32) load_vec<TAURUS_F32, 4>(e.residual, from, f);
-            else if (e.out_dtype == TAURUS_BF16) load_vec<TAURUS_BF16, 4>(e.residual, from, f);
-            else load_vec<TAURUS_F16, 4>(e.residual, from, f);
-            add(x, f);
-        };
-        if (in && has_v) take(at, v);
-        if (in && has_w) take(at + 16, w);
-    }
-    const int64_t row = r * e.out_stride;
-    if (e.out_dtype == TAURUS_BF16) put_pair16<TAURUS_BF16>(e.out, row, c, cols, in, v, w);
-    else if (e.out_dtype == TAURUS_F16) put_pair16<TAURUS_F16>(e.out, row, c, cols, in, v, w);
-    else if (in) {
-        put4(e.out, TAURUS_F32, row, at, cols, v);
-        put4(e.out, TAURUS_F32, row, at + 16, cols, w);
-    }
-}
-
 // A product out [rows][cols] of `depth` terms, of operands `m` (rows of out)
 // and `n` (columns).
 enum { PRODUCT_Y, PRODUCT_DX, PRODUCT_DW };

@@ -1,13 +1,15 @@
 // Large products of 16-bit operands (linear.hpp): tiles of 256 x 256, the
 // contraction in stages of 64.
 //
-// Eight waves of 128 x 64 values share a compute unit, two a SIMD.  They work in
-// two groups of four, half a step apart: while one group's matrix instructions
-// run, the other reads its next operands from LDS, and a barrier hands over.  A
-// stage is four such steps (32 of the contraction by 64 rows).  Stages go from
-// memory straight into LDS, in two buffers of 64 KB: the next stage's pieces
-// are asked for in the first two steps of this one, when the last wave has read
-// the buffer that they go to, and waited for in its last step.
+// Eight waves of 128 x 64 values share a compute unit, two a SIMD.  A stage is
+// four steps (32 of the contraction by 64 rows), whose operands a wave reads
+// from LDS one step ahead, while the step before is multiplied.  Stages go from
+// memory straight into LDS, in two buffers of 64 KB, as one stream over a
+// workgroup's tiles: before a stage's last step its operands are in registers,
+// and a barrier says so of all waves and that the next stage is in LDS; then its
+// buffer takes the stage after that, and the last step's products run while
+// the next stage's first operands come.  So there is one barrier a stage, and a
+// tile's epilogue runs while the next tile's first stages are on their way.
 //
 // The layouts in LDS are those of product.hpp.  A wave's load fills 1 KB in lane
 // order, so the exchange is made in the addresses that the lanes read from.
@@ -143,88 +145,205 @@ __device__ inline WidePlace wide_place(const WideArgs& a, uint32_t tile) {
     return {first + in % tall, in / tall};
 }
 
+// The epilogue of a wave's 128 x 64 values: lane li holds rows r + 16 i, values
+// c + 16 j + 4 lk to + 3 of each, for columns in whole eights.  All lanes take
+// part (put_pair16).  The residual's values of the next row are on their way
+// while this row's are stored.
+template <int DT, int ACT>
+__device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[8][4]) {
+    const Epilogue& e = p.e;
+    const int cols = (int)p.cols, at = c + 4 * ((threadIdx.x & 63) >> 4);
+    const bool half = e.out_dtype != TAURUS_F32, is_bf16 = e.out_dtype == TAURUS_BF16;
+    float bias[4][4];
+    if (e.bias)
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) bias[j][k] = 0.f;
+            if (at + 16 * j < cols) load_vec<TAURUS_F32, 4>(e.bias, at + 16 * j, bias[j]);
+        }
+    uint2 raw[4];
+    auto bring = [&](int i) {
+        if (!e.residual || !half || r + 16 * i >= p.rows) return;
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            if (at + 16 * j < cols) {
+                const auto s = load_stored<TAURUS_BF16, 4>(e.residual, (r + 16 * i) * e.residual_stride + at + 16 * j);
+                raw[j] = make_uint2(s.v[0], s.v[1]);
+            }
+    };
+    bring(0);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        __builtin_amdgcn_sched_barrier(0);  // a row at a time, which keeps addresses few
+        const int64_t row = r + 16 * i;
+        const bool in = row < p.rows;
+        uint2 mine[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) mine[j] = raw[j];
+        if (i < 7) bring(i + 1);
+        if (e.bias)
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int k = 0; k < 4; k++) acc[i][j][k] += bias[j][k];
+        if (e.pre)
+#pragma unroll
+            for (int j = 0; j < 4; j += 2)
+                put_pair16<DT>(e.pre, row * e.pre_stride, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int k = 0; k < 4; k++) acc[i][j][k] = activation<ACT>(acc[i][j][k]);
+        if (e.residual) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                float f[4];
+                if (half) {
+                    Stored<TAURUS_BF16, 4> b;
+                    Stored<TAURUS_F16, 4> h;
+                    b.v[0] = h.v[0] = mine[j].x;
+                    b.v[1] = h.v[1] = mine[j].y;
+                    if (is_bf16) decode<TAURUS_BF16, 4>(b, f);
+                    else decode<TAURUS_F16, 4>(h, f);
+                } else {
+                    if (!in || at + 16 * j >= cols) continue;
+                    load_vec<TAURUS_F32, 4>(e.residual, row * e.residual_stride + at + 16 * j, f);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; k++) acc[i][j][k] += f[k];
+            }
+        }
+        const int64_t to = row * e.out_stride;
+        if (half) {
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                if (is_bf16) put_pair16<TAURUS_BF16>(e.out, to, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
+                else put_pair16<TAURUS_F16>(e.out, to, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
+            }
+        } else if (in) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) put4(e.out, TAURUS_F32, to, at + 16 * j, cols, acc[i][j]);
+        }
+    }
+}
+
+// What a workgroup's b-th item is: a tile, or one part of one.
+struct WideItem {
+    int64_t r0, c0, k0;
+    int depth, stages;
+    uint32_t sums;  // which tile's room of the workspace the sums go to
+    bool cut;
+    __device__ WideItem(const WideArgs& a, uint32_t b) : sums(0), cut(b >= a.whole) {
+        uint32_t tile, part = 0;
+        if (cut) {
+            const uint32_t i = wide_turn(b - a.whole, a.cut * a.p.splits);
+            part = i / a.cut;
+            tile = a.whole + i % a.cut;
+            sums = i;
+        } else {
+            tile = wide_turn(b, a.whole);
+        }
+        const WidePlace at = wide_place(a, tile);
+        r0 = at.row * WIDE;
+        c0 = at.col * WIDE;
+        k0 = part * a.p.per;
+        depth = (int)(cut && (int)part + 1 < a.p.splits ? a.p.per : a.p.depth - k0);
+        stages = (depth + WIDE_STAGE - 1) / WIDE_STAGE;
+    }
+};
+
 template <int KIND, int DT, int ACT>
 __global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
     typedef std::conditional_t<KIND == PRODUCT_DW, WideAcross<DT>, WideAlong<DT>> OpM;
     typedef std::conditional_t<KIND == PRODUCT_DX, WideAlong<DT>, WideAcross<DT>> OpN;
     __shared__ __align__(1024) char lds[4 * WIDE_BYTES];
-    const bool cut = blockIdx.x >= a.whole;
-    uint32_t tile, part = 0;
-    if (cut) {
-        const uint32_t i = wide_turn(blockIdx.x - a.whole, a.cut * a.p.splits);
-        part = i / a.cut;
-        tile = a.whole + i % a.cut;
-    } else {
-        tile = wide_turn(blockIdx.x, a.whole);
-    }
-    const WidePlace at = wide_place(a, tile);
-    const int64_t r0 = at.row * WIDE, c0 = at.col * WIDE, k0 = part * a.p.per;
-    const int depth = (int)(cut && (int)part + 1 < a.p.splits ? a.p.per : a.p.depth - k0);
-    const OpM om(a.p.m, a.p.ms, r0, a.p.rows, k0, depth);
-    const OpN on(a.p.n, a.p.ns, c0, a.p.cols, k0, depth);
-    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), group = wave >> 2;
-    const int m0 = group * 128, n0 = (wave & 3) * 64;
-    const int stages = (depth + WIDE_STAGE - 1) / WIDE_STAGE;
-
-    floatx4 acc[8][4];
-#pragma unroll
-    for (int i = 0; i < 8; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    bring(om, 0, lds, 0);
-    bring(on, 0, lds, WIDE_BYTES);
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    // the second group is half a step behind: it meets one barrier more here,
-    // the first one more at the end
-    if (group == 1) asm volatile("s_barrier" ::: "memory");
-    for (int t = 0; t < stages; t++) {
-        const char* mine = lds + (t & 1) * 2 * WIDE_BYTES;
-        const uint32_t next = (uint32_t)((t + 1) & 1) * 2 * WIDE_BYTES;
-        const bool more = t + 1 < stages;
-        uint4 fn[4];
-#pragma unroll
-        for (int step = 0; step < 4; step++) {
-            const int kb = step >> 1, half = step & 1;
-            uint4 fm[4];
-            if (half == 0)
-#pragma unroll
-                for (int j = 0; j < 4; j++) fn[j] = OpN::read(mine + WIDE_BYTES, n0 + 16 * j, kb);
-#pragma unroll
-            for (int i = 0; i < 4; i++) fm[i] = OpM::read(mine, m0 + 64 * half + 16 * i, kb);
-            if (step == 0 && more) bring(om, t + 1, lds, next);
-            if (step == 1 && more) bring(on, t + 1, lds, next + WIDE_BYTES);
-            // all reads of this step are done before the barrier: past the last
-            // one's, the other group may ask for what overwrites them
-            if (step == 3) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            else asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[4 * half + i][j] = mfma16<DT>(fn[j], fm[i], acc[4 * half + i][j]);
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            asm volatile("s_barrier" ::: "memory");
-        }
-    }
-    if (group == 0) asm volatile("s_barrier" ::: "memory");
-
+    const uint32_t items = a.whole + a.cut * a.p.splits;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int m0 = (wave >> 2) * 128, n0 = (wave & 3) * 64;
     const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
-    float* sums = cut ? a.p.part + (int64_t)(part * a.cut + tile - a.whole) * (WIDE * WIDE) : nullptr;
+
+    // the stages' stream to LDS: the next to bring
+    WideItem coming(a, blockIdx.x);
+    uint32_t coming_b = blockIdx.x;
+    int coming_t = 0;
+    OpM om(a.p.m, a.p.ms, coming.r0, a.p.rows, coming.k0, coming.depth);
+    OpN on(a.p.n, a.p.ns, coming.c0, a.p.cols, coming.k0, coming.depth);
+    auto bring_next = [&](uint32_t to) {
+        if (coming_b >= items) return;
+        bring(om, coming_t, lds, to);
+        bring(on, coming_t, lds, to + WIDE_BYTES);
+        if (++coming_t < coming.stages) return;
+        coming_t = 0;
+        coming_b += gridDim.x;
+        if (coming_b >= items) return;
+        coming = WideItem(a, coming_b);
+        om = OpM(a.p.m, a.p.ms, coming.r0, a.p.rows, coming.k0, coming.depth);
+        on = OpN(a.p.n, a.p.ns, coming.c0, a.p.cols, coming.k0, coming.depth);
+    };
+    uint4 fn[2][4], fm[2][4];
+    auto read_n = [&](const char* at, int kb, uint4 (&f)[4]) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        const int mr = m0 + 16 * i + li;
+        for (int j = 0; j < 4; j++) f[j] = OpN::read(at + WIDE_BYTES, n0 + 16 * j, kb);
+    };
+    auto read_m = [&](const char* at, int kb, int half, uint4 (&f)[4]) {
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-            if (cut) {
-                float* out = sums + mr * WIDE + n0 + 16 * j + 4 * lk;
-                *reinterpret_cast<floatx4*>(out) = acc[i][j];
-                *reinterpret_cast<floatx4*>(out + 16) = acc[i][j + 1];
-            } else {
-                finish_pair<DT, ACT>(a.p.e, r0 + mr, (int)c0 + n0 + 16 * j, (int)a.p.cols, r0 + mr < a.p.rows, acc[i][j],
-                                     acc[i][j + 1]);
+        for (int i = 0; i < 4; i++) f[i] = OpM::read(at, m0 + 64 * half + 16 * i, kb);
+    };
+    floatx4 acc[8][4];
+    auto multiply = [&](const uint4 (&n)[4], const uint4 (&m)[4], auto half) {
+        constexpr int H = decltype(half)::value;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[4 * H + i][j] = mfma16<DT>(n[j], m[i], acc[4 * H + i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    std::integral_constant<int, 0> upper;
+    std::integral_constant<int, 1> lower;
+
+    bring_next(0);
+    bring_next(2 * WIDE_BYTES);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    uint32_t buffer = 0;
+    for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
+        const WideItem item(a, b);
+        read_n(lds + buffer, 0, fn[0]);
+        read_m(lds + buffer, 0, 0, fm[0]);
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < item.stages; t++) {
+            const char* mine = lds + buffer;
+            const char* next = lds + (buffer ^ 2 * WIDE_BYTES);
+            read_m(mine, 0, 1, fm[1]);
+            read_n(mine, 1, fn[1]);
+            multiply(fn[0], fm[0], upper);
+            read_m(mine, 1, 0, fm[0]);
+            multiply(fn[0], fm[1], lower);
+            read_m(mine, 1, 1, fm[1]);
+            multiply(fn[1], fm[0], upper);
+            // this wave has read the stage; the next one's pieces that it asked
+            // for are there
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            bring_next(buffer);
+            if (t + 1 < item.stages) {
+                read_n(next, 0, fn[0]);
+                read_m(next, 0, 0, fm[0]);
             }
+            multiply(fn[1], fm[1], lower);
+            buffer ^= 2 * WIDE_BYTES;
+        }
+        if (item.cut) {  // a part's sums
+            float* out = a.p.part + (int64_t)item.sums * (WIDE * WIDE) + (m0 + li) * WIDE + n0 + 4 * lk;
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) *reinterpret_cast<floatx4*>(out + 16 * i * WIDE + 16 * j) = acc[i][j];
+        } else {
+            finish_tile<DT, ACT>(a.p, item.r0 + m0 + li, (int)item.c0 + n0, acc);
         }
     }
 }
@@ -287,7 +406,7 @@ template <int KIND, int DT>
 static void wide_launch(const WideArgs& a, int act, hipStream_t s) {
     auto go = [&](auto c) {
         constexpr int ACT = decltype(c)::value;
-        k_linear_wide<KIND, DT, ACT><<<a.whole + a.cut * a.p.splits, 512, 0, s>>>(a);
+        k_linear_wide<KIND, DT, ACT><<<std::min(a.whole + a.cut * a.p.splits, (uint32_t)compute_units()), 512, 0, s>>>(a);
         TAURUS_CHECK_LAUNCH();
         if (a.cut) {
             k_wide_join<DT, ACT><<<a.cut * 64, 256, 0, s>>>(a);
