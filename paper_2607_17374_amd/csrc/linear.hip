@@ -15,17 +15,14 @@
 
 namespace taurus {
 
-template <int KIND, int DT, int TM, int TN, bool AL>
-struct ProductOps {
+// Tiles of 128 rows and 64 columns, which leave room for four workgroups a
+// compute unit: any alignment, few rows, and 32-bit types.
+constexpr int TM = 128, TN = 64;
+template <int KIND, int DT, bool AL, int ACT>
+struct ProductTiles {
     typedef std::conditional_t<KIND == PRODUCT_DW, Across<DT, TM, AL>, Along<DT, TM, AL>> OpM;
     typedef std::conditional_t<KIND == PRODUCT_DX, Along<DT, TN, AL>, Across<DT, TN, AL>> OpN;
-};
-template <int KIND, int DT, int TM, int TN, bool AL, int ACT>
-struct ProductTiles {
-    typedef ProductOps<KIND, DT, TM, TN, AL> Ops;
-    typedef typename Ops::OpM OpM;
-    typedef typename Ops::OpN OpN;
-    static constexpr int WN = TN / 64, WM = 4 / WN, MI = TM / WM / 16, NI = 4;
+    static constexpr int MI = 2, NI = 4;  // a wave 32 rows
     const ProductArgs& a;
     int64_t b;
     int m0, n0;
@@ -58,26 +55,35 @@ struct ProductTiles {
     }
     __device__ void done(floatx4 (&acc)[MI][NI], typename Tile<DT>::sums_t (&)[1]) {
         const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
+        const int64_t r = r0 + m0 + li;
+        const int c = (int)c0 + 4 * lk, cols = (int)a.cols;
+        Residual4 ahead[MI][NI];
+        if (!a.part)
+#pragma unroll
+            for (int i = 0; i < MI; i++)
+#pragma unroll
+                for (int j = 0; j < NI; j++)
+                    if (r + 16 * i < a.rows) ahead[i][j].load(a.e, r + 16 * i, c + 16 * j, cols);
 #pragma unroll
         for (int i = 0; i < MI; i++) {
-            const int64_t r = r0 + m0 + 16 * i + li;
-            if (r >= a.rows) continue;
+            __builtin_amdgcn_sched_barrier(0);  // a row at a time, which keeps addresses few
+            const int64_t row = r + 16 * i;
+            if (row >= a.rows) continue;
 #pragma unroll
             for (int j = 0; j < NI; j++) {
-                const int c = (int)c0 + n0 + 16 * j + 4 * lk;
-                if (a.part) put4(a.part, TAURUS_F32, (split * a.rows + r) * a.cols, c, (int)a.cols, acc[i][j]);
-                else finish4<DT, ACT>(a.e, r, c, (int)a.cols, acc[i][j]);
+                if (a.part) put4(a.part, TAURUS_F32, (split * a.rows + row) * a.cols, c + 16 * j, cols, acc[i][j]);
+                else finish4<DT, ACT>(a.e, row, c + 16 * j, cols, acc[i][j], &ahead[i][j]);
             }
         }
     }
 };
-template <int KIND, int DT, int TM, int TN, bool AL, int ACT>
-__global__ __launch_bounds__(256, TM * TN == 128 * 128 ? 3 : 4) void k_linear(ProductArgs a) {
-    typedef ProductTiles<KIND, DT, TM, TN, AL, ACT> T;
+template <int KIND, int DT, bool AL, int ACT>
+__global__ __launch_bounds__(256, 4) void k_linear(ProductArgs a) {
+    typedef ProductTiles<KIND, DT, AL, ACT> T;
     __shared__ __align__(16) char lds[T::OpM::BYTES + T::OpN::BYTES];
-    const int wave = threadIdx.x >> 6, m0 = wave / T::WN * T::MI * 16, n0 = wave % T::WN * 64;
-    T tiles(a, m0, n0);
-    stream_tiles<DT, typename T::OpM, typename T::OpN, T::MI, T::NI, false>(tiles, lds, m0, n0);
+    const int m0 = (threadIdx.x >> 6) * 32;
+    T tiles(a, m0, 0);
+    stream_tiles<DT, typename T::OpM, typename T::OpN, T::MI, T::NI, false>(tiles, lds, m0, 0);
 }
 
 // The parts' sums added in order, then the epilogue: a thread four values.
@@ -171,20 +177,16 @@ static bool whole_words(int dtype, const void* p, int64_t cols, int64_t stride) 
 
 // How a product is cut.
 struct ProductPlan {
-    int tm, tn;
     int64_t row_tiles, per;
     int col_tiles, splits;
     int64_t part;  // fp32 sums of the workspace
 };
-static ProductPlan product_plan(int dtype, bool al, int64_t rows, int64_t cols, int64_t depth) {
+static ProductPlan product_plan(int dtype, int64_t rows, int64_t cols, int64_t depth) {
     ProductPlan p{};
     const int stage = dtype == TAURUS_F32 ? 32 : 64;
-    p.tm = 128;
-    p.tn = dtype == TAURUS_F32 || !al || cols <= 64 ? 64 : 128;
-    if (ceil_div(rows, p.tm) * ceil_div(cols, p.tn) < 512) p.tn = 64;
-    p.row_tiles = ceil_div(rows, p.tm);
-    p.col_tiles = (int)ceil_div(cols, p.tn);
-    const int64_t tiles = p.row_tiles * p.col_tiles, resident = 256 * (p.tm * p.tn == 128 * 128 ? 3 : 4);
+    p.row_tiles = ceil_div(rows, TM);
+    p.col_tiles = (int)ceil_div(cols, TN);
+    const int64_t tiles = p.row_tiles * p.col_tiles, resident = 256 * 4;
     const int64_t stages = ceil_div(depth, stage);
     // as many parts as fill the chip, of at least four stages
     int64_t splits = std::max<int64_t>(1, std::min(resident / std::max<int64_t>(tiles, 1), stages / 4));
@@ -196,34 +198,26 @@ static ProductPlan product_plan(int dtype, bool al, int64_t rows, int64_t cols, 
     p.part = p.splits > 1 ? p.splits * rows * cols : 0;
     return p;
 }
-template <int KIND, int DT, int TM, int TN, bool AL, int ACT>
-static void product_launch(const ProductArgs& a, hipStream_t s) {
-    const int64_t tiles = a.row_tiles * a.col_tiles * a.splits;
-    const int64_t resident = (int64_t)(TM * TN == 128 * 128 ? 3 : 4) * compute_units();
-    k_linear<KIND, DT, TM, TN, AL, ACT><<<(unsigned)std::min(tiles, resident), 256, 0, s>>>(a);
-    TAURUS_CHECK_LAUNCH();
-}
 template <int KIND, int DT, int ACT>
-static void product_tiles(const ProductArgs& a, const ProductPlan& p, bool al, hipStream_t s) {
-    if (!al) return product_launch<KIND, DT, 128, 64, false, ACT>(a, s);
-    if constexpr (DT != TAURUS_F32) {
-        if (p.tn == 128) return product_launch<KIND, DT, 128, 128, true, ACT>(a, s);
-    }
-    product_launch<KIND, DT, 128, 64, true, ACT>(a, s);
+static void product_tiles(const ProductArgs& a, bool al, hipStream_t s) {
+    const unsigned grid = (unsigned)std::min(a.row_tiles * a.col_tiles * a.splits, (int64_t)4 * compute_units());
+    if (al) k_linear<KIND, DT, true, ACT><<<grid, 256, 0, s>>>(a);
+    else k_linear<KIND, DT, false, ACT><<<grid, 256, 0, s>>>(a);
+    TAURUS_CHECK_LAUNCH();
 }
 template <int KIND, int DT>
 static void product(ProductArgs a, float* part, int act, hipStream_t s) {
     if (wide_takes(KIND, DT, a)) return wide_product(KIND, DT, a, part, act, s);
     const int64_t m_width = KIND == PRODUCT_DW ? a.rows : a.depth, n_width = KIND == PRODUCT_DX ? a.depth : a.cols;
     const bool al = whole_words(DT, a.m, m_width, a.ms) && whole_words(DT, a.n, n_width, a.ns);
-    const ProductPlan p = product_plan(DT, al, a.rows, a.cols, a.depth);
+    const ProductPlan p = product_plan(DT, a.rows, a.cols, a.depth);
     a.part = p.splits > 1 ? part : nullptr;
     a.per = p.per;
     a.row_tiles = p.row_tiles;
     a.col_tiles = p.col_tiles;
     a.splits = p.splits;
     if (p.splits > 1) {  // the sums alone: one kernel for all activations
-        product_tiles<KIND, DT, TAURUS_ACT_NONE>(a, p, al, s);
+        product_tiles<KIND, DT, TAURUS_ACT_NONE>(a, al, s);
         const unsigned grid = grid_for(std::min<int64_t>(ceil_div(a.rows * ceil_div(a.cols, 4), 256), 4096));
         if constexpr (KIND == PRODUCT_Y) {
             with_act(act, [&](auto c) { k_linear_join<DT, decltype(c)::value><<<grid, 256, 0, s>>>(a); });
@@ -232,9 +226,9 @@ static void product(ProductArgs a, float* part, int act, hipStream_t s) {
         }
         TAURUS_CHECK_LAUNCH();
     } else if constexpr (KIND == PRODUCT_Y) {
-        with_act(act, [&](auto c) { product_tiles<KIND, DT, decltype(c)::value>(a, p, al, s); });
+        with_act(act, [&](auto c) { product_tiles<KIND, DT, decltype(c)::value>(a, al, s); });
     } else {
-        product_tiles<KIND, DT, TAURUS_ACT_NONE>(a, p, al, s);
+        product_tiles<KIND, DT, TAURUS_ACT_NONE>(a, al, s);
     }
 }
 template <int KIND>
@@ -255,10 +249,9 @@ struct LinearWork {
     void* dz = nullptr;
     int64_t dz_stride = 0, blocks = 0, bytes = 0;
 };
-// whether rows are whole words is known at the call: room for both
+// the alignment is known at the call: room for both ways
 static int64_t part_values(int dtype, int64_t rows, int64_t cols, int64_t depth) {
-    return std::max(std::max(product_plan(dtype, true, rows, cols, depth).part, product_plan(dtype, false, rows, cols, depth).part),
-                    wide_part(rows, cols, depth));
+    return std::max(product_plan(dtype, rows, cols, depth).part, wide_part(rows, cols, depth));
 }
 static int64_t forward_bytes(int dtype, int64_t m, int64_t d_in, int64_t d_out) {
     Carve c;

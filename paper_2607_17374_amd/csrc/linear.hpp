@@ -21,9 +21,43 @@ struct Epilogue {
     void* pre;  // z in the operands' type, or null
     int64_t pre_stride;
 };
+// Four values of the residual as stored, asked for ahead of their use; those
+// past the row's end are missing.
+struct Residual4 {
+    uint32_t v[4];
+    __device__ void load(const Epilogue& e, int64_t r, int c, int cols) {
+        if (!e.residual || c + 4 > cols) return;
+        const int64_t at = r * e.residual_stride + c;
+        if (e.out_dtype == TAURUS_F32) {
+            const auto s = load_stored<TAURUS_F32, 4>(e.residual, at);
+            for (int i = 0; i < 4; i++) v[i] = s.v[i];
+        } else {
+            const auto s = load_stored<TAURUS_BF16, 4>(e.residual, at);
+            v[0] = s.v[0];
+            v[1] = s.v[1];
+        }
+    }
+    __device__ void add(const Epilogue& e, float (&f)[4]) const {
+        float g[4];
+        if (e.out_dtype == TAURUS_F32) {
+            for (int i = 0; i < 4; i++) g[i] = __uint_as_float(v[i]);
+        } else if (e.out_dtype == TAURUS_BF16) {
+            Stored<TAURUS_BF16, 4> s;
+            s.v[0] = v[0];
+            s.v[1] = v[1];
+            decode<TAURUS_BF16, 4>(s, g);
+        } else {
+            Stored<TAURUS_F16, 4> s;
+            s.v[0] = v[0];
+            s.v[1] = v[1];
+            decode<TAURUS_F16, 4>(s, g);
+        }
+        for (int i = 0; i < 4; i++) f[i] += g[i];
+    }
+};
 // Values c .. c + E - 1 of row r, c + E <= cols.
 template <int DT, int ACT, int E>
-__device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E]) {
+__device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E], const Residual4* ahead = nullptr) {
     if (e.bias) {
         float b[E];
         load_vec<TAURUS_F32, E>(e.bias, c, b);
@@ -33,7 +67,9 @@ __device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E]
     if (e.pre) store_vec<DT, E>(e.pre, r * e.pre_stride + c, v);
 #pragma unroll
     for (int i = 0; i < E; i++) v[i] = activation<ACT>(v[i]);
-    if (e.residual) {
+    if (e.residual && ahead) {
+        if constexpr (E == 4) ahead->add(e, v);
+    } else if (e.residual) {
         float f[E];
         const int64_t at = r * e.residual_stride + c;
         if (e.out_dtype == TAURUS_F32) load_vec<TAURUS_F32, E>(e.residual, at, f);
@@ -46,10 +82,11 @@ __device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E]
 }
 // four consecutive values of a row of `cols`
 template <int DT, int ACT>
-__device__ inline void finish4(const Epilogue& e, int64_t r, int c, int cols, floatx4 v) {
+__device__ inline void finish4(const Epilogue& e, int64_t r, int c, int cols, floatx4 v,
+                               const Residual4* ahead = nullptr) {
     if (c + 4 <= cols) {
         float f[4] = {v[0], v[1], v[2], v[3]};
-        finish<DT, ACT, 4>(e, r, c, f);
+        finish<DT, ACT, 4>(e, r, c, f, ahead);
         return;
     }
 #pragma unroll

@@ -293,11 +293,15 @@ __global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
     floatx4 acc[8][4];
     auto multiply = [&](const uint4 (&n)[4], const uint4 (&m)[4], auto half) {
         constexpr int H = decltype(half)::value;
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 4; i++)
 #pragma unroll
             for (int j = 0; j < 4; j++) acc[4 * H + i][j] = mfma16<DT>(n[j], m[i], acc[4 * H + i][j]);
+#pragma unroll
+        for (int g = 0; g < 8; g++) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
     std::integral_constant<int, 0> upper;
@@ -389,6 +393,12 @@ static WidePlan wide_plan(int64_t rows, int64_t cols, int64_t depth) {
     p.splits = (int)ceil_div(stages, each);
     return p;
 }
+// Products with less to do than this leave much of the chip idle in tiles of
+// this size, or spend more on joining parts than they save (bf16, y / dx / dW,
+// tiles of 128 x 64 against these: 4,096 x 1,024 -> 1,024 (4.3e9) 31 / 29 / 29
+// us against 32 / 30 / 35; 4,096 x 4,096 -> 512 (8.6e9) 41 / 36 / 42 against 43
+// / 24 / 43; 4,096 x 4,096 -> 1,024 (17e9) 67 / 58 / 70 against 56 / 36 / 54).
+constexpr double WIDE_WORK = 6e9;
 bool wide_takes(int kind, int dtype, const ProductArgs& a) {
     if (dtype == TAURUS_F32) return false;
     auto whole = [](const void* p, int64_t width, int64_t stride) {
@@ -396,7 +406,7 @@ bool wide_takes(int kind, int dtype, const ProductArgs& a) {
     };
     const int64_t m_width = kind == PRODUCT_DW ? a.rows : a.depth, n_width = kind == PRODUCT_DX ? a.depth : a.cols;
     return whole(a.m, m_width, a.ms) && whole(a.n, n_width, a.ns) && a.cols % 8 == 0 && a.rows >= 256 && a.cols >= 256 &&
-           a.depth >= 256 && ceil_div(a.rows, WIDE) * ceil_div(a.cols, WIDE) <= WIDE_TILES;
+           a.depth >= 256 && (double)a.rows * a.cols * a.depth >= WIDE_WORK && ceil_div(a.rows, WIDE) * ceil_div(a.cols, WIDE) <= WIDE_TILES;
 }
 int64_t wide_part(int64_t rows, int64_t cols, int64_t depth) {
     const WidePlan p = wide_plan(rows, cols, depth);
