@@ -251,7 +251,7 @@ struct LinearWork {
 };
 // the alignment is known at the call: room for both ways
 static int64_t part_values(int dtype, int64_t rows, int64_t cols, int64_t depth) {
-    return std::max(product_plan(dtype, rows, cols, depth).part, wide_part(rows, cols, depth));
+    return std::max(product_plan(dtype, rows, cols, depth).part, wide_part(dtype, rows, cols, depth));
 }
 static int64_t forward_bytes(int dtype, int64_t m, int64_t d_in, int64_t d_out) {
     Carve c;

@@ -111,10 +111,10 @@ struct ProductArgs {
     int col_tiles, splits;
 };
 
-// Large products of 16-bit operands (linear_wide.hip).  Whether one is taken,
+// Large products (linear_wide.hip).  Whether one is taken,
 // and the fp32 values it leaves in the workspace.
 bool wide_takes(int kind, int dtype, const ProductArgs& a);
-int64_t wide_part(int64_t rows, int64_t cols, int64_t depth);
+int64_t wide_part(int dtype, int64_t rows, int64_t cols, int64_t depth);
 void wide_product(int kind, int dtype, ProductArgs a, float* part, int act, hipStream_t s);
 
 }  // namespace taurus

@@ -1,5 +1,5 @@
-// Large products of 16-bit operands (linear.hpp): tiles of 256 x 256, the
-// contraction in stages of 64.
+// Large products (linear.hpp): tiles of 256 x 256, the contraction in stages of
+// 128 bytes a row (64 values of 16 bits, 32 of fp32).
 //
 // Eight waves of 128 x 64 values share a compute unit, two a SIMD.  A stage is
 // four steps (32 of the contraction by 64 rows), whose operands a wave reads
@@ -20,7 +20,7 @@
 
 namespace taurus {
 
-constexpr int WIDE = 256, WIDE_STAGE = 64, WIDE_BYTES = 256 * 128;  // of an operand's stage
+constexpr int WIDE = 256, WIDE_BYTES = 256 * 128;  // of an operand's stage
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -50,56 +50,74 @@ __device__ inline void zero_to_lds(char* lds, uint32_t to) {
 // first row's (Along) or the first contraction row's (Across) address.
 template <int DT>
 struct WideAlong {
+    static constexpr int E = Tile<DT>::E, STAGE = Tile<DT>::STAGE, SZ = type_bytes<DT>;
+    typedef typename Tile<DT>::frag frag;
     const char* at;
     uint32_t offset[4];
     int depth, col;  // of this lane's pieces in a stage
     __device__ WideAlong(const void* base, int64_t stride, int64_t first, int64_t rows, int64_t k0, int depth_)
         : depth(depth_) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        at = static_cast<const char*>(base) + (first * stride + k0) * 2;
+        at = static_cast<const char*>(base) + (first * stride + k0) * SZ;
         const int p = (lane & 7) ^ (lane >> 3);
-        col = p * 8;
+        col = p * E;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             const int64_t row = min((int64_t)(q * 8 + wave) * 8 + (lane >> 3), rows - 1 - first);
-            offset[q] = (uint32_t)(row * stride * 2) + p * 16;
+            offset[q] = (uint32_t)(row * stride * SZ) + p * 16;
         }
     }
-    __device__ const char* stage(int t) const { return at + (int64_t)t * WIDE_STAGE * 2; }
-    __device__ bool holds(int t, int) const { return t * WIDE_STAGE + col < depth; }
+    __device__ const char* stage(int t) const { return at + (int64_t)t * STAGE * SZ; }
+    __device__ bool holds(int t, int) const { return t * STAGE + col < depth; }
     // rows [r0, r0 + 16), matrix step kb
-    static __device__ inline uint4 read(const char* lds, int r0, int kb) { return Along<DT, WIDE, true>::read(lds, r0, kb); }
+    static __device__ inline frag read(const char* lds, int r0, int kb) { return Along<DT, WIDE, true>::read(lds, r0, kb); }
 };
+// Rows of 256 values.  Of 16 bits: 32-byte units exchanged as product.hpp's; of
+// fp32: 64-byte units by the row's second pair of bits, so that the four rows
+// that are read together fall on different banks.
 template <int DT>
 struct WideAcross {
-    typedef Across<DT, 128, true> Half;  // the same exchange of 32-byte units
+    static constexpr int E = Tile<DT>::E, STAGE = Tile<DT>::STAGE, SZ = type_bytes<DT>;
+    static constexpr int PITCH = WIDE * SZ, PIECES = PITCH / 16, ROWS = 64 / PIECES;  // rows a wave's load fills
+    static constexpr int UNIT = SZ == 2 ? 2 : 4;                                      // pieces
+    typedef typename Tile<DT>::frag frag;
     const char* at;
     int64_t step;
     uint32_t offset[4];
     int depth, row;
     __device__ WideAcross(const void* base, int64_t stride, int64_t first, int64_t cols, int64_t k0, int depth_)
-        : step(stride * 2), depth(depth_) {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        at = static_cast<const char*>(base) + (k0 * stride + first) * 2;
-        row = wave * 2 + (lane >> 5);
+        : step(stride * SZ), depth(depth_) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = lane % PIECES;
+        at = static_cast<const char*>(base) + (k0 * stride + first) * SZ;
+        row = wave * ROWS + lane / PIECES;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
-            const int k = q * 16 + row;
-            const int64_t c = min((int64_t)unit_of(k, (lane & 31) >> 1) * 16 + (lane & 1) * 8, cols - 8 - first);
-            offset[q] = (uint32_t)(k * step) + (uint32_t)c * 2;
+            const int k = q * 8 * ROWS + row;
+            const int64_t c = min((int64_t)(unit_of(k, p / UNIT) * UNIT + p % UNIT) * E, cols - E - first);
+            offset[q] = (uint32_t)(k * step) + (uint32_t)c * SZ;
         }
     }
-    static __device__ inline int unit_of(int k, int u) { return u ^ ((k & 3) | (((k >> 3) & 1) << 2)); }
-    __device__ const char* stage(int t) const { return at + (int64_t)t * WIDE_STAGE * step; }
-    __device__ bool holds(int t, int q) const { return t * WIDE_STAGE + q * 16 + row < depth; }
-    static __device__ inline uint4 read(const char* lds, int b, int kb) {
+    static __device__ inline int unit_of(int k, int u) {
+        if constexpr (SZ == 2) return u ^ ((k & 3) | (((k >> 3) & 1) << 2));
+        else return u ^ ((k >> 2) & 3);
+    }
+    __device__ const char* stage(int t) const { return at + (int64_t)t * STAGE * step; }
+    __device__ bool holds(int t, int q) const { return t * STAGE + q * 8 * ROWS + row < depth; }
+    static __device__ inline frag read(const char* lds, int b, int kb) {
         const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
-        typedef __attribute__((address_space(3))) s16x4* lds4;
-        const int k = kb * 32 + 8 * lk + (li >> 2);
-        const char* a = lds + k * 512 + unit_of(k, b >> 4) * 32 + (li & 3) * 8;
-        const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(const_cast<char*>(a))));
-        const uint2 hi = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(const_cast<char*>(a + 2048))));
-        return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        if constexpr (SZ == 4) {
+            const float* a = reinterpret_cast<const float*>(lds + (kb * 16 + 4 * lk) * PITCH + ((b >> 4) ^ lk) * 64) + li;
+            constexpr int S = PITCH / 4;
+            return make_float4(a[0], a[S], a[2 * S], a[3 * S]);
+        } else {
+            typedef __attribute__((address_space(3))) s16x4* lds4;
+            const int k = kb * 32 + 8 * lk + (li >> 2);
+            const char* a = lds + k * PITCH + unit_of(k, b >> 4) * 32 + (li & 3) * 8;
+            const uint2 lo = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(const_cast<char*>(a))));
+            const uint2 hi = __builtin_bit_cast(
+                uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(const_cast<char*>(a + 4 * PITCH))));
+            return make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
     }
 };
 template <class Op>
@@ -107,7 +125,7 @@ __device__ inline void bring(const Op& op, int t, char* lds, uint32_t to) {
     const u32x4 rs = far_rsrc(op.stage(t));
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t start = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-    if ((t + 1) * WIDE_STAGE <= op.depth) {
+    if ((t + 1) * Op::STAGE <= op.depth) {
 #pragma unroll
         for (int q = 0; q < 4; q++) load_to_lds(rs, op.offset[q], start + to + (q * 8 + wave) * 1024);
     } else {
@@ -146,9 +164,9 @@ __device__ inline WidePlace wide_place(const WideArgs& a, uint32_t tile) {
 }
 
 // The epilogue of a wave's 128 x 64 values: lane li holds rows r + 16 i, values
-// c + 16 j + 4 lk to + 3 of each, for columns in whole eights.  All lanes take
-// part (put_pair16).  The residual's values of the next row are on their way
-// while this row's are stored.
+// c + 16 j + 4 lk to + 3 of each, for columns in whole fours.  All lanes take
+// part (put_pair16).  The next row of a residual of 16 bits is on its way while
+// this row is stored (there are no registers for one of fp32).
 template <int DT, int ACT>
 __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[8][4]) {
     const Epilogue& e = p.e;
@@ -187,10 +205,17 @@ __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, float
             for (int j = 0; j < 4; j++)
 #pragma unroll
                 for (int k = 0; k < 4; k++) acc[i][j][k] += bias[j][k];
-        if (e.pre)
+        if (e.pre) {
+            if constexpr (DT == TAURUS_F32) {
+                if (in)
 #pragma unroll
-            for (int j = 0; j < 4; j += 2)
-                put_pair16<DT>(e.pre, row * e.pre_stride, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
+                    for (int j = 0; j < 4; j++) put4(e.pre, DT, row * e.pre_stride, at + 16 * j, cols, acc[i][j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; j += 2)
+                    put_pair16<DT>(e.pre, row * e.pre_stride, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
+            }
+        }
 #pragma unroll
         for (int j = 0; j < 4; j++)
 #pragma unroll
@@ -234,7 +259,7 @@ struct WideItem {
     int depth, stages;
     uint32_t sums;  // which tile's room of the workspace the sums go to
     bool cut;
-    __device__ WideItem(const WideArgs& a, uint32_t b) : sums(0), cut(b >= a.whole) {
+    __device__ WideItem(const WideArgs& a, uint32_t b, int stage) : sums(0), cut(b >= a.whole) {
         uint32_t tile, part = 0;
         if (cut) {
             const uint32_t i = wide_turn(b - a.whole, a.cut * a.p.splits);
@@ -249,7 +274,7 @@ struct WideItem {
         c0 = at.col * WIDE;
         k0 = part * a.p.per;
         depth = (int)(cut && (int)part + 1 < a.p.splits ? a.p.per : a.p.depth - k0);
-        stages = (depth + WIDE_STAGE - 1) / WIDE_STAGE;
+        stages = (depth + stage - 1) / stage;
     }
 };
 
@@ -264,7 +289,9 @@ __global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
     const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
 
     // the stages' stream to LDS: the next to bring
-    WideItem coming(a, blockIdx.x);
+    constexpr int STAGE = Tile<DT>::STAGE;
+    typedef typename Tile<DT>::frag frag;
+    WideItem coming(a, blockIdx.x, STAGE);
     uint32_t coming_b = blockIdx.x;
     int coming_t = 0;
     OpM om(a.p.m, a.p.ms, coming.r0, a.p.rows, coming.k0, coming.depth);
@@ -277,26 +304,42 @@ __global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
         coming_t = 0;
         coming_b += gridDim.x;
         if (coming_b >= items) return;
-        coming = WideItem(a, coming_b);
+        coming = WideItem(a, coming_b, STAGE);
         om = OpM(a.p.m, a.p.ms, coming.r0, a.p.rows, coming.k0, coming.depth);
         on = OpN(a.p.n, a.p.ns, coming.c0, a.p.cols, coming.k0, coming.depth);
     };
-    uint4 fn[2][4], fm[2][4];
-    auto read_n = [&](const char* at, int kb, uint4 (&f)[4]) {
+    frag fn[2][4], fm[2][4];
+    auto read_n = [&](const char* at, int kb, frag (&f)[4]) {
 #pragma unroll
         for (int j = 0; j < 4; j++) f[j] = OpN::read(at + WIDE_BYTES, n0 + 16 * j, kb);
     };
-    auto read_m = [&](const char* at, int kb, int half, uint4 (&f)[4]) {
+    auto read_m = [&](const char* at, int kb, int half, frag (&f)[4]) {
 #pragma unroll
         for (int i = 0; i < 4; i++) f[i] = OpM::read(at, m0 + 64 * half + 16 * i, kb);
     };
     floatx4 acc[8][4];
-    auto multiply = [&](const uint4 (&n)[4], const uint4 (&m)[4], auto half) {
+    auto multiply = [&](const frag (&n)[4], const frag (&m)[4], auto half) {
         constexpr int H = decltype(half)::value;
+        if constexpr (DT == TAURUS_F32) {  // a component at a time, to different sums in turn
+            auto step = [&](auto get) {
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+                for (int i = 0; i < 4; i++)
 #pragma unroll
-            for (int j = 0; j < 4; j++) acc[4 * H + i][j] = mfma16<DT>(n[j], m[i], acc[4 * H + i][j]);
+                    for (int j = 0; j < 4; j++)
+                        acc[4 * H + i][j] =
+                            __builtin_amdgcn_mfma_f32_16x16x4f32(get(n[j]), get(m[i]), acc[4 * H + i][j], 0, 0, 0);
+            };
+            step([](const frag& f) { return f.x; });
+            step([](const frag& f) { return f.y; });
+            step([](const frag& f) { return f.z; });
+            step([](const frag& f) { return f.w; });
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) acc[4 * H + i][j] = mfma16<DT>(n[j], m[i], acc[4 * H + i][j]);
+        }
+        // LDS reads of the step ahead between the products
 #pragma unroll
         for (int g = 0; g < 8; g++) {
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
@@ -312,7 +355,7 @@ __global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     uint32_t buffer = 0;
     for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
-        const WideItem item(a, b);
+        const WideItem item(a, b, STAGE);
         read_n(lds + buffer, 0, fn[0]);
         read_m(lds + buffer, 0, 0, fm[0]);
 #pragma unroll
@@ -375,21 +418,22 @@ struct WidePlan {
     int splits;
 };
 // A part's sums are written and read, about 0.1 us for the whole chip; a stage
-// takes about 0.9 us: cutting r tiles of s stages into p parts costs about 0.9
-// s / p + 0.1 r p, least at 3 sqrt(s / r) parts.
-static WidePlan wide_plan(int64_t rows, int64_t cols, int64_t depth) {
-    const int64_t tiles = ceil_div(rows, WIDE) * ceil_div(cols, WIDE), stages = ceil_div(depth, WIDE_STAGE);
+// takes about 1.5 us (fp32: 6): cutting r tiles of s stages into p parts costs
+// about s / p times that and 0.1 r p, least at sqrt(s / r) times 3.9 (7.7) parts.
+static WidePlan wide_plan(int dtype, int64_t rows, int64_t cols, int64_t depth) {
+    const int stage = dtype == TAURUS_F32 ? 32 : 64;
+    const int64_t tiles = ceil_div(rows, WIDE) * ceil_div(cols, WIDE), stages = ceil_div(depth, stage);
     constexpr int64_t CUS = 256;  // of the chip; a workgroup fills one
     const int64_t rest = tiles % CUS;
-    WidePlan p{tiles, 0, stages * WIDE_STAGE, 1};
+    WidePlan p{tiles, 0, stages * stage, 1};
     if (!rest || stages < 4) return p;
-    const int64_t best = (int64_t)(3.0 * sqrt((double)stages / (double)rest));
+    const int64_t best = (int64_t)((dtype == TAURUS_F32 ? 7.7 : 3.9) * sqrt((double)stages / (double)rest));
     const int64_t parts = std::min(std::min(CUS / rest, stages / 2), best);
     if (parts < 2) return p;
     const int64_t each = ceil_div(stages, parts);
     p.whole = tiles - rest;
     p.cut = rest;
-    p.per = each * WIDE_STAGE;
+    p.per = each * stage;
     p.splits = (int)ceil_div(stages, each);
     return p;
 }
@@ -400,16 +444,16 @@ static WidePlan wide_plan(int64_t rows, int64_t cols, int64_t depth) {
 // / 24 / 43; 4,096 x 4,096 -> 1,024 (17e9) 67 / 58 / 70 against 56 / 36 / 54).
 constexpr double WIDE_WORK = 6e9;
 bool wide_takes(int kind, int dtype, const ProductArgs& a) {
-    if (dtype == TAURUS_F32) return false;
-    auto whole = [](const void* p, int64_t width, int64_t stride) {
-        return width % 8 == 0 && stride % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+    const int e = 16 / dtype_size(dtype);  // rows of whole 16-byte pieces
+    auto whole = [e](const void* p, int64_t width, int64_t stride) {
+        return width % e == 0 && stride % e == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
     };
     const int64_t m_width = kind == PRODUCT_DW ? a.rows : a.depth, n_width = kind == PRODUCT_DX ? a.depth : a.cols;
-    return whole(a.m, m_width, a.ms) && whole(a.n, n_width, a.ns) && a.cols % 8 == 0 && a.rows >= 256 && a.cols >= 256 &&
+    return whole(a.m, m_width, a.ms) && whole(a.n, n_width, a.ns) && a.cols % e == 0 && a.rows >= 256 && a.cols >= 256 &&
            a.depth >= 256 && (double)a.rows * a.cols * a.depth >= WIDE_WORK && ceil_div(a.rows, WIDE) * ceil_div(a.cols, WIDE) <= WIDE_TILES;
 }
-int64_t wide_part(int64_t rows, int64_t cols, int64_t depth) {
-    const WidePlan p = wide_plan(rows, cols, depth);
+int64_t wide_part(int dtype, int64_t rows, int64_t cols, int64_t depth) {
+    const WidePlan p = wide_plan(dtype, rows, cols, depth);
     return p.cut * p.splits * WIDE * WIDE;
 }
 template <int KIND, int DT>
@@ -427,7 +471,7 @@ static void wide_launch(const WideArgs& a, int act, hipStream_t s) {
     else go(std::integral_constant<int, TAURUS_ACT_NONE>{});
 }
 void wide_product(int kind, int dtype, ProductArgs p, float* part, int act, hipStream_t s) {
-    const WidePlan plan = wide_plan(p.rows, p.cols, p.depth);
+    const WidePlan plan = wide_plan(dtype, p.rows, p.cols, p.depth);
     p.part = part;
     p.per = plan.per;
     p.splits = plan.splits;
@@ -440,7 +484,8 @@ void wide_product(int kind, int dtype, ProductArgs p, float* part, int act, hipS
         else if (kind == PRODUCT_DX) wide_launch<PRODUCT_DX, DT>(a, act, s);
         else wide_launch<PRODUCT_DW, DT>(a, act, s);
     };
-    if (dtype == TAURUS_BF16) of(std::integral_constant<int, TAURUS_BF16>{});
+    if (dtype == TAURUS_F32) of(std::integral_constant<int, TAURUS_F32>{});
+    else if (dtype == TAURUS_BF16) of(std::integral_constant<int, TAURUS_BF16>{});
     else of(std::integral_constant<int, TAURUS_F16>{});
 }
 

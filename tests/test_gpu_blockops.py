@@ -215,6 +215,49 @@ def test_linear_large(dtype, case):
     check_linear_grad(x, w, normal((m, n), dtype, case + 5), act, [F32, dtype][case % 2], pre)
 
 
+WIDE = [  # rows, d_in, d_out of products in tiles of 256 x 256: a single partial
+    # round of tiles, whole rounds and a rest, a rest too large to cut, rests of
+    # every tile and stage
+    (2049, 1032, 2904), (5000, 520, 3208), (16_500, 264, 1480), (772, 4100, 2060), (30_001, 256, 840),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(WIDE)))
+def test_linear_wide(dtype, case):
+    m, k, n = WIDE[case]
+    act, out_dtype = ACTS[case % 5], [dtype, F32][case % 2]
+    note(f"linear wide {dtype} m={m} k={k} n={n} {act} -> {out_dtype}")
+    x, w, b = normal((m, k), dtype, case), normal((k, n), dtype, case + 1, k ** -0.5), normal((n,), F32, case + 2)
+    res = normal((m, n), out_dtype, case + 3) if case % 3 != 1 else None
+    check_linear(x, w, b, res, act, out_dtype, case % 2 == 0)
+    pre = None if act == "none" else normal((m, n), dtype, case + 4, 2.0)
+    check_linear_grad(x, w, normal((m, n), dtype, case + 5), act, [F32, dtype][case % 2], pre)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_linear_wide_strided(dtype):
+    """Rows that are wide apart, whose surroundings are NaN, and special values
+    in the last rows and columns."""
+    note(f"linear wide strided {dtype}")
+    m, k, n = 2050, 1040, 2912
+    x, w, b = normal((m, k), dtype, 1), normal((k, n), dtype, 2, k ** -0.5), normal((n,), F32, 3)
+    wide = torch.full((m, n + 24), 7.0, dtype=dtype, device="cuda")
+    out = wide[:, 8:8 + n]
+    got, pre = T.linear(strided(x, 8, 16), w.cuda(), b.cuda(), strided(b.to(dtype).expand(m, n), 16, 8), act="relu", out=out, pre=True)
+    z, tz, y, ty = linear_reference(x, w, b, b.to(dtype).expand(m, n), "relu")
+    close(out, y, ty, dtype, "out")
+    close(pre, z, tz, dtype, "pre")
+    assert (torch.cat([wide[:, :8], wide[:, 8 + n:]], 1) == 7.0).all()
+    x[:], w[:] = 1, 1
+    x[1, 0], x[m - 1, k - 1], w[3, n - 1] = math.inf, math.nan, -math.inf
+    out = T.linear(strided(x, 8, 0), w.cuda(), out_dtype=F32).cpu()
+    rest = torch.ones(m, dtype=torch.bool)
+    rest[1] = rest[m - 1] = False
+    assert (out[rest][:, :n - 1] == k).all() and (out[rest][:, n - 1] == -math.inf).all()
+    assert (out[1, :n - 1] == math.inf).all() and torch.isnan(out[1, n - 1]) and torch.isnan(out[m - 1]).all()
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_act_at_any_argument(act, dtype):
