@@ -9,6 +9,7 @@ call runs on.  Names follow the C ABI (``linear`` = taurus_linear, ...).
 """
 from __future__ import annotations
 
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -25,6 +26,12 @@ def _act(act) -> int:
     if act not in _ACT:
         raise ValueError(f"act must be one of {', '.join(_ACT)}, got {act!r}")
     return _ACT[act]
+
+
+@functools.lru_cache(maxsize=4096)
+def _bytes(call: str, *sizes) -> int:
+    """A call's workspace: follows from the sizes alone."""
+    return getattr(N.lib(), call)(*sizes)
 
 
 def _needed(need, names) -> None:
@@ -57,7 +64,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
         out, op, os = c.out(out, (m, d_out), dtype, "out", x, weight, bias, residual)
         z = torch.empty((m, d_out), dtype=x.dtype, device=c.device) if pre else None
         L = N.lib()
-        nbytes = L.taurus_linear_bytes(code, m, d_in, d_out)
+        nbytes = _bytes("taurus_linear_bytes", code, m, d_in, d_out)
         work, kp = c.work(nbytes, "taurus_linear_bytes")
         N.check(L.taurus_linear(xp, code, m, d_in, xs, wp, d_out, bp, rp, rs, act_code, op, out_code, os,
                                 None if z is None else z.data_ptr(), d_out, kp, nbytes, c.ptr), "taurus_linear")
@@ -88,7 +95,7 @@ def linear_grad(grad: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: 
         dw = torch.empty((d_in, d_out), dtype=weight_dtype, device=c.device) if "weight" in need else None
         db = torch.empty(d_out, dtype=torch.float32, device=c.device) if "bias" in need else None
         L = N.lib()
-        nbytes = L.taurus_linear_grad_bytes(code, m, d_in, d_out, act_code)
+        nbytes = _bytes("taurus_linear_grad_bytes", code, m, d_in, d_out, act_code)
         work, kp = c.work(nbytes, "taurus_linear_grad_bytes")
         N.check(L.taurus_linear_grad(gp, gs, xp, xs, code, m, d_in, d_out, wp, zp, zs, act_code,
                                      None if dx is None else dx.data_ptr(), d_in,
@@ -99,11 +106,15 @@ def linear_grad(grad: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: 
 
 # ----------------------------------------------------------- residual norm --
 
+_NORM_KEYS = {"kind", "weight", "bias", "eps"}
+
+
 def check_norm_args(norm: Optional[dict], what: str) -> None:
-    unknown = set(norm or ()) - {"kind", "weight", "bias", "eps"}
-    if unknown:
-        raise ValueError(f"{what} does not know {', '.join(sorted(unknown))}")
-    if norm is not None and norm.get("kind", "layer") not in _NORM:
+    if norm is None:
+        return
+    if not norm.keys() <= _NORM_KEYS:
+        raise ValueError(f"{what} does not know {', '.join(sorted(norm.keys() - _NORM_KEYS))}")
+    if norm.get("kind", "layer") not in _NORM:
         raise ValueError(f"{what}'s kind must be one of {', '.join(_NORM)}, got {norm['kind']!r}")
 
 
@@ -112,12 +123,17 @@ class _Norm:
     __slots__ = ("kind", "weight", "bias", "wp", "bp", "eps")
 
     def __init__(self, c: _Call, norm: Optional[dict], d: int, what: str):
+        self.kind, self.eps = N.NORM_NONE, 1e-5
+        self.weight = self.bias = self.wp = self.bp = None
+        if norm is None:
+            return
         check_norm_args(norm, what)
-        given = norm or {}
-        self.kind = N.NORM_NONE if norm is None else _NORM[given.get("kind", "layer")]
-        self.weight, self.bias, self.eps = given.get("weight"), given.get("bias"), given.get("eps", 1e-5)
-        self.wp = c.dense(self.weight, (d,), torch.float32, f"{what}'s weight")
-        self.bp = c.dense(self.bias, (d,), torch.float32, f"{what}'s bias")
+        self.kind, self.eps = _NORM[norm.get("kind", "layer")], norm.get("eps", 1e-5)
+        self.weight, self.bias = norm.get("weight"), norm.get("bias")
+        if self.weight is not None:
+            self.wp = c.dense(self.weight, (d,), torch.float32, f"{what}'s weight")
+        if self.bias is not None:
+            self.bp = c.dense(self.bias, (d,), torch.float32, f"{what}'s bias")
 
 
 def _gate(c: _Call, gate: Optional[torch.Tensor], off: Optional[torch.Tensor], d: int):
@@ -209,7 +225,7 @@ def residual_norm_grad(grad_y: Optional[torch.Tensor], grad_h: Optional[torch.Te
                              new("pre" in need and b.bias is not None, d))
         p = [None if t is None else t.data_ptr() for t in g]
         L = N.lib()
-        nbytes = L.taurus_residual_norm_grad_bytes(code, m, d, segs, int(off is not None))
+        nbytes = _bytes("taurus_residual_norm_grad_bytes", code, m, d, segs, int(off is not None))
         work, kp = c.work(nbytes, "taurus_residual_norm_grad_bytes")
         N.check(L.taurus_residual_norm_grad(
             gyp, gys, ghp, ghs, yp, y_code, ys, fp, code, fs, m, d, scale, gp, op, segs, a.kind, a.wp, a.bp, b.kind,
@@ -245,7 +261,7 @@ def label_log_probs(x: torch.Tensor, labels: Optional[torch.Tensor] = None, scal
             return torch.empty(shape, dtype=dtype, device=c.device) if wanted else None
 
         L = N.lib()
-        nbytes = L.taurus_label_log_probs_bytes(code, m, classes, top)
+        nbytes = _bytes("taurus_label_log_probs_bytes", code, m, classes, top)
         work, kp = c.work(nbytes, "taurus_label_log_probs_bytes")
         r = LabelLogProbs(new(labels is not None, m), new(True, (m, 2)), new(entropy, m), new(top > 0, (m, top)),
                           new(top > 0, (m, top), torch.int32))

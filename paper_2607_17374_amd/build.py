@@ -12,7 +12,7 @@ BUILD = os.path.join(HERE, "_build")
 SO = os.path.join(HERE, "libtaurus.so")
 SOURCES = ["prims.hip", "csr.hip", "gemm.hip", "sample.hip", "reorder.hip", "reorder_ta.hip", "resident.hip",
            "gather.hip", "layer.hip", "rows.hip", "grouped.hip", "norm.hip",
-           "linear.hip", "linear_wide.hip", "resnorm.hip", "labels.hip"]
+           "linear.hip", "linear_wide.hip", "linear_few.hip", "resnorm.hip", "labels.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

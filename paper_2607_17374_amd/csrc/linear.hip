@@ -206,25 +206,36 @@ static void product_tiles(const ProductArgs& a, bool al, hipStream_t s) {
     TAURUS_CHECK_LAUNCH();
 }
 template <int KIND, int DT>
+static void join(const ProductArgs& a, int act, hipStream_t s) {
+    const unsigned grid = grid_for(std::min<int64_t>(ceil_div(a.rows * ceil_div(a.cols, 4), 256), 4096));
+    if constexpr (KIND == PRODUCT_Y) {
+        with_act(act, [&](auto c) { k_linear_join<DT, decltype(c)::value><<<grid, 256, 0, s>>>(a); });
+    } else {
+        k_linear_join<DT, TAURUS_ACT_NONE><<<grid, 256, 0, s>>>(a);
+    }
+    TAURUS_CHECK_LAUNCH();
+}
+template <int KIND, int DT>
 static void product(ProductArgs a, float* part, int act, hipStream_t s) {
+    a.part = part;
+    if (KIND == PRODUCT_Y && few_takes(DT, a.rows, a.cols)) {
+        few_product(DT, a, act, s);
+        a.splits = few_plan(DT, a.rows, a.cols, a.depth).parts;
+        if (a.splits > 1) join<KIND, DT>(a, act, s);
+        return;
+    }
     if (wide_takes(KIND, DT, a)) return wide_product(KIND, DT, a, part, act, s);
     const int64_t m_width = KIND == PRODUCT_DW ? a.rows : a.depth, n_width = KIND == PRODUCT_DX ? a.depth : a.cols;
     const bool al = whole_words(DT, a.m, m_width, a.ms) && whole_words(DT, a.n, n_width, a.ns);
     const ProductPlan p = product_plan(DT, a.rows, a.cols, a.depth);
-    a.part = p.splits > 1 ? part : nullptr;
+    if (p.splits == 1) a.part = nullptr;
     a.per = p.per;
     a.row_tiles = p.row_tiles;
     a.col_tiles = p.col_tiles;
     a.splits = p.splits;
     if (p.splits > 1) {  // the sums alone: one kernel for all activations
         product_tiles<KIND, DT, TAURUS_ACT_NONE>(a, al, s);
-        const unsigned grid = grid_for(std::min<int64_t>(ceil_div(a.rows * ceil_div(a.cols, 4), 256), 4096));
-        if constexpr (KIND == PRODUCT_Y) {
-            with_act(act, [&](auto c) { k_linear_join<DT, decltype(c)::value><<<grid, 256, 0, s>>>(a); });
-        } else {
-            k_linear_join<DT, TAURUS_ACT_NONE><<<grid, 256, 0, s>>>(a);
-        }
-        TAURUS_CHECK_LAUNCH();
+        join<KIND, DT>(a, act, s);
     } else if constexpr (KIND == PRODUCT_Y) {
         with_act(act, [&](auto c) { product_tiles<KIND, DT, decltype(c)::value>(a, al, s); });
     } else {
@@ -255,7 +266,7 @@ static int64_t part_values(int dtype, int64_t rows, int64_t cols, int64_t depth)
 }
 static int64_t forward_bytes(int dtype, int64_t m, int64_t d_in, int64_t d_out) {
     Carve c;
-    c.take<float>(part_values(dtype, m, d_out, d_in));
+    c.take<float>(few_takes(dtype, m, d_out) ? few_plan(dtype, m, d_out, d_in).part : part_values(dtype, m, d_out, d_in));
     return c.bytes();
 }
 static LinearWork gradient_work(void* work, int dtype, int64_t m, int64_t d_in, int64_t d_out, int act) {

@@ -80,6 +80,15 @@ __device__ inline void finish(const Epilogue& e, int64_t r, int c, float (&v)[E]
     }
     store_as<E>(e.out_dtype, e.out, r * e.out_stride + c, v);
 }
+// the same with the activation known at run time (uniform)
+template <int DT, int E>
+__device__ inline void finish_any(const Epilogue& e, int act, int64_t r, int c, float (&v)[E]) {
+    if (act == TAURUS_ACT_RELU) finish<DT, TAURUS_ACT_RELU, E>(e, r, c, v);
+    else if (act == TAURUS_ACT_SILU) finish<DT, TAURUS_ACT_SILU, E>(e, r, c, v);
+    else if (act == TAURUS_ACT_GELU) finish<DT, TAURUS_ACT_GELU, E>(e, r, c, v);
+    else if (act == TAURUS_ACT_GELU_TANH) finish<DT, TAURUS_ACT_GELU_TANH, E>(e, r, c, v);
+    else finish<DT, TAURUS_ACT_NONE, E>(e, r, c, v);
+}
 // four consecutive values of a row of `cols`
 template <int DT, int ACT>
 __device__ inline void finish4(const Epilogue& e, int64_t r, int c, int cols, floatx4 v,
@@ -110,6 +119,16 @@ struct ProductArgs {
     int64_t row_tiles;
     int col_tiles, splits;
 };
+
+// Maps of few rows (linear_few.hip).
+bool few_takes(int dtype, int64_t rows, int64_t cols);
+struct FewPlan {
+    int64_t per;   // contraction values of a part
+    int parts;
+    int64_t part;  // fp32 values of the workspace
+};
+FewPlan few_plan(int dtype, int64_t rows, int64_t cols, int64_t depth);
+void few_product(int dtype, ProductArgs a, int act, hipStream_t s);  // a.part: the workspace
 
 // Large products (linear_wide.hip).  Whether one is taken,
 // and the fp32 values it leaves in the workspace.

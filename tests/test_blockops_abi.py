@@ -82,8 +82,8 @@ BAD = [
     (_linear, dict(os=7), "apart"), (_linear, dict(res=P, rs=7), "apart"), (_linear, dict(pre=P, ps=7), "apart"),
     (_linear, dict(bias=P + 2), "bias is not aligned"), (_linear, dict(x=P + 1), "x is not aligned"),
     (_linear, dict(res=P + 2), "residual is not aligned"), (_linear, dict(pre=P + 1), "pre is not aligned"),
-    (_linear, dict(k=4096, xs=4096, bytes=16), "workspace has 16"), (_linear, dict(k=4096, xs=4096, work=None), "workspace is null"),
-    (_linear, dict(k=4096, xs=4096, work=P + 4), "16-byte aligned"),
+    (_linear, dict(m=100, k=4096, xs=4096, bytes=16), "workspace has 16"), (_linear, dict(m=100, k=4096, xs=4096, work=None), "workspace is null"),
+    (_linear, dict(m=100, k=4096, xs=4096, work=P + 4), "16-byte aligned"),
     (_linear_grad, dict(wdt=5), "none of"), (_linear_grad, dict(gs=7), "apart"), (_linear_grad, dict(xs=7), "apart"),
     (_linear_grad, dict(dxs=7), "apart"), (_linear_grad, dict(w=None), "weight is null"),
     (_linear_grad, dict(x=None), "x is null"), (_linear_grad, dict(pre=None), "pre is null"),
@@ -141,7 +141,9 @@ def test_nothing_to_do_is_ok_without_pointers():
 def test_workspace_sizes():
     L = N.lib()
     assert L.taurus_linear_bytes(N.BF16, 1_000_000, 256, 256) == 0       # tiles fill the chip
-    assert L.taurus_linear_bytes(N.BF16, 3, 4096, 1024) >= 2 * 3 * 1024 * 4
+    assert L.taurus_linear_bytes(N.BF16, 32, 1024, 1024) == 0            # few rows: one launch
+    assert L.taurus_linear_bytes(N.BF16, 32, 4096, 1024) >= 2 * 32 * 1024 * 4
+    assert L.taurus_linear_bytes(N.BF16, 65, 4096, 1024) >= 2 * 65 * 1024 * 4
     assert L.taurus_label_log_probs_bytes(N.BF16, 100_000, 1000, 5) == 0
     assert L.taurus_label_log_probs_bytes(N.BF16, 3, 100_000, 5) > 0
     # dz, where there is an activation

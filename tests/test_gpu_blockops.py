@@ -111,7 +111,9 @@ def linear_reference(x, w, b, res, act):
 LINEAR = [  # rows, d_in, d_out
     (1, 1, 1), (3, 5, 7), (2, 9, 1), (1, 1024, 1024), (3, 64, 64), (17, 130, 47), (128, 64, 128), (129, 200, 65),
     (200, 1000, 136), (513, 256, 256), (1000, 72, 300), (64, 4096, 96), (16, 2050, 40), (5, 8, 2000), (700, 33, 90),
-    (300, 520, 264), (0, 16, 8),
+    (300, 520, 264), (0, 16, 8), (1, 2048, 8200), (16, 31, 4100), (17, 96, 8193), (32, 300, 33), (33, 513, 70), (64, 40, 9000),
+    (5, 7, 3), (48, 1000, 7), (65, 1000, 7), (9, 4, 4), (3, 4100, 70), (20, 3000, 24), (32, 9000, 10),
+    (1, 2049, 1),
 ]
 
 
