@@ -423,14 +423,21 @@ def _answer(h: torch.Tensor, head: dict, stream):
     return label_log_probs(h, head.pop("labels", None), stream=stream, **head)
 
 
-def _check_head(head: dict) -> None:
+def _check_head(head: dict, n: int, width: Optional[int]) -> None:
+    """The head fits n rows of `width` values (None: not known)."""
     unknown = set(head) - {"linear", "labels", "scale", "top", "entropy"}
     if unknown:
         raise ValueError(f"head does not know {', '.join(sorted(unknown))}")
-    for m in head.get("linear", ()):
+    for m in head["linear"]:
         unknown = set(m) - {"weight", "bias", "act"}
         if unknown or "weight" not in m:
             raise ValueError("head's linear maps have weight, bias and act, got " + ", ".join(sorted(m)))
+        if m["weight"].dim() != 2 or width not in (None, m["weight"].shape[0]):
+            raise ValueError(f"head's linear map of shape {tuple(m['weight'].shape)} takes no rows of {width} values")
+        width = m["weight"].shape[1]
+    labels = head.get("labels")
+    if labels is not None and labels.numel() != n:
+        raise ValueError(f"head has {labels.numel()} labels for {n} vertices")
 
 
 def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Tensor, layers: list,
@@ -467,7 +474,7 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     _check_blocks(layers, x.dtype)
     if head is not None:
         head = dict(head, linear=list(head.get("linear", ())))
-        _check_head(head)
+        _check_head(head, n, layers[-1]["d_out"] if layers else None)
     h = x if encoder is None else _encode(x, encoder, n, layers[0]["d_in"] if layers else None, stream)
     results, stats = [], []
     block, norm, rows = None, None, h[:n]  # rows: the residual stream

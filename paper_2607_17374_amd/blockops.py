@@ -30,8 +30,12 @@ def _act(act) -> int:
 
 @functools.lru_cache(maxsize=4096)
 def _bytes(call: str, *sizes) -> int:
-    """A call's workspace: follows from the sizes alone."""
-    return getattr(N.lib(), call)(*sizes)
+    """A call's workspace: follows from the sizes alone (refused ones are not
+    remembered)."""
+    nbytes = getattr(N.lib(), call)(*sizes)
+    if nbytes < 0:
+        raise N.TaurusError(int(nbytes), call, N.last_error())
+    return nbytes
 
 
 def _needed(need, names) -> None:

@@ -170,6 +170,14 @@ def test_linear_workspace_is_bounded(dtype, size, m, k, n):
         assert N.lib().taurus_linear_grad_bytes(dtype, m, k, n, act) <= parts + dz + sums + 2048 * 512 * 4 + 1024
 
 
+def test_refused_sizes_are_told_every_time():
+    from paper_2607_17374_amd import blockops
+    for _ in range(2):
+        with pytest.raises(T.TaurusError, match="alternatives"):
+            blockops._bytes("taurus_label_log_probs_bytes", N.F32, 4, 4, 5)
+        N.lib().taurus_linear_bytes(N.F32, -1, 4, 4)  # another message in between
+
+
 def test_wrapper_refuses_host_tensors():
     x, v, ids = torch.zeros(4, 8), torch.zeros(4), torch.zeros(4, dtype=torch.int32)
     w = torch.zeros(8, 8)
@@ -201,6 +209,9 @@ LAYER = dict(d_in=8, d_out=8)
     ([dict(LAYER)], dict(labelz=1), "head does not know labelz"),
     ([dict(LAYER)], dict(linear=[dict(bias=1)]), "head's linear maps"),
     ([dict(LAYER)], dict(linear=[dict(weight=1, residual=2)]), "head's linear maps"),
+    ([dict(LAYER)], dict(linear=[dict(weight=torch.zeros(9, 4))]), "takes no rows of 8 values"),
+    ([dict(LAYER)], dict(linear=[dict(weight=torch.zeros(8, 4)), dict(weight=torch.zeros(5, 4))]), "takes no rows of 4 values"),
+    ([dict(LAYER)], dict(labels=torch.zeros(5)), "5 labels for 4 vertices"),
 ])
 def test_model_refuses_blocks_and_heads_that_do_not_fit(layers, head, text):
     x, off = torch.zeros(4, 8), torch.tensor([0, 4])
