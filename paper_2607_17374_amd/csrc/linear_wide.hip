@@ -20,7 +20,13 @@
 
 namespace taurus {
 
-constexpr int WIDE = 256, WIDE_BYTES = 256 * 128;  // of an operand's stage
+// T x T tiles: 256 by eight waves of 128 x 64, one workgroup a compute unit; 128
+// by four of 64 x 64, two.
+template <int T>
+struct Wide {
+    static constexpr int WAVES = T == 256 ? 8 : 4, THREADS = WAVES * 64, BYTES = T * 128;  // of an operand's stage
+    static constexpr int MI = T == 256 ? 8 : 4, NI = 4, PER_CU = T == 256 ? 1 : 2;
+};
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -48,7 +54,7 @@ __device__ inline void zero_to_lds(char* lds, uint32_t to) {
 
 // One operand of a tile: how its stages come to LDS and are read.  `at` is the
 // first row's (Along) or the first contraction row's (Across) address.
-template <int DT>
+template <int DT, int T>
 struct WideAlong {
     static constexpr int E = Tile<DT>::E, STAGE = Tile<DT>::STAGE, SZ = type_bytes<DT>;
     typedef typename Tile<DT>::frag frag;
@@ -63,22 +69,23 @@ struct WideAlong {
         col = p * E;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
-            const int64_t row = min((int64_t)(q * 8 + wave) * 8 + (lane >> 3), rows - 1 - first);
+            const int64_t row = min((int64_t)(q * Wide<T>::WAVES + wave) * 8 + (lane >> 3), rows - 1 - first);
             offset[q] = (uint32_t)(row * stride * SZ) + p * 16;
         }
     }
     __device__ const char* stage(int t) const { return at + (int64_t)t * STAGE * SZ; }
     __device__ bool holds(int t, int) const { return t * STAGE + col < depth; }
     // rows [r0, r0 + 16), matrix step kb
-    static __device__ inline frag read(const char* lds, int r0, int kb) { return Along<DT, WIDE, true>::read(lds, r0, kb); }
+    static __device__ inline frag read(const char* lds, int r0, int kb) { return Along<DT, T, true>::read(lds, r0, kb); }
 };
-// Rows of 256 values.  Of 16 bits: 32-byte units exchanged as product.hpp's; of
+// Rows of T values.  Of 16 bits: 32-byte units exchanged as product.hpp's; of
 // fp32: 64-byte units by the row's second pair of bits, so that the four rows
 // that are read together fall on different banks.
-template <int DT>
+template <int DT, int T>
 struct WideAcross {
     static constexpr int E = Tile<DT>::E, STAGE = Tile<DT>::STAGE, SZ = type_bytes<DT>;
-    static constexpr int PITCH = WIDE * SZ, PIECES = PITCH / 16, ROWS = 64 / PIECES;  // rows a wave's load fills
+    static constexpr int PITCH = T * SZ, PIECES = PITCH / 16, ROWS = 64 / PIECES;  // rows a wave's load fills
+    static constexpr int STEP = Wide<T>::WAVES * ROWS;
     static constexpr int UNIT = SZ == 2 ? 2 : 4;                                      // pieces
     typedef typename Tile<DT>::frag frag;
     const char* at;
@@ -92,7 +99,7 @@ struct WideAcross {
         row = wave * ROWS + lane / PIECES;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
-            const int k = q * 8 * ROWS + row;
+            const int k = q * STEP + row;
             const int64_t c = min((int64_t)(unit_of(k, p / UNIT) * UNIT + p % UNIT) * E, cols - E - first);
             offset[q] = (uint32_t)(k * step) + (uint32_t)c * SZ;
         }
@@ -102,7 +109,7 @@ struct WideAcross {
         else return u ^ ((k >> 2) & 3);
     }
     __device__ const char* stage(int t) const { return at + (int64_t)t * STAGE * step; }
-    __device__ bool holds(int t, int q) const { return t * STAGE + q * 8 * ROWS + row < depth; }
+    __device__ bool holds(int t, int q) const { return t * STAGE + q * STEP + row < depth; }
     static __device__ inline frag read(const char* lds, int b, int kb) {
         const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
         if constexpr (SZ == 4) {
@@ -120,18 +127,19 @@ struct WideAcross {
         }
     }
 };
-template <class Op>
+template <int T, class Op>
 __device__ inline void bring(const Op& op, int t, char* lds, uint32_t to) {
+    constexpr int WAVES = Wide<T>::WAVES;
     const u32x4 rs = far_rsrc(op.stage(t));
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const uint32_t start = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     if ((t + 1) * Op::STAGE <= op.depth) {
 #pragma unroll
-        for (int q = 0; q < 4; q++) load_to_lds(rs, op.offset[q], start + to + (q * 8 + wave) * 1024);
+        for (int q = 0; q < 4; q++) load_to_lds(rs, op.offset[q], start + to + (q * WAVES + wave) * 1024);
     } else {
 #pragma unroll
         for (int q = 0; q < 4; q++) {
-            const uint32_t at = to + (q * 8 + wave) * 1024;
+            const uint32_t at = to + (q * WAVES + wave) * 1024;
             if (op.holds(t, q)) load_to_lds(rs, op.offset[q], start + at);
             else zero_to_lds(lds, at);
         }
@@ -163,12 +171,12 @@ __device__ inline WidePlace wide_place(const WideArgs& a, uint32_t tile) {
     return {first + in % tall, in / tall};
 }
 
-// The epilogue of a wave's 128 x 64 values: lane li holds rows r + 16 i, values
+// The epilogue of a wave's 16 MI x 64 values: lane li holds rows r + 16 i, values
 // c + 16 j + 4 lk to + 3 of each, for columns in whole fours.  All lanes take
 // part (put_pair16).  The next row of a residual of 16 bits is on its way while
 // this row is stored (there are no registers for one of fp32).
-template <int DT, int ACT>
-__device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[8][4]) {
+template <int DT, int ACT, int MI>
+__device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[MI][4]) {
     const Epilogue& e = p.e;
     const int cols = (int)p.cols, at = c + 4 * ((threadIdx.x & 63) >> 4);
     const bool half = e.out_dtype != TAURUS_F32, is_bf16 = e.out_dtype == TAURUS_BF16;
@@ -192,14 +200,14 @@ __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, float
     };
     bring(0);
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
+    for (int i = 0; i < MI; i++) {
         __builtin_amdgcn_sched_barrier(0);  // a row at a time, which keeps addresses few
         const int64_t row = r + 16 * i;
         const bool in = row < p.rows;
         uint2 mine[4];
 #pragma unroll
         for (int j = 0; j < 4; j++) mine[j] = raw[j];
-        if (i < 7) bring(i + 1);
+        if (i + 1 < MI) bring(i + 1);
         if (e.bias)
 #pragma unroll
             for (int j = 0; j < 4; j++)
@@ -259,7 +267,7 @@ struct WideItem {
     int depth, stages;
     uint32_t sums;  // which tile's room of the workspace the sums go to
     bool cut;
-    __device__ WideItem(const WideArgs& a, uint32_t b, int stage) : sums(0), cut(b >= a.whole) {
+    __device__ WideItem(const WideArgs& a, uint32_t b, int stage, int tall) : sums(0), cut(b >= a.whole) {
         uint32_t tile, part = 0;
         if (cut) {
             const uint32_t i = wide_turn(b - a.whole, a.cut * a.p.splits);
@@ -270,75 +278,82 @@ struct WideItem {
             tile = wide_turn(b, a.whole);
         }
         const WidePlace at = wide_place(a, tile);
-        r0 = at.row * WIDE;
-        c0 = at.col * WIDE;
+        r0 = at.row * tall;
+        c0 = at.col * tall;
         k0 = part * a.p.per;
         depth = (int)(cut && (int)part + 1 < a.p.splits ? a.p.per : a.p.depth - k0);
         stages = (depth + stage - 1) / stage;
     }
 };
 
-template <int KIND, int DT, int ACT>
-__global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
-    typedef std::conditional_t<KIND == PRODUCT_DW, WideAcross<DT>, WideAlong<DT>> OpM;
-    typedef std::conditional_t<KIND == PRODUCT_DX, WideAlong<DT>, WideAcross<DT>> OpN;
-    __shared__ __align__(1024) char lds[4 * WIDE_BYTES];
+template <int KIND, int DT, int ACT, int T>
+__global__ __launch_bounds__(Wide<T>::THREADS, 2) void k_linear_wide(WideArgs a) {
+    typedef std::conditional_t<KIND == PRODUCT_DW, WideAcross<DT, T>, WideAlong<DT, T>> OpM;
+    typedef std::conditional_t<KIND == PRODUCT_DX, WideAlong<DT, T>, WideAcross<DT, T>> OpN;
+    constexpr int BYTES = Wide<T>::BYTES, MI = Wide<T>::MI;
+    __shared__ __align__(1024) char lds[4 * BYTES];
     const uint32_t items = a.whole + a.cut * a.p.splits;
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int m0 = (wave >> 2) * 128, n0 = (wave & 3) * 64;
+    const int m0 = T == 256 ? (wave >> 2) * 128 : (wave >> 1) * 64, n0 = T == 256 ? (wave & 3) * 64 : (wave & 1) * 64;
     const int lane = threadIdx.x & 63, li = lane & 15, lk = lane >> 4;
 
     // the stages' stream to LDS: the next to bring
     constexpr int STAGE = Tile<DT>::STAGE;
     typedef typename Tile<DT>::frag frag;
-    WideItem coming(a, blockIdx.x, STAGE);
+    WideItem coming(a, blockIdx.x, STAGE, T);
     uint32_t coming_b = blockIdx.x;
     int coming_t = 0;
     OpM om(a.p.m, a.p.ms, coming.r0, a.p.rows, coming.k0, coming.depth);
     OpN on(a.p.n, a.p.ns, coming.c0, a.p.cols, coming.k0, coming.depth);
-    auto bring_next = [&](uint32_t to) {
+    auto bring_m = [&](uint32_t to) {
+        if (coming_b < items) bring<T>(om, coming_t, lds, to);
+    };
+    auto bring_n = [&](uint32_t to) {
         if (coming_b >= items) return;
-        bring(om, coming_t, lds, to);
-        bring(on, coming_t, lds, to + WIDE_BYTES);
+        bring<T>(on, coming_t, lds, to + BYTES);
         if (++coming_t < coming.stages) return;
         coming_t = 0;
         coming_b += gridDim.x;
         if (coming_b >= items) return;
-        coming = WideItem(a, coming_b, STAGE);
+        coming = WideItem(a, coming_b, STAGE, T);
         om = OpM(a.p.m, a.p.ms, coming.r0, a.p.rows, coming.k0, coming.depth);
         on = OpN(a.p.n, a.p.ns, coming.c0, a.p.cols, coming.k0, coming.depth);
     };
     frag fn[2][4], fm[2][4];
     auto read_n = [&](const char* at, int kb, frag (&f)[4]) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) f[j] = OpN::read(at + WIDE_BYTES, n0 + 16 * j, kb);
+        for (int j = 0; j < 4; j++) f[j] = OpN::read(at + BYTES, n0 + 16 * j, kb);
     };
     auto read_m = [&](const char* at, int kb, int half, frag (&f)[4]) {
 #pragma unroll
         for (int i = 0; i < 4; i++) f[i] = OpM::read(at, m0 + 64 * half + 16 * i, kb);
     };
-    floatx4 acc[8][4];
-    auto multiply = [&](const frag (&n)[4], const frag (&m)[4], auto half) {
-        constexpr int H = decltype(half)::value;
-        if constexpr (DT == TAURUS_F32) {  // a component at a time, to different sums in turn
-            auto step = [&](auto get) {
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        acc[4 * H + i][j] =
-                            __builtin_amdgcn_mfma_f32_16x16x4f32(get(n[j]), get(m[i]), acc[4 * H + i][j], 0, 0, 0);
-            };
-            step([](const frag& f) { return f.x; });
-            step([](const frag& f) { return f.y; });
-            step([](const frag& f) { return f.z; });
-            step([](const frag& f) { return f.w; });
-        } else {
+    floatx4 acc[MI][4];
+    // a quarter of a step's products: fp32 a component, to different sums in turn
+    auto quarter = [&](const frag (&n)[4], const frag (&m)[4], auto half, auto q) {
+        constexpr int H = decltype(half)::value, Q = decltype(q)::value;
+        if constexpr (DT == TAURUS_F32) {
+            auto get = [](const frag& f) { return Q == 0 ? f.x : Q == 1 ? f.y : Q == 2 ? f.z : f.w; };
 #pragma unroll
             for (int i = 0; i < 4; i++)
 #pragma unroll
-                for (int j = 0; j < 4; j++) acc[4 * H + i][j] = mfma16<DT>(n[j], m[i], acc[4 * H + i][j]);
+                for (int j = 0; j < 4; j++)
+                    acc[4 * H + i][j] =
+                        __builtin_amdgcn_mfma_f32_16x16x4f32(get(n[j]), get(m[i]), acc[4 * H + i][j], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[4 * H + Q][j] = mfma16<DT>(n[j], m[Q], acc[4 * H + Q][j]);
         }
+    };
+    std::integral_constant<int, 0> upper;
+    std::integral_constant<int, 1> lower;
+    std::integral_constant<int, 2> third;
+    std::integral_constant<int, 3> fourth;
+    auto multiply = [&](const frag (&n)[4], const frag (&m)[4], auto half) {
+        quarter(n, m, half, upper);
+        quarter(n, m, half, lower);
+        quarter(n, m, half, third);
+        quarter(n, m, half, fourth);
         // LDS reads of the step ahead between the products
 #pragma unroll
         for (int g = 0; g < 8; g++) {
@@ -347,88 +362,107 @@ __global__ __launch_bounds__(512, 2) void k_linear_wide(WideArgs a) {
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    std::integral_constant<int, 0> upper;
-    std::integral_constant<int, 1> lower;
 
-    bring_next(0);
-    bring_next(2 * WIDE_BYTES);
+    bring_m(0);
+    bring_n(0);
+    bring_m(2 * BYTES);
+    bring_n(2 * BYTES);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     uint32_t buffer = 0;
     for (uint32_t b = blockIdx.x; b < items; b += gridDim.x) {
-        const WideItem item(a, b, STAGE);
+        const WideItem item(a, b, STAGE, T);
         read_n(lds + buffer, 0, fn[0]);
         read_m(lds + buffer, 0, 0, fm[0]);
 #pragma unroll
-        for (int i = 0; i < 8; i++)
+        for (int i = 0; i < MI; i++)
 #pragma unroll
             for (int j = 0; j < 4; j++) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
         for (int t = 0; t < item.stages; t++) {
             const char* mine = lds + buffer;
-            const char* next = lds + (buffer ^ 2 * WIDE_BYTES);
-            read_m(mine, 0, 1, fm[1]);
+            const char* next = lds + (buffer ^ 2 * BYTES);
             read_n(mine, 1, fn[1]);
-            multiply(fn[0], fm[0], upper);
-            read_m(mine, 1, 0, fm[0]);
-            multiply(fn[0], fm[1], lower);
-            read_m(mine, 1, 1, fm[1]);
-            multiply(fn[1], fm[0], upper);
+            if constexpr (MI == 8) {
+                read_m(mine, 0, 1, fm[1]);
+                multiply(fn[0], fm[0], upper);
+                read_m(mine, 1, 0, fm[0]);
+                multiply(fn[0], fm[1], lower);
+                read_m(mine, 1, 1, fm[1]);
+                multiply(fn[1], fm[0], upper);
+            } else {  // two steps
+                read_m(mine, 1, 0, fm[1]);
+                multiply(fn[0], fm[0], upper);
+            }
             // this wave has read the stage; the next one's pieces that it asked
             // for are there
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            bring_next(buffer);
             if (t + 1 < item.stages) {
                 read_n(next, 0, fn[0]);
                 read_m(next, 0, 0, fm[0]);
             }
-            multiply(fn[1], fm[1], lower);
-            buffer ^= 2 * WIDE_BYTES;
+            const std::integral_constant<int, MI / 8> last;
+            quarter(fn[1], fm[1], last, upper);
+            __builtin_amdgcn_sched_barrier(0);
+            bring_m(buffer);
+            __builtin_amdgcn_sched_barrier(0);
+            quarter(fn[1], fm[1], last, lower);
+            __builtin_amdgcn_sched_barrier(0);
+            bring_n(buffer);
+            __builtin_amdgcn_sched_barrier(0);
+            quarter(fn[1], fm[1], last, third);
+            quarter(fn[1], fm[1], last, fourth);
+            __builtin_amdgcn_sched_barrier(0);
+            buffer ^= 2 * BYTES;
         }
         if (item.cut) {  // a part's sums
-            float* out = a.p.part + (int64_t)item.sums * (WIDE * WIDE) + (m0 + li) * WIDE + n0 + 4 * lk;
+            float* out = a.p.part + (int64_t)item.sums * (T * T) + (m0 + li) * T + n0 + 4 * lk;
 #pragma unroll
-            for (int i = 0; i < 8; i++)
+            for (int i = 0; i < MI; i++)
 #pragma unroll
-                for (int j = 0; j < 4; j++) *reinterpret_cast<floatx4*>(out + 16 * i * WIDE + 16 * j) = acc[i][j];
+                for (int j = 0; j < 4; j++) *reinterpret_cast<floatx4*>(out + 16 * i * T + 16 * j) = acc[i][j];
         } else {
-            finish_tile<DT, ACT>(a.p, item.r0 + m0 + li, (int)item.c0 + n0, acc);
+            finish_tile<DT, ACT, MI>(a.p, item.r0 + m0 + li, (int)item.c0 + n0, acc);
         }
     }
 }
 
 // The parts of the cut tiles added in order, then the epilogue: a thread four
-// values, a workgroup four rows of a tile.
-template <int DT, int ACT>
+// values, a workgroup 1,024 of a tile.
+template <int DT, int ACT, int T>
 __global__ __launch_bounds__(256) void k_wide_join(WideArgs a) {
-    const uint32_t i = blockIdx.x / 64;
+    constexpr int PER = T * T / 1024;
+    const uint32_t i = blockIdx.x / PER;
     const WidePlace at = wide_place(a, a.whole + i);
-    const int row = (int)(blockIdx.x % 64) * 4 + (threadIdx.x >> 6), col = (threadIdx.x & 63) * 4;
-    const int64_t r = at.row * WIDE + row;
-    const int c = (int)at.col * WIDE + col;
+    const int v = (int)(blockIdx.x % PER) * 1024 + threadIdx.x * 4, row = v / T, col = v % T;
+    const int64_t r = at.row * T + row;
+    const int c = (int)at.col * T + col;
     if (r >= a.p.rows || c >= a.p.cols) return;
-    const float* p = a.p.part + (int64_t)i * (WIDE * WIDE) + row * WIDE + col;
-    floatx4 v{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.p.splits; s++) v += *reinterpret_cast<const floatx4*>(p + (int64_t)s * a.cut * (WIDE * WIDE));
-    finish4<DT, ACT>(a.p.e, r, c, (int)a.p.cols, v);
+    const float* p = a.p.part + (int64_t)i * (T * T) + v;
+    floatx4 sum{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.p.splits; s++) sum += *reinterpret_cast<const floatx4*>(p + (int64_t)s * a.cut * (T * T));
+    finish4<DT, ACT>(a.p.e, r, c, (int)a.p.cols, sum);
 }
 
 // ---------------------------------------------------------------- launches --
 
 struct WidePlan {
+    int tile;
     int64_t whole, cut, per;
     int splits;
 };
-// A part's sums are written and read, about 0.1 us for the whole chip; a stage
-// takes about 1.5 us (fp32: 6): cutting r tiles of s stages into p parts costs
-// about s / p times that and 0.1 r p, least at sqrt(s / r) times 3.9 (7.7) parts.
+static int wide_tile(int dtype) { return dtype == TAURUS_F32 ? 128 : 256; }
+// A part's sums are written and read, about 0.1 us for the whole chip and 256 x
+// 256 values; a stage of such a tile takes a compute unit about 1.5 us (fp32:
+// 6): cutting r tiles of s stages into p parts costs about s / p times that and
+// 0.1 r p, least at sqrt(s / r) times 3.9 (7.7) parts.
 static WidePlan wide_plan(int dtype, int64_t rows, int64_t cols, int64_t depth) {
-    const int stage = dtype == TAURUS_F32 ? 32 : 64;
-    const int64_t tiles = ceil_div(rows, WIDE) * ceil_div(cols, WIDE), stages = ceil_div(depth, stage);
-    constexpr int64_t CUS = 256;  // of the chip; a workgroup fills one
-    const int64_t rest = tiles % CUS;
-    WidePlan p{tiles, 0, stages * stage, 1};
+    const int stage = dtype == TAURUS_F32 ? 32 : 64, tile = wide_tile(dtype);
+    const int64_t tiles = ceil_div(rows, tile) * ceil_div(cols, tile), stages = ceil_div(depth, stage);
+    const int64_t resident = tile == 256 ? 256 : 512;
+    const int64_t rest = tiles % resident;
+    WidePlan p{tile, tiles, 0, stages * stage, 1};
     if (!rest || stages < 4) return p;
     const int64_t best = (int64_t)((dtype == TAURUS_F32 ? 7.7 : 3.9) * sqrt((double)stages / (double)rest));
-    const int64_t parts = std::min(std::min(CUS / rest, stages / 2), best);
+    const int64_t parts = std::min(std::min(resident / rest, stages / 2), best);
     if (parts < 2) return p;
     const int64_t each = ceil_div(stages, parts);
     p.whole = tiles - rest;
@@ -450,20 +484,22 @@ bool wide_takes(int kind, int dtype, const ProductArgs& a) {
     };
     const int64_t m_width = kind == PRODUCT_DW ? a.rows : a.depth, n_width = kind == PRODUCT_DX ? a.depth : a.cols;
     return whole(a.m, m_width, a.ms) && whole(a.n, n_width, a.ns) && a.cols % e == 0 && a.rows >= 256 && a.cols >= 256 &&
-           a.depth >= 256 && (double)a.rows * a.cols * a.depth >= WIDE_WORK && ceil_div(a.rows, WIDE) * ceil_div(a.cols, WIDE) <= WIDE_TILES;
+           a.depth >= 256 && (double)a.rows * a.cols * a.depth >= WIDE_WORK && ceil_div(a.rows, 128) * ceil_div(a.cols, 128) <= WIDE_TILES;
 }
 int64_t wide_part(int dtype, int64_t rows, int64_t cols, int64_t depth) {
     const WidePlan p = wide_plan(dtype, rows, cols, depth);
-    return p.cut * p.splits * WIDE * WIDE;
+    return p.cut * p.splits * p.tile * p.tile;
 }
 template <int KIND, int DT>
 static void wide_launch(const WideArgs& a, int act, hipStream_t s) {
+    constexpr int T = DT == TAURUS_F32 ? 128 : 256;
+    const uint32_t items = a.whole + a.cut * a.p.splits, resident = (uint32_t)(Wide<T>::PER_CU * compute_units());
     auto go = [&](auto c) {
         constexpr int ACT = decltype(c)::value;
-        k_linear_wide<KIND, DT, ACT><<<std::min(a.whole + a.cut * a.p.splits, (uint32_t)compute_units()), 512, 0, s>>>(a);
+        k_linear_wide<KIND, DT, ACT, T><<<std::min(items, resident), Wide<T>::THREADS, 0, s>>>(a);
         TAURUS_CHECK_LAUNCH();
         if (a.cut) {
-            k_wide_join<DT, ACT><<<a.cut * 64, 256, 0, s>>>(a);
+            k_wide_join<DT, ACT, T><<<a.cut * (T * T / 1024), 256, 0, s>>>(a);
             TAURUS_CHECK_LAUNCH();
         }
     };
@@ -475,8 +511,8 @@ void wide_product(int kind, int dtype, ProductArgs p, float* part, int act, hipS
     p.part = part;
     p.per = plan.per;
     p.splits = plan.splits;
-    p.row_tiles = ceil_div(p.rows, WIDE);
-    p.col_tiles = (int)ceil_div(p.cols, WIDE);
+    p.row_tiles = ceil_div(p.rows, plan.tile);
+    p.col_tiles = (int)ceil_div(p.cols, plan.tile);
     const WideArgs a{p, (uint32_t)plan.whole, (uint32_t)plan.cut};
     auto of = [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
