@@ -433,15 +433,23 @@ __device__ inline TopList top_of_wave(const Waiting<N>& x, int top, uint2* room)
             return list;
         }
     }
+    const uint2 none = make_uint2(0, 0);
+    if (lane < 4 && n + lane < ROOM) room[n + lane] = none;  // to whole fours, below every key
     x.gather(from, room, 0, ROOM);
-    const uint2 none = make_uint2(0, 0), a = lane < n ? room[lane] : none, b = lane + 64 < n ? room[lane + 64] : none;
+    const uint2 a = lane < n ? room[lane] : none, b = lane + 64 < n ? room[lane + 64] : none;
     const uint64_t ka = whole_key(a), kb = whole_key(b);
     int ra = 0, rb = 0;
 #pragma unroll 1
-    for (int i = 0; i < n; i++) {
-        const uint64_t other = whole_key(room[i]);
-        ra += other > ka;
-        rb += other > kb;
+    for (int i = 0; i < n; i += 4) {
+        const uint4* four = reinterpret_cast<const uint4*>(room + i);
+        const uint4 p = four[0], q = four[1];
+        const uint64_t other[4] = {whole_key(make_uint2(p.x, p.y)), whole_key(make_uint2(p.z, p.w)),
+                                   whole_key(make_uint2(q.x, q.y)), whole_key(make_uint2(q.z, q.w))};
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            ra += other[k] > ka;
+            rb += other[k] > kb;
+        }
     }
     __builtin_amdgcn_wave_barrier();
     if (lane < n && ra < 64) room[ra] = a;
@@ -504,7 +512,7 @@ __global__ __launch_bounds__(256) void k_labels_stream(LabelArgs a) {
     constexpr int TEAMS = 256 / TEAM, U = 16 / E;
     __shared__ Sums4 sums;
     __shared__ Lists4 lists;
-    __shared__ uint2 room[4][ROOM];
+    __shared__ __align__(16) uint2 room[4][ROOM];
     const int tid = threadIdx.x % TEAM, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int64_t items = a.m * a.parts;
     for (int64_t item = (int64_t)blockIdx.x * TEAMS + threadIdx.x / TEAM; item < items;
@@ -590,7 +598,7 @@ template <int DT>
 __global__ __launch_bounds__(256) void k_labels_join(LabelArgs a) {
     __shared__ Sums4 sums;
     __shared__ Lists4 lists;
-    __shared__ uint2 room[4][ROOM];
+    __shared__ __align__(16) uint2 room[4][ROOM];
     constexpr int N = 8;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     for (int64_t r = blockIdx.x; r < a.m; r += gridDim.x) {
