@@ -259,7 +259,7 @@ __device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const
 // wave works on these; what it reads of a row by class (the label, the
 // alternatives) it reads from LDS.
 template <int DT, int E, int P, int LG>
-__global__ __launch_bounds__(256, 4) void k_labels_rows(LabelArgs a) {
+__global__ __launch_bounds__(256, 5) void k_labels_rows(LabelArgs a) {
     __shared__ uint2 lists[4][LG >= 4 ? (64 >> LG) * TOP_LIST : 1];
     __shared__ __align__(16) float rows[4][64 * P * E];
     const int wave = threadIdx.x >> 6;
@@ -700,6 +700,7 @@ static LabelPlan label_plan(int dtype, int64_t m, int64_t c) {
         p.p = 1;
         while (p.p < most && vecs > p.p) p.p *= 2;
         while (vecs > (int64_t)p.p << p.lg) p.lg++;
+        if (p.e == 4 && p.p == 4 && vecs <= (int64_t)3 << p.lg) p.p = 3;  // a quarter less to go through
         return p;
     }
     p.stream = true;
@@ -731,14 +732,17 @@ template <int DT, int E>
 static void labels_e(const LabelArgs& a, const LabelPlan& p, hipStream_t s) {
     if (!p.stream) {
         // as many workgroups as are resident
-        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.m, 256 >> p.lg), 4 * compute_units());
+        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.m, 256 >> p.lg), 5 * compute_units());
         auto go = [&](auto n, auto lg) {
             constexpr int P = decltype(n)::value, LG = decltype(lg)::value;
-            if constexpr (E * P == 16 || LG == 0) k_labels_rows<DT, E, P, LG><<<grid, 256, 0, s>>>(a);
+            if constexpr (E * P == 16 || E * P == 12 || LG == 0) k_labels_rows<DT, E, P, LG><<<grid, 256, 0, s>>>(a);
         };
         auto go_p = [&](auto lg) {
             if constexpr (E == 8 || E == 4) {
                 if (p.p * E == 16) return go(std::integral_constant<int, 16 / E>{}, lg);
+            }
+            if constexpr (E == 4) {
+                if (p.p == 3) return go(std::integral_constant<int, 3>{}, lg);
             }
             // rows of so few classes are one lane's
             if (p.p == 1) go(std::integral_constant<int, 1>{}, lg);

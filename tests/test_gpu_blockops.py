@@ -680,7 +680,7 @@ def check_labels_grad(x, labels, scale, r, g, h, xs=None):
 
 
 LABELS = [  # rows, classes, alternatives
-    (1, 1, 1), (5, 2, 2), (9, 3, 0), (300, 47, 5), (64, 64, 64), (1000, 172, 3), (7, 1000, 20), (50, 1024, 64),
+    (1, 1, 1), (5, 2, 2), (9, 3, 0), (77, 11, 4), (33, 96, 8), (50, 700, 20), (300, 47, 5), (64, 64, 64), (1000, 172, 3), (7, 1000, 20), (50, 1024, 64),
     (3, 1025, 1), (40, 1500, 10), (2100, 1100, 4), (5, 40_003, 64), (2, 300_001, 20), (130, 5000, 8), (1200, 2050, 0),
     (0, 9, 2), (2500, 17, 17), (1, 70_000, 50),
 ]
