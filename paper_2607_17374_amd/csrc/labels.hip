@@ -255,11 +255,16 @@ __device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const
     return true;
 }
 
+// Workgroups a compute unit.  Five keep more rows on their way (fp32, 12 values
+// a lane, 1,000,000 x 172, top 5: 201 us for 205 with four); fp32 of 16 values
+// a lane does not fit their registers (390,625 x 256: 81 us for 74).
+template <int DT, int E, int P>
+constexpr int ROWS_PER_CU = DT == TAURUS_F32 && E * P == 16 ? 4 : 5;
 // P vectors a lane, 2^LG lanes a row.  The next rows are on their way while the
 // wave works on these; what it reads of a row by class (the label, the
 // alternatives) it reads from LDS.
 template <int DT, int E, int P, int LG>
-__global__ __launch_bounds__(256, 5) void k_labels_rows(LabelArgs a) {
+__global__ __launch_bounds__(256, (ROWS_PER_CU<DT, E, P>)) void k_labels_rows(LabelArgs a) {
     __shared__ uint2 lists[4][LG >= 4 ? (64 >> LG) * TOP_LIST : 1];
     __shared__ __align__(16) float rows[4][64 * P * E];
     const int wave = threadIdx.x >> 6;
@@ -731,11 +736,13 @@ static LabelWork label_work(void* work, const LabelPlan& p, int64_t m, int64_t t
 template <int DT, int E>
 static void labels_e(const LabelArgs& a, const LabelPlan& p, hipStream_t s) {
     if (!p.stream) {
-        // as many workgroups as are resident
-        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.m, 256 >> p.lg), 5 * compute_units());
         auto go = [&](auto n, auto lg) {
             constexpr int P = decltype(n)::value, LG = decltype(lg)::value;
-            if constexpr (E * P == 16 || E * P == 12 || LG == 0) k_labels_rows<DT, E, P, LG><<<grid, 256, 0, s>>>(a);
+            if constexpr (E * P == 16 || E * P == 12 || LG == 0) {
+                // as many workgroups as are resident
+                const int64_t most = ROWS_PER_CU<DT, E, P> * compute_units();
+                k_labels_rows<DT, E, P, LG><<<(unsigned)std::min(ceil_div(a.m, 256 >> LG), most), 256, 0, s>>>(a);
+            }
         };
         auto go_p = [&](auto lg) {
             if constexpr (E == 8 || E == 4) {
