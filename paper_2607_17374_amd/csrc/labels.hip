@@ -9,7 +9,15 @@
 // 2^lg lanes, longer ones stream through a wave or a workgroup with running M,
 // S and T = sum of e^(l - M) (l - M): moving M by d = M - M' scales S by e^d and
 // makes T e^d (T + d S).  Few long rows are cut into parts, joined by a second
-// launch.  Both are bound by memory.
+// launch.
+//
+// Bound by memory, but for alternatives of short rows, whose ranking keeps the
+// vector units as busy.  Measured (a copy reaches 5.15 TB/s): 100M fp32 logits in
+// rows of 256, labels alone, 74 us, 5.4 TB/s; 1,000,000 fp32 rows of 172 with five
+// alternatives 200 us, 3.7 TB/s; the gradient of 8,192 bf16 rows of 32,003 with
+// entropy 222 us, 4.7 TB/s; 5 bf16 rows of 128,003 with 20 alternatives 11.5 us
+// and 9.5 to join (what a wave ranks in turn: the list of its values, of the
+// workgroup's, of the parts').
 //
 // l = -inf (a masked class) adds nothing: differences are held at LOWEST, whose
 // exponential is 0 in fp32, so no 0 times infinity appears.  NaN and +inf make

@@ -69,9 +69,6 @@ __device__ inline float2 lanes_sum2(float2 v, int lg) {
 __device__ inline float lanes_max(float v, int lg) {
     return lanes_all(v, lg, [](float a, float b) { return fmaxf(a, b); });
 }
-__device__ inline int lanes_min(int v, int lg) {
-    return lanes_all(v, lg, [](int a, int b) { return min(a, b); });
-}
 // the sum over lanes that agree in their low lg bits (the same columns of a
 // wave's groups)
 __device__ inline float groups_sum(float v, int lg) {

@@ -9,7 +9,17 @@
 // too: every part leaves fp32 sums in the workspace, and k_linear_join adds
 // them in order and does the epilogue.  With an activation, dz is formed once,
 // rounded to x's type (what the matrix cores take; fp32 stays), by the pass
-// that adds its columns for db before that rounding.
+// that adds its columns for db before that rounding: a pass bound by memory,
+// which the two products that read dz would each have to repeat.
+//
+// Three forms of the product, by size and alignment: few rows of y are bound by
+// reading W (linear_few.hip), large products by the matrix cores
+// (linear_wide.hip), all others go through the tiles here.
+//
+// Measured: dz and db of 33,001 bf16 rows of 1,536 (GELU) 65 us, 4.7 TB/s (of
+// 5.15 of a copy), their sums joined in 5; with dx (114 us, 0.89 PFLOP/s) and dW
+// (114, and 10 to join its parts) of 1,000 columns 286 us.  The tiles here:
+// 4,096 bf16 rows 1,024 -> 1,024 31 / 29 / 29 us (y / dx / dW).
 #include "columns.hpp"
 #include "linear.hpp"
 

@@ -1,9 +1,10 @@
 // Linear maps of few rows (linear.hpp): bound by reading the weight once.
 //
 // A workgroup takes 16 C columns (C a lane) and all rows, in blocks of 16.  Its
-// eight waves share the contraction, a block of 32 (fp32: 16) in turn.  A lane
-// reads C values of each weight row of its eight (four) straight from memory
-// into registers: 16 lanes make a row's segment, four lane groups the block.
+// eight waves (sixteen, from 512 values on) share the contraction, a block of 32
+// (fp32: 16) in turn.  A lane reads C values of each weight row of its
+// eight (four) straight from memory into registers: 16 lanes make a row's
+// segment, four lane groups the block.
 // The matrix instruction wants a column's values along the contraction in a
 // lane: those are the lane's own, so 16-bit values are put in order by one byte
 // permutation for every two, and fp32 ones need none.  Which 16 columns a
@@ -12,6 +13,12 @@
 // in one launch.  Long contractions of few columns are cut into parts too, since
 // a compute unit has only so much of memory under way; k_linear_join adds their
 // sums.
+//
+// Measured (a captured call after the other, 1 to 32 rows): bf16 1,024 -> 1,024
+// 5.5 us, 4,096 -> 4,096 9.0 (3.7 TB/s of W), 4,096 -> 16,384 24.9 (5.4 TB/s);
+// fp32 4,096 -> 4,096 16 (4.2 TB/s; through the tiles of linear.hip 48).  Three
+// rows with GELU and residual, 1,024 -> 1,024: 10.5 us a call, which is the
+// host's.  More rows (33 to 64) cost these small maps more than the tiles do.
 #include "linear.hpp"
 
 namespace taurus {
@@ -161,7 +168,7 @@ static int few_cols(int dtype, int64_t cols) {
 }
 // Parts of the contraction, of at least 1,024 values, that give the chip's 256
 // compute units a workgroup each: the launch that joins them costs about 3 us
-// (one bf16 row 4,096 -> 1,024: 11.9 us uncut, 7.7 in eight parts; 4,096 ->
+// (one bf16 row 4,096 -> 1,024: 11.9 us uncut, 7.7 in four parts; 4,096 ->
 // 4,096: 13.3 and 9.0; 1,024 -> 1,024, uncut: 5.5; 4,096 -> 16,384: 24.4, 5.5 TB/s).
 FewPlan few_plan(int dtype, int64_t rows, int64_t cols, int64_t depth) {
     const int64_t blocks = ceil_div(cols, 16 * few_cols(dtype, cols));

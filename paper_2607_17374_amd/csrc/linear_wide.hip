@@ -1,15 +1,29 @@
-// Large products (linear.hpp): tiles of 256 x 256, the contraction in stages of
-// 128 bytes a row (64 values of 16 bits, 32 of fp32).
+// Large products (linear.hpp), bound by the matrix cores: tiles of 256 x 256 of
+// 16 bits, 128 x 128 of fp32, the contraction in stages of 128 bytes a row (64
+// values of 16 bits, 32 of fp32).
 //
-// Eight waves of 128 x 64 values share a compute unit, two a SIMD.  A stage is
-// four steps (32 of the contraction by 64 rows), whose operands a wave reads
-// from LDS one step ahead, while the step before is multiplied.  Stages go from
-// memory straight into LDS, in two buffers of 64 KB, as one stream over a
-// workgroup's tiles: before a stage's last step its operands are in registers,
-// and a barrier says so of all waves and that the next stage is in LDS; then its
-// buffer takes the stage after that, and the last step's products run while
-// the next stage's first operands come.  So there is one barrier a stage, and a
-// tile's epilogue runs while the next tile's first stages are on their way.
+// Eight waves share a compute unit, two a SIMD: of 16 bits one workgroup, a wave
+// 128 x 64 values (the larger a wave's share, the fewer LDS reads a product);
+// of fp32, whose products take sixteen times as long, two workgroups of four
+// waves of 64 x 64, one of which multiplies while the other stores.  A stage is
+// steps of a matrix instruction's depth (fp32: four's) by 64 rows, whose
+// operands a wave reads from LDS one step ahead, while the step before is
+// multiplied.  Stages go from memory straight into LDS, in two buffers, as one
+// stream over a workgroup's tiles: before a stage's last step its operands are
+// in registers, and a barrier says so of all waves and that the next stage is
+// in LDS; then its buffer takes the stage after that, asked for between the
+// last step's products, while the next stage's first operands come.  So there
+// is one barrier a stage, and a tile's epilogue runs while the next tile's
+// first stages are on their way.
+//
+// Measured (y / dx / dW): 8,192 x 8,192 -> 8,192 bf16 810 / 793 / 820 us (1.36 /
+// 1.39 / 1.34 PFLOP/s); 8,192 x 8,192 -> 4,096 fp32 3,890 / 3,885 / 3,906 us
+// (0.141 of the 0.157 PFLOP/s of the fp32 matrix cores, which are busy for 0.88
+// of the cycles); 16,384 x 2,048 -> 8,192 bf16 460, with bias, SiLU and z
+// stored 516.  Two groups of waves half a step apart, with eight barriers a
+// stage, do the large ones as fast and those with an epilogue slower (570 us
+// for 519); fp32 in tiles of 256 (200,003 x 256 -> 256, ReLU and residual: 311
+// us for 283) ends with a longer last round and epilogues that nothing hides.
 //
 // The layouts in LDS are those of product.hpp.  A wave's load fills 1 KB in lane
 // order, so the exchange is made in the addresses that the lanes read from.
@@ -25,7 +39,7 @@ namespace taurus {
 template <int T>
 struct Wide {
     static constexpr int WAVES = T == 256 ? 8 : 4, THREADS = WAVES * 64, BYTES = T * 128;  // of an operand's stage
-    static constexpr int MI = T == 256 ? 8 : 4, NI = 4, PER_CU = T == 256 ? 1 : 2;
+    static constexpr int MI = T == 256 ? 8 : 4, PER_CU = T == 256 ? 1 : 2;
 };
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -472,11 +486,14 @@ static WidePlan wide_plan(int dtype, int64_t rows, int64_t cols, int64_t depth) 
     return p;
 }
 // Products with less to do than this leave much of the chip idle in tiles of
-// this size, or spend more on joining parts than they save (bf16, y / dx / dW,
-// tiles of 128 x 64 against these: 4,096 x 1,024 -> 1,024 (4.3e9) 31 / 29 / 29
+// this size, or spend more on joining parts than they save (y / dx / dW, tiles
+// of 128 x 64 against these; bf16: 4,096 x 1,024 -> 1,024 (4.3e9) 31 / 29 / 29
 // us against 32 / 30 / 35; 4,096 x 4,096 -> 512 (8.6e9) 41 / 36 / 42 against 43
-// / 24 / 43; 4,096 x 4,096 -> 1,024 (17e9) 67 / 58 / 70 against 56 / 36 / 54).
-constexpr double WIDE_WORK = 6e9;
+// / 24 / 43; 4,096 x 4,096 -> 1,024 (17e9) 67 / 58 / 70 against 56 / 36 / 54;
+// fp32: 4,000 x 512 -> 512 (1.0e9) 37 / 36 / 39 against 38 / 36 / 42; 8,000 x
+// 512 -> 512 (2.1e9) 54 / 52 / 54 against 42 / 42 / 54; 16,000 x 512 -> 512
+// (4.2e9) 82 / 78 / 88 against 73 / 72 / 80).
+static double wide_work(int dtype) { return dtype == TAURUS_F32 ? 2e9 : 6e9; }
 bool wide_takes(int kind, int dtype, const ProductArgs& a) {
     const int e = 16 / dtype_size(dtype);  // rows of whole 16-byte pieces
     auto whole = [e](const void* p, int64_t width, int64_t stride) {
@@ -484,7 +501,8 @@ bool wide_takes(int kind, int dtype, const ProductArgs& a) {
     };
     const int64_t m_width = kind == PRODUCT_DW ? a.rows : a.depth, n_width = kind == PRODUCT_DX ? a.depth : a.cols;
     return whole(a.m, m_width, a.ms) && whole(a.n, n_width, a.ns) && a.cols % e == 0 && a.rows >= 256 && a.cols >= 256 &&
-           a.depth >= 256 && (double)a.rows * a.cols * a.depth >= WIDE_WORK && ceil_div(a.rows, 128) * ceil_div(a.cols, 128) <= WIDE_TILES;
+           a.depth >= 256 && (double)a.rows * a.cols * a.depth >= wide_work(dtype) &&
+           ceil_div(a.rows, 128) * ceil_div(a.cols, 128) <= WIDE_TILES;
 }
 int64_t wide_part(int dtype, int64_t rows, int64_t cols, int64_t depth) {
     const WidePlan p = wide_plan(dtype, rows, cols, depth);

@@ -26,6 +26,14 @@
 // A workgroup leaves one row of sums, k_join_columns adds those.  A segment
 // that lies within a worker's rows has its gate's gradient written at once; of
 // others each worker leaves its part in the workspace, for k_resnorm_gates.
+//
+// Measured (a copy reaches 5.15 TB/s): 1,000,000 bf16 rows of 256, layer norm and
+// gate, forward 416 us, 4.9 TB/s; 33,000 rows of 4,096, RMS norms and gate, fp32
+// stream, gradient 468 us and 11 for its columns, 5.1 TB/s; 300,001 fp16 rows
+// of 128 in 9,000 segments, layer norms, gradient 113 us and 6 for gates, 4 for
+// columns, 3.7 TB/s (three reductions and two norms a row beside memory: a team
+// of 16 lanes has eight channels each).  Four waves a SIMD leave the gradient too
+// few registers (253 us), two hide less (143).
 #include "columns.hpp"
 #include "lanes.hpp"
 #include "rowops.hpp"

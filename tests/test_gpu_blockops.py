@@ -217,11 +217,20 @@ def test_linear_large(dtype, case):
     check_linear_grad(x, w, normal((m, n), dtype, case + 5), act, [F32, dtype][case % 2], pre)
 
 
-WIDE = [  # rows, d_in, d_out of products in tiles of 256 x 256: a single partial
+WIDE = [  # rows, d_in, d_out of products in tiles of 256 x 256 (fp32: 128 x 128): a single partial
     # round of tiles, whole rounds and a rest, a rest too large to cut, rests of
     # every tile and stage
     (2049, 1032, 2904), (5000, 520, 3208), (16_500, 264, 1480), (772, 4100, 2060), (30_001, 256, 840),
 ]
+
+
+@pytest.mark.parametrize("m,k,n", [(260, 8196, 1000), (30_000, 260, 264), (999, 2052, 1004), (2048, 1024, 1024)])
+def test_linear_wide_f32(m, k, n):
+    """The smallest that go through these tiles."""
+    note(f"linear wide float32 m={m} k={k} n={n}")
+    x, w, b = normal((m, k), F32, m), normal((k, n), F32, m + 1, k ** -0.5), normal((n,), F32, m + 2)
+    check_linear(x, w, b, normal((m, n), F32, m + 3), "silu", F32, True)
+    check_linear_grad(x, w, normal((m, n), F32, m + 4), "silu", F32, normal((m, n), F32, m + 5, 2.0))
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
