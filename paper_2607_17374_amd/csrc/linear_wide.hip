@@ -187,8 +187,8 @@ __device__ inline WidePlace wide_place(const WideArgs& a, uint32_t tile) {
 
 // The epilogue of a wave's 16 MI x 64 values: lane li holds rows r + 16 i, values
 // c + 16 j + 4 lk to + 3 of each, for columns in whole fours.  All lanes take
-// part (put_pair16).  The next row of a residual of 16 bits is on its way while
-// this row is stored (there are no registers for one of fp32).
+// part (put_pair16).  The residual's next row is on its way while this one is
+// stored (in 256 x 256 tiles there are no registers for one of fp32).
 template <int DT, int ACT, int MI>
 __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[MI][4]) {
     const Epilogue& e = p.e;
@@ -202,15 +202,24 @@ __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, float
             for (int k = 0; k < 4; k++) bias[j][k] = 0.f;
             if (at + 16 * j < cols) load_vec<TAURUS_F32, 4>(e.bias, at + 16 * j, bias[j]);
         }
-    uint2 raw[4];
+    constexpr bool ROOM = MI == 4;
+    Stored<ROOM ? TAURUS_F32 : TAURUS_BF16, 4> raw[4];
     auto bring = [&](int i) {
-        if (!e.residual || !half || r + 16 * i >= p.rows) return;
+        if (!e.residual || !(half || ROOM) || r + 16 * i >= p.rows) return;
+        const int64_t row = (r + 16 * i) * e.residual_stride;
 #pragma unroll
-        for (int j = 0; j < 4; j++)
-            if (at + 16 * j < cols) {
-                const auto s = load_stored<TAURUS_BF16, 4>(e.residual, (r + 16 * i) * e.residual_stride + at + 16 * j);
-                raw[j] = make_uint2(s.v[0], s.v[1]);
+        for (int j = 0; j < 4; j++) {
+            if (at + 16 * j >= cols) continue;
+            if constexpr (ROOM) {
+                if (!half) {
+                    raw[j] = load_stored<TAURUS_F32, 4>(e.residual, row + at + 16 * j);
+                    continue;
+                }
             }
+            const auto s = load_stored<TAURUS_BF16, 4>(e.residual, row + at + 16 * j);
+            raw[j].v[0] = s.v[0];
+            raw[j].v[1] = s.v[1];
+        }
     };
     bring(0);
 #pragma unroll
@@ -218,7 +227,7 @@ __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, float
         __builtin_amdgcn_sched_barrier(0);  // a row at a time, which keeps addresses few
         const int64_t row = r + 16 * i;
         const bool in = row < p.rows;
-        uint2 mine[4];
+        std::remove_reference_t<decltype(raw[0])> mine[4];
 #pragma unroll
         for (int j = 0; j < 4; j++) mine[j] = raw[j];
         if (i + 1 < MI) bring(i + 1);
@@ -249,10 +258,12 @@ __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, float
                 if (half) {
                     Stored<TAURUS_BF16, 4> b;
                     Stored<TAURUS_F16, 4> h;
-                    b.v[0] = h.v[0] = mine[j].x;
-                    b.v[1] = h.v[1] = mine[j].y;
+                    b.v[0] = h.v[0] = mine[j].v[0];
+                    b.v[1] = h.v[1] = mine[j].v[1];
                     if (is_bf16) decode<TAURUS_BF16, 4>(b, f);
                     else decode<TAURUS_F16, 4>(h, f);
+                } else if constexpr (ROOM) {
+                    decode<TAURUS_F32, 4>(mine[j], f);
                 } else {
                     if (!in || at + 16 * j >= cols) continue;
                     load_vec<TAURUS_F32, 4>(e.residual, row * e.residual_stride + at + 16 * j, f);
