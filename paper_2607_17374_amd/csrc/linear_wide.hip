@@ -185,15 +185,25 @@ __device__ inline WidePlace wide_place(const WideArgs& a, uint32_t tile) {
     return {first + in % tall, in / tall};
 }
 
-// The epilogue of a wave's 16 MI x 64 values: lane li holds rows r + 16 i, values
-// c + 16 j + 4 lk to + 3 of each, for columns in whole fours.  All lanes take
-// part (put_pair16).  The residual's next row is on its way while this one is
-// stored (in 256 x 256 tiles there are no registers for one of fp32).
-template <int DT, int ACT, int MI>
-__device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[MI][4]) {
+// Keeps what follows from v where it is used: the epilogue's addresses, made
+// before the tiles' loop, would take registers that the products need.
+__device__ inline int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+// The epilogue of a wave's 16 MI x 64 values: lane li holds rows r + li + 16 i,
+// values c + 16 j + 4 lk to + 3 of each, for columns in whole 16-byte pieces.
+// All lanes take part (pair16).  The residual's next row is on its way while
+// this one is stored (in 256 x 256 tiles there are no registers for one of
+// fp32).  An address is the wave's, which goes from row to row, and 32 bits of
+// the lane's (at most 16 rows of the widest stride).
+template <int DT, int OUT, int ACT, int MI>
+__device__ inline void finish_rows(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[MI][4]) {
     const Epilogue& e = p.e;
-    const int cols = (int)p.cols, at = c + 4 * ((threadIdx.x & 63) >> 4);
-    const bool half = e.out_dtype != TAURUS_F32, is_bf16 = e.out_dtype == TAURUS_BF16;
+    const int lane = here(threadIdx.x & 63), li = lane & 15, four = 4 * (lane >> 4), eight = pair_column(lane);
+    const int cols = (int)p.cols, at = c + four, pair = c + eight;
+    constexpr bool HALF = OUT != TAURUS_F32, AHEAD = HALF || MI == 4;
+    constexpr int SZ = type_bytes<OUT>, PRE_SZ = type_bytes<DT>;
     float bias[4][4];
     if (e.bias)
 #pragma unroll
@@ -202,88 +212,82 @@ __device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, float
             for (int k = 0; k < 4; k++) bias[j][k] = 0.f;
             if (at + 16 * j < cols) load_vec<TAURUS_F32, 4>(e.bias, at + 16 * j, bias[j]);
         }
-    constexpr bool ROOM = MI == 4;
-    Stored<ROOM ? TAURUS_F32 : TAURUS_BF16, 4> raw[4];
-    auto bring = [&](int i) {
-        if (!e.residual || !(half || ROOM) || r + 16 * i >= p.rows) return;
-        const int64_t row = (r + 16 * i) * e.residual_stride;
+    const char* res = static_cast<const char*>(e.residual) + (r * e.residual_stride + c) * SZ;
+    char* out = static_cast<char*>(e.out) + (r * e.out_stride + c) * SZ;
+    char* pre = static_cast<char*>(e.pre) + (r * e.pre_stride + c) * PRE_SZ;
+    const uint32_t res_at = (uint32_t)(li * (int)e.residual_stride + four) * SZ;
+    const uint32_t out_at = (uint32_t)(li * (int)e.out_stride + (HALF ? eight : four)) * SZ;
+    const uint32_t pre_at = (uint32_t)(li * (int)e.pre_stride + (PRE_SZ == 2 ? eight : four)) * PRE_SZ;
+    const int left = (int)min(p.rows - r, (int64_t)1024) - li;  // row 16 i is there for less
+    auto bring = [&](int i, Stored<OUT, 4> (&raw)[4]) {
+        if (16 * i < left) {
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            if (at + 16 * j >= cols) continue;
-            if constexpr (ROOM) {
-                if (!half) {
-                    raw[j] = load_stored<TAURUS_F32, 4>(e.residual, row + at + 16 * j);
-                    continue;
-                }
+            for (int j = 0; j < 4; j++)
+                if (at + 16 * j < cols) raw[j] = load_stored<OUT, 4>(res + res_at + 16 * SZ * j, 0);
+        }
+        res += 16 * e.residual_stride * SZ;
+    };
+    // a row's values in type TO
+    auto put = [&](auto type, char* to, uint32_t lane_at, bool in, const floatx4 (&v)[4]) {
+        constexpr int TO = decltype(type)::value;
+        to += lane_at;
+        if constexpr (TO == TAURUS_F32) {
+            if (!in) return;
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                if (at + 16 * j < cols) store_vec<TO, 4>(to + 64 * j, 0, reinterpret_cast<const float(&)[4]>(v[j]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                const uint4 z = pair16<TO>(v[j], v[j + 1]);
+                if (!in || pair + 16 * j >= cols) continue;
+                if (DT != TAURUS_F32 || pair + 16 * j + 8 <= cols)
+                    *reinterpret_cast<typename Raw<16, 2>::type*>(to + 32 * j) =
+                        typename Raw<16, 2>::type{z.x, z.y, z.z, z.w};
+                else  // columns in whole fours
+                    *reinterpret_cast<typename Raw<8, 2>::type*>(to + 32 * j) = typename Raw<8, 2>::type{z.x, z.y};
             }
-            const auto s = load_stored<TAURUS_BF16, 4>(e.residual, row + at + 16 * j);
-            raw[j].v[0] = s.v[0];
-            raw[j].v[1] = s.v[1];
         }
     };
-    bring(0);
+    Stored<OUT, 4> raw[2][4];
+    if (AHEAD && e.residual) bring(0, raw[0]);
 #pragma unroll
     for (int i = 0; i < MI; i++) {
         __builtin_amdgcn_sched_barrier(0);  // a row at a time, which keeps addresses few
-        const int64_t row = r + 16 * i;
-        const bool in = row < p.rows;
-        std::remove_reference_t<decltype(raw[0])> mine[4];
-#pragma unroll
-        for (int j = 0; j < 4; j++) mine[j] = raw[j];
-        if (i + 1 < MI) bring(i + 1);
+        const bool in = 16 * i < left;
+        if (AHEAD && e.residual && i + 1 < MI) bring(i + 1, raw[(i + 1) & 1]);
         if (e.bias)
 #pragma unroll
             for (int j = 0; j < 4; j++)
 #pragma unroll
                 for (int k = 0; k < 4; k++) acc[i][j][k] += bias[j][k];
         if (e.pre) {
-            if constexpr (DT == TAURUS_F32) {
-                if (in)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) put4(e.pre, DT, row * e.pre_stride, at + 16 * j, cols, acc[i][j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; j += 2)
-                    put_pair16<DT>(e.pre, row * e.pre_stride, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
-            }
+            put(std::integral_constant<int, DT>{}, pre, pre_at, in, acc[i]);
+            pre += 16 * e.pre_stride * PRE_SZ;
         }
 #pragma unroll
         for (int j = 0; j < 4; j++)
 #pragma unroll
             for (int k = 0; k < 4; k++) acc[i][j][k] = activation<ACT>(acc[i][j][k]);
         if (e.residual) {
+            if (!AHEAD) bring(i, raw[i & 1]);
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 float f[4];
-                if (half) {
-                    Stored<TAURUS_BF16, 4> b;
-                    Stored<TAURUS_F16, 4> h;
-                    b.v[0] = h.v[0] = mine[j].v[0];
-                    b.v[1] = h.v[1] = mine[j].v[1];
-                    if (is_bf16) decode<TAURUS_BF16, 4>(b, f);
-                    else decode<TAURUS_F16, 4>(h, f);
-                } else if constexpr (ROOM) {
-                    decode<TAURUS_F32, 4>(mine[j], f);
-                } else {
-                    if (!in || at + 16 * j >= cols) continue;
-                    load_vec<TAURUS_F32, 4>(e.residual, row * e.residual_stride + at + 16 * j, f);
-                }
+                decode<OUT, 4>(raw[i & 1][j], f);
 #pragma unroll
                 for (int k = 0; k < 4; k++) acc[i][j][k] += f[k];
             }
         }
-        const int64_t to = row * e.out_stride;
-        if (half) {
-#pragma unroll
-            for (int j = 0; j < 4; j += 2) {
-                if (is_bf16) put_pair16<TAURUS_BF16>(e.out, to, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
-                else put_pair16<TAURUS_F16>(e.out, to, c + 16 * j, cols, in, acc[i][j], acc[i][j + 1]);
-            }
-        } else if (in) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) put4(e.out, TAURUS_F32, to, at + 16 * j, cols, acc[i][j]);
-        }
+        put(std::integral_constant<int, OUT>{}, out, out_at, in, acc[i]);
+        out += 16 * e.out_stride * SZ;
     }
+}
+template <int DT, int ACT, int MI>
+__device__ inline void finish_tile(const ProductArgs& p, int64_t r, int c, floatx4 (&acc)[MI][4]) {
+    if (p.e.out_dtype == TAURUS_F32) finish_rows<DT, TAURUS_F32, ACT>(p, r, c, acc);
+    else if (p.e.out_dtype == TAURUS_BF16) finish_rows<DT, TAURUS_BF16, ACT>(p, r, c, acc);
+    else finish_rows<DT, TAURUS_F16, ACT>(p, r, c, acc);
 }
 
 // What a workgroup's b-th item is: a tile, or one part of one.
@@ -445,7 +449,7 @@ __global__ __launch_bounds__(Wide<T>::THREADS, 2) void k_linear_wide(WideArgs a)
 #pragma unroll
                 for (int j = 0; j < 4; j++) *reinterpret_cast<floatx4*>(out + 16 * i * T + 16 * j) = acc[i][j];
         } else {
-            finish_tile<DT, ACT, MI>(a.p, item.r0 + m0 + li, (int)item.c0 + n0, acc);
+            finish_tile<DT, ACT, MI>(a.p, item.r0 + m0, (int)item.c0 + n0, acc);
         }
     }
 }

@@ -376,28 +376,36 @@ __device__ inline void put4(void* out, int dtype, int64_t row_at, int c, int n, 
             store_as<1>(dtype, out, row_at + c + e, f);
         }
 }
-// Two blocks of 16 columns of a row, columns c + 4 lk of each in v and w,
-// stored as 16-bit values.  Lanes 16 apart exchange halves, so that a lane
-// stores eight consecutive values: the first block's for even lk, the
-// second's for odd.
+// Two values rounded to 16 bits, the first in the low half.
+template <int DT>
+__device__ inline uint32_t pack16(float a, float b) {
+    typedef float floatx2 __attribute__((ext_vector_type(2)));
+    typedef std::conditional_t<DT == TAURUS_BF16, __bf16, _Float16> half;
+    typedef half halfx2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2{a, b}, halfx2));
+}
+// Two blocks of 16 columns of a row, columns c + 4 lk of each in v and w, as
+// 16-bit values.  Lanes 16 apart exchange halves, so that a lane has eight
+// consecutive ones: the first block's for even lk, the second's for odd, from
+// column c + pair_column() on.
+template <int DT>
+__device__ inline uint4 pair16(floatx4 v, floatx4 w) {
+    // rows 1 and 3 of the first with rows 0 and 2 of the second
+    const auto lo = __builtin_amdgcn_permlane16_swap(pack16<DT>(v[0], v[1]), pack16<DT>(w[0], w[1]), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(pack16<DT>(v[2], v[3]), pack16<DT>(w[2], w[3]), false, false);
+    return make_uint4(lo[0], hi[0], lo[1], hi[1]);
+}
+__device__ inline int pair_column(int lane) {
+    const int lk = lane >> 4;
+    return 16 * (lk & 1) + 8 * (lk >> 1);
+}
 template <int DT>
 __device__ inline void put_pair16(void* out, int64_t row_at, int c, int n, bool in, floatx4 v, floatx4 w) {
-    auto pack = [](float a, float b) {
-        if constexpr (DT == TAURUS_BF16)
-            return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) |
-                   (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
-        else
-            return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)a) |
-                   (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
-    };
-    const int lk = (threadIdx.x & 63) >> 4;
-    // rows 1 and 3 of the first with rows 0 and 2 of the second
-    const auto lo = __builtin_amdgcn_permlane16_swap(pack(v[0], v[1]), pack(w[0], w[1]), false, false);
-    const auto hi = __builtin_amdgcn_permlane16_swap(pack(v[2], v[3]), pack(w[2], w[3]), false, false);
-    const int at = c + 16 * (lk & 1) + 8 * (lk >> 1);
+    const uint4 packed = pair16<DT>(v, w);
+    const int at = c + pair_column(threadIdx.x & 63);
     if (!in || at >= n) return;
     uint16_t* p = static_cast<uint16_t*>(out) + row_at + at;
-    const uint32_t z[4] = {(uint32_t)lo[0], (uint32_t)hi[0], (uint32_t)lo[1], (uint32_t)hi[1]};
+    const uint32_t z[4] = {packed.x, packed.y, packed.z, packed.w};
     if (at + 8 <= n) {
         *reinterpret_cast<typename Raw<16, 2>::type*>(p) = typename Raw<16, 2>::type{z[0], z[1], z[2], z[3]};
         return;

@@ -224,13 +224,15 @@ WIDE = [  # rows, d_in, d_out of products in tiles of 256 x 256 (fp32: 128 x 128
 ]
 
 
+@pytest.mark.parametrize("out_dtype", DTYPES)
 @pytest.mark.parametrize("m,k,n", [(260, 8196, 1000), (30_000, 260, 264), (999, 2052, 1004), (2048, 1024, 1024)])
-def test_linear_wide_f32(m, k, n):
+def test_linear_wide_f32(m, k, n, out_dtype):
     """The smallest that go through these tiles."""
-    note(f"linear wide float32 m={m} k={k} n={n}")
+    note(f"linear wide float32 m={m} k={k} n={n} -> {out_dtype}")
     x, w, b = normal((m, k), F32, m), normal((k, n), F32, m + 1, k ** -0.5), normal((n,), F32, m + 2)
-    check_linear(x, w, b, normal((m, n), F32, m + 3), "silu", F32, True)
-    check_linear_grad(x, w, normal((m, n), F32, m + 4), "silu", F32, normal((m, n), F32, m + 5, 2.0))
+    check_linear(x, w, b, normal((m, n), out_dtype, m + 3), "silu", out_dtype, True)
+    if out_dtype == F32:
+        check_linear_grad(x, w, normal((m, n), F32, m + 4), "silu", F32, normal((m, n), F32, m + 5, 2.0))
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
