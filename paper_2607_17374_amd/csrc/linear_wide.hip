@@ -16,14 +16,15 @@
 // is one barrier a stage, and a tile's epilogue runs while the next tile's
 // first stages are on their way.
 //
-// Measured (y / dx / dW): 8,192 x 8,192 -> 8,192 bf16 810 / 793 / 820 us (1.36 /
-// 1.39 / 1.34 PFLOP/s); 8,192 x 8,192 -> 4,096 fp32 3,890 / 3,885 / 3,906 us
+// Measured (y / dx / dW): 8,192 x 8,192 -> 8,192 bf16 776 / 781 / 820 us (1.42 /
+// 1.41 / 1.34 PFLOP/s); 8,192 x 8,192 -> 4,096 fp32 3,890 / 3,885 / 3,906 us
 // (0.141 of the 0.157 PFLOP/s of the fp32 matrix cores, which are busy for 0.88
-// of the cycles); 16,384 x 2,048 -> 8,192 bf16 460, with bias, SiLU and z
-// stored 516.  Two groups of waves half a step apart, with eight barriers a
+// of the cycles); 16,384 x 2,048 -> 8,192 bf16 438, with bias, SiLU and z
+// stored 502.  Two groups of waves half a step apart, with eight barriers a
 // stage, do the large ones as fast and those with an epilogue slower (570 us
-// for 519); fp32 in tiles of 256 (200,003 x 256 -> 256, ReLU and residual: 311
-// us for 283) ends with a longer last round and epilogues that nothing hides.
+// for 519).  200,003 x 256 -> 256 fp32, ReLU and residual: 255 us, 283 before the
+// epilogue's present form, 311 in tiles of 256 (a longer last round, epilogues
+// that nothing hides).
 //
 // The layouts in LDS are those of product.hpp.  A wave's load fills 1 KB in lane
 // order, so the exchange is made in the addresses that the lanes read from.
@@ -90,7 +91,9 @@ struct WideAlong {
     __device__ const char* stage(int t) const { return at + (int64_t)t * STAGE * SZ; }
     __device__ bool holds(int t, int) const { return t * STAGE + col < depth; }
     // rows [r0, r0 + 16), matrix step kb
-    static __device__ inline frag read(const char* lds, int r0, int kb) { return Along<DT, T, true>::read(lds, r0, kb); }
+    static __device__ inline frag read(const char* lds, int r0, int kb) {
+        return Along<DT, T, true>::read(lds, r0, kb);
+    }
 };
 // Rows of T values.  Of 16 bits: 32-byte units exchanged as product.hpp's; of
 // fp32: 64-byte units by the row's second pair of bits, so that the four rows
