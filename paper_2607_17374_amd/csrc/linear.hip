@@ -198,8 +198,16 @@ static ProductPlan product_plan(int dtype, int64_t rows, int64_t cols, int64_t d
     p.col_tiles = (int)ceil_div(cols, TN);
     const int64_t tiles = p.row_tiles * p.col_tiles, resident = 256 * 4;
     const int64_t stages = ceil_div(depth, stage);
-    // as many parts as fill the chip, of at least four stages
-    int64_t splits = std::max<int64_t>(1, std::min(resident / std::max<int64_t>(tiles, 1), stages / 4));
+    // as many parts as fill the chip, of at least four stages, and no more than
+    // pay: a workgroup takes about 1 us a stage (fp32: 2.5), and writing and
+    // reading a part's sums takes v us, 8 bytes a value at 4 TB/s, so that p parts
+    // of s stages cost s / p + p v, least at sqrt(s / v) parts (1,000 bf16 rows
+    // 2,048 -> 512: dx 11.4 us uncut, 19.5 in two parts; y 20.9 in two, 17.7 in
+    // five)
+    const double a_stage = dtype == TAURUS_F32 ? 2.5 : 1.0, sums = (double)rows * cols * 8 / 4e6;
+    const int64_t pays = (int64_t)sqrt((double)stages * a_stage / std::max(sums, 1e-3));
+    int64_t splits = std::max<int64_t>(
+        1, std::min(std::min(resident / std::max<int64_t>(tiles, 1), stages / 4), pays));
     const int64_t each = ceil_div(stages, splits);
     p.splits = (int)ceil_div(std::max<int64_t>(stages, 1), std::max<int64_t>(each, 1));
     p.per = std::max<int64_t>(each, 1) * stage;
