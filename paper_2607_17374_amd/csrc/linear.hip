@@ -19,7 +19,7 @@
 // Measured: dz and db of 33,001 bf16 rows of 1,536 (GELU) 64 us, 4.8 TB/s (of
 // 5.15 of a copy), their sums joined in 5; with dx (110 us, 0.93 PFLOP/s) and dW
 // (108, and 10 to join its parts) of 1,000 columns 275 us.  The tiles here:
-// 4,096 bf16 rows 1,024 -> 1,024 31 / 29 / 29 us (y / dx / dW).
+// 4,096 bf16 rows 1,024 -> 1,024 26 / 23 / 31 us (y / dx / dW).
 #include "columns.hpp"
 #include "linear.hpp"
 

@@ -505,10 +505,10 @@ static WidePlan wide_plan(int dtype, int64_t rows, int64_t cols, int64_t depth) 
 }
 // Products with less to do than this leave much of the chip idle in tiles of
 // this size, or spend more on joining parts than they save (y / dx / dW, tiles
-// of 128 x 64 against these; bf16: 4,096 x 1,024 -> 1,024 (4.3e9) 31 / 29 / 29
+// of 128 x 64 against these; bf16: 4,096 x 1,024 -> 1,024 (4.3e9) 26 / 23 / 31
 // us against 32 / 30 / 35; 4,096 x 4,096 -> 512 (8.6e9) 41 / 36 / 42 against 43
 // / 24 / 43; 4,096 x 4,096 -> 1,024 (17e9) 67 / 58 / 70 against 56 / 36 / 54;
-// fp32: 4,000 x 512 -> 512 (1.0e9) 37 / 36 / 39 against 38 / 36 / 42; 8,000 x
+// fp32: 4,000 x 512 -> 512 (1.0e9) 37 / 34 / 35 against 38 / 36 / 42; 8,000 x
 // 512 -> 512 (2.1e9) 54 / 52 / 54 against 42 / 42 / 54; 16,000 x 512 -> 512
 // (4.2e9) 82 / 78 / 88 against 73 / 72 / 80).
 static double wide_work(int dtype) { return dtype == TAURUS_F32 ? 2e9 : 6e9; }
