@@ -278,13 +278,15 @@ struct LinearWork {
     void* dz = nullptr;
     int64_t dz_stride = 0, blocks = 0, bytes = 0;
 };
-// the alignment is known at the call: room for both ways
-static int64_t part_values(int dtype, int64_t rows, int64_t cols, int64_t depth) {
-    return std::max(product_plan(dtype, rows, cols, depth).part, wide_part(dtype, rows, cols, depth));
+// the alignment is known at the call: where the sizes allow both ways, room for
+// either
+static int64_t part_values(int kind, int dtype, int64_t rows, int64_t cols, int64_t depth) {
+    return std::max(product_plan(dtype, rows, cols, depth).part, wide_part(kind, dtype, rows, cols, depth));
 }
 static int64_t forward_bytes(int dtype, int64_t m, int64_t d_in, int64_t d_out) {
     Carve c;
-    c.take<float>(few_takes(dtype, m, d_out) ? few_plan(dtype, m, d_out, d_in).part : part_values(dtype, m, d_out, d_in));
+    c.take<float>(few_takes(dtype, m, d_out) ? few_plan(dtype, m, d_out, d_in).part
+                                             : part_values(PRODUCT_Y, dtype, m, d_out, d_in));
     return c.bytes();
 }
 static LinearWork gradient_work(void* work, int dtype, int64_t m, int64_t d_in, int64_t d_out, int act) {
@@ -296,7 +298,8 @@ static LinearWork gradient_work(void* work, int dtype, int64_t m, int64_t d_in, 
         w.dz_stride = (d_out + 7) & ~(int64_t)7;
         w.dz = c.take<char>(m * w.dz_stride * dtype_size(dtype));
     }
-    w.part = c.take<float>(std::max(part_values(dtype, m, d_in, d_out), part_values(dtype, d_in, d_out, m)));
+    w.part = c.take<float>(
+        std::max(part_values(PRODUCT_DX, dtype, m, d_in, d_out), part_values(PRODUCT_DW, dtype, d_in, d_out, m)));
     w.bytes = c.bytes();
     return w;
 }

@@ -130,10 +130,12 @@ struct FewPlan {
 FewPlan few_plan(int dtype, int64_t rows, int64_t cols, int64_t depth);
 void few_product(int dtype, ProductArgs a, int act, hipStream_t s);  // a.part: the workspace
 
-// Large products (linear_wide.hip).  Whether one is taken,
-// and the fp32 values it leaves in the workspace.
+// Large products (linear_wide.hip).  Whether these sizes are taken, whether
+// these arrays are too, and the fp32 values that the sizes leave in the
+// workspace (0 where they are not taken).
+bool wide_sizes(int kind, int dtype, int64_t rows, int64_t cols, int64_t depth);
 bool wide_takes(int kind, int dtype, const ProductArgs& a);
-int64_t wide_part(int dtype, int64_t rows, int64_t cols, int64_t depth);
+int64_t wide_part(int kind, int dtype, int64_t rows, int64_t cols, int64_t depth);
 void wide_product(int kind, int dtype, ProductArgs a, float* part, int act, hipStream_t s);
 
 }  // namespace taurus

@@ -512,17 +512,19 @@ static WidePlan wide_plan(int dtype, int64_t rows, int64_t cols, int64_t depth) 
 // 512 -> 512 (2.1e9) 54 / 52 / 54 against 42 / 42 / 54; 16,000 x 512 -> 512
 // (4.2e9) 82 / 78 / 88 against 73 / 72 / 80).
 static double wide_work(int dtype) { return dtype == TAURUS_F32 ? 2e9 : 6e9; }
-bool wide_takes(int kind, int dtype, const ProductArgs& a) {
+bool wide_sizes(int kind, int dtype, int64_t rows, int64_t cols, int64_t depth) {
     const int e = 16 / dtype_size(dtype);  // rows of whole 16-byte pieces
-    auto whole = [e](const void* p, int64_t width, int64_t stride) {
-        return width % e == 0 && stride % e == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0;
-    };
-    const int64_t m_width = kind == PRODUCT_DW ? a.rows : a.depth, n_width = kind == PRODUCT_DX ? a.depth : a.cols;
-    return whole(a.m, m_width, a.ms) && whole(a.n, n_width, a.ns) && a.cols % e == 0 && a.rows >= 256 && a.cols >= 256 &&
-           a.depth >= 256 && (double)a.rows * a.cols * a.depth >= wide_work(dtype) &&
-           ceil_div(a.rows, 128) * ceil_div(a.cols, 128) <= WIDE_TILES;
+    const int64_t m_width = kind == PRODUCT_DW ? rows : depth, n_width = kind == PRODUCT_DX ? depth : cols;
+    return m_width % e == 0 && n_width % e == 0 && cols % e == 0 && rows >= 256 && cols >= 256 && depth >= 256 &&
+           (double)rows * cols * depth >= wide_work(dtype) && ceil_div(rows, 128) * ceil_div(cols, 128) <= WIDE_TILES;
 }
-int64_t wide_part(int dtype, int64_t rows, int64_t cols, int64_t depth) {
+bool wide_takes(int kind, int dtype, const ProductArgs& a) {
+    const int e = 16 / dtype_size(dtype);
+    auto whole = [e](const void* p, int64_t stride) { return stride % e == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+    return wide_sizes(kind, dtype, a.rows, a.cols, a.depth) && whole(a.m, a.ms) && whole(a.n, a.ns);
+}
+int64_t wide_part(int kind, int dtype, int64_t rows, int64_t cols, int64_t depth) {
+    if (!wide_sizes(kind, dtype, rows, cols, depth)) return 0;
     const WidePlan p = wide_plan(dtype, rows, cols, depth);
     return p.cut * p.splits * p.tile * p.tile;
 }

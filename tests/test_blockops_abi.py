@@ -170,6 +170,27 @@ def test_linear_workspace_is_bounded(dtype, size, m, k, n):
         assert N.lib().taurus_linear_grad_bytes(dtype, m, k, n, act) <= parts + dz + sums + 2048 * 512 * 4 + 1024
 
 
+@pytest.mark.parametrize("dtype,m,k,n", [
+    (N.BF16, 40, 4096, 50), (N.BF16, 1_000_000, 64, 64), (N.BF16, 1_000_000, 1, 1), (N.F32, 1_000_000, 64, 64),
+    (N.F16, 200_000, 1000, 47), (N.BF16, 16_384, 2048, 8191), (N.F32, 300_000, 256, 255), (N.BF16, 255, 8192, 8192),
+    (N.F32, 700, 512, 512), (N.BF16, 700, 1024, 1024),
+])
+def test_no_workspace_for_large_tiles_that_sizes_rule_out(dtype, m, k, n):
+    """Widths that are no whole 16-byte pieces, less than 256 a side or few
+    multiply-adds leave only parts of the smaller tiles, of at least four stages
+    each: as many sums of the product itself, not of tiles of 256 x 256."""
+    size, stage = (4, 32) if dtype == N.F32 else (2, 64)
+
+    def parts(rows, cols, depth):
+        n = min(1024, -(-depth // stage) // 4)
+        return n * rows * cols * 4 if n > 1 else 0
+
+    assert N.lib().taurus_linear_bytes(dtype, m, k, n) <= parts(m, n, k) + 256
+    sums = min(m // 32 + 1, 2048) * n * 4
+    if m >= 256:  # a gradient of fewer rows can have a side that is taken
+        assert N.lib().taurus_linear_grad_bytes(dtype, m, k, n, N.ACT_NONE) <= max(parts(m, k, n), parts(k, n, m)) + sums + 512
+
+
 def test_refused_sizes_are_told_every_time():
     from paper_2607_17374_amd import blockops
     for _ in range(2):
