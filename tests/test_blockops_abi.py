@@ -27,6 +27,21 @@ def test_argument_types_match_the_header():
         assert N.SIGNATURES[name][0] == kinds[m.group(1)], name
 
 
+def test_assembly_leaves_m0_as_it_was():
+    """m0 is reserved, so no clobber tells the compiler that assembly writes it:
+    what writes it saves it first and puts it back last."""
+    csrc, found = os.path.join(ROOT, "paper_2607_17374_amd", "csrc"), 0
+    for name in sorted(os.listdir(csrc)):
+        for block in re.findall(r"\basm\b[^(;]*\((.*?)\);", open(os.path.join(csrc, name)).read(), flags=re.S):
+            lines = [x for s in re.findall(r'"([^"]*)"', block.split("\n        :")[0]) for x in s.split("\\n\\t") if x]
+            if not any(re.match(r"\w+ m0,", x) for x in lines):
+                continue
+            found += 1
+            saved = re.fullmatch(r"s_mov_b32 (%\d+), m0", lines[0])
+            assert saved and lines[-1] == f"s_mov_b32 m0, {saved.group(1)}", (name, lines)
+    assert found
+
+
 P = 1 << 20  # a pointer no refused call follows
 
 
