@@ -752,16 +752,18 @@ static void labels_e(const LabelArgs& a, const LabelPlan& p, hipStream_t s) {
                 k_labels_rows<DT, E, P, LG><<<(unsigned)std::min(ceil_div(a.m, 256 >> LG), most), 256, 0, s>>>(a);
             }
         };
+        // whole 16-byte vectors: rows from four (fp32) or eight classes on
+        constexpr bool WHOLE = E * type_bytes<DT> == 16;
         auto go_p = [&](auto lg) {
-            if constexpr (E == 8 || E == 4) {
+            if constexpr (WHOLE) {
                 if (p.p * E == 16) return go(std::integral_constant<int, 16 / E>{}, lg);
             }
-            if constexpr (E == 4) {
+            if constexpr (WHOLE && E == 4) {
                 if (p.p == 3) return go(std::integral_constant<int, 3>{}, lg);
             }
             // rows of so few classes are one lane's
             if (p.p == 1) go(std::integral_constant<int, 1>{}, lg);
-            else if constexpr (E < 8) go(std::integral_constant<int, 2>{}, lg);
+            else if constexpr (E == 2 || E == 4) go(std::integral_constant<int, 2>{}, lg);
         };
         switch (p.lg) {
             case 0: go_p(std::integral_constant<int, 0>{}); break;

@@ -206,6 +206,28 @@ def test_no_workspace_for_large_tiles_that_sizes_rule_out(dtype, m, k, n):
         assert N.lib().taurus_linear_grad_bytes(dtype, m, k, n, N.ACT_NONE) <= max(parts(m, k, n), parts(k, n, m)) + sums + 512
 
 
+def test_label_kernels_are_those_that_rows_reach():
+    """Every kernel of rows in registers is some number of classes', and every
+    number has its own: vectors a row's type and width allow, sixteen values a
+    lane, three vectors of fp32 where they hold the row."""
+    reached = set()
+    for dtype in (N.F32, N.BF16, N.F16):
+        for c in range(1, 1025):
+            e = 4 if dtype == N.F32 else 8
+            while e > c:
+                e //= 2
+            vecs, p, lg = -(-c // e), 1, 0
+            while p < 16 // e and vecs > p:
+                p *= 2
+            while vecs > p << lg:
+                lg += 1
+            if (e, p) == (4, 4) and vecs <= 3 << lg:
+                p = 3
+            reached.add((dtype, e, p, lg))
+    names = re.findall(rb"k_labels_rowsILi(\d)ELi(\d)ELi(\d)ELi(\d)EEE", open(N.LIB_PATH, "rb").read())
+    assert {tuple(int(v) for v in n) for n in names} == reached
+
+
 def test_refused_sizes_are_told_every_time():
     from paper_2607_17374_amd import blockops
     for _ in range(2):
