@@ -391,9 +391,29 @@ def _encode(x: torch.Tensor, encoder: dict, n: int, d_in: Optional[int], stream)
     return h if norm is None else group_norm(h, stream=stream, **norm)
 
 
-def _check_blocks(layers: list, stream_dtype) -> None:
+def _fits(t, shape, dtype, device, what: str) -> None:
+    """An operator's array, checked before the layers that it comes after run
+    (device None: not known)."""
+    if not torch.is_tensor(t) or t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {getattr(t, 'dtype', type(t).__name__)}")
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous with shape {shape}, got shape {tuple(t.shape)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{what} must be on {device}, got {t.device}")
+
+
+def _check_row_norm(norm: Optional[dict], d: int, device, what: str) -> None:
+    for name in ("weight", "bias"):
+        if norm is not None and norm.get(name) is not None:
+            _fits(norm[name], (d,), torch.float32, device, f"{what}'s {name}")
+    eps = 1e-5 if norm is None else norm.get("eps", 1e-5)
+    if not 0 <= eps < float("inf"):
+        raise ValueError(f"{what}'s eps {eps} is not in [0, inf)")
+
+
+def _check_blocks(layers: list, stream_dtype, device) -> None:
     """The layers' norms and residual blocks fit what enters them (stream_dtype:
-    the first layer's input)."""
+    the first layer's input; device: the graph's, None if not known)."""
     for spec in layers:
         _check_norm(spec.get("norm"))
         block = spec.get("residual")
@@ -408,10 +428,20 @@ def _check_blocks(layers: list, stream_dtype) -> None:
         check_norm_args(block.get("pre"), "pre")
         if spec.get("norm") is not None:
             raise ValueError("a layer has a norm or a residual, whose post is the norm of its output")
-        if spec["d_in"] != spec["d_out"]:
-            raise ValueError(f"a layer of {spec['d_in']} to {spec['d_out']} values has no residual")
+        d = spec["d_out"]
+        if spec["d_in"] != d:
+            raise ValueError(f"a layer of {spec['d_in']} to {d} values has no residual")
+        if d > N.RESIDUAL_MOST:
+            raise ValueError(f"a residual has at most {N.RESIDUAL_MOST} channels, not {d}")
         if stream_dtype not in (out_dtype, torch.float32):
             raise ValueError(f"the residual stream is {stream_dtype}, the layer's output {out_dtype}")
+        gate, off = block.get("gate"), block.get("off")
+        if off is not None:
+            _fits(off, (max(off.numel(), 1),), torch.int64, device, "off")
+        if gate is not None:
+            _fits(gate, (d,) if off is None else (off.numel() - 1, d), torch.float32, device, "gate")
+        _check_row_norm(block.get("post"), d, device, "post")
+        _check_row_norm(block.get("pre"), d, device, "pre")
 
 
 def _answer(h: torch.Tensor, head: dict, stream):
@@ -471,7 +501,7 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
 
     Returns (outputs, stats); the outputs are complete."""
     layers = list(layers)
-    _check_blocks(layers, x.dtype)
+    _check_blocks(layers, x.dtype, None if row_off is None else row_off.device)
     if head is not None:
         head = dict(head, linear=list(head.get("linear", ())))
         _check_head(head, n, layers[-1]["d_out"] if layers else None)

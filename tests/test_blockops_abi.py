@@ -277,6 +277,36 @@ def test_model_refuses_blocks_and_heads_that_do_not_fit(layers, head, text):
         T.run_layers(4, off, x, x, layers, chunk=4, head=head)
 
 
+V8, ELSEWHERE = torch.zeros(8), torch.zeros(8, device="meta")  # the graph is on the CPU
+
+
+@pytest.mark.parametrize("block,text", [
+    (dict(gate=torch.zeros(9)), "gate must be contiguous with shape"), (dict(gate=V8.double()), "gate must be torch.float32"),
+    (dict(gate=ELSEWHERE), "gate must be on cpu"), (dict(gate=torch.zeros(16)[::2]), "gate must be contiguous"),
+    (dict(gate=V8, off=torch.tensor([0, 4])), "gate must be contiguous with shape"),
+    (dict(gate=torch.zeros(2, 8), off=torch.tensor([0, 4])), "gate must be contiguous with shape"),
+    (dict(off=torch.tensor([0, 4], dtype=torch.int32)), "off must be torch.int64"),
+    (dict(off=torch.tensor([[0, 4]])), "off must be contiguous"), (dict(off=torch.zeros(0, dtype=torch.int64)), "^off must be"),
+    (dict(off=torch.zeros(2, dtype=torch.int64, device="meta")), "off must be on cpu"),
+    (dict(post=dict(weight=torch.zeros(7))), "post's weight must be contiguous"),
+    (dict(post=dict(bias=V8.to(torch.bfloat16))), "post's bias must be torch.float32"),
+    (dict(pre=dict(weight=ELSEWHERE)), "pre's weight must be on cpu"), (dict(pre=dict(bias=torch.zeros(1, 8))), "pre's bias"),
+    (dict(pre=dict(eps=-1.0)), "pre's eps"), (dict(post=dict(kind="rms", eps=float("nan"))), "post's eps"),
+])
+def test_model_refuses_a_blocks_arrays_before_any_layer(block, text):
+    """In the second layer, so that the first would have run."""
+    x, off = torch.zeros(4, 8), torch.tensor([0, 4])
+    with pytest.raises(ValueError, match=text):
+        T.run_layers(4, off, x, x, [dict(LAYER), dict(LAYER, residual=block)], chunk=4)
+
+
+def test_model_refuses_blocks_of_too_many_channels():
+    x, off, wide = torch.zeros(4, 8), torch.tensor([0, 4]), dict(d_in=8193, d_out=8193)
+    with pytest.raises(ValueError, match="at most 8192 channels"):
+        T.run_layers(4, off, x, x, [dict(wide), dict(wide, residual={})], chunk=4)
+    assert _resnorm(d=N.RESIDUAL_MOST + 1, xs=1 << 14, fs=1 << 14, ys=1 << 14, hs=1 << 14) == N.E_INVALID
+
+
 class _FakeRun:
     """run_layers' parts as a log of what they are asked, without a device."""
 
