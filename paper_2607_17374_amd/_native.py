@@ -20,6 +20,7 @@ EVICT_PENDING, EVICT_RANDOM, EVICT_FIFO, EVICT_LRU = 0, 1, 2, 3
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 RESIDUAL_MOST = 8192  # channels of a row
+CLASSES_MOST, TOP_MOST = 1 << 22, 64
 NOALLOC_SCRATCH_BYTES, NOALLOC_MAX_EDGES = 32 << 20, 1 << 20
 
 STATUS_NAMES = {OK: "OK", E_INVALID: "E_INVALID", E_OOM: "E_OOM", E_DEVICE: "E_DEVICE",

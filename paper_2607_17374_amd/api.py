@@ -14,7 +14,7 @@ import numpy as np
 import torch
 
 from . import _native as N
-from .blockops import check_norm_args, label_log_probs, linear, residual_norm
+from .blockops import check_act, check_norm_args, label_log_probs, linear, residual_norm
 from .rowops import group_norm, grouped_linear, lookup_rows
 
 _TORCH_DTYPE = {N.F32: torch.float32, N.BF16: torch.bfloat16, N.F16: torch.float16}
@@ -411,15 +411,17 @@ def _check_row_norm(norm: Optional[dict], d: int, device, what: str) -> None:
         raise ValueError(f"{what}'s eps {eps} is not in [0, inf)")
 
 
-def _check_blocks(layers: list, stream_dtype, device) -> None:
+def _check_blocks(layers: list, stream_dtype, device):
     """The layers' norms and residual blocks fit what enters them (stream_dtype:
-    the first layer's input; device: the graph's, None if not known)."""
+    the first layer's input; device: the graph's, None if not known).  Returns
+    the type of the rows that leave the last."""
+    rows_dtype = stream_dtype
     for spec in layers:
         _check_norm(spec.get("norm"))
         block = spec.get("residual")
         out_dtype = _TORCH_DTYPE[spec.get("out_dtype", N.F32)]
         if block is None:
-            stream_dtype = out_dtype
+            stream_dtype = rows_dtype = out_dtype
             continue
         unknown = set(block) - {"scale", "gate", "off", "post", "pre"}
         if unknown:
@@ -442,6 +444,8 @@ def _check_blocks(layers: list, stream_dtype, device) -> None:
             _fits(gate, (d,) if off is None else (off.numel() - 1, d), torch.float32, device, "gate")
         _check_row_norm(block.get("post"), d, device, "post")
         _check_row_norm(block.get("pre"), d, device, "pre")
+        rows_dtype = stream_dtype if block.get("pre") is None else out_dtype
+    return rows_dtype
 
 
 def _answer(h: torch.Tensor, head: dict, stream):
@@ -453,8 +457,9 @@ def _answer(h: torch.Tensor, head: dict, stream):
     return label_log_probs(h, head.pop("labels", None), stream=stream, **head)
 
 
-def _check_head(head: dict, n: int, width: Optional[int]) -> None:
-    """The head fits n rows of `width` values (None: not known)."""
+def _check_head(head: dict, n: int, width: Optional[int], dtype, device) -> None:
+    """The head fits n rows of `width` values (None: not known) of this type;
+    device: the graph's, None if not known."""
     unknown = set(head) - {"linear", "labels", "scale", "top", "entropy"}
     if unknown:
         raise ValueError(f"head does not know {', '.join(sorted(unknown))}")
@@ -464,10 +469,23 @@ def _check_head(head: dict, n: int, width: Optional[int]) -> None:
             raise ValueError("head's linear maps have weight, bias and act, got " + ", ".join(sorted(m)))
         if m["weight"].dim() != 2 or width not in (None, m["weight"].shape[0]):
             raise ValueError(f"head's linear map of shape {tuple(m['weight'].shape)} takes no rows of {width} values")
+        _fits(m["weight"], tuple(m["weight"].shape), dtype, device, "the weight of a head's linear map")
         width = m["weight"].shape[1]
-    labels = head.get("labels")
+        if m.get("bias") is not None:
+            _fits(m["bias"], (width,), torch.float32, device, "the bias of a head's linear map")
+        check_act(m.get("act", "none"))
+    labels, top, scale = head.get("labels"), head.get("top", 0), head.get("scale", 1.0)
     if labels is not None and labels.numel() != n:
         raise ValueError(f"head has {labels.numel()} labels for {n} vertices")
+    if labels is not None:
+        _fits(labels, (n,), torch.int32, device, "labels")
+    if width is not None and not 1 <= width <= N.CLASSES_MOST:
+        raise ValueError(f"head answers with 1 to {N.CLASSES_MOST} classes, not {width}")
+    most = N.TOP_MOST if width is None else min(width, N.TOP_MOST)
+    if not 0 <= top <= most:
+        raise ValueError(f"head's top {top} is not in [0, {most}]")
+    if not 0 < scale < float("inf"):
+        raise ValueError(f"head's scale {scale} is not positive and finite")
 
 
 def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Tensor, layers: list,
@@ -501,10 +519,11 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
 
     Returns (outputs, stats); the outputs are complete."""
     layers = list(layers)
-    _check_blocks(layers, x.dtype, None if row_off is None else row_off.device)
+    device = None if row_off is None else row_off.device
+    rows_dtype = _check_blocks(layers, x.dtype, device)
     if head is not None:
         head = dict(head, linear=list(head.get("linear", ())))
-        _check_head(head, n, layers[-1]["d_out"] if layers else None)
+        _check_head(head, n, layers[-1]["d_out"] if layers else None, rows_dtype, device)
     h = x if encoder is None else _encode(x, encoder, n, layers[0]["d_in"] if layers else None, stream)
     results, stats = [], []
     block, norm, rows = None, None, h[:n]  # rows: the residual stream

@@ -22,9 +22,13 @@ _ACT = {"none": N.ACT_NONE, "relu": N.ACT_RELU, "silu": N.ACT_SILU, "gelu": N.AC
 _NORM = {"layer": N.NORM_LAYER, "rms": N.NORM_RMS}
 
 
-def _act(act) -> int:
+def check_act(act) -> None:
     if act not in _ACT:
         raise ValueError(f"act must be one of {', '.join(_ACT)}, got {act!r}")
+
+
+def _act(act) -> int:
+    check_act(act)
     return _ACT[act]
 
 

@@ -307,6 +307,48 @@ def test_model_refuses_blocks_of_too_many_channels():
     assert _resnorm(d=N.RESIDUAL_MOST + 1, xs=1 << 14, fs=1 << 14, ys=1 << 14, hs=1 << 14) == N.E_INVALID
 
 
+W84, HALF84 = torch.zeros(8, 4), torch.zeros(8, 4, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("head,text", [
+    (dict(linear=[dict(weight=HALF84)]), "weight of a head's linear map must be torch.float32"),
+    (dict(linear=[dict(weight=W84), dict(weight=HALF84[:4])]), "weight of a head's linear map must be torch.float32"),
+    (dict(linear=[dict(weight=torch.zeros(4, 8).t())]), "weight of a head's linear map must be contiguous"),
+    (dict(linear=[dict(weight=torch.zeros(8, 4, device="meta"))]), "weight of a head's linear map must be on cpu"),
+    (dict(linear=[dict(weight=W84, bias=torch.zeros(5))]), "bias of a head's linear map must be contiguous"),
+    (dict(linear=[dict(weight=W84, bias=HALF84[0])]), "bias of a head's linear map must be torch.float32"),
+    (dict(linear=[dict(weight=W84, act="tanh")]), "act must be one of"),
+    (dict(labels=torch.zeros(4, dtype=torch.int64)), "labels must be torch.int32"),
+    (dict(labels=torch.zeros(4, dtype=torch.int32, device="meta")), "labels must be on cpu"),
+    (dict(labels=torch.zeros(2, 2, dtype=torch.int32)), "labels must be contiguous"),
+    (dict(top=9), r"top 9 is not in \[0, 8\]"), (dict(top=-1), "top -1"), (dict(linear=[dict(weight=W84)], top=5), r"\[0, 4\]"),
+    (dict(linear=[dict(weight=torch.zeros(8, 99))], top=65), r"\[0, 64\]"),
+    (dict(linear=[dict(weight=torch.zeros(8, 0))]), "1 to 4194304 classes, not 0"),
+    (dict(scale=0.0), "scale 0.0"), (dict(scale=float("nan")), "scale nan"), (dict(scale=float("inf")), "scale inf"),
+])
+def test_model_refuses_a_head_before_any_layer(head, text):
+    x, off = torch.zeros(4, 8), torch.tensor([0, 4])
+    with pytest.raises(ValueError, match=text):
+        T.run_layers(4, off, x, x, [dict(LAYER)], chunk=4, head=head)
+
+
+@pytest.mark.parametrize("layers,dtype", [
+    ([dict(LAYER, out_dtype=N.BF16)], torch.bfloat16), ([dict(LAYER)], torch.float32), ([], torch.float16),
+    ([dict(LAYER, out_dtype=N.F16, residual={})], torch.float16),
+    ([dict(LAYER), dict(LAYER, out_dtype=N.BF16, residual={})], torch.float32),  # y: the stream's type
+    ([dict(LAYER), dict(LAYER, out_dtype=N.BF16, residual=dict(pre=dict(kind="rms")))], torch.bfloat16),
+    ([dict(LAYER), dict(LAYER, out_dtype=N.BF16, residual=dict(pre={})), dict(LAYER, out_dtype=N.F16, in_dtype=N.BF16)], torch.float16),
+])
+def test_model_knows_the_type_that_the_head_takes(layers, dtype):
+    """Maps of the rows' type pass the checks (and end at the graph, which is no
+    device tensor here); those of another type are refused."""
+    x, off = torch.zeros(4, 8, dtype=torch.float16), torch.tensor([0, 4])
+    for other in (torch.float32, torch.bfloat16, torch.float16):
+        text = "row_off must be a device tensor" if other == dtype else "weight of a head's linear map must be"
+        with pytest.raises(ValueError, match=text):
+            T.run_layers(4, off, x, x, layers, chunk=4, head=dict(linear=[dict(weight=torch.zeros(8, 4, dtype=other))], top=4))
+
+
 class _FakeRun:
     """run_layers' parts as a log of what they are asked, without a device."""
 
