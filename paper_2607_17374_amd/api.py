@@ -15,7 +15,7 @@ import torch
 
 from . import _native as N
 from .blockops import check_act, check_norm_args, label_log_probs, linear, residual_norm
-from .rowops import group_norm, grouped_linear, lookup_rows
+from .rowops import _overlap, group_norm, grouped_linear, lookup_rows
 
 _TORCH_DTYPE = {N.F32: torch.float32, N.BF16: torch.bfloat16, N.F16: torch.float16}
 
@@ -448,6 +448,39 @@ def _check_blocks(layers: list, stream_dtype, device):
     return rows_dtype
 
 
+def _check_places(x, layers: list, outs, n: int, head: bool, device) -> None:
+    """What a residual or the head reads and writes lies on the graph's device,
+    and a given output is one that a residual can write.  x: the rows that enter
+    the first layer."""
+    if device is None:
+        return
+
+    def here(t, what):
+        if t.device != device:
+            raise ValueError(f"{what} must be on {device}, where the graph is, got {t.device}: residuals and heads take "
+                             "no rows from the host")
+
+    rows, what = x, "x"
+    for i, spec in enumerate(layers):
+        out = outs[i] if outs is not None and i < len(outs) else None
+        if spec.get("residual") is not None:
+            here(rows, what)
+            if out is not None:
+                here(out, f"outs[{i}]")
+                if tuple(out.shape) != (n, spec["d_out"]) or out.dtype != rows.dtype:
+                    raise ValueError(f"outs[{i}] must hold the residual stream, {rows.dtype} of shape {(n, spec['d_out'])}, "
+                                     f"got {out.dtype} of {tuple(out.shape)}")
+                if _overlap(out, rows):
+                    raise ValueError(f"outs[{i}] overlaps the rows that enter its block")
+            else:
+                out = rows
+        elif out is None:  # made where x is
+            out = torch.empty(0, dtype=_TORCH_DTYPE[spec.get("out_dtype", N.F32)], device=x.device)
+        rows, what = out, f"outs[{i}]"
+    if head:
+        here(rows, what)
+
+
 def _answer(h: torch.Tensor, head: dict, stream):
     """Log probabilities of the classes of rows h."""
     head = dict(head)
@@ -509,7 +542,9 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     layer's output is f; y = x + scale * gate * post(f) is the layer's output
     and the stream of the next block, and the next layer takes pre(y) (y
     without pre).  Offsets must hold every vertex.  The stream has the layers'
-    out_dtype or fp32.
+    out_dtype or fp32.  The rows that enter a block, its output and the rows that
+    enter the head lie on the graph's device: x and outputs in host memory, as
+    plain layers take them, go with neither.
 
     head answers with classes: a dict of linear (a list of dicts of linear's
     weight, bias and act, applied one after another to the last layer's rows,
@@ -521,6 +556,8 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
     layers = list(layers)
     device = None if row_off is None else row_off.device
     rows_dtype = _check_blocks(layers, x.dtype, device)
+    rows = x[:n] if encoder is None else torch.empty(0, dtype=x.dtype, device=x.device)  # an encoder's are new
+    _check_places(rows, layers, outs, n, head is not None, device)
     if head is not None:
         head = dict(head, linear=list(head.get("linear", ())))
         _check_head(head, n, layers[-1]["d_out"] if layers else None, rows_dtype, device)

@@ -349,6 +349,44 @@ def test_model_knows_the_type_that_the_head_takes(layers, dtype):
             T.run_layers(4, off, x, x, layers, chunk=4, head=dict(linear=[dict(weight=torch.zeros(8, 4, dtype=other))], top=4))
 
 
+def _meta(dtype=torch.float32, d=8):
+    return torch.zeros(4, d, dtype=dtype, device="meta")
+
+
+HOST, BLOCK, SHARED = "where the graph is", dict(LAYER, residual={}), torch.zeros(4, 8)
+
+
+@pytest.mark.parametrize("x,layers,outs,head,text", [
+    (_meta(), [BLOCK], None, None, "x must be on cpu, " + HOST),
+    (SHARED, [dict(LAYER), BLOCK], [_meta(), None], None, r"outs\[0\] must be on cpu, " + HOST),
+    (SHARED, [dict(LAYER), BLOCK], [None, _meta()], None, r"outs\[1\] must be on cpu, " + HOST),
+    (SHARED, [dict(LAYER)], [_meta()], {}, r"outs\[0\] must be on cpu, " + HOST),
+    (_meta(), [dict(LAYER)], None, {}, r"outs\[0\] must be on cpu, " + HOST),  # made where x is
+    (_meta(), [], None, {}, "x must be on cpu, " + HOST),
+    (SHARED, [dict(LAYER), BLOCK], [None, torch.zeros(4, 8, dtype=torch.float16)], None, r"outs\[1\] must hold the residual stream"),
+    (SHARED, [dict(LAYER), BLOCK], [None, torch.zeros(5, 8)], None, r"outs\[1\] must hold the residual stream"),
+    (SHARED, [dict(LAYER), dict(BLOCK, out_dtype=N.BF16)], [None, torch.zeros(4, 8, dtype=torch.bfloat16)], None,
+     r"outs\[1\] must hold the residual stream, torch.float32"),
+    (SHARED, [BLOCK], [SHARED], None, r"outs\[0\] overlaps"),
+    (SHARED, [dict(LAYER), BLOCK], [torch.zeros(4, 8)] * 2, None, r"outs\[1\] overlaps"),
+    # a plain layer's rows may be anywhere, and a block's given outputs be the stream
+    (_meta(), [dict(LAYER)], [_meta()], None, "row_off must be a device tensor"),
+    (_meta(), [dict(LAYER), BLOCK], [torch.zeros(4, 8), torch.zeros(4, 8)], {}, "row_off must be a device tensor"),
+    (SHARED, [BLOCK, dict(BLOCK, out_dtype=N.BF16)], [torch.zeros(4, 8), torch.zeros(4, 8)], {}, "row_off must be a device tensor"),
+])
+def test_model_refuses_rows_that_lie_elsewhere_before_any_layer(x, layers, outs, head, text):
+    with pytest.raises(ValueError, match=text):
+        T.run_layers(4, torch.tensor([0, 4]), SHARED, x, layers, chunk=4, outs=outs, head=head)
+
+
+def test_model_takes_the_table_of_an_encoder_as_output():
+    """The encoder's rows are new: a block may write over the table they came
+    from (the call ends at the lookup, which the table's place is refused by)."""
+    x, off = torch.zeros(4, 8), torch.tensor([0, 4])
+    with pytest.raises(ValueError, match="table must be a device tensor"):
+        T.run_layers(4, off, x, x, [BLOCK], chunk=4, outs=[x], encoder=dict(ids=torch.zeros(4, dtype=torch.int32)))
+
+
 class _FakeRun:
     """run_layers' parts as a log of what they are asked, without a device."""
 
