@@ -271,6 +271,46 @@ def test_linear_wide_strided(dtype):
     assert (out[1, :n - 1] == math.inf).all() and torch.isnan(out[1, n - 1]) and torch.isnan(out[m - 1]).all()
 
 
+def whole(shape, dtype, seed):
+    """Whole numbers from -2 to 2, none of them zero."""
+    g = torch.Generator().manual_seed(seed)
+    return torch.tensor([-2.0, -1.0, 1.0, 2.0])[torch.randint(0, 4, shape, generator=g)].to(dtype)
+
+
+EXACT = [  # rows, d_in, d_out: contractions cut into many parts and joined, long slope passes, rests of rows, stages and
+    # tiles, few rows with a long contraction, the widest outputs of few rows
+    (30_001, 256, 840), (40_003, 64, 72), (16_500, 264, 1480), (300_007, 3, 5), (70_001, 33, 47), (100_001, 16, 8),
+    (9_999, 520, 264), (20_480, 256, 256), (4_097, 1032, 1000), (257, 8200, 300), (2_000, 96, 1),
+    (40, 9000, 50), (20, 9000, 40), (32, 4096, 8200), (17, 513, 16_387), (31, 512, 4096), (3, 20_000, 70), (16, 6000, 9),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(EXACT)))
+def test_linear_exact(dtype, case):
+    """Sums of whole numbers, which fp32 holds exactly (up to 4 a term, below
+    2^24) in whatever order and parts they are added: a row, column or term that
+    is lost, doubled or of a neighbour shows in an output that is not equal."""
+    m, k, n = EXACT[case]
+    act = ["none", "relu"][case % 2]
+    note(f"linear exact {dtype} m={m} k={k} n={n} {act}")
+    assert 4 * max(m, k, n) + 4 < 2 ** 24
+    x, w, grad = whole((m, k), dtype, case), whole((k, n), dtype, case + 1), whole((m, n), dtype, case + 2)
+    b, res = whole((n,), F32, case + 3), whole((m, n), F32, case + 4)
+    z = x.double() @ w.double() + b.double()
+    want = (z.clamp(min=0) if act == "relu" else z) + res.double()
+    out, pre = T.linear(x.cuda(), w.cuda(), b.cuda(), res.cuda(), act=act, out_dtype=F32, pre=True)
+    assert torch.equal(out.cpu().double(), want)
+    assert torch.equal(pre.cpu(), z.to(F32).to(dtype))
+    pre = whole((m, n), dtype, case + 5)
+    dz = torch.where(pre > 0, grad, 0).double() if act == "relu" else grad.double()
+    for weight_dtype in (F32, dtype):
+        dx, dw, db = T.linear_grad(grad.cuda(), x.cuda(), w.cuda(), pre.cuda(), act=act, weight_dtype=weight_dtype)
+        assert torch.equal(dw.cpu(), (x.double().t() @ dz).to(F32).to(weight_dtype))
+        assert torch.equal(dx.cpu(), (dz @ w.double().t()).to(F32).to(dtype))
+        assert torch.equal(db.cpu().double(), dz.sum(0))
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_linear_act_at_any_argument(act, dtype):
