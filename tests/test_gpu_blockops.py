@@ -271,6 +271,20 @@ def test_linear_wide_strided(dtype):
     assert (out[1, :n - 1] == math.inf).all() and torch.isnan(out[1, n - 1]) and torch.isnan(out[m - 1]).all()
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(6))
+def test_linear_few_rows_into_many_columns(dtype, case):
+    """17 to 32 rows (and 16, one block) with the most columns a lane and sixteen
+    waves: from 512 values on into at least 8,192 columns, fp32 4,096."""
+    m, k, n = [(32, 1024, 8192), (17, 512, 8200), (25, 4100, 8195), (32, 2048, 16_400), (16, 777, 8300), (31, 515, 4099)][case]
+    act, out_dtype = ACTS[case % 5], [dtype, F32][case % 2]
+    note(f"linear few rows {dtype} m={m} k={k} n={n} {act} -> {out_dtype}")
+    x, w, b = normal((m, k), dtype, case), normal((k, n), dtype, case + 1, k ** -0.5), normal((n,), F32, case + 2)
+    check_linear(x, w, b, normal((m, n), out_dtype, case + 3) if case % 3 else None, act, out_dtype, case % 2 == 0)
+    pre = None if act == "none" else normal((m, n), dtype, case + 4, 2.0)
+    check_linear_grad(x, w, normal((m, n), dtype, case + 5), act, F32, pre)
+
+
 def whole(shape, dtype, seed):
     """Whole numbers from -2 to 2, none of them zero."""
     g = torch.Generator().manual_seed(seed)
