@@ -272,6 +272,32 @@ def test_linear_wide_strided(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("out_dtype", DTYPES)
+def test_linear_wide_at_odd_addresses(dtype, out_dtype):
+    """What the large products write and the residual they read lie at any
+    address of a value, an odd number of values apart; only x and the weight
+    choose them."""
+    note(f"linear wide at odd addresses {dtype} -> {out_dtype}")
+    m, k, n = 1050, 1040, 5808
+    x, w, b = normal((m, k), dtype, 1), normal((k, n), dtype, 2, k ** -0.5), normal((n,), F32, 3)
+    res = normal((m, n), out_dtype, 4)
+    wide, wide_z = (torch.full((m, n + 4), 7.0, dtype=t, device="cuda") for t in (out_dtype, dtype))
+    out, z, rs = wide[:, 1:1 + n], wide_z[:, 3:3 + n], strided(res, 2, 3)
+    xd, wd, bd = x.cuda(), w.cuda(), b.cuda()
+    code = {F32: N.F32, BF16: N.BF16, F16: N.F16}
+    nbytes = N.lib().taurus_linear_bytes(code[dtype], m, k, n)
+    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device="cuda")
+    N.check(N.lib().taurus_linear(xd.data_ptr(), code[dtype], m, k, k, wd.data_ptr(), n, bd.data_ptr(), rs.data_ptr(),
+                                  rs.stride(0), N.ACT_GELU, out.data_ptr(), code[out_dtype], out.stride(0), z.data_ptr(),
+                                  z.stride(0), work.data_ptr(), nbytes, torch.cuda.current_stream().cuda_stream), "taurus_linear")
+    want_z, tz, y, ty = linear_reference(x, w, b, res, "gelu")
+    close(out, y, ty, out_dtype, "out")
+    close(z, want_z, tz, dtype, "pre")
+    for t, at in ((wide, 1), (wide_z, 3)):
+        assert (torch.cat([t[:, :at], t[:, at + n:]], 1) == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("case", range(6))
 def test_linear_few_rows_into_many_columns(dtype, case):
     """17 to 32 rows (and 16, one block) with the most columns a lane and sixteen
