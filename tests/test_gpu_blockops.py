@@ -881,6 +881,43 @@ def test_label_log_probs_of_any_size(c):
     assert torch.isnan(T.label_log_probs(-x[4:5].cuda(), labels[:1].cuda(), 4.0).logp[0])
 
 
+COUNTED = [  # rows, classes: of every form, in parts and not, with and without a rest of a vector
+    (300, 47), (70, 172), (9, 1000), (40, 1024), (3, 1025), (2100, 1100), (1200, 2050), (130, 5000), (5, 40_003),
+    (2, 300_001), (1, 70_000), (1030, 20_001), (3, 300_000),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(COUNTED)))
+def test_label_log_probs_counts_every_class(dtype, case):
+    """Rows whose live classes all have a logit of 0, the others -inf: S is their
+    number, which fp32 holds exactly however it is added, so that a class lost
+    or counted twice moves log S by 1 / S, against 6 u of log S.  The live ones
+    of a row: all (a lost vector moves log S by 8 / c); the last vector's; the
+    first's; a wave's length around every multiple of 1,024 and around the
+    borders of parts; every second."""
+    m, c = COUNTED[case]
+    note(f"label_log_probs counted {dtype} m={m} c={c}")
+    e = min(c, 4 if dtype == F32 else 8)
+    j = torch.arange(c)
+    parts = max(1, min(1024 // m, c // 2048))
+    per = -(-(-(-c // e)) // parts) * e  # classes of a part
+    near = lambda p: ((j + 3) % p < 6) & (j > 3)
+    masks = [torch.ones(c, dtype=torch.bool), j >= c - e, j < e, near(1024) | (j == c - 1), near(per) | (j == 0), j % 2 == 1]
+    for first in range(0, len(masks), m):
+        live = torch.stack([masks[(first + r) % len(masks)] for r in range(m)])
+        x = torch.where(live, 0.0, -math.inf).to(dtype)
+        labels = torch.tensor([int(v.nonzero()[-1]) for v in masks], dtype=torch.int32)[(first + torch.arange(m)) % len(masks)]
+        r = T.label_log_probs(x.cuda(), labels.cuda(), 1.0, top=min(c, 3), entropy=True)
+        log_s = live.sum(1).double().log()
+        close(r.stats, torch.stack([torch.zeros(m).double(), log_s], 1), 6 * U * torch.stack([log_s, log_s], 1), F32, "stats")
+        close(r.logp, -log_s, 6 * U * log_s, F32, "logp")
+        close(r.entropy, log_s, 6 * U * log_s, F32, "entropy")
+        firsts = torch.stack([torch.nn.functional.pad(v.nonzero().flatten()[:min(c, 3)].int(), (0, max(0, min(c, 3) - int(v.sum()))),
+                                                      value=-1) for v in masks])
+        assert torch.equal(r.top_ids.cpu(), firsts[(first + torch.arange(m)) % len(masks)])
+
+
 def test_label_log_probs_differences():
     note("label_log_probs differences")
     m, c = 6, 30
