@@ -635,6 +635,52 @@ def test_residual_norm_strided(dtype, d, pad, lead):
                        normal((m, d), dtype, 9), (pad, lead))
 
 
+COUNTED_ROWS = [  # rows, channels, segments (None: one gate for all): many rows a worker, segments within one and over
+    # several workers, teams of lanes and of all waves
+    (300_001, 128, 9000), (100_003, 24, None), (200_001, 8, 40), (33_000, 512, None), (33_001, 520, 3), (20_000, 600, 300),
+    (5000, 4096, 5), (3001, 8192, None), (70_007, 3, 2000), (9001, 2050, 9000),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", range(len(COUNTED_ROWS)))
+def test_residual_norm_sums_are_exact(dtype, case):
+    """The sums over rows on whole numbers, which fp32 holds exactly however they
+    are added (at most 24 a row, 300,001 rows: below 2^24): the statistics given
+    are whole, and the norm before has weights of 0, so that what comes back
+    through it is 0 and its own sums are whole too."""
+    m, d, segments = COUNTED_ROWS[case]
+    stream = [dtype, F32][case % 2]
+    note(f"residual_norm sums {dtype} stream {stream} m={m} d={d} segments={segments}")
+    f, y = whole((m, d), dtype, case), whole((m, d), stream, case + 1)
+    gy, gh = whole((m, d), stream, case + 2).sign(), whole((m, d), dtype, case + 3).sign()
+    g = torch.Generator().manual_seed(case + 4)
+    stats = torch.stack([torch.randint(-1, 2, (m,), generator=g), torch.randint(1, 3, (m,), generator=g)] * 2, 1).float()
+    off = None
+    if segments is not None:
+        off = torch.cat([torch.zeros(1), torch.randint(0, m + 1, (segments - 1,), generator=g).sort().values, torch.tensor([m])]).long()
+    gate = whole((d,) if off is None else (segments, d), F32, case + 5)
+    w, b, zero = whole((d,), F32, case + 6), whole((d,), F32, case + 7), torch.zeros(d)
+    got = T.residual_norm_grad(gy.cuda(), gh.cuda(), y.cuda(), f.cuda(), stats.cuda(), gate=gate.cuda(),
+                               off=None if off is None else off.cuda(), post=dict(kind="rms", weight=w.cuda(), bias=b.cuda()),
+                               pre=dict(kind="layer", weight=zero.cuda(), bias=zero.cuda()))
+    hat1 = (f.float() - stats[:, 0:1]) * stats[:, 1:2]
+    hat2 = (y.float() - stats[:, 2:3]) * stats[:, 3:4]
+    gy, gh = gy.float(), gh.float()
+    assert torch.equal(got.x.float().cpu(), gy)
+    each, terms = gy * (w * hat1 + b), gy * hat1
+    if off is None:
+        dgate, rows = each.double().sum(0), gate.expand(m, d)
+    else:
+        seg = torch.searchsorted(off, torch.arange(m), right=True) - 1
+        dgate, rows = torch.zeros(segments, d, dtype=torch.float64).index_add_(0, seg, each.double()), gate[seg]
+    for got_sum, want in ((got.gate, dgate), (got.post_weight, (rows * terms).double().sum(0)),
+                          (got.post_bias, (rows * gy).double().sum(0)), (got.pre_weight, (gh * hat2).double().sum(0)),
+                          (got.pre_bias, gh.double().sum(0))):
+        assert float(want.abs().max()) < 2 ** 24
+        assert torch.equal(got_sum.cpu().double(), want)
+
+
 def test_residual_norm_special_rows():
     """Constant rows, rows far from zero, infinities and NaN: each keeps to
     itself."""
