@@ -551,7 +551,9 @@ int taurus_linear(const void* x, int32_t dtype, int64_t m, int64_t d_in, int64_t
  *     dbias   = sum over rows of dz[r]      float[d_out]
  * Each may be NULL and is then not computed.  The residual's gradient is grad
  * itself.  For dx and dweight dz is rounded to dtype, as the matrix cores take
- * it; dbias adds it unrounded.  act'(0) of ReLU is 0.
+ * it (with an activation of 16-bit rows that is a rounding besides the
+ * result's; with fp32 arrays there is none); dbias adds it unrounded.  act'(0)
+ * of ReLU is 0.
  */
 int64_t taurus_linear_grad_bytes(int32_t dtype, int64_t m, int64_t d_in, int64_t d_out, int32_t act);
 int taurus_linear_grad(const void* grad, int64_t grad_stride, const void* x, int64_t x_stride, int32_t dtype,

@@ -84,7 +84,9 @@ def linear_grad(grad: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, pre: 
     """taurus_linear_grad: (dx of x's type, dweight of weight_dtype, dbias
     float32) from grad [m][d_out], x's type, and the z that linear gave (pre;
     not needed without an activation); None in the place of those that `need`
-    does not name.  The residual's gradient is grad."""
+    does not name.  The residual's gradient is grad.  Behind an activation,
+    grad act'(z) of 16-bit arrays is rounded to their type before dx and dweight
+    are formed; fp32 arrays avoid that."""
     _needed(need, ("x", "weight", "bias"))
     with _Call(x, stream, "x") as c:
         xp, xs = c.rows(x, None, "x")

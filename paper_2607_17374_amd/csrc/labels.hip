@@ -263,9 +263,13 @@ __device__ inline bool top_at_once(const LabelArgs& a, int64_t r, bool in, const
     return true;
 }
 
-// Workgroups a compute unit.  Five keep more rows on their way (fp32, 12 values
-// a lane, 1,000,000 x 172, top 5: 201 us for 205 with four); fp32 of 16 values
-// a lane does not fit their registers (390,625 x 256: 81 us for 74).
+// Workgroups a compute unit.  Five keep more rows on their way than four, also
+// where a lane then lacks two registers (16 bits from 257 classes on, fp32 with
+// 12 values a lane from 513 on).  Call after call, five / four: 1,000,000 x 172
+// fp32 labels alone 137 / 140 us, top 5 181 / 187, bf16 114 / 118 and 197 / 206;
+// 100,000 x 1,000 bf16 45 / 47 and 111 / 117, fp16 46 / 48 and 110 / 115; 150,000
+// x 700 fp32 81 / 79 and 138 / 145.  fp32 of 16 values a lane needs four (390,625
+// x 256: 74 us for 81 with five).
 template <int DT, int E, int P>
 constexpr int ROWS_PER_CU = DT == TAURUS_F32 && E * P == 16 ? 4 : 5;
 // P vectors a lane, 2^LG lanes a row.  The next rows are on their way while the

@@ -19,7 +19,7 @@
 // one) takes consecutive rows, as many as the others, and has the next ones
 // under way while it works on these.
 //
-// The gradient's column sums stay in registers too.  The gate is the same for
+// The gradient's column sums are kept beside them.  The gate is the same for
 // all rows of a segment, so that with A = sum of dy fhat and B = sum of dy over
 // a worker's rows of one,
 //     dgate = scale (w A + b B),   dw += scale gate A,   db += scale gate B.
@@ -32,8 +32,21 @@
 // stream, gradient 468 us and 11 for its columns, 5.1 TB/s; 300,001 fp16 rows
 // of 128 in 9,000 segments, layer norms, gradient 113 us and 6 for gates, 4 for
 // columns, 3.7 TB/s (three reductions and two norms a row beside memory: a team
-// of 16 lanes has eight channels each).  Four waves a SIMD leave the gradient too
-// few registers (253 us), two hide less (143).
+// of 16 lanes has eight channels each).  Call after call, gradient / forward:
+// 300,001 rows of 128, segments' gates, layer norms, fp32 222 / 135 us (4.2 / 4.6
+// TB/s), bf16 on an fp32 stream 164 / 106 (4.2 / 4.4), bf16 115 / 67 (4.0 / 4.6);
+// a gate by channel 196, 150 and 105 us; 9,000 rows of 4,096 in nine segments
+// 217 / 125, 182 / 95, 136 / 61.
+//
+// Registers of the gradient: four waves a SIMD leave too few (253 us for 135 of
+// the fp16 rows by segment).  At three, a segment's gate fits with 16-bit rows on
+// a stream of their type; on an fp32 stream 8 to 9 registers go to memory, of
+// fp32 rows 33 to 35 (by channel 7, where lanes are left over), of the longest
+// rows, at two, 6 to 33.  Three / two, with as many workers as fit: 300,001 fp16
+// rows of 128 by segment 116 / 117 us, by channel 105 / 103; 75,000 of 512 120 /
+// 118; on an fp32 stream 164 / 160, 150 / 148, 171 / 166; fp32 223 / 206, 195 /
+// 194, 231 / 212: the bound suits 16-bit rows, fp32 ones by segment would be
+// better off with two.
 #include "columns.hpp"
 #include "lanes.hpp"
 #include "rowops.hpp"
