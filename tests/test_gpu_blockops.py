@@ -1043,6 +1043,26 @@ def test_graph_replays(dtype, m, c):
             assert torch.equal(a, c_) and torch.equal(b, c_), (seed, i)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_results_repeat_whatever_memory_held(dtype):
+    """The same bits again, with workspaces and outputs in memory that held NaN
+    (large products and cut ones, sums joined over workgroups, long label rows)."""
+    note(f"repeats {dtype}")
+    t, u = everything_inputs(1, dtype), everything_inputs(2, dtype, m=9, c=40_000)
+    u["off"] = ranges([4, 0, 1, 4]).cuda()
+    m, k, n = 16_500, 264, 1480
+    x, w, g, z = (normal(s, dtype, 3 + i).cuda() for i, s in enumerate([(m, k), (k, n), (m, n), (m, n)]))
+
+    def run():
+        return [*everything(t), *everything(u), T.linear(x, w, act="silu"), *T.linear_grad(g, x, w, z, act="gelu")]
+    want = run()
+    for _ in range(3):
+        junk = [torch.full((1 << s,), math.nan, device="cuda") for s in range(10, 26)]
+        del junk  # what is made next lies there
+        for i, (a, b) in enumerate(zip(run(), want)):
+            assert a is None and b is None or torch.equal(a, b), i
+
+
 def test_streams():
     """Two streams at once, and the stream argument, give the eager bits."""
     note("streams")
