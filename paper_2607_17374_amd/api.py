@@ -570,7 +570,7 @@ def run_layers(n: int, row_off: torch.Tensor, col_dst: torch.Tensor, x: torch.Te
         norm, block = spec.pop("norm", None), spec.pop("residual", None)
         shape, dtype = (n, spec["d_out"]), _TORCH_DTYPE[spec.get("out_dtype", N.F32)]
         result = outs[i] if outs is not None and outs[i] is not None else torch.empty(
-            shape, dtype=dtype if block is None else rows.dtype, device=x.device)
+            shape, dtype=dtype if block is None else rows.dtype, device=x.device if block is None else rows.device)
         out = result if norm is None and block is None else torch.empty(shape, dtype=dtype, device=result.device)
         L = Layer(n, row_off, col_dst, out=out, chunk=chunk, stream=stream, profile=profile, plan=plan, **spec)
         L.push_all(h)

@@ -448,3 +448,12 @@ def test_model_carries_the_residual_stream(monkeypatch):
     run.log.clear()
     run([LAYER])
     assert [k for k, _ in run.log] == ["push"]
+
+
+def test_model_puts_a_blocks_output_where_its_rows_are(monkeypatch):
+    """Behind a plain layer that streams x from elsewhere into a given output."""
+    run = _FakeRun(monkeypatch)
+    given = torch.zeros(4, 8)
+    outs, _ = T.run_layers(4, None, None, _meta(), [LAYER, BLOCK], chunk=4, stream=run, outs=[given, None], head=dict(top=0))
+    assert outs[0] is given and outs[1].device == given.device
+    assert [k for k, _ in run.log] == ["push", "push", "block", "answer", "wait"]

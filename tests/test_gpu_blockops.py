@@ -1265,3 +1265,32 @@ def test_blocks_and_a_head_in_a_model():
     for p, q in zip([*again[:2], *again[2]], [*outs[:2], *outs[2]]):
         assert torch.equal(p, q)
     assert again[0] is given[0] and again[1] is given[1]
+
+
+def test_blocks_behind_a_layer_that_streams_from_the_host():
+    """x in pinned host memory through a plain layer, then a block and a head on
+    the device; a block on the host's rows is refused before anything is
+    written."""
+    from fixtures import workloads as WL
+    from tests import harness as H
+    note("blocks behind a streamed layer")
+    n, d = WL.SAGE_RMAT_4K.n, 32
+    src, dst = WL.graph(WL.SAGE_RMAT_4K)
+    row_off, col_dst = T.build_csr(n, torch.from_numpy(src).cuda(), torch.from_numpy(dst).cuda())
+    x = normal((n, d), F32, 1)
+    host = x.pin_memory()
+    layers = [dict(agg=N.SAGE_MEAN, d_in=d, d_out=d, weight_cat=normal((d, 2 * d), F32, 2 + i, 0.2).numpy(), bias=None,
+                   relu=True, layer=1 + i) for i in range(2)]
+    layers[1]["residual"] = dict(gate=normal((d,), F32, 4).cuda(), pre=dict(kind="rms"))
+    want, _ = T.run_layers(n, row_off, col_dst, x.cuda(), layers, chunk=1024, head=dict(top=3, entropy=True))
+    first = torch.empty(n, d, device="cuda")
+    got, _ = T.run_layers(n, row_off, col_dst, host, layers, chunk=1024, outs=[first, None], head=dict(top=3, entropy=True))
+    assert got[0] is first and got[1].is_cuda
+    for a, b in ((got[0], want[0]), (got[1], want[1]), (got[2].entropy, want[2].entropy), (got[2].top_logp, want[2].top_logp)):
+        r = H.compare(a.view(n, -1).cpu().numpy(), b.view(n, -1).double().cpu().numpy(), H.RTOL[N.F32])
+        assert r["n_bad"] == 0, r
+    first.fill_(7.0)
+    for rows, outs in ((host, [None, None]), (x.cuda(), [first, host])):
+        with pytest.raises(ValueError, match="where the graph is"):
+            T.run_layers(n, row_off, col_dst, rows, [layers[1], layers[1]], chunk=1024, outs=outs)
+    assert (first == 7.0).all()
